@@ -51,7 +51,7 @@
  *  - Concurrency. Calls are reentrant; two calls that share a workspace must
  *    not overlap on the GPU.
  *  - Supported shapes: head_dim 128, H_q / H_kv at most 32 (at most 8 for
- *    token-level selection and decode), H_kv at most 64, N < 2^31,
+ *    token-level selection and scale_decode_step), H_kv at most 64, N < 2^31,
  *    outer_chunk a multiple of sub_chunk.
  */
 #ifndef SCALE_H
@@ -319,6 +319,129 @@ int scale_decode_workspace_size(const scale_params_t *p, size_t *bytes);
 int scale_decode_step(const scale_params_t *p, int64_t t, const void *q_t, const void *k, const void *v,
                       void *cache, size_t cache_bytes, void *out_t, void *ws, size_t ws_bytes,
                       scale_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Serving over a paged cache shared by a batch: rotary positions, writing new
+ * tokens into the cache (bf16, or 8 bits quantised as they are written),
+ * reading rows back, and attention of new tokens over all earlier ones. The
+ * calls above take post-RoPE bf16 keys of one sequence: scale_rope makes
+ * them, scale_cache_read gives them back from a cache of either type.
+ *
+ * Row tensors (q, k, v, out: bf16 [rows][heads][128]) have a row stride in
+ * elements (a multiple of 8, at least heads * 128), so a slice of a joint QKV
+ * projection is taken as it lies; heads and head_dim are contiguous. Every
+ * pointer is a device pointer of the current device, row tensors and pages
+ * 16-byte aligned. Inputs and outputs must not overlap, except that scale_rope
+ * and scale_cache_append may write their rotated rows in place (same pointer
+ * and stride). n_rows = 0 enqueues nothing. */
+
+/* How the cache holds a row of 128 values. */
+typedef enum {
+    SCALE_CACHE_BF16 = 0, /* bf16 */
+    SCALE_CACHE_E4M3 = 1  /* 8-bit floats (4 exponent, 3 mantissa bits) times 2^e, one e per row */
+} scale_cache_dtype_t;
+
+/* A paged cache of keys and values. The value of an 8-bit row is code * 2^e
+ * with e = scale byte - 127; every such value is exact in bf16. */
+typedef struct {
+    void *k_pages;         /* bf16 or e4m3 [num_pages][page_size][H_kv][128]                 */
+    void *v_pages;
+    uint8_t *k_scales;     /* [num_pages][H_kv][page_size], 16-byte aligned; NULL for bf16    */
+    uint8_t *v_scales;
+    int32_t dtype;         /* scale_cache_dtype_t                                            */
+    int32_t num_kv_heads;  /* 1..64                                                          */
+    int32_t page_size;     /* tokens; a multiple of 16 (SCALE_ERR_UNSUPPORTED otherwise)     */
+    int64_t num_pages;     /* num_pages * page_size < 2^31 - 256                             */
+} scale_cache_t;
+
+/* The new (or asked-for) tokens of a batch of sequences. Sequence b has the rows
+ * [row_start[b], row_start[b + 1]) of the row tensors, which are the last tokens
+ * of its kv_len[b] tokens in the cache: row r is its token
+ * kv_len[b] - (row_start[b + 1] - r). Token t of sequence b is row t % page_size
+ * of page page_table[b * table_stride + t / page_size].
+ *  - The lists are read on the device, so a captured call follows their contents.
+ *    row_start ascends; rows outside [row_start[0], row_start[n_seqs]) are
+ *    left as they were. Sequences may have no rows.
+ *  - A row with a negative token (kv_len less than the sequence's rows) has no
+ *    place in the cache: it is not written, reads as zeros and attends to nothing.
+ *  - A page-table entry outside [0, num_pages), or past the table's width, is
+ *    not dereferenced: its tokens are not written and read as zero keys and values.
+ *  - Two rows of a batch must not share a place in the cache when they are written. */
+typedef struct {
+    const int32_t *row_start;  /* [n_seqs + 1]                                               */
+    const int32_t *kv_len;     /* [n_seqs]                                                   */
+    const int32_t *page_table; /* [n_seqs][table_stride]                                     */
+    int32_t n_seqs;            /* 1..4096                                                    */
+    int32_t table_stride;
+    int32_t n_rows;            /* rows of the row tensors: at least row_start[n_seqs]        */
+    int32_t max_rows;          /* bound on a sequence's rows; only scale_cache_attend uses
+                                  it: rows of a sequence past it are left as they were       */
+} scale_batch_t;
+
+/* Rotary positions with several axes. Pair i of a head turns by the angle
+ * positions[axis[i]][row] * inv_freq[i]; pair i is dimensions (i, i + 64), or
+ * (2 i, 2 i + 1) when `adjacent` is set. A pair that does not turn has
+ * inv_freq 0. The angle is reduced to a turn in 64-bit integers, so it is as
+ * exact at position 2^31 as at 1; the products are fp32, rounded once. */
+typedef struct {
+    const double *inv_freq;    /* fp64 [64], radians per position                            */
+    const int32_t *positions;  /* int32 [n_axes][n_rows]                                     */
+    int32_t n_axes;            /* 1..4                                                       */
+    int32_t adjacent;
+    uint8_t axis[64];          /* axis of pair i                                             */
+} scale_rope_t;
+
+/* q and k turned to their rows' positions: q_out = rope(q), k_out = rope(k).
+ * k may be NULL (num_kv_heads 0). num_q_heads at most 256, num_kv_heads 64. */
+int scale_rope(const scale_rope_t *rope, int32_t n_rows, int32_t num_q_heads, const void *q, int64_t q_stride,
+               void *q_out, int64_t q_out_stride, int32_t num_kv_heads, const void *k, int64_t k_stride,
+               void *k_out, int64_t k_out_stride, scale_stream_t stream);
+
+/* The rows k and v written to their places in the cache. With `rope`, k is
+ * turned on the way, and q (NULL and num_q_heads 0: none) into q_out, all in one
+ * launch; a turned key goes into an 8-bit cache from fp32, rounded once. Without
+ * `rope` q must be NULL.
+ * An 8-bit row gets e = the least exponent, at least -100, with max |x| <= 448 * 2^e
+ * over its finite values, and codes e4m3(x / 2^e), rounded to nearest even;
+ * infinities become the largest code, NaN stays NaN. */
+int scale_cache_append(const scale_cache_t *cache, const scale_batch_t *batch, const void *k, int64_t k_stride,
+                       const void *v, int64_t v_stride, const scale_rope_t *rope, int32_t num_q_heads,
+                       const void *q, int64_t q_stride, void *q_out, int64_t q_out_stride, scale_stream_t stream);
+
+/* The batch's rows read from the cache: k_out, v_out bf16 [n_rows][H_kv][128]
+ * (row_start spanning kv_len reads whole sequences, for scale_build_reps and
+ * scale_select). Either output may be NULL. */
+int scale_cache_read(const scale_cache_t *cache, const scale_batch_t *batch, void *k_out, int64_t k_out_stride,
+                     void *v_out, int64_t v_out_stride, scale_stream_t stream);
+
+/* Attention of the batch's rows over their sequences in the cache (the rows' own
+ * keys and values among them, appended before). Row r, token p of sequence b,
+ * query head h:
+ *   keys K(p) = {t <= p : t < n_sink or t >= p - n_local}  (n_local < 0: all t <= p)
+ *   out[r][h] = sum_{t in K(p)} softmax_t(attn_scale * q_r^(h) . k_t^(h/g)) v_t^(h/g)
+ *   lse[r][h] = log sum_{t in K(p)} exp(attn_scale * q_r^(h) . k_t^(h/g))
+ * A row without keys gets out = 0 and lse = -inf. Keys and values that no row of
+ * a sequence's call sees may hold anything. A value row that is not finite makes
+ * the rows that see it not finite, and may make so rows of the same call up to
+ * 128 tokens before it.
+ *   q, out bf16 [n_rows][num_q_heads][128];  lse fp32 [n_rows][num_q_heads] or NULL
+ *   ws     scale_cache_attend_workspace_size() bytes, initialised once with
+ *          scale_workspace_init(); a device problem is recorded in its status word.
+ * num_q_heads / num_kv_heads at most 32 (SCALE_ERR_UNSUPPORTED otherwise). */
+typedef struct {
+    int32_t num_q_heads;
+    int32_t n_sink;    /* leading tokens that every row sees                               */
+    int32_t n_local;   /* earlier tokens of the window before a row's own; < 0: all        */
+    float attn_scale;  /* 0 means 1/sqrt(128)                                              */
+} scale_attend_t;
+
+/* Workspace of scale_cache_attend for these heads and this batch's n_seqs, n_rows and
+ * max_rows (no pointer of either struct is looked at). Synchronous, host only. */
+int scale_cache_attend_workspace_size(const scale_attend_t *attend, const scale_cache_t *cache,
+                                      const scale_batch_t *batch, size_t *bytes);
+int scale_cache_attend(const scale_attend_t *attend, const scale_cache_t *cache, const scale_batch_t *batch,
+                       const void *q, int64_t q_stride, void *out, int64_t out_stride, float *lse, void *ws,
+                       size_t ws_bytes, scale_stream_t stream);
 
 /* Synchronous: waits for `stream`, then reads the device status word of `ws`
  * into *status (SCALE_OK, SCALE_ERR_TIMEOUT or SCALE_ERR_DEVICE). The word is

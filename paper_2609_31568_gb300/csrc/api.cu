@@ -11,6 +11,8 @@ namespace scale {
 
 static std::atomic<uint64_t> g_timeout_ns{4000000000ull};
 
+uint64_t wait_timeout_ns() { return g_timeout_ns.load(); }
+
 int derive(const scale_params_t* p, Derived* d)
 {
     if (!p || !d) return SCALE_ERR_INVALID_ARG;

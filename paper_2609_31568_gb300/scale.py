@@ -27,6 +27,8 @@ SCALE_ERR_TIMEOUT = -5
 SCALE_ERR_DEVICE = -6
 SCALE_MODE_PER_CLUSTER = 0
 SCALE_MODE_PER_SUBCHUNK = 1
+SCALE_CACHE_BF16 = 0
+SCALE_CACHE_E4M3 = 1
 
 
 class ScaleLibraryMissing(RuntimeError):
@@ -74,6 +76,104 @@ def kv_pages(k_pages, v_pages, page_table, page_size: int) -> ScaleKvPages:
     return ScaleKvPages(_ptr(k_pages), _ptr(v_pages), _ptr(page_table), page_size, k_pages.shape[0])
 
 
+class ScaleCache(ctypes.Structure):
+    """scale_cache_t: the paged K/V cache of a batch (device pointers)."""
+
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int64)]
+
+
+class ScaleBatch(ctypes.Structure):
+    """scale_batch_t: the new tokens of a batch of sequences (device pointers)."""
+
+    _fields_ = [("row_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("n_seqs", ctypes.c_int32), ("table_stride", ctypes.c_int32), ("n_rows", ctypes.c_int32),
+                ("max_rows", ctypes.c_int32)]
+
+
+class ScaleRope(ctypes.Structure):
+    """scale_rope_t: rotary positions with several axes (device pointers)."""
+
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("n_axes", ctypes.c_int32),
+                ("adjacent", ctypes.c_int32), ("axis", ctypes.c_uint8 * 64)]
+
+
+class ScaleAttend(ctypes.Structure):
+    """scale_attend_t."""
+
+    _fields_ = [("num_q_heads", ctypes.c_int32), ("n_sink", ctypes.c_int32), ("n_local", ctypes.c_int32),
+                ("attn_scale", ctypes.c_float)]
+
+
+def kv_cache(k_pages, v_pages, k_scales=None, v_scales=None) -> ScaleCache:
+    """Descriptor of a paged cache: pages bf16 [num_pages][page_size][H_kv][128], or 8-bit (uint8 or
+    float8_e4m3fn) with scales uint8 [num_pages][H_kv][page_size]. It keeps the tensors alive."""
+    if k_pages.dim() != 4 or k_pages.shape[3] != 128 or k_pages.shape != v_pages.shape:
+        raise ValueError("pages are [num_pages][page_size][num_kv_heads][128], the same for keys and values")
+    pages, page, heads = k_pages.shape[:3]
+    if k_pages.dtype != v_pages.dtype or (k_scales is None) != (v_scales is None):
+        raise ValueError("keys and values of a cache have the same type")
+    if k_scales is None:
+        if k_pages.itemsize != 2 or not k_pages.is_floating_point():
+            raise ValueError("a cache without scales holds bf16 rows")
+        dtype = SCALE_CACHE_BF16
+    else:
+        if k_pages.itemsize != 1:
+            raise ValueError("a cache with scales holds 8-bit rows")
+        for s in (k_scales, v_scales):
+            if tuple(s.shape) != (pages, heads, page) or s.itemsize != 1:
+                raise ValueError("scales are uint8 [num_pages][num_kv_heads][page_size]")
+        dtype = SCALE_CACHE_E4M3
+    c = ScaleCache(_ptr(k_pages), _ptr(v_pages), _ptr(k_scales), _ptr(v_scales), dtype, heads, page, pages)
+    c.tensors = (k_pages, v_pages, k_scales, v_scales)
+    return c
+
+
+def allocate_kv_cache(num_pages: int, page_size: int, num_kv_heads: int, e4m3: bool = False, device="cuda") -> ScaleCache:
+    """An empty paged cache, allocated with torch: zero rows (and scales of 1)."""
+    import torch
+
+    shape = (num_pages, page_size, num_kv_heads, 128)
+    if not e4m3:
+        return kv_cache(*(torch.zeros(shape, dtype=torch.bfloat16, device=device) for _ in range(2)))
+    return kv_cache(*(torch.zeros(shape, dtype=torch.uint8, device=device) for _ in range(2)),
+                    *(torch.full((num_pages, num_kv_heads, page_size), 127, dtype=torch.uint8, device=device)
+                      for _ in range(2)))
+
+
+def kv_batch(row_start, kv_len, page_table, n_rows: int, max_rows: int) -> ScaleBatch:
+    """Descriptor of a batch: row_start int32 [n_seqs + 1], kv_len int32 [n_seqs], page_table int32
+    [n_seqs][pages], on the device. It keeps the tensors alive."""
+    n = kv_len.shape[0]
+    if kv_len.dim() != 1 or tuple(row_start.shape) != (n + 1,) or page_table.dim() != 2 or page_table.shape[0] != n:
+        raise ValueError("a batch has row_start [n_seqs + 1], kv_len [n_seqs] and page_table [n_seqs][pages]")
+    _int32(row_start, kv_len, page_table)
+    b = ScaleBatch(_ptr(row_start), _ptr(kv_len), _ptr(page_table), n, page_table.shape[1], n_rows, max_rows)
+    b.tensors = (row_start, kv_len, page_table)
+    return b
+
+
+def rope_axes(inv_freq, positions, axis=None, adjacent: bool = False) -> ScaleRope:
+    """Descriptor of rotary positions: inv_freq fp64 [64], positions int32 [n_axes][n_rows], `axis` the
+    axis of each of the 64 pairs (default: all the first). It keeps the tensors alive."""
+    if tuple(inv_freq.shape) != (64,) or inv_freq.itemsize != 8 or not inv_freq.is_floating_point():
+        raise ValueError("inv_freq is fp64 [64]")
+    if positions.dim() != 2:
+        raise ValueError("positions is int32 [n_axes][n_rows]")
+    _int32(positions)
+    axis = [0] * 64 if axis is None else [int(x) for x in axis]
+    if len(axis) != 64 or not all(0 <= x < positions.shape[0] for x in axis):
+        raise ValueError("axis gives one of the position axes for each of the 64 pairs")
+    r = ScaleRope(_ptr(inv_freq), _ptr(positions), positions.shape[0], int(adjacent), (ctypes.c_uint8 * 64)(*axis))
+    r.tensors = (inv_freq, positions)
+    return r
+
+
+def attend_params(*, num_q_heads: int, n_sink: int = 0, n_local: int = -1, attn_scale: float = 0.0) -> ScaleAttend:
+    return ScaleAttend(num_q_heads, n_sink, n_local, attn_scale)
+
+
 def params(*, num_q_heads, num_kv_heads, head_dim=128, sub_chunk, n_tokens, max_cluster_subchunks,
            outer_chunk=0, theta=-1.0, block_size, top_k, n_sink, n_local, select_scale=1.0,
            attn_scale=0.0) -> ScaleParams:
@@ -118,6 +218,8 @@ def load() -> ctypes.CDLL:
         P, i32, i64, sz, u64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_uint64
         pp = ctypes.POINTER(ScaleParams)
         kp = ctypes.POINTER(ScaleKvPages)
+        cp, bp = ctypes.POINTER(ScaleCache), ctypes.POINTER(ScaleBatch)
+        rp, ap = ctypes.POINTER(ScaleRope), ctypes.POINTER(ScaleAttend)
         sig = {
             "scale_workspace_size": [pp, i32, ctypes.POINTER(sz)],
             "scale_workspace_init": [P, sz, P],
@@ -135,6 +237,11 @@ def load() -> ctypes.CDLL:
             "scale_decode_workspace_size": [pp, ctypes.POINTER(sz)],
             "scale_decode_step": [pp, i64, P, P, P, P, sz, P, P, sz, P],
             "scale_sparse_prefill": [pp, i32, i64, i64, P, P, P, P, P, P, P, P, P, sz, P],
+            "scale_rope": [rp, i32, i32, P, i64, P, i64, i32, P, i64, P, i64, P],
+            "scale_cache_append": [cp, bp, P, i64, P, i64, rp, i32, P, i64, P, i64, P],
+            "scale_cache_read": [cp, bp, P, i64, P, i64, P],
+            "scale_cache_attend_workspace_size": [ap, cp, bp, ctypes.POINTER(sz)],
+            "scale_cache_attend": [ap, cp, bp, P, i64, P, i64, P, P, sz, P],
             "scale_get_device_status": [P, P, ctypes.POINTER(i32)],
             "scale_retrieval_calls": [pp, i32, P, i32, ctypes.POINTER(i64), ctypes.POINTER(i64)],
             "scale_prefill_host_arena_size": [pp, i32, ctypes.POINTER(sz)],
@@ -165,6 +272,27 @@ def _ptr(x) -> int | None:
     if hasattr(x, "ctypes"):
         return x.ctypes.data
     raise TypeError(f"cannot pass {type(x).__name__} as a pointer")
+
+
+def _int32(*tensors) -> None:
+    for x in tensors:
+        if x.itemsize != 4 or x.is_floating_point():
+            raise ValueError("expected int32 tensors")
+
+
+def _rows(x, n_rows: int, heads: int | None = None) -> tuple:
+    """(address, row stride in elements, heads) of a bf16 row tensor [rows][heads][128] whose rows may
+    lie apart; (None, 0, 0) for None."""
+    if x is None:
+        return None, 0, 0
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 3 or shape[2] != 128 or shape[0] < n_rows or (heads is not None and shape[1] != heads):
+        raise ValueError(f"expected a row tensor [{n_rows}][{'heads' if heads is None else heads}][128], got {tuple(shape)}")
+    if x.itemsize != 2 or not x.is_floating_point():
+        raise ValueError("row tensors are bf16")
+    if stride[2] != 1 or (shape[1] > 1 and stride[1] != 128):
+        raise ValueError("the heads of a row must be contiguous")
+    return x.data_ptr(), stride[0] if shape[0] > 1 else max(stride[0], shape[1] * 128), shape[1]
 
 
 def _nbytes(x) -> int:
@@ -345,6 +473,58 @@ def decode_cache_selection(cache, p) -> tuple:
     k = max(p.top_k, 1)
     raw = cache[off: off + (k + 1) * 4].view(torch.int32).cpu().numpy()
     return raw[:k].copy(), int(raw[k])
+
+
+def scale_rope(rope: ScaleRope, q, k, q_out, k_out, stream=None) -> None:
+    """Rotary positions: q_out = rope(q), k_out = rope(k) (k and k_out may be None; outputs may be the inputs)."""
+    n = rope.tensors[1].shape[1]
+    qp, qs, hq = _rows(q, n)
+    qo, qos, _ = _rows(q_out, n, hq)
+    kp, ks, hkv = _rows(k, n)
+    ko, kos, _ = _rows(k_out, n, hkv)
+    _check("scale_rope", load().scale_rope(ctypes.byref(rope), n, hq, qp, qs, qo, qos, hkv, kp, ks, ko, kos,
+                                           _stream(stream)))
+
+
+def scale_cache_append(cache: ScaleCache, batch: ScaleBatch, k, v, rope: ScaleRope | None = None, q=None, q_out=None,
+                       stream=None) -> None:
+    """New keys (turned when `rope` is given) and values into the cache; q turned into q_out in the same launch."""
+    n = batch.n_rows
+    if rope is not None and rope.tensors[1].shape[1] != n:
+        raise ValueError("rope's positions are [n_axes][n_rows]")
+    kp, ks, _ = _rows(k, n, cache.num_kv_heads)
+    vp, vs, _ = _rows(v, n, cache.num_kv_heads)
+    qp, qs, hq = _rows(q, n)
+    qo, qos, _ = _rows(q_out, n, hq)
+    _check("scale_cache_append", load().scale_cache_append(
+        ctypes.byref(cache), ctypes.byref(batch), kp, ks, vp, vs, None if rope is None else ctypes.byref(rope), hq, qp,
+        qs, qo, qos, _stream(stream)))
+
+
+def scale_cache_read(cache: ScaleCache, batch: ScaleBatch, k_out, v_out, stream=None) -> None:
+    """The batch's rows of the cache as bf16 rows (either output may be None)."""
+    kp, ks, _ = _rows(k_out, batch.n_rows, cache.num_kv_heads)
+    vp, vs, _ = _rows(v_out, batch.n_rows, cache.num_kv_heads)
+    _check("scale_cache_read", load().scale_cache_read(ctypes.byref(cache), ctypes.byref(batch), kp, ks, vp, vs,
+                                                       _stream(stream)))
+
+
+def scale_cache_attend_workspace_size(attend: ScaleAttend, cache: ScaleCache, batch: ScaleBatch) -> int:
+    n = ctypes.c_size_t()
+    _check("scale_cache_attend_workspace_size", load().scale_cache_attend_workspace_size(
+        ctypes.byref(attend), ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(n)))
+    return n.value
+
+
+def scale_cache_attend(attend: ScaleAttend, cache: ScaleCache, batch: ScaleBatch, q, out, lse, ws, stream=None) -> None:
+    """Attention of the batch's rows over their sequences in the cache; lse fp32 [n_rows][H_q] or None."""
+    qp, qs, _ = _rows(q, batch.n_rows, attend.num_q_heads)
+    op, os_, _ = _rows(out, batch.n_rows, attend.num_q_heads)
+    if lse is not None and (lse.numel() < batch.n_rows * attend.num_q_heads or lse.itemsize != 4):
+        raise ValueError("lse is fp32 [n_rows][num_q_heads]")
+    _check("scale_cache_attend", load().scale_cache_attend(
+        ctypes.byref(attend), ctypes.byref(cache), ctypes.byref(batch), qp, qs, op, os_, _ptr(lse), _ptr(ws),
+        _nbytes(ws), _stream(stream)))
 
 
 def scale_get_device_status(ws, stream=None) -> int:
