@@ -12,6 +12,596 @@ namespace {
 
 using namespace scale_ptx;
 
+// ---------------------------------------------------------------- what a sequence asks for
+
+// Rows and keys of sequence b. Its computed rows are [row0, row0 + rows), tokens
+// pos0 .. pos0 + rows - 1; no row sees a key outside [0, n_sink) and [lo, pos0 + rows).
+struct Seq {
+    int row0, rows;
+    int pos0, lo;
+};
+
+__device__ __forceinline__ Seq seq_of(const AttendView& a, const BatchView& b, int i)
+{
+    Seq s;
+    s.row0 = b.row_start[i];
+    const int end = b.row_start[i + 1];
+    const int n = s.row0 < 0 || end <= s.row0 ? 0 : end - s.row0;
+    s.rows = n < b.max_rows ? n : b.max_rows;
+    if (s.rows > b.n_rows - s.row0) s.rows = b.n_rows - s.row0 > 0 ? b.n_rows - s.row0 : 0;
+    const int len = b.kv_len[i];
+    s.pos0 = (len > 0 ? len : 0) - n;
+    s.lo = a.n_local >= 0 && s.pos0 > a.n_local ? s.pos0 - a.n_local : 0;
+    return s;
+}
+
+// ---------------------------------------------------------------- few rows: decode
+
+constexpr int kStep = 16;       // keys of a step; a page holds whole steps
+constexpr int kRowsMax = 16;    // (token, query head) rows of a KV head that k_rows takes
+constexpr int kRowsWarps = 8;
+constexpr int kRowsThreads = 32 * kRowsWarps;
+constexpr int kMaxSms = 160;
+constexpr int kMaxParts = 2 * kMaxSms * kRowsWarps;  // partial results
+constexpr int kMinSteps = 2;    // steps of a warp before another one helps
+constexpr float kRaise = 8.0f;  // log2 units by which a logit may pass the reference
+
+__host__ __device__ constexpr int rows_stages(bool e4m3) { return e4m3 ? 6 : 3; }
+__host__ __device__ constexpr int rows_step_bytes(bool e4m3) { return e4m3 ? 2 * kStep * kHeadDim + 2 * kStep : 4 * kStep * kHeadDim; }
+__host__ __device__ constexpr int rows_ring_bytes(bool e4m3) { return kRowsWarps * rows_stages(e4m3) * rows_step_bytes(e4m3); }
+
+// Steps of a sequence: those of the sinks, then those from the window's first.
+struct Steps {
+    int sinks, first, n;
+};
+
+__device__ __forceinline__ Steps steps_of(const AttendView& a, const Seq& s)
+{
+    Steps x;
+    const int last = s.pos0 + s.rows - 1;  // below 0: one step that nothing of is seen, whose rows get 0
+    x.first = s.lo / kStep;
+    const int sinks = static_cast<int>((static_cast<int64_t>(a.n_sink) + kStep - 1) / kStep);
+    x.sinks = sinks < x.first ? sinks : x.first;
+    x.n = last < 0 ? 1 : x.sinks + last / kStep + 1 - x.first;
+    return x;
+}
+
+struct RowsArgs {
+    AttendView a;
+    CacheView c;
+    BatchView b;
+    int64_t* before;   // [n_seqs + 1] steps (of one KV head) of the sequences before, for k_rows_merge
+    float* part_o;     // [kMaxParts][rows][128]
+    float2* part_ml;   // [kMaxParts][rows] (reference, sum)
+    int part_rows;
+};
+
+__device__ __forceinline__ int64_t run_start(int64_t work, int64_t warps, int64_t w) { return work * w / warps; }
+
+// Warps that share the work.
+__device__ __forceinline__ int64_t runs_of(int64_t work, int64_t warps)
+{
+    const int64_t n = (work + kMinSteps - 1) / kMinSteps;
+    return n < warps ? (n > 0 ? n : 1) : warps;
+}
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool real)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait()
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x)
+{
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+
+// d += a (16 x 16) b (16 x 8), bf16 or f16
+template <bool F16>
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    if (F16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// One KV head's item of a sequence, as a warp walks it.
+struct Item {
+    int b, j;    // sequence, KV head
+    int step;    // next step of it
+    Seq s;
+    Steps x;
+};
+
+// Attention of sequences with at most kRowsMax rows (new tokens times query heads of a KV head).
+//
+// The work is one list of 16-key steps, sequence by sequence and KV head by KV head, cut into equal runs, one
+// per warp, whatever the lengths: a warp walks its run with a ring of its own in shared memory, so nothing in
+// the loop waits for another warp and the copies run on across items. The rows are the N side of the
+// products: S^T = K Q^T with the step's 16 keys as M, O^T += V^T P^T with 16 dimensions as M, so rows are
+// padded to 8 and not to 16 and a thread keeps the same two rows in both; P changes sides by a register
+// transpose. The reference of a row's exponentials is raised only when a logit passes it by 2^8, so a step
+// mostly has no reduction. A run that holds a part of an item leaves (O, reference, sum) to k_rows_merge.
+//
+// 8-bit rows stay codes up to the registers and become f16 there (exact, one conversion per two values);
+// a key's scale multiplies its logit, a value's scale 2^e moves into the exponent, w' = 2^(s + e - m), and the sum
+// takes w' 2^-e. Q is brought to f16 by a power of two per row. P is rounded to bf16 beside bf16 values, to
+// f16 (11 bits) beside codes.
+//
+// Keys that no row sees are not read: their places are filled with zeros, so nothing that lies there
+// reaches a sum. Bound by HBM: K and V once.
+template <int NT, bool E4M3>
+__global__ void __launch_bounds__(kRowsThreads, 1) k_rows(const __grid_constant__ RowsArgs args)
+{
+    constexpr int kStages = rows_stages(E4M3);
+    constexpr int kRow = E4M3 ? kHeadDim : 2 * kHeadDim;  // bytes of a held row
+    constexpr int kTile = kStep * kRow;
+    constexpr int kChunks = kRow / 16;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ int64_t s_sum[kRowsWarps];
+    const AttendView& a = args.a;
+    const CacheView& c = args.c;
+    const BatchView& bt = args.b;
+    int64_t* before = reinterpret_cast<int64_t*>(smem + rows_ring_bytes(E4M3));
+    pdl_enter();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int quad = lane & 3, oct = lane >> 2;
+
+    // ---- steps before every sequence: each thread sums its stretch of them
+    {
+        const int per = (bt.n_seqs + kRowsThreads - 1) / kRowsThreads;
+        const int i0 = tid * per, i1 = i0 + per < bt.n_seqs ? i0 + per : bt.n_seqs;
+        int64_t sum = 0;
+        for (int i = i0; i < i1; ++i) {
+            const Seq s = seq_of(a, bt, i);
+            before[i] = sum;
+            if (s.rows > 0 && s.rows * a.g <= kRowsMax) sum += steps_of(a, s).n;
+        }
+        int64_t incl = sum;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t y = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+            if (lane >= o) incl += y;
+        }
+        if (lane == 31) s_sum[warp] = incl;
+        __syncthreads();
+        int64_t base = incl - sum;
+        for (int w = 0; w < warp; ++w) base += s_sum[w];
+        for (int i = i0; i < i1; ++i) before[i] += base;
+        if (tid == kRowsThreads - 1) before[bt.n_seqs] = base + sum;
+        __syncthreads();
+        if (blockIdx.x == 0)
+            for (int i = tid; i <= bt.n_seqs; i += kRowsThreads) args.before[i] = before[i];
+    }
+    const int64_t work = before[bt.n_seqs] * c.Hkv;
+    const int64_t runs = runs_of(work, static_cast<int64_t>(gridDim.x) * kRowsWarps);
+    const int64_t run = static_cast<int64_t>(warp) * gridDim.x + blockIdx.x;  // the first runs on different SMs
+    if (run >= runs) return;
+    const int64_t x0 = run_start(work, runs, run);
+    const int64_t n = run_start(work, runs, run + 1) - x0;
+    if (n == 0) return;
+
+    const uint32_t ring = smem_addr(smem) + warp * kStages * rows_step_bytes(E4M3);
+
+    auto enter = [&](Item& it, int b) {  // the first sequence from b on that has steps
+        while (before[b + 1] == before[b]) ++b;
+        it.b = b;
+        it.s = seq_of(a, bt, b);
+        it.x = steps_of(a, it.s);
+    };
+    Item load, use;
+    {
+        int lo = 0, hi = bt.n_seqs;  // the last sequence whose steps start at or before x0
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (before[mid] * c.Hkv <= x0) lo = mid;
+            else hi = mid;
+        }
+        enter(load, lo);
+        const int64_t rem = x0 - before[load.b] * c.Hkv;
+        load.j = static_cast<int>(rem / load.x.n);
+        load.step = static_cast<int>(rem - static_cast<int64_t>(load.j) * load.x.n);
+        use = load;
+    }
+    // first token of step i of an item
+    auto token_of = [&](const Item& it, int i) { return (i < it.x.sinks ? i : it.x.first + i - it.x.sinks) * kStep; };
+    auto advance = [&](Item& it) {
+        if (++it.step < it.x.n) return;
+        it.step = 0;
+        if (++it.j < c.Hkv) return;
+        it.j = 0;
+        if (it.b + 1 < bt.n_seqs && before[it.b + 1] < before[bt.n_seqs]) enter(it, it.b + 1);
+    };
+    // The keys of a step that some row sees, as bits: seen(t) = t <= last and (t >= lo or t < n_sink)
+    auto copy_step = [&](int stage, int place) {
+        const int t0 = token_of(load, load.step);
+        const int last = load.s.pos0 + load.s.rows - 1;
+        const uint32_t dst = ring + stage * rows_step_bytes(E4M3);
+        const int64_t first = place < 0 ? 0 : place;
+#pragma unroll
+        for (int i = 0; i < kTile / 512; ++i) {
+            const int id = i * 32 + lane, row = id / kChunks, ch = id % kChunks;
+            const int t = t0 + row;
+            const bool real = place >= 0 && t <= last && (t >= load.s.lo || t < a.n_sink);
+            const int64_t at = ((real ? first + row : 0) * c.Hkv + load.j) * kRow + ch * 16;
+            const uint32_t to = dst + row * kRow + ((ch ^ (row & 7)) << 4);
+            cp_async16(to, c.k + at, real);
+            cp_async16(to + kTile, c.v + at, real);
+        }
+        if (E4M3 && lane < 2) {  // the step's 16 scales lie in one page
+            const int64_t page = first / c.page_size;
+            const int64_t at = (page * c.Hkv + load.j) * c.page_size + (first - page * c.page_size);
+            cp_async16(dst + 2 * kTile + lane * kStep, (lane ? c.vs : c.ks) + at, place >= 0);
+        }
+    };
+
+    uint32_t qf[NT][8][2];            // Q^T, 16 dimensions at a time
+    float q_scale[NT][2];             // 8-bit: the power of two that Q's row was divided by
+    float o[8][NT][4];                // O^T: 16 dimensions at a time
+    float m[NT][2], l[NT][2];         // per row: reference (log2 units, a warp's), sum of this lane's keys
+    auto begin_item = [&]() {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int r = nt * 8 + oct;  // this lane's row of Q
+            const bool live = r < use.s.rows * a.g;
+            const auto* q = static_cast<const __nv_bfloat16*>(a.q) + static_cast<int64_t>(use.s.row0 + (live ? r / a.g : 0)) * a.q_stride +
+                            (use.j * a.g + (live ? r % a.g : 0)) * kHeadDim;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                // bf16: dimensions 16 i + 2 quad (+1), and 8 further; 8-bit: four in a row, as the codes come
+                if (E4M3) {
+                    const uint2 x = *reinterpret_cast<const uint2*>(q + 16 * i + 4 * quad);
+                    qf[nt][i][0] = live ? x.x : 0u;
+                    qf[nt][i][1] = live ? x.y : 0u;
+                } else {
+                    qf[nt][i][0] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * quad) : 0u;
+                    qf[nt][i][1] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 8 + 2 * quad) : 0u;
+                }
+            }
+            if (E4M3) {
+                uint32_t top = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t lo = (qf[nt][i][e] << 16) & 0x7FFFFFFFu, hi = qf[nt][i][e] & 0x7FFF0000u;
+                        top = max(top, max(lo >= 0x7F800000u ? 0u : lo, hi >= 0x7F800000u ? 0u : hi));
+                    }
+                top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+                top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+                // |q| 2^-ex < 2^15, with both powers of two in range
+                int ex = static_cast<int>(top >> 23) - 127 - 14;
+                ex = ex < -100 ? -100 : ex;
+                const float down = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
+                const float up = __uint_as_float(static_cast<uint32_t>(127 + ex) << 23);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        qf[nt][i][e] = pack_f16x2(__uint_as_float(qf[nt][i][e] << 16) * down,
+                                                  __uint_as_float(qf[nt][i][e] & 0xFFFF0000u) * down);
+                // rows 2 quad, 2 quad + 1 of the tile are held by the lanes 8 quad, 8 quad + 4
+                q_scale[nt][0] = __shfl_sync(0xFFFFFFFFu, up, 8 * quad);
+                q_scale[nt][1] = __shfl_sync(0xFFFFFFFFu, up, 8 * quad + 4);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[i][nt][e] = 0.f;
+            m[nt][0] = m[nt][1] = -INFINITY;
+            l[nt][0] = l[nt][1] = 0.f;
+        }
+    };
+    // (O, reference, sum) of the item's steps [from, to) to the output, or to this run's partial results.
+    auto end_item = [&](int from, int to) {
+        const bool whole = from == 0 && to == use.x.n;
+        const int64_t slot = 2 * run + (from == 0);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float sum = l[nt][e];
+                sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 4);
+                sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 8);
+                sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 16);
+                const int r = nt * 8 + 2 * quad + e;
+                if (r >= use.s.rows * a.g) continue;
+                const int64_t row = use.s.row0 + r / a.g;
+                const int h = use.j * a.g + r % a.g;
+                if (whole) {
+                    const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+                    auto* out = static_cast<__nv_bfloat16*>(a.out) + row * a.out_stride + h * kHeadDim;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float y0 = o[i][nt][e] * inv, y1 = o[i][nt][2 + e] * inv;
+                        if (E4M3) {
+                            *reinterpret_cast<uint32_t*>(out + 16 * i + 2 * oct) = pack_bf16x2(y0, y1);
+                        } else {
+                            out[16 * i + oct] = __float2bfloat16_rn(y0);
+                            out[16 * i + 8 + oct] = __float2bfloat16_rn(y1);
+                        }
+                    }
+                    if (a.lse && oct == 0)
+                        a.lse[row * a.Hq + h] = sum > 0.f ? (m[nt][e] + __log2f(sum)) * 0.6931471805599453f : -INFINITY;
+                } else {
+                    float* part = args.part_o + (slot * args.part_rows + r) * kHeadDim;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        part[16 * i + (E4M3 ? 2 * oct : oct)] = o[i][nt][e];
+                        part[16 * i + (E4M3 ? 2 * oct + 1 : 8 + oct)] = o[i][nt][2 + e];
+                    }
+                    if (oct == 0) args.part_ml[slot * args.part_rows + r] = make_float2(m[nt][e], sum);
+                }
+            }
+    };
+
+    int next = cache_row(c, bt, load.b, token_of(load, load.step));  // the next step to load
+    auto load_next = [&](int64_t i, int stage) {
+        if (i < n) {
+            copy_step(stage, next);
+            advance(load);
+            if (i + 1 < n) next = cache_row(c, bt, load.b, token_of(load, load.step));
+        }
+        cp_async_commit();
+    };
+#pragma unroll 1
+    for (int i = 0; i < kStages - 1; ++i) load_next(i, i);
+    begin_item();
+    int from = use.step;
+    int stage = 0;
+#pragma unroll 1
+    for (int64_t i = 0; i < n; ++i) {
+        cp_async_wait<kStages - 2>();
+        __syncwarp();
+        // the stage that step i - 1 was in is free: every lane is past its reads
+        load_next(i + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
+        const uint32_t kt = ring + stage * rows_step_bytes(E4M3), vt = kt + kTile;
+        // ---- S^T = K Q^T
+        float s[NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
+        if (E4M3) {
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {  // matrices: keys 0-7 and 8-15 of chunk 2 h, then of chunk 2 h + 1
+                uint32_t r[4];
+                const int row = lane & 15, ch = 2 * h + (lane >> 4);
+                ldsm4(r, kt + row * kRow + ((ch ^ (row & 7)) << 4));
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t f[4] = {e4m3x2_to_f16x2(r[2 * e]), e4m3x2_to_f16x2(r[2 * e + 1]),
+                                           e4m3x2_to_f16x2(r[2 * e] >> 16), e4m3x2_to_f16x2(r[2 * e + 1] >> 16)};
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma16816<true>(s[nt], f, qf[nt][2 * h + e][0], qf[nt][2 * h + e][1]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < 8; ++h) {  // matrices: keys 0-7, 8-15 of dimensions 16 h .. + 7, then of the next eight
+                uint32_t r[4];
+                const int row = lane & 15, ch = 2 * h + (lane >> 4);
+                ldsm4(r, kt + row * kRow + ((ch ^ (row & 7)) << 4));
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma16816<false>(s[nt], r, qf[nt][h][0], qf[nt][h][1]);
+            }
+        }
+        // ---- logits in log2 units: s[nt][2 x + e] is key oct + 8 x, row 2 quad + e
+        float ev[2] = {0.f, 0.f}, back[2] = {1.f, 1.f};
+        if (E4M3) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                uint32_t ks, vs;
+                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(ks) : "r"(kt + 2 * kTile + oct + 8 * x));
+                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(vs) : "r"(kt + 2 * kTile + kStep + oct + 8 * x));
+                vs = vs == 0 ? 127u : vs < 253u ? vs : 253u;  // 0: a page outside the pool; the limit: hidden places hold anything
+                const float k2 = scale_value(ks) * a.scale_log2;
+                ev[x] = static_cast<float>(static_cast<int>(vs) - 127);
+                back[x] = __uint_as_float((254u - vs) << 23);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) s[nt][2 * x + e] = fmaf(s[nt][2 * x + e], q_scale[nt][e] * k2, ev[x]);
+            }
+        } else {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[nt][e] *= a.scale_log2;
+        }
+        const int t0 = token_of(use, use.step);
+        const int last = use.s.pos0 + use.s.rows - 1;
+        if (t0 + kStep - 1 > use.s.pos0 || (a.n_local >= 0 && last - t0 > a.n_local && t0 + kStep - 1 >= a.n_sink)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int p = use.s.pos0 + (nt * 8 + 2 * quad + e) / a.g;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int t = t0 + oct + 8 * x;
+                        if (t > p || (a.n_local >= 0 && p - t > a.n_local && t >= a.n_sink)) s[nt][2 * x + e] = -INFINITY;
+                    }
+                }
+        }
+        // ---- references
+        bool high = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) high |= fmaxf(s[nt][e], s[nt][2 + e]) > m[nt][e] + kRaise;
+        if (__any_sync(0xFFFFFFFFu, high)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float top = fmaxf(s[nt][e], s[nt][2 + e]);
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
+                    top = fmaxf(top, m[nt][e]);
+                    const float alpha = top == -INFINITY ? 1.f : ex2(m[nt][e] - top);
+                    m[nt][e] = top;
+                    l[nt][e] *= alpha;
+#pragma unroll
+                    for (int h = 0; h < 8; ++h) {
+                        o[h][nt][e] *= alpha;
+                        o[h][nt][2 + e] *= alpha;
+                    }
+                }
+        }
+        // ---- weights, and P^T
+        uint32_t pf[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            float w[4];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float base = m[nt][e] == -INFINITY ? 0.f : m[nt][e];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    w[2 * x + e] = ex2(s[nt][2 * x + e] - base);
+                    l[nt][e] = fmaf(w[2 * x + e], back[x], l[nt][e]);
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+                pf[nt][x] = transpose8x8(E4M3 ? pack_f16x2(w[2 * x], w[2 * x + 1]) : pack_bf16x2(w[2 * x], w[2 * x + 1]));
+        }
+        // ---- O^T += V^T P^T
+        if (E4M3) {
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                uint32_t r[4];
+                const int row = lane & 15, ch = 2 * h + (lane >> 4);
+                ldsm4_t(r, vt + row * kRow + ((ch ^ (row & 7)) << 4));
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    // codes of dimensions (2 oct, 2 oct + 1) of two keys to one dimension of two keys
+                    const uint32_t y0 = __byte_perm(r[2 * e], 0, 0x3120), y1 = __byte_perm(r[2 * e + 1], 0, 0x3120);
+                    const uint32_t f[4] = {e4m3x2_to_f16x2(y0), e4m3x2_to_f16x2(y0 >> 16), e4m3x2_to_f16x2(y1), e4m3x2_to_f16x2(y1 >> 16)};
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma16816<true>(o[2 * h + e][nt], f, pf[nt][0], pf[nt][1]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < 8; ++h) {  // matrices: dimensions 16 h .. + 7 and the next eight of keys 0-7, then of keys 8-15
+                uint32_t r[4];
+                const int row = (lane & 7) + (lane >> 4) * 8, ch = 2 * h + ((lane >> 3) & 1);
+                ldsm4_t(r, vt + row * kRow + ((ch ^ (row & 7)) << 4));
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma16816<false>(o[h][nt], r, pf[nt][0], pf[nt][1]);
+            }
+        }
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+        if (use.step + 1 == use.x.n || i + 1 == n) {
+            end_item(from, use.step + 1);
+            if (i + 1 < n) {
+                advance(use);
+                begin_item();
+                from = 0;
+            }
+        } else {
+            ++use.step;
+        }
+    }
+    cp_async_wait<0>();
+}
+
+// Items that several runs of k_rows share: CTA (item, row), a warp for every eighth run, four dimensions a lane.
+__global__ void __launch_bounds__(256) k_rows_merge(const __grid_constant__ RowsArgs args, int64_t warps)
+{
+    __shared__ float s_o[8][kHeadDim], s_l[8], s_m[8];
+    pdl_enter();
+    const AttendView& a = args.a;
+    const int b = blockIdx.x / args.c.Hkv, j = blockIdx.x - b * args.c.Hkv, r = blockIdx.y;
+    const int64_t n = args.before[b + 1] - args.before[b];
+    if (n == 0) return;
+    const int64_t work = args.before[args.b.n_seqs] * args.c.Hkv, runs = runs_of(work, warps);
+    const int64_t x0 = args.before[b] * args.c.Hkv + n * j, x1 = x0 + n;
+    auto owner = [&](int64_t x) {
+        int64_t w = x * runs / work;
+        while (run_start(work, runs, w) > x) --w;
+        while (run_start(work, runs, w + 1) <= x) ++w;
+        return w;
+    };
+    const int64_t w0 = owner(x0), w1 = owner(x1 - 1);
+    if (w0 == w1) return;
+    const Seq s = seq_of(a, args.b, b);
+    if (r >= s.rows * a.g) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    auto part = [&](int64_t w) { return (2 * w + (w == w0)) * args.part_rows + r; };
+    // the reference of all runs, then each warp's sums against it
+    float top = -INFINITY;
+    for (int64_t w = w0 + threadIdx.x; w <= w1; w += 256) top = fmaxf(top, __ldcg(&args.part_ml[part(w)]).x);
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    if (lane == 0) s_m[warp] = top;
+    __syncthreads();
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, s_m[i]);
+    const float base = top == -INFINITY ? 0.f : top;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
+#pragma unroll 4
+    for (int64_t w = w0 + warp; w <= w1; w += 8) {
+        const float2 ml = __ldcg(&args.part_ml[part(w)]);
+        const float4 x = __ldcg(reinterpret_cast<const float4*>(args.part_o + part(w) * kHeadDim) + lane);
+        const float f = ex2(ml.x - base);
+        sum = fmaf(ml.y, f, sum);
+        acc.x = fmaf(x.x, f, acc.x);
+        acc.y = fmaf(x.y, f, acc.y);
+        acc.z = fmaf(x.z, f, acc.z);
+        acc.w = fmaf(x.w, f, acc.w);
+    }
+    *reinterpret_cast<float4*>(&s_o[warp][4 * lane]) = acc;
+    if (lane == 0) s_l[warp] = sum;
+    __syncthreads();
+    if (threadIdx.x >= kHeadDim) return;
+    float y = 0.f, total = 0.f;
+    for (int i = 0; i < 8; ++i) {
+        y += s_o[i][threadIdx.x];
+        total += s_l[i];
+    }
+    const int64_t row = s.row0 + r / a.g;
+    const int h = j * a.g + r % a.g;
+    static_cast<__nv_bfloat16*>(a.out)[row * a.out_stride + h * kHeadDim + threadIdx.x] =
+        __float2bfloat16_rn(total > 0.f ? y / total : 0.f);
+    if (a.lse && threadIdx.x == 0)
+        a.lse[row * a.Hq + h] = total > 0.f ? (top + __log2f(total)) * 0.6931471805599453f : -INFINITY;
+}
+
 // One warp per (row, query head): a key at a time, an online softmax in log2 units.
 template <bool E4M3>
 __global__ void __launch_bounds__(256) k_attend_warp(const AttendView a, const CacheView c, const BatchView b)
@@ -24,6 +614,7 @@ __global__ void __launch_bounds__(256) k_attend_warp(const AttendView a, const C
     int p = -1;
     const int seq = seq_of_row(b, row, &p);
     if (seq < 0 || row - b.row_start[seq] >= b.max_rows) return;
+    if (seq_of(a, b, seq).rows * a.g <= kRowsMax) return;  // k_rows'
     const int j = h / a.g;
     const auto* q = static_cast<const __nv_bfloat16*>(a.q) + row * a.q_stride + h * kHeadDim + 4 * lane;
     float x[4], o[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
@@ -70,24 +661,74 @@ __global__ void __launch_bounds__(256) k_attend_warp(const AttendView a, const C
 
 }  // namespace
 
+namespace {
+
+// Workspace regions (byte offsets); the status word comes first.
+struct AttendWs {
+    size_t before, part_ml, part_o, end;
+    int part_rows;
+};
+
+AttendWs attend_layout(int Hq, int Hkv, int n_seqs, int max_rows)
+{
+    AttendWs w{};
+    size_t off = 256;
+    auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off = align_up(off + bytes, kAlign);
+        return at;
+    };
+    const int64_t rows = static_cast<int64_t>(max_rows) * (Hq / Hkv);
+    w.part_rows = rows <= 8 ? 8 : kRowsMax;
+    w.before = take((static_cast<size_t>(n_seqs) + 1) * sizeof(int64_t));
+    w.part_ml = take(static_cast<size_t>(kMaxParts) * w.part_rows * sizeof(float2));
+    w.part_o = take(static_cast<size_t>(kMaxParts) * w.part_rows * kHeadDim * sizeof(float));
+    w.end = off;
+    return w;
+}
+
+template <int NT, bool E4M3>
+cudaError_t run_rows(const RowsArgs& r, int sms, cudaStream_t st)
+{
+    auto kern = k_rows<NT, E4M3>;
+    const size_t smem = rows_ring_bytes(E4M3) + (static_cast<size_t>(r.b.n_seqs) + 1) * sizeof(int64_t);
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e != cudaSuccess) return e;
+    e = launch_after(st, dim3(sms), kRowsThreads, smem, 1, kern, r);
+    if (e != cudaSuccess) return e;
+    const int64_t rows = static_cast<int64_t>(r.b.max_rows) * r.a.g;
+    return launch_after(st, dim3(r.b.n_seqs * r.c.Hkv, static_cast<unsigned>(rows < r.part_rows ? rows : r.part_rows)), 256, 0, 1,
+                        k_rows_merge, r, static_cast<int64_t>(sms) * kRowsWarps);
+}
+
+}  // namespace
+
 size_t attend_ws_bytes(int Hq, int Hkv, int n_seqs, int n_rows, int max_rows)
 {
-    (void)Hq;
-    (void)Hkv;
-    (void)n_seqs;
     (void)n_rows;
-    (void)max_rows;
-    return 256;
+    return attend_layout(Hq, Hkv, n_seqs, max_rows).end;
 }
 
 cudaError_t launch_attend(const AttendView& a, const CacheView& c, bool e4m3, const BatchView& b, uint8_t* ws,
                           uint64_t timeout_ns, cudaStream_t st)
 {
-    (void)ws;
     (void)timeout_ns;
-    const int64_t grid = (static_cast<int64_t>(b.n_rows) * a.Hq + 7) / 8;
-    if (grid > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
-    return launch_after(st, dim3(static_cast<unsigned>(grid)), 256, 0, 1, e4m3 ? k_attend_warp<true> : k_attend_warp<false>, a, c, b);
+    int sms = 0;
+    cudaError_t e = device_sms(&sms);
+    if (e != cudaSuccess) return e;
+    sms = sms < kMaxSms ? sms : kMaxSms;
+    const AttendWs lay = attend_layout(a.Hq, c.Hkv, b.n_seqs, b.max_rows);
+    RowsArgs r{a, c, b, reinterpret_cast<int64_t*>(ws + lay.before), reinterpret_cast<float*>(ws + lay.part_o),
+               reinterpret_cast<float2*>(ws + lay.part_ml), lay.part_rows};
+    const int64_t rows = static_cast<int64_t>(b.max_rows) * a.g;
+    if (rows > kRowsMax) {
+        const int64_t grid = (static_cast<int64_t>(b.n_rows) * a.Hq + 7) / 8;
+        if (grid > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
+        e = launch_after(st, dim3(static_cast<unsigned>(grid)), 256, 0, 1, e4m3 ? k_attend_warp<true> : k_attend_warp<false>, a, c, b);
+        if (e != cudaSuccess) return e;
+    }
+    if (rows <= 8) return e4m3 ? run_rows<1, true>(r, sms, st) : run_rows<1, false>(r, sms, st);
+    return e4m3 ? run_rows<2, true>(r, sms, st) : run_rows<2, false>(r, sms, st);
 }
 
 }  // namespace scale
