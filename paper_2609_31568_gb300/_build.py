@@ -19,8 +19,8 @@ ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2",
               "-Xptxas", "-v", "--use_fast_math", "-DNDEBUG"]
 SOURCES = ["api.cu", "reps.cu", "select.cu", "select_tok.cu", "attn.cu", "noalloc.cu", "decode.cu", "score.cu",
-           "cache_api.cu", "cache.cu", "attend.cu"]
-HEADERS = ["scale_internal.h", "ptx_sm103.cuh", "score.cuh", "launch.cuh", "tma_host.h", "cache.cuh"]
+           "cache_api.cu", "cache.cu", "attend.cu", "attend_chunk.cu"]
+HEADERS = ["scale_internal.h", "ptx_sm103.cuh", "score.cuh", "launch.cuh", "tma_host.h", "cache.cuh", "attend.cuh", "attn_mma.cuh"]
 
 
 def _nvcc() -> str:

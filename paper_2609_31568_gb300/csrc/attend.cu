@@ -2,7 +2,7 @@
 // paged cache (scale_cache_attend).
 #include <cuda_bf16.h>
 
-#include "cache.cuh"
+#include "attend.cuh"
 #include "launch.cuh"
 #include "ptx_sm103.cuh"
 #include "scale_internal.h"
@@ -12,36 +12,11 @@ namespace {
 
 using namespace scale_ptx;
 
-// ---------------------------------------------------------------- what a sequence asks for
-
-// Rows and keys of sequence b. Its computed rows are [row0, row0 + rows), tokens
-// pos0 .. pos0 + rows - 1; no row sees a key outside [0, n_sink) and [lo, pos0 + rows).
-struct Seq {
-    int row0, rows;
-    int pos0, lo;
-};
-
-__device__ __forceinline__ Seq seq_of(const AttendView& a, const BatchView& b, int i)
-{
-    Seq s;
-    s.row0 = b.row_start[i];
-    const int end = b.row_start[i + 1];
-    const int n = s.row0 < 0 || end <= s.row0 ? 0 : end - s.row0;
-    s.rows = n < b.max_rows ? n : b.max_rows;
-    if (s.rows > b.n_rows - s.row0) s.rows = b.n_rows - s.row0 > 0 ? b.n_rows - s.row0 : 0;
-    const int len = b.kv_len[i];
-    s.pos0 = (len > 0 ? len : 0) - n;
-    s.lo = a.n_local >= 0 && s.pos0 > a.n_local ? s.pos0 - a.n_local : 0;
-    return s;
-}
-
 // ---------------------------------------------------------------- few rows: decode
 
 constexpr int kStep = 16;       // keys of a step; a page holds whole steps
-constexpr int kRowsMax = 16;    // (token, query head) rows of a KV head that k_rows takes
 constexpr int kRowsWarps = 8;
 constexpr int kRowsThreads = 32 * kRowsWarps;
-constexpr int kMaxSms = 160;
 constexpr int kMaxParts = 2 * kMaxSms * kRowsWarps;  // partial results
 constexpr int kMinSteps = 2;    // steps of a warp before another one helps
 constexpr float kRaise = 8.0f;  // log2 units by which a logit may pass the reference
@@ -188,7 +163,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_rows(const __grid_constant_
         for (int i = i0; i < i1; ++i) {
             const Seq s = seq_of(a, bt, i);
             before[i] = sum;
-            if (s.rows > 0 && s.rows * a.g <= kRowsMax) sum += steps_of(a, s).n;
+            if (s.rows > 0 && few_rows(s, a.g)) sum += steps_of(a, s).n;
         }
         int64_t incl = sum;
         for (int o = 1; o < 32; o <<= 1) {
@@ -602,74 +577,17 @@ __global__ void __launch_bounds__(256) k_rows_merge(const __grid_constant__ Rows
         a.lse[row * a.Hq + h] = total > 0.f ? (top + __log2f(total)) * 0.6931471805599453f : -INFINITY;
 }
 
-// One warp per (row, query head): a key at a time, an online softmax in log2 units.
-template <bool E4M3>
-__global__ void __launch_bounds__(256) k_attend_warp(const AttendView a, const CacheView c, const BatchView b)
-{
-    pdl_enter();
-    const int lane = threadIdx.x & 31;
-    const int64_t task = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-    const int row = static_cast<int>(task / a.Hq), h = static_cast<int>(task - static_cast<int64_t>(row) * a.Hq);
-    if (row >= b.n_rows) return;
-    int p = -1;
-    const int seq = seq_of_row(b, row, &p);
-    if (seq < 0 || row - b.row_start[seq] >= b.max_rows) return;
-    if (seq_of(a, b, seq).rows * a.g <= kRowsMax) return;  // k_rows'
-    const int j = h / a.g;
-    const auto* q = static_cast<const __nv_bfloat16*>(a.q) + row * a.q_stride + h * kHeadDim + 4 * lane;
-    float x[4], o[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
-    for (int i = 0; i < 4; ++i) x[i] = __bfloat162float(q[i]);
-    const int lo = a.n_local >= 0 && p > a.n_local ? p - a.n_local : 0;
-    for (int t = 0; t <= p; ++t) {
-        if (t >= a.n_sink && t < lo) t = lo;
-        const int place = cache_row(c, b, seq, t);
-        float k[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
-        if (place >= 0) {
-            const int64_t at = (static_cast<int64_t>(place) * c.Hkv + j) * kHeadDim + 4 * lane;
-            for (int kv = 0; kv < 2; ++kv) {
-                uint2 w;
-                if (E4M3) {
-                    const int page = place / c.page_size;
-                    const uint8_t s = (kv ? c.vs : c.ks)[(static_cast<int64_t>(page) * c.Hkv + j) * c.page_size + place - page * c.page_size];
-                    w = e4m3x4_to_bf16(*reinterpret_cast<const uint32_t*>((kv ? c.v : c.k) + at), scale_value(s));
-                } else {
-                    w = *reinterpret_cast<const uint2*>((kv ? c.v : c.k) + 2 * at);
-                }
-                float* y = kv ? v : k;
-                y[0] = __uint_as_float(w.x << 16);
-                y[1] = __uint_as_float(w.x & 0xFFFF0000u);
-                y[2] = __uint_as_float(w.y << 16);
-                y[3] = __uint_as_float(w.y & 0xFFFF0000u);
-            }
-        }
-        float s = 0.f;
-        for (int i = 0; i < 4; ++i) s += x[i] * k[i];
-        for (int i = 16; i > 0; i >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, i);
-        s *= a.scale_log2;
-        const float m_new = fmaxf(m, s);
-        const float base = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = ex2(m - base), w = ex2(s - base);
-        l = l * alpha + w;
-        for (int i = 0; i < 4; ++i) o[i] = o[i] * alpha + w * v[i];
-        m = m_new;
-    }
-    const float inv = l > 0.f ? 1.0f / l : 0.f;
-    auto* out = static_cast<__nv_bfloat16*>(a.out) + row * a.out_stride + h * kHeadDim + 4 * lane;
-    for (int i = 0; i < 4; ++i) out[i] = __float2bfloat16_rn(o[i] * inv);
-    if (a.lse && lane == 0) a.lse[static_cast<int64_t>(row) * a.Hq + h] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
-}
-
 }  // namespace
 
 namespace {
 
 // Workspace regions (byte offsets); the status word comes first.
 struct AttendWs {
-    size_t before, part_ml, part_o, end;
+    size_t before, part_ml, part_o, chunks, end;
     int part_rows;
 };
 
-AttendWs attend_layout(int Hq, int Hkv, int n_seqs, int max_rows)
+AttendWs attend_layout(int Hq, int Hkv, int n_seqs, int n_rows, int max_rows)
 {
     AttendWs w{};
     size_t off = 256;
@@ -683,6 +601,7 @@ AttendWs attend_layout(int Hq, int Hkv, int n_seqs, int max_rows)
     w.before = take((static_cast<size_t>(n_seqs) + 1) * sizeof(int64_t));
     w.part_ml = take(static_cast<size_t>(kMaxParts) * w.part_rows * sizeof(float2));
     w.part_o = take(static_cast<size_t>(kMaxParts) * w.part_rows * kHeadDim * sizeof(float));
+    w.chunks = take(rows > kRowsMax ? chunk_ws_bytes(Hq / Hkv, Hkv, n_seqs, n_rows, max_rows) : 0);
     w.end = off;
     return w;
 }
@@ -705,27 +624,26 @@ cudaError_t run_rows(const RowsArgs& r, int sms, cudaStream_t st)
 
 size_t attend_ws_bytes(int Hq, int Hkv, int n_seqs, int n_rows, int max_rows)
 {
-    (void)n_rows;
-    return attend_layout(Hq, Hkv, n_seqs, max_rows).end;
+    return attend_layout(Hq, Hkv, n_seqs, n_rows, max_rows).end;
 }
 
 cudaError_t launch_attend(const AttendView& a, const CacheView& c, bool e4m3, const BatchView& b, uint8_t* ws,
                           uint64_t timeout_ns, cudaStream_t st)
 {
-    (void)timeout_ns;
     int sms = 0;
     cudaError_t e = device_sms(&sms);
     if (e != cudaSuccess) return e;
     sms = sms < kMaxSms ? sms : kMaxSms;
-    const AttendWs lay = attend_layout(a.Hq, c.Hkv, b.n_seqs, b.max_rows);
+    const AttendWs lay = attend_layout(a.Hq, c.Hkv, b.n_seqs, b.n_rows, b.max_rows);
     RowsArgs r{a, c, b, reinterpret_cast<int64_t*>(ws + lay.before), reinterpret_cast<float*>(ws + lay.part_o),
                reinterpret_cast<float2*>(ws + lay.part_ml), lay.part_rows};
     const int64_t rows = static_cast<int64_t>(b.max_rows) * a.g;
     if (rows > kRowsMax) {
-        const int64_t grid = (static_cast<int64_t>(b.n_rows) * a.Hq + 7) / 8;
-        if (grid > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
-        e = launch_after(st, dim3(static_cast<unsigned>(grid)), 256, 0, 1, e4m3 ? k_attend_warp<true> : k_attend_warp<false>, a, c, b);
-        if (e != cudaSuccess) return e;
+        // One sequence that may have many rows: whatever it has goes there. A batch is split by what its
+        // sequences have, which only the device knows.
+        const int few = b.n_seqs == 1 ? 0 : kRowsMax;
+        e = launch_chunks(a, c, e4m3, b, few, sms, reinterpret_cast<int32_t*>(ws + kStatusOffset), ws + lay.chunks, timeout_ns, st);
+        if (e != cudaSuccess || few == 0) return e;
     }
     if (rows <= 8) return e4m3 ? run_rows<1, true>(r, sms, st) : run_rows<1, false>(r, sms, st);
     return e4m3 ? run_rows<2, true>(r, sms, st) : run_rows<2, false>(r, sms, st);

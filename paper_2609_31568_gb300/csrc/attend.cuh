@@ -1,0 +1,41 @@
+// attend.cuh -- what the two routes of scale_cache_attend share: the rows and
+// keys of a sequence, and which route takes it.
+#pragma once
+
+#include "cache.cuh"
+
+namespace scale {
+
+constexpr int kRowsMax = 16;  // (token, query head) rows of a KV head that k_rows takes
+constexpr int kMaxSms = 160;  // SMs that a call uses at most
+
+// Rows and keys of sequence b. Its computed rows are [row0, row0 + rows), tokens
+// pos0 .. pos0 + rows - 1; no row sees a key outside [0, n_sink) and [lo, pos0 + rows).
+struct Seq {
+    int row0, rows;
+    int pos0, lo;
+};
+
+__device__ __forceinline__ Seq seq_of(const AttendView& a, const BatchView& b, int i)
+{
+    Seq s;
+    s.row0 = b.row_start[i];
+    const int end = b.row_start[i + 1];
+    const int n = s.row0 < 0 || end <= s.row0 ? 0 : end - s.row0;
+    s.rows = n < b.max_rows ? n : b.max_rows;
+    if (s.rows > b.n_rows - s.row0) s.rows = b.n_rows - s.row0 > 0 ? b.n_rows - s.row0 : 0;
+    const int len = b.kv_len[i];
+    s.pos0 = (len > 0 ? len : 0) - n;
+    s.lo = a.n_local >= 0 && s.pos0 > a.n_local ? s.pos0 - a.n_local : 0;
+    return s;
+}
+
+// Whether k_rows takes the sequence (when its call has that route).
+__device__ __forceinline__ bool few_rows(const Seq& s, int g) { return s.rows <= kRowsMax && s.rows * g <= kRowsMax; }
+
+// Sequences with more than `few` rows per KV head (tokens times query heads), on the tensor cores.
+size_t chunk_ws_bytes(int g, int Hkv, int n_seqs, int n_rows, int max_rows);
+cudaError_t launch_chunks(const AttendView& a, const CacheView& c, bool e4m3, const BatchView& b, int few, int sms,
+                          int32_t* status, uint8_t* ws, uint64_t timeout_ns, cudaStream_t st);
+
+}  // namespace scale

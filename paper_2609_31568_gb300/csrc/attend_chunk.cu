@@ -1,0 +1,813 @@
+// attend_chunk.cu -- attention of many new tokens of a sequence over its paged
+// cache, on the tensor cores (scale_cache_attend's route for more than kRowsMax
+// rows per KV head).
+//
+// A query tile is 128 rows (token, query head) of one KV head: 128 / g tokens with
+// the g query heads that share its keys, which one TMA box of g heads lays down in
+// that order. A CTA holds two tiles of neighbouring tokens, walks the 128-key tiles
+// of the sequence that some row of them sees, and is otherwise built as
+// k_sparse_attn (attn.cu): a TMA producer, one thread that issues tcgen05.mma, two
+// groups of four softmax warps with S, P and O in TMEM. What differs:
+//  - a key tile is gathered from pages of any multiple of 16 tokens, in boxes of
+//    the largest power of two that divides the page, one lane of the producer's
+//    warp per box;
+//  - 8-bit keys and values land as codes and four further warps turn them into the
+//    bf16 tiles, exactly, scales and all, so the products are those of a bf16 cache
+//    that holds the same values;
+//  - k_chunk_plan lays out the work: the query tiles of all sequences, and where those
+//    are fewer than the SMs keep busy, each cut along its keys, with (O, reference,
+//    sum) of the pieces merged by k_chunk_merge.
+#include <cuda_bf16.h>
+
+#include "attend.cuh"
+#include "attn_mma.cuh"
+#include "launch.cuh"
+#include "tma_host.h"
+
+namespace scale {
+namespace {
+
+constexpr int kTile = 128;            // keys of a tile, rows of a query tile
+constexpr int kPlanThreads = 1024;
+constexpr int kCuts = 3;              // pieces per SM that the plan considers, at most
+constexpr int kPieceTiles = 6;        // what a CTA's start and end take, in key tiles
+
+// A CTA's work. Rows [row0, row0 + ntok) of the row tensors are tokens pos ..; key tiles
+// [k0, k1) of those the job's rows see; slot >= 0: partial results there.
+struct ChunkJob {
+    int b, j, row0, ntok;
+    int pos, k0, k1, slot;
+};
+
+// Pieces of a query tile that k_chunk_merge puts together.
+struct ChunkMerge {
+    int j, row0, ntok, slot;
+    int pieces, pad[3];
+};
+
+struct ChunkPlan {
+    int32_t* counts;  // jobs, merges
+    ChunkJob* jobs;
+    ChunkMerge* merges;
+    int max_jobs, max_merges, max_slots;
+};
+
+struct ChunkArgs {
+    AttendView a;
+    CacheView c;
+    BatchView b;
+    ChunkPlan p;
+    int few;           // sequences of at most so many rows per KV head are not ours
+    int sms;
+    int tile_tokens;   // tokens of a query tile
+    int box;           // tokens of a TMA box: divides the page and the key tile
+    float* part_o;     // [slots][2 tiles or 1][128][128]
+    float2* part_ml;   // [slots][2 tiles or 1][128] (reference, sum)
+    int part_rows;     // 256 or 128
+    int32_t* status;
+    uint64_t timeout_ns;
+};
+
+// Key tiles that rows at tokens [pos, pos + n) see: those of the sinks, then from
+// the window's first. One tile of which nothing is seen for rows before the first token.
+struct Tiles {
+    int sinks, first, n;
+};
+__device__ __forceinline__ Tiles tiles_of(const AttendView& a, int pos, int n)
+{
+    Tiles t;
+    const int last = pos + n - 1;
+    const int lo = a.n_local >= 0 && pos > a.n_local ? pos - a.n_local : 0;
+    t.first = lo / kTile;
+    const int sinks = static_cast<int>((static_cast<int64_t>(a.n_sink) + kTile - 1) / kTile);
+    t.sinks = sinks < t.first ? sinks : t.first;
+    t.n = last < 0 ? 1 : t.sinks + last / kTile + 1 - t.first;
+    return t;
+}
+
+__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* s_warp, int64_t* total)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int64_t incl = x;
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane >= o) incl += y;
+    }
+    __syncthreads();  // the scan before is read
+    if (lane == 31) s_warp[warp] = incl;
+    __syncthreads();
+    if (warp == 0) {
+        int64_t v = lane < static_cast<int>(blockDim.x) / 32 ? s_warp[lane] : 0;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t y = __shfl_up_sync(0xFFFFFFFFu, v, o);
+            if (lane >= o) v += y;
+        }
+        s_warp[lane] = v;
+    }
+    __syncthreads();
+    *total = s_warp[31];
+    return incl - x + (warp ? s_warp[warp - 1] : 0);
+}
+
+// The list of jobs: one CTA. Items are (sequence, KV head, pair of query tiles), a KV head's pairs from the
+// last (the one with most keys) to the first, so that the CTAs running at a time share the keys of few heads.
+// Fewer than two items per SM are cut along their keys into pieces of at most C tiles: C is the one of W
+// / (f SMs), f = 1 .. kCuts, and "whole" for which ceil(pieces / SMs) rounds of C + kPieceTiles end first.
+__global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_constant__ ChunkArgs a)
+{
+    __shared__ int s_before[kMaxSeqs + 1];  // items (of one KV head) of the sequences before
+    __shared__ int64_t s_warp[32];
+    __shared__ int s_pieces[kCuts + 1], s_longest;
+    __shared__ unsigned long long s_work;
+    pdl_enter();
+    const int tid = threadIdx.x;
+    const int per_item = 2 * a.tile_tokens;
+    const int per = (a.b.n_seqs + kPlanThreads - 1) / kPlanThreads;
+    const int i0 = tid * per < a.b.n_seqs ? tid * per : a.b.n_seqs, i1 = i0 + per < a.b.n_seqs ? i0 + per : a.b.n_seqs;
+    int64_t mine = 0;
+    for (int i = i0; i < i1; ++i) {
+        const Seq s = seq_of(a.a, a.b, i);
+        s_before[i] = static_cast<int>(mine);
+        if (s.rows > 0 && static_cast<int64_t>(s.rows) * a.a.g > a.few) mine += (s.rows + per_item - 1) / per_item;
+    }
+    int64_t all;
+    const int64_t base = block_scan(mine, s_warp, &all);
+    const int64_t items = all * a.c.Hkv;
+    if (items > a.p.max_jobs) {  // row_start does not ascend within n_rows
+        if (tid == 0) {
+            record_status(a.status, SCALE_ERR_DEVICE);
+            a.p.counts[0] = a.p.counts[1] = 0;
+        }
+        return;
+    }
+    for (int i = i0; i < i1; ++i) s_before[i] += static_cast<int>(base);
+    if (tid == 0) {
+        s_before[a.b.n_seqs] = static_cast<int>(all);
+        s_work = 0;
+        s_longest = 0;
+        for (int f = 0; f <= kCuts; ++f) s_pieces[f] = 0;
+    }
+    __syncthreads();
+    // item x: sequences outermost, then KV heads, then pairs from the last
+    auto item = [&](int64_t x, ChunkJob* jb, Tiles* t) {
+        int lo = 0, hi = a.b.n_seqs;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (static_cast<int64_t>(s_before[mid]) * a.c.Hkv <= x) lo = mid;
+            else hi = mid;
+        }
+        const int n = s_before[lo + 1] - s_before[lo];
+        const int rem = static_cast<int>(x - static_cast<int64_t>(s_before[lo]) * a.c.Hkv);
+        const Seq s = seq_of(a.a, a.b, lo);
+        jb->b = lo;
+        jb->j = rem / n;
+        const int first = (n - 1 - (rem - jb->j * n)) * per_item;
+        jb->row0 = s.row0 + first;
+        jb->ntok = s.rows - first < per_item ? s.rows - first : per_item;
+        jb->pos = s.pos0 + first;
+        *t = tiles_of(a.a, jb->pos, jb->ntok);
+        jb->k0 = 0;
+        jb->k1 = t->n;
+        jb->slot = -1;
+    };
+    if (items > 2 * a.sms || items == 0) {
+        for (int64_t x = tid; x < items; x += kPlanThreads) {
+            ChunkJob jb;
+            Tiles t;
+            item(x, &jb, &t);
+            a.p.jobs[x] = jb;
+        }
+        if (tid == 0) {
+            a.p.counts[0] = static_cast<int>(items);
+            a.p.counts[1] = 0;
+        }
+        return;
+    }
+    // at most 2 kMaxSms items: one per thread
+    ChunkJob jb{};
+    Tiles t{};
+    if (tid < items) {
+        item(tid, &jb, &t);
+        atomicAdd(&s_work, static_cast<unsigned long long>(t.n));
+        atomicMax(&s_longest, t.n);
+    }
+    __syncthreads();
+    int cut[kCuts + 1];
+    cut[0] = s_longest;
+    for (int f = 1; f <= kCuts; ++f) {
+        const int64_t len = (static_cast<int64_t>(s_work) + static_cast<int64_t>(f) * a.sms - 1) / (static_cast<int64_t>(f) * a.sms);
+        cut[f] = len < 2 ? 2 : static_cast<int>(len);
+    }
+    if (tid < items)
+        for (int f = 0; f <= kCuts; ++f) atomicAdd(&s_pieces[f], (t.n + cut[f] - 1) / cut[f]);
+    __syncthreads();
+    int best = 0;
+    int64_t best_time = 0;
+    for (int f = 0; f <= kCuts; ++f) {
+        const int64_t rounds = (s_pieces[f] + a.sms - 1) / a.sms;
+        const int64_t time = rounds * (cut[f] + kPieceTiles);
+        if (f == 0 || time < best_time) {
+            best = f;
+            best_time = time;
+        }
+    }
+    const int pieces = tid < items ? (t.n + cut[best] - 1) / cut[best] : 0;
+    int64_t jobs, slots, merges;
+    const int64_t at = block_scan(pieces, s_warp, &jobs);
+    const int64_t slot = block_scan(pieces > 1 ? pieces : 0, s_warp, &slots);
+    const int64_t merge = block_scan(pieces > 1 ? 1 : 0, s_warp, &merges);
+    if (jobs > a.p.max_jobs || slots > a.p.max_slots || merges > a.p.max_merges) {  // as above
+        if (tid == 0) {
+            record_status(a.status, SCALE_ERR_DEVICE);
+            a.p.counts[0] = a.p.counts[1] = 0;
+        }
+        return;
+    }
+    for (int i = 0; i < pieces; ++i) {
+        ChunkJob x = jb;
+        x.k0 = static_cast<int>(static_cast<int64_t>(t.n) * i / pieces);
+        x.k1 = static_cast<int>(static_cast<int64_t>(t.n) * (i + 1) / pieces);
+        x.slot = pieces > 1 ? static_cast<int>(slot) + i : -1;
+        a.p.jobs[at + i] = x;
+    }
+    if (pieces > 1) a.p.merges[merge] = ChunkMerge{jb.j, jb.row0, jb.ntok, static_cast<int>(slot), pieces, {0, 0, 0}};
+    if (tid == 0) {
+        a.p.counts[0] = static_cast<int>(jobs);
+        a.p.counts[1] = static_cast<int>(merges);
+    }
+}
+
+// Dynamic shared memory (offsets from the 1024-aligned base).
+constexpr uint32_t kOffQ = 0;
+constexpr uint32_t kOffK = kOffQ + 2 * kTileBytes;
+constexpr uint32_t kOffV = kOffK + 2 * kTileBytes;
+constexpr uint32_t kOffRaw = kOffV + 2 * kTileBytes;  // 8-bit: codes of a K tile, then of a V tile
+constexpr uint32_t kRawBytes = kTile * kHeadDim;
+__host__ __device__ constexpr uint32_t chunk_smem(bool e4m3) { return kOffRaw + (e4m3 ? 2 * kRawBytes : 0) + 1024; }
+
+struct RawBarriers {
+    uint64_t full[2], empty[2];  // codes of K, of V: landed; turned
+};
+
+// Threads: warps 0-7 softmax, 8 producer, 9 MMA; 8-bit: 12-15 turn codes into bf16 (10 and 11 idle, for whole
+// groups of four warps in the register split: 2 x 128 x 200 + 2 x 128 x 56 = 512 x 128).
+__host__ __device__ constexpr int chunk_threads(bool e4m3) { return e4m3 ? 512 : 320; }
+
+template <bool E4M3>
+__global__ void __launch_bounds__(chunk_threads(E4M3), 1)
+k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
+        const __grid_constant__ CUtensorMap tv, const __grid_constant__ ChunkArgs a)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ Barriers bars;
+    __shared__ RawBarriers raw;
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile int abort_flag;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        abort_flag = 0;
+        mbar_init(&bars.q_full, 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&bars.kv_full[i], E4M3 ? 128 : 1);
+            mbar_init(&bars.s_full[i][0], 1);
+            mbar_init(&bars.s_full[i][1], 1);
+            mbar_init(&bars.p_full[i], 128);
+            mbar_init(&raw.full[i], 1);
+            mbar_init(&raw.empty[i], 128);
+        }
+        mbar_init(&bars.o_full, 1);
+        mbar_init(&bars.drain, 1);
+        fence_barrier_init();
+    }
+    if (tid == 256) {
+        tma_prefetch_desc(&tq);
+        tma_prefetch_desc(&tk);
+        tma_prefetch_desc(&tv);
+    }
+    __syncthreads();
+    pdl_enter();
+    const int n_jobs = a.p.counts[0];
+    const int4 j0 = reinterpret_cast<const int4*>(a.p.jobs + blockIdx.x)[0];
+    const int4 j1 = reinterpret_cast<const int4*>(a.p.jobs + blockIdx.x)[1];
+    if (static_cast<int>(blockIdx.x) >= n_jobs) return;
+    const ChunkJob job{j0.x, j0.y, j0.z, j0.w, j1.x, j1.y, j1.z, j1.w};
+    const int tt = a.tile_tokens, g = a.a.g;
+    const int nq = job.ntok > tt ? 2 : 1;
+    const int last = job.pos + job.ntok - 1;  // token of the last row
+    const int lo = a.a.n_local >= 0 && job.pos > a.a.n_local ? job.pos - a.a.n_local : 0;
+    const Tiles tiles = tiles_of(a.a, job.pos, job.ntok);
+    const int T = job.k1 - job.k0;
+    // first token of the job's key tile t
+    auto token_of = [&](int t) {
+        const int i = job.k0 + t;
+        return (i < tiles.sinks ? i : tiles.first + i - tiles.sinks) * kTile;
+    };
+    // whether some key of the tile at t0 is seen by no row: not seen(t) = t > last or (t < lo and t >= n_sink)
+    auto has_unseen = [&](int t0) { return t0 + kTile - 1 > last || (t0 < lo && t0 + kTile - 1 >= a.a.n_sink); };
+
+    uint8_t* smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+    if (warp == 9) {
+        tmem_alloc(&tmem_slot, 512);
+        tmem_relinquish();
+    }
+    // rows of a query tile past its g tt: zeros
+    if (g * tt < kTile) {
+        const int n = (kTile - g * tt) * 8;  // 16-byte pieces of a half
+        for (int i = tid; i < 4 * n; i += chunk_threads(E4M3)) {
+            const int part = i / n, x = i - part * n;
+            *reinterpret_cast<uint4*>(smem + kOffQ + part * kHalf + g * tt * 128 + x * 16) = make_uint4(0, 0, 0, 0);
+        }
+        fence_proxy_async_smem();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+
+    if (warp >= 8) {
+        if (E4M3) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (warp == 8) {
+            // ------------------------------------------------------------ producer: a lane per box
+            const int boxes = kTile / a.box;
+            const int halves = E4M3 ? 1 : 2;
+            const int bx = lane / halves, hf = lane - bx * halves;  // 8 boxes of 16 tokens at most: 16 lanes
+            const bool mine = bx < boxes;
+            const int32_t pool_rows = a.c.num_pages * a.c.page_size;
+            if (lane == 0) {
+                mbar_arrive_expect_tx(&bars.q_full, static_cast<uint32_t>(nq * 2 * g * tt * 128));
+                for (int qt = 0; qt < nq; ++qt)
+                    for (int h = 0; h < 2; ++h)
+                        tma_load_3d(smem + kOffQ + qt * kTileBytes + h * kHalf, &tq, &bars.q_full, h * 64, job.j * g,
+                                    job.row0 + qt * tt);
+            }
+            uint64_t* const s_last = bars.s_full[nq - 1];
+            int steps = 0, issued_k = 0, issued_v = 0;
+            int32_t row_v = 0;  // pool row of this lane's box in tile t - 1
+            auto row_of = [&](int t) {
+                const int r = mine ? cache_row(a.c, a.b, job.b, token_of(t) + bx * a.box) : 0;
+                return r < 0 ? pool_rows : r;  // past the end: zeros
+            };
+            int32_t row_k = T > 0 ? row_of(0) : 0;
+            for (int t = 0; t <= T; ++t) {
+                const int st = t & 1;
+                bool ok = true;
+                if (E4M3) {
+                    // K(t) into the raw K tile, V(t - 1) into the raw V tile, once the tile before was turned
+                    for (int kv = 1; kv >= 0; --kv) {
+                        if (kv ? t == 0 : t == T) continue;
+                        const int u = kv ? t - 1 : t;
+                        if (u > 0 && !mbar_wait_bounded(&raw.empty[kv], (u - 1) & 1, a.timeout_ns, &abort_flag)) ok = false;
+                        ok = __all_sync(0xFFFFFFFFu, ok);
+                        if (!ok) break;
+                        if (lane == 0) mbar_arrive_expect_tx(&raw.full[kv], kRawBytes);
+                        if (kv) ++issued_v;
+                        else ++issued_k;
+                        __syncwarp();
+                        if (mine)
+                            tma_load_3d(smem + kOffRaw + kv * kRawBytes + bx * a.box * kHeadDim, kv ? &tv : &tk, &raw.full[kv], 0,
+                                        job.j, kv ? row_v : row_k);
+                    }
+                } else {
+                    if (t >= 2 && !mbar_wait_bounded(&s_last[st], ((t - 2) >> 1) & 1, a.timeout_ns, &abort_flag)) ok = false;
+                    ok = __all_sync(0xFFFFFFFFu, ok);
+                    if (ok) {
+                        const bool has_k = t < T, has_v = t >= 1;
+                        if (lane == 0)
+                            mbar_arrive_expect_tx(&bars.kv_full[st], (has_k ? kTileBytes : 0u) + (has_v ? kTileBytes : 0u));
+                        ++steps;
+                        __syncwarp();
+                        const uint32_t to = hf * kHalf + bx * a.box * 128;
+                        if (mine && has_v)
+                            tma_load_3d(smem + kOffV + ((t - 1) & 1) * kTileBytes + to, &tv, &bars.kv_full[st], hf * 64, job.j, row_v);
+                        if (mine && has_k)
+                            tma_load_3d(smem + kOffK + st * kTileBytes + to, &tk, &bars.kv_full[st], hf * 64, job.j, row_k);
+                    }
+                }
+                if (!ok) {
+                    if (lane == 0) fail(&abort_flag, a.status);
+                    break;
+                }
+                row_v = row_k;
+                if (t + 1 < T) row_k = row_of(t + 1);
+            }
+            __syncwarp();
+            if (abort_flag && lane == 0) {
+                // every copy in flight lands before the CTA ends
+                mbar_wait_bounded(&bars.q_full, 0, a.timeout_ns, nullptr);
+                const int n0 = E4M3 ? issued_k : (steps + 1) / 2, n1 = E4M3 ? issued_v : steps / 2;
+                if (n0) mbar_wait_bounded(E4M3 ? &raw.full[0] : &bars.kv_full[0], (n0 - 1) & 1, a.timeout_ns, nullptr);
+                if (n1) mbar_wait_bounded(E4M3 ? &raw.full[1] : &bars.kv_full[1], (n1 - 1) & 1, a.timeout_ns, nullptr);
+            }
+        } else if (warp == 9) {
+            // ------------------------------------------------------------ MMA issuer
+            if (lane == 0) {
+                const uint32_t id_qk = idesc_bf16_f32(128, 128, 0);
+                const uint32_t id_pv = idesc_bf16_f32(128, 128, 1);
+                bool ok = mbar_wait_bounded(&bars.q_full, 0, a.timeout_ns, &abort_flag);
+                const uint64_t qdesc0 = sdesc_sw128(smem_addr(smem + kOffQ), 16, 1024);
+                const uint64_t kdesc0 = sdesc_sw128(smem_addr(smem + kOffK), 16, 1024);
+                const uint64_t vdesc0 = sdesc_sw128(smem_addr(smem + kOffV), kHalf, 1024);
+                // the last key tile may lie after every row of the first query tile
+                const bool skip_last = T > 1 && token_of(T - 1) > job.pos + tt - 1;
+                if (ok)
+                    ok = nq == 2 ? mma_issue_loop<2>(&bars, tmem, qdesc0, kdesc0, vdesc0, id_qk, id_pv, T, skip_last,
+                                                     a.timeout_ns, &abort_flag)
+                                 : mma_issue_loop<1>(&bars, tmem, qdesc0, kdesc0, vdesc0, id_qk, id_pv, T, false,
+                                                     a.timeout_ns, &abort_flag);
+                if (!ok) {
+                    fail(&abort_flag, a.status);
+                    mma_commit(&bars.drain);
+                    mbar_wait_bounded(&bars.drain, 0, a.timeout_ns, nullptr);
+                }
+            }
+        } else if (E4M3 && warp >= 12) {
+            // ------------------------------------------------------------ codes to bf16
+            // Eight lanes take a row, 16 codes each; 16 rows of a pass lie in one page. The two 16-byte
+            // pieces of bf16 go to the swizzled place, the lanes of the second half in the other order, so that
+            // eight lanes write 128 bytes of different banks.
+            const int x = tid - 384, sub = x & 7, r16 = x >> 3;
+            bool ok = true;
+            uint32_t vscale[2] = {0, 0};  // scale bytes of the V rows of tile t - 1 (passes 0-3, 4-7)
+            uint64_t* const s_last = bars.s_full[nq - 1];
+            for (int t = 0; t <= T && ok; ++t) {
+                const int st = t & 1;
+                uint32_t kscale[2] = {0, 0}, vnext[2] = {0, 0};
+                if (t < T) {
+                    const int t0 = token_of(t);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int place = cache_row(a.c, a.b, job.b, t0 + 16 * i);
+                        uint32_t ks = 0, vs = 0;
+                        if (place >= 0) {
+                            const int page = place / a.c.page_size;
+                            const int64_t at = (static_cast<int64_t>(page) * a.c.Hkv + job.j) * a.c.page_size + place - page * a.c.page_size + r16;
+                            ks = a.c.ks[at];
+                            vs = a.c.vs[at];
+                        }
+                        kscale[i >> 2] |= ks << (8 * (i & 3));
+                        vnext[i >> 2] |= vs << (8 * (i & 3));
+                    }
+                }
+                // the bf16 tiles of this step were last read by MMAs of step t - 2
+                if (t >= 2) ok = mbar_wait_bounded(&s_last[st], ((t - 2) >> 1) & 1, a.timeout_ns, &abort_flag);
+                for (int kv = 1; kv >= 0 && ok; --kv) {
+                    if (kv ? t == 0 : t == T) continue;
+                    const int u = kv ? t - 1 : t;
+                    ok = mbar_wait_bounded(&raw.full[kv], u & 1, a.timeout_ns, &abort_flag);
+                    if (!ok) break;
+                    const uint8_t* from = smem + kOffRaw + kv * kRawBytes;
+                    uint8_t* to = smem + (kv ? kOffV : kOffK) + (u & 1) * kTileBytes + (sub >> 2) * kHalf;
+                    const int t0 = token_of(u);
+                    const bool unseen = kv && has_unseen(t0);
+#pragma unroll 2
+                    for (int i = 0; i < 8; ++i) {
+                        const int row = 16 * i + r16;
+                        const uint4 w = *reinterpret_cast<const uint4*>(from + row * kHeadDim + sub * 16);
+                        const float s = scale_value(((kv ? vscale[i >> 2] : kscale[i >> 2]) >> (8 * (i & 3))) & 255u);
+                        const uint2 y0 = e4m3x4_to_bf16(w.x, s), y1 = e4m3x4_to_bf16(w.y, s);
+                        const uint2 y2 = e4m3x4_to_bf16(w.z, s), y3 = e4m3x4_to_bf16(w.w, s);
+                        uint4 p = make_uint4(y0.x, y0.y, y1.x, y1.y), q = make_uint4(y2.x, y2.y, y3.x, y3.y);
+                        if (unseen) {
+                            const int tok = t0 + row;
+                            if (tok > last || (tok < lo && tok >= a.a.n_sink)) p = q = make_uint4(0, 0, 0, 0);
+                        }
+                        const int c0 = 2 * (sub & 3), late = sub >> 2;
+                        uint8_t* dst = to + row * 128;
+                        *reinterpret_cast<uint4*>(dst + (((c0 + late) ^ (row & 7)) << 4)) = late ? q : p;
+                        *reinterpret_cast<uint4*>(dst + (((c0 + 1 - late) ^ (row & 7)) << 4)) = late ? p : q;
+                    }
+                    mbar_arrive(&raw.empty[kv]);
+                }
+                if (!ok) break;
+                fence_proxy_async_smem();
+                mbar_arrive(&bars.kv_full[st]);
+                vscale[0] = vnext[0];
+                vscale[1] = vnext[1];
+            }
+            if (!ok) fail(&abort_flag, a.status);
+        }
+    } else {
+        if (E4M3) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+        if ((warp >> 2) < nq) {
+            // ------------------------------------------------------------ softmax + epilogue
+            const int qt = warp >> 2;
+            const int quarter = warp & 3;
+            const int r = quarter * 32 + lane;
+            const int pos_first = job.pos + qt * tt;                      // tokens of the tile
+            const int pos_last = qt + 1 == nq ? last : pos_first + tt - 1;
+            int p = pos_first + r / g;
+            p = p < pos_last ? p : pos_last;  // rows past the tile's end see what its last row sees
+            const uint32_t lane_base = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+            const uint32_t s_addr = lane_base + qt * 256;
+            const uint32_t o_addr = s_addr + 128;
+            float m_run = -INFINITY, l_run = 0.f;
+            bool ok = true;
+            // S row of a tile; columns [lim, 128) and [gap, low) are not seen
+            auto load_s = [&](uint32_t (&sr)[128], bool masked, int lim, int gap, int low) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    tmem_ld32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[c * 32]));
+                tmem_ld_wait();
+                if (masked) {
+#pragma unroll
+                    for (int c = 0; c < 128; ++c)
+                        if (c >= lim || (c >= gap && c < low)) sr[c] = 0xFF800000u;
+                }
+            };
+            // p = 2^(s scale - m) of keys [64 h, 64 h + 64) as bf16 pairs; returns their sum
+            auto exp_half = [&](const float* s, int h, float neg_m, uint32_t (&pk)[32]) {
+                float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    float x0, x1;
+                    ffma2(x0, x1, s[h * 64 + 2 * i], s[h * 64 + 2 * i + 1], a.a.scale_log2, a.a.scale_log2, neg_m, neg_m);
+                    x0 = ex2(x0);
+                    x1 = ex2(x1);
+                    const int jj = (i & 3) * 2;
+                    fadd2(acc[jj], acc[jj + 1], acc[jj], acc[jj + 1], x0, x1);
+                    pk[i] = pack_bf16x2(x0, x1);
+                }
+                return ((acc[0] + acc[1]) + (acc[2] + acc[3])) + ((acc[4] + acc[5]) + (acc[6] + acc[7]));
+            };
+            for (int t = 0; t < T; ++t) {
+                const bool got = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.s_full[qt][t & 1], (t >> 1) & 1, a.timeout_ns, &abort_flag));
+                if (!got) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const int t0 = token_of(t);
+                const bool masked = t0 + kTile - 1 > pos_first ||
+                                    (a.a.n_local >= 0 && pos_last - t0 > a.a.n_local && t0 + kTile - 1 >= a.a.n_sink);
+                const int lim = p - t0 + 1;  // keys t0 + c with c >= lim are in the future
+                const int gap = a.a.n_sink - t0, low = a.a.n_local >= 0 && p - t0 > a.a.n_local ? p - t0 - a.a.n_local : 0;
+                // The fast and the exact path of k_sparse_attn: exponentials against the reference as it
+                // stands unless the tile's sum shows a logit far above it.
+                bool exact = !__all_sync(0xFFFFFFFFu, m_run != -INFINITY);
+                float sum;
+#pragma unroll 1
+                for (;;) {
+                    uint32_t sr[128];
+                    load_s(sr, masked, lim, gap, low);
+                    const float* s = reinterpret_cast<const float*>(sr);
+                    if (exact) {
+                        float mx8[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) mx8[i] = s[i];
+#pragma unroll
+                        for (int c = 8; c < 120; c += 16)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) mx8[i] = fmax3(mx8[i], s[c + 2 * i], s[c + 2 * i + 1]);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) mx8[i] = fmaxf(mx8[i], s[120 + i]);
+                        const float mx = fmax3(fmax3(mx8[0], mx8[1], mx8[2]), fmax3(mx8[3], mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7]));
+                        const float m_new = fmaxf(m_run, mx * a.a.scale_log2);
+                        const bool raise = m_new > m_run + kRescaleThreshold;
+                        // the O rescale is warp-collective: taken by the whole warp when any row needs it
+                        if (__any_sync(0xFFFFFFFFu, raise)) {
+                            const float alpha = raise ? ex2(m_run - m_new) : 1.0f;
+                            l_run *= alpha;
+                            if (t > 0) {
+#pragma unroll 1
+                                for (int c = 0; c < 8; ++c) {
+                                    uint32_t v[16];
+                                    tmem_ld16(o_addr + c * 16, v);
+                                    tmem_ld_wait();
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
+                                    tmem_st16(o_addr + c * 16, v);
+                                }
+                            }
+                            if (raise) m_run = m_new;
+                        }
+                    }
+                    const float neg_m = (m_run == -INFINITY) ? 0.f : -m_run;
+                    uint32_t pk[2][32];
+                    sum = exp_half(s, 0, neg_m, pk[0]);
+                    sum += exp_half(s, 1, neg_m, pk[1]);
+                    if (!exact && __any_sync(0xFFFFFFFFu, !(sum <= kFastSumLimit))) {
+                        exact = true;
+                        continue;
+                    }
+                    tmem_st32(s_addr, pk[0]);
+                    tmem_st32(s_addr + 32, pk[1]);
+                    break;
+                }
+                l_run += sum;
+                tmem_st_wait();
+                if (!E4M3 && qt == 0 && has_unseen(t0)) {
+                    // value rows that no row of the CTA sees: 0 times what lies there may be NaN. The MMA thread
+                    // waits for this group before either tile's product with them.
+                    const bool landed = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.kv_full[(t + 1) & 1], ((t + 1) >> 1) & 1, a.timeout_ns, &abort_flag));
+                    if (!landed) {
+                        ok = false;
+                        break;
+                    }
+                    const int tok = t0 + r;
+                    if (tok > last || (tok < lo && tok >= a.a.n_sink)) {
+                        uint8_t* row = smem + kOffV + (t & 1) * kTileBytes + r * 128;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            *reinterpret_cast<uint4*>(row + (i >> 3) * kHalf + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async_smem();
+                }
+                tc_fence_before();
+                mbar_arrive(&bars.p_full[qt]);
+            }
+            bool go = __all_sync(0xFFFFFFFFu, ok && !abort_flag);
+            if (go) go = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.o_full, 0, a.timeout_ns, &abort_flag));
+            if (go) {
+                tc_fence_after();
+                // Every MMA is done and every copy landed, so the tiles in shared memory are free: a warp
+                // stages its 32 output rows there and stores whole rows.
+                const int rows = (qt + 1 == nq ? job.ntok - qt * tt : tt) * g - quarter * 32;  // of this warp, if more than 0
+                if (job.slot < 0) {
+                    const float inv_l = l_run > 0.f ? 1.0f / l_run : 0.f;
+                    uint32_t v[128];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tmem_ld32(o_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&v[c * 32]));
+                    tmem_ld_wait();
+                    uint8_t* stage = smem + kOffQ + qt * kTileBytes + quarter * 32 * 256;
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            w[i] = pack_bf16x2(__uint_as_float(v[8 * c + 2 * i]) * inv_l, __uint_as_float(v[8 * c + 2 * i + 1]) * inv_l);
+                        if (!(l_run > 0.f)) w[0] = w[1] = w[2] = w[3] = l_run == 0.f ? 0u : 0x7FFF7FFFu;  // no keys: 0; NaN stays
+                        *reinterpret_cast<uint4*>(stage + lane * 256 + ((c ^ (lane & 15)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                    __syncwarp();
+                    const int c = lane & 15;
+#pragma unroll 4
+                    for (int i = 0; i < 16; ++i) {
+                        const int x = 2 * i + (lane >> 4), rr = quarter * 32 + x;
+                        const uint4 w = *reinterpret_cast<const uint4*>(stage + x * 256 + ((c ^ (x & 15)) << 4));
+                        if (x < rows) {
+                            const int64_t row = job.row0 + qt * tt + rr / g;
+                            auto* out = static_cast<__nv_bfloat16*>(a.a.out) + row * a.a.out_stride + (job.j * g + rr % g) * kHeadDim;
+                            reinterpret_cast<uint4*>(out)[c] = w;
+                        }
+                    }
+                    if (a.a.lse && lane < rows)
+                        a.a.lse[static_cast<int64_t>(job.row0 + qt * tt + r / g) * a.a.Hq + job.j * g + r % g] =
+                            l_run == 0.f ? -INFINITY : (m_run + __log2f(l_run)) * 0.6931471805599453f;
+                } else {
+                    uint8_t* stage = smem + warp * 32 * 512;  // 128 KB: the Q and K tiles
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t v[32];
+                        tmem_ld32(o_addr + c * 32, v);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            *reinterpret_cast<uint4*>(stage + lane * 512 + (((c * 8 + i) ^ lane) << 4)) =
+                                make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                    }
+                    __syncwarp();
+                    const int64_t at = static_cast<int64_t>(job.slot) * a.part_rows + qt * kTile + quarter * 32;
+                    for (int x = 0; x < 32 && x < rows; ++x)
+                        reinterpret_cast<uint4*>(a.part_o + (at + x) * kHeadDim)[lane] =
+                            *reinterpret_cast<const uint4*>(stage + x * 512 + ((lane ^ x) << 4));
+                    if (lane < rows) a.part_ml[at + lane] = make_float2(m_run, l_run);
+                }
+            } else {
+                fail(&abort_flag, a.status);
+            }
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 9) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// Pieces of a query tile pair put together: a warp per row, four dimensions a lane.
+__global__ void __launch_bounds__(256) k_chunk_merge(const __grid_constant__ ChunkArgs a)
+{
+    pdl_enter();
+    if (static_cast<int>(blockIdx.x) >= a.p.counts[1]) return;
+    const ChunkMerge& mg = a.p.merges[blockIdx.x];
+    const int lane = threadIdx.x & 31, per_tile = a.tile_tokens * a.a.g;
+    const int x = blockIdx.y * 8 + (threadIdx.x >> 5);  // live row of the pair
+    if (x >= mg.ntok * a.a.g) return;
+    const int r = x < per_tile ? x : kTile + x - per_tile;  // its row of the tiles
+    float top = -INFINITY;
+    for (int i = lane; i < mg.pieces; i += 32)
+        top = fmaxf(top, __ldcg(&a.part_ml[static_cast<int64_t>(mg.slot + i) * a.part_rows + r]).x);
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    const float base = top == -INFINITY ? 0.f : top;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < mg.pieces; ++i) {
+        const int64_t at = static_cast<int64_t>(mg.slot + i) * a.part_rows + r;
+        const float2 ml = __ldcg(&a.part_ml[at]);
+        const float4 o = __ldcg(reinterpret_cast<const float4*>(a.part_o + at * kHeadDim) + lane);
+        const float f = ex2(ml.x - base);
+        sum = fmaf(ml.y, f, sum);
+        acc.x = fmaf(o.x, f, acc.x);
+        acc.y = fmaf(o.y, f, acc.y);
+        acc.z = fmaf(o.z, f, acc.z);
+        acc.w = fmaf(o.w, f, acc.w);
+    }
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    const int64_t row = mg.row0 + x / a.a.g;
+    const int h = mg.j * a.a.g + x % a.a.g;
+    auto* out = static_cast<__nv_bfloat16*>(a.a.out) + row * a.a.out_stride + h * kHeadDim;
+    reinterpret_cast<uint2*>(out)[lane] = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+    if (a.a.lse && lane == 0) a.a.lse[row * a.a.Hq + h] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * 0.6931471805599453f;
+}
+
+// Workspace regions (byte offsets from the route's part of the workspace).
+struct ChunkWs {
+    size_t counts, jobs, merges, part_ml, part_o, end;
+    int max_jobs, max_merges, max_slots, part_rows;
+};
+
+ChunkWs chunk_layout(int g, int Hkv, int n_seqs, int n_rows, int max_rows)
+{
+    ChunkWs w{};
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off = align_up(off + bytes, kAlign);
+        return at;
+    };
+    const int tt = kTile / g;
+    // every sequence adds one incomplete pair of tiles at most; none has more than max_rows
+    int64_t pairs = static_cast<int64_t>(n_rows) / (2 * tt) + n_seqs;
+    const int64_t each = (static_cast<int64_t>(max_rows) + 2 * tt - 1) / (2 * tt);
+    if (pairs > each * n_seqs) pairs = each * n_seqs;
+    const int64_t items = pairs * Hkv;
+    const int64_t cut = items < 2 * kMaxSms ? items : 2 * kMaxSms;  // items that may be cut
+    const int64_t slots = cut + kCuts * kMaxSms;
+    w.max_merges = static_cast<int>(cut);
+    w.max_jobs = static_cast<int>(items > slots ? items : slots);
+    w.max_slots = static_cast<int>(slots);
+    w.part_rows = max_rows > tt ? 2 * kTile : kTile;
+    w.counts = take(2 * sizeof(int32_t));
+    w.jobs = take(static_cast<size_t>(w.max_jobs) * sizeof(ChunkJob));
+    w.merges = take(static_cast<size_t>(w.max_merges) * sizeof(ChunkMerge));
+    w.part_ml = take(static_cast<size_t>(slots) * w.part_rows * sizeof(float2));
+    w.part_o = take(static_cast<size_t>(slots) * w.part_rows * kHeadDim * sizeof(float));
+    w.end = off;
+    return w;
+}
+
+template <bool E4M3>
+cudaError_t run_chunks(const ChunkArgs& a, cudaStream_t st)
+{
+    CUtensorMap tq, tk, tv;
+    const uint64_t pool = static_cast<uint64_t>(a.c.num_pages) * a.c.page_size;
+    bool ok = scale_host::make_rows_map(&tq, a.a.q, kHeadDim, a.a.Hq, a.a.q_stride, a.b.n_rows, a.a.g, a.tile_tokens);
+    if (E4M3)
+        ok = ok && scale_host::make_byte_rows_map(&tk, a.c.k, kHeadDim, a.c.Hkv, pool, a.box) &&
+             scale_host::make_byte_rows_map(&tv, a.c.v, kHeadDim, a.c.Hkv, pool, a.box);
+    else
+        ok = ok && scale_host::make_token_major_map(&tk, a.c.k, kHeadDim, a.c.Hkv, pool, 64, a.box) &&
+             scale_host::make_token_major_map(&tv, a.c.v, kHeadDim, a.c.Hkv, pool, 64, a.box);
+    if (!ok) return cudaErrorInvalidValue;
+    cudaError_t e = cudaFuncSetAttribute(k_chunk<E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(chunk_smem(E4M3)));
+    if (e == cudaSuccess) e = launch_after(st, dim3(1), kPlanThreads, 0, 1, k_chunk_plan, a);
+    if (e == cudaSuccess)
+        e = launch_after(st, dim3(a.p.max_jobs), chunk_threads(E4M3), chunk_smem(E4M3), 1, k_chunk<E4M3>, tq, tk, tv, a);
+    if (e == cudaSuccess) e = launch_after(st, dim3(a.p.max_merges, a.part_rows / 8), 256, 0, 1, k_chunk_merge, a);
+    return e;
+}
+
+}  // namespace
+
+size_t chunk_ws_bytes(int g, int Hkv, int n_seqs, int n_rows, int max_rows)
+{
+    return chunk_layout(g, Hkv, n_seqs, n_rows, max_rows).end;
+}
+
+cudaError_t launch_chunks(const AttendView& a, const CacheView& c, bool e4m3, const BatchView& b, int few, int sms,
+                          int32_t* status, uint8_t* ws, uint64_t timeout_ns, cudaStream_t st)
+{
+    const ChunkWs w = chunk_layout(a.g, c.Hkv, b.n_seqs, b.n_rows, b.max_rows);
+    ChunkArgs x{};
+    x.a = a;
+    x.c = c;
+    x.b = b;
+    x.p = ChunkPlan{reinterpret_cast<int32_t*>(ws + w.counts), reinterpret_cast<ChunkJob*>(ws + w.jobs),
+                    reinterpret_cast<ChunkMerge*>(ws + w.merges), w.max_jobs, w.max_merges, w.max_slots};
+    x.few = few;
+    x.sms = sms;
+    x.tile_tokens = kTile / a.g;
+    x.box = 16;
+    while (x.box < kTile && c.page_size % (2 * x.box) == 0) x.box *= 2;
+    x.part_o = reinterpret_cast<float*>(ws + w.part_o);
+    x.part_ml = reinterpret_cast<float2*>(ws + w.part_ml);
+    x.part_rows = w.part_rows;
+    x.status = status;
+    x.timeout_ns = timeout_ns;
+    return e4m3 ? run_chunks<true>(x, st) : run_chunks<false>(x, st);
+}
+
+}  // namespace scale

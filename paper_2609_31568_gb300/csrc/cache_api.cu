@@ -112,12 +112,13 @@ int check_turned(int heads, int most, const void* x, int64_t xs, const void* y, 
 
 constexpr int kMaxRopeHeads = 256;
 
-int check_attend(const scale_attend_t* a, const CacheView& c)
+int check_attend(const scale_attend_t* a, const CacheView& c, const BatchView& b)
 {
     if (!a || a->num_q_heads <= 0 || a->num_q_heads % c.Hkv || a->n_sink < 0 || !std::isfinite(a->attn_scale) ||
         a->attn_scale < 0.f)
         return SCALE_ERR_INVALID_ARG;
-    if (a->num_q_heads / c.Hkv > 32) return SCALE_ERR_UNSUPPORTED;
+    if (a->num_q_heads / c.Hkv > 32 || static_cast<int64_t>(b.n_rows) * a->num_q_heads >= (1ll << 37))
+        return SCALE_ERR_UNSUPPORTED;
     return SCALE_OK;
 }
 
@@ -231,7 +232,7 @@ int scale_cache_attend_workspace_size(const scale_attend_t* attend, const scale_
     int rc = check_cache(cache, &c, &e4m3);
     if (rc) return rc;
     if ((rc = check_batch(batch, &b))) return rc;
-    if ((rc = check_attend(attend, c))) return rc;
+    if ((rc = check_attend(attend, c, b))) return rc;
     if (!bytes) return SCALE_ERR_INVALID_ARG;
     *bytes = attend_ws_bytes(attend->num_q_heads, c.Hkv, b.n_seqs, b.n_rows, b.max_rows);
     return SCALE_OK;
@@ -247,7 +248,7 @@ int scale_cache_attend(const scale_attend_t* attend, const scale_cache_t* cache,
     int rc = check_cache(cache, &c, &e4m3);
     if (rc) return rc;
     if ((rc = check_batch(batch, &b))) return rc;
-    if ((rc = check_attend(attend, c))) return rc;
+    if ((rc = check_attend(attend, c, b))) return rc;
     const int Hq = attend->num_q_heads;
     if (!stride_ok(q_stride, Hq) || !stride_ok(out_stride, Hq)) return SCALE_ERR_INVALID_ARG;
     if (b.n_rows && overlap(q, q_stride, Hq, out, out_stride, Hq, b.n_rows)) return SCALE_ERR_INVALID_ARG;

@@ -71,4 +71,37 @@ inline bool make_dense_bf16_map(CUtensorMap* map, const void* base, uint32_t ran
     return r == CUDA_SUCCESS;
 }
 
+// A 3-D map over the rows of a bf16 tensor whose heads lie `head_dim` and whose rows
+// `row_stride` elements apart, with a box of 64 dimensions x box_h heads x box_t rows, 128-byte
+// swizzle, zeros outside. Returns false on failure.
+inline bool make_rows_map(CUtensorMap* map, const void* base, uint64_t head_dim, uint64_t n_heads, uint64_t row_stride,
+                          uint64_t n_rows, uint32_t box_h, uint32_t box_t)
+{
+    auto enc = tensor_map_encoder();
+    if (!enc) return false;
+    const cuuint64_t dims[3] = {head_dim, n_heads, n_rows};
+    const cuuint64_t strides[2] = {head_dim * 2, row_stride * 2};
+    const cuuint32_t box[3] = {64, box_h, box_t};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// A 3-D map over 8-bit rows [n_rows][n_heads][head_dim] with a box of one head of box_t rows, not
+// swizzled, zeros outside. Returns false on failure.
+inline bool make_byte_rows_map(CUtensorMap* map, const void* base, uint64_t head_dim, uint64_t n_heads, uint64_t n_rows,
+                               uint32_t box_t)
+{
+    auto enc = tensor_map_encoder();
+    if (!enc) return false;
+    const cuuint64_t dims[3] = {head_dim, n_heads, n_rows};
+    const cuuint64_t strides[2] = {head_dim, head_dim * n_heads};
+    const cuuint32_t box[3] = {static_cast<cuuint32_t>(head_dim), 1, box_t};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace scale_host
