@@ -51,13 +51,18 @@ struct RowsArgs {
     int part_rows;
 };
 
-__device__ __forceinline__ int64_t run_start(int64_t work, int64_t warps, int64_t w) { return work * w / warps; }
-
-// Warps that share the work.
-__device__ __forceinline__ int64_t runs_of(int64_t work, int64_t warps)
+// Steps of a run when `warps` warps share the work; the last runs may be shorter or none.
+__device__ __forceinline__ int64_t run_steps(int64_t work, int64_t warps)
 {
-    const int64_t n = (work + kMinSteps - 1) / kMinSteps;
-    return n < warps ? (n > 0 ? n : 1) : warps;
+    const int64_t n = work >> 32 ? (work + warps - 1) / warps
+                                 : (static_cast<uint32_t>(work) + static_cast<uint32_t>(warps) - 1) / static_cast<uint32_t>(warps);
+    return n < kMinSteps ? kMinSteps : n;
+}
+
+// x / n, mostly of 32-bit numbers.
+__device__ __forceinline__ int64_t run_of(int64_t x, int64_t n)
+{
+    return (x | n) >> 32 ? x / n : static_cast<uint32_t>(x) / static_cast<uint32_t>(n);
 }
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool real)
@@ -104,13 +109,6 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
-{
-    uint32_t r;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
 }
 
 // One KV head's item of a sequence, as a warp walks it.
@@ -181,12 +179,11 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_rows(const __grid_constant_
             for (int i = tid; i <= bt.n_seqs; i += kRowsThreads) args.before[i] = before[i];
     }
     const int64_t work = before[bt.n_seqs] * c.Hkv;
-    const int64_t runs = runs_of(work, static_cast<int64_t>(gridDim.x) * kRowsWarps);
+    const int64_t per_run = run_steps(work, static_cast<int64_t>(gridDim.x) * kRowsWarps);
     const int64_t run = static_cast<int64_t>(warp) * gridDim.x + blockIdx.x;  // the first runs on different SMs
-    if (run >= runs) return;
-    const int64_t x0 = run_start(work, runs, run);
-    const int64_t n = run_start(work, runs, run + 1) - x0;
-    if (n == 0) return;
+    const int64_t x0 = run * per_run;
+    if (x0 >= work) return;
+    const int64_t n = work - x0 < per_run ? work - x0 : per_run;
 
     const uint32_t ring = smem_addr(smem) + warp * kStages * rows_step_bytes(E4M3);
 
@@ -206,7 +203,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_rows(const __grid_constant_
         }
         enter(load, lo);
         const int64_t rem = x0 - before[load.b] * c.Hkv;
-        load.j = static_cast<int>(rem / load.x.n);
+        load.j = static_cast<int>(run_of(rem, load.x.n));
         load.step = static_cast<int>(rem - static_cast<int64_t>(load.j) * load.x.n);
         use = load;
     }
@@ -276,9 +273,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_rows(const __grid_constant_
                     }
                 top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
                 top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-                // |q| 2^-ex < 2^15, with both powers of two in range
-                int ex = static_cast<int>(top >> 23) - 127 - 14;
-                ex = ex < -100 ? -100 : ex;
+                const int ex = f16_exponent(top);
                 const float down = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
                 const float up = __uint_as_float(static_cast<uint32_t>(127 + ex) << 23);
 #pragma unroll
@@ -525,15 +520,9 @@ __global__ void __launch_bounds__(256) k_rows_merge(const __grid_constant__ Rows
     const int b = blockIdx.x / args.c.Hkv, j = blockIdx.x - b * args.c.Hkv, r = blockIdx.y;
     const int64_t n = args.before[b + 1] - args.before[b];
     if (n == 0) return;
-    const int64_t work = args.before[args.b.n_seqs] * args.c.Hkv, runs = runs_of(work, warps);
-    const int64_t x0 = args.before[b] * args.c.Hkv + n * j, x1 = x0 + n;
-    auto owner = [&](int64_t x) {
-        int64_t w = x * runs / work;
-        while (run_start(work, runs, w) > x) --w;
-        while (run_start(work, runs, w + 1) <= x) ++w;
-        return w;
-    };
-    const int64_t w0 = owner(x0), w1 = owner(x1 - 1);
+    const int64_t per_run = run_steps(args.before[args.b.n_seqs] * args.c.Hkv, warps);
+    const int64_t x0 = args.before[b] * args.c.Hkv + n * j;
+    const int64_t w0 = run_of(x0, per_run), w1 = run_of(x0 + n - 1, per_run);
     if (w0 == w1) return;
     const Seq s = seq_of(a, args.b, b);
     if (r >= s.rows * a.g) return;
@@ -549,7 +538,7 @@ __global__ void __launch_bounds__(256) k_rows_merge(const __grid_constant__ Rows
     const float base = top == -INFINITY ? 0.f : top;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float sum = 0.f;
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t w = w0 + warp; w <= w1; w += 8) {
         const float2 ml = __ldcg(&args.part_ml[part(w)]);
         const float4 x = __ldcg(reinterpret_cast<const float4*>(args.part_o + part(w) * kHeadDim) + lane);

@@ -33,6 +33,14 @@ __device__ __forceinline__ Seq seq_of(const AttendView& a, const BatchView& b, i
 // Whether k_rows takes the sequence (when its call has that route).
 __device__ __forceinline__ bool few_rows(const Seq& s, int g) { return s.rows <= kRowsMax && s.rows * g <= kRowsMax; }
 
+// Exponent of the power of two that brings values of at most `top` (fp32 bits, finite) below 2^15, inside f16;
+// it and its negative are exponents of normal fp32 values.
+__device__ __forceinline__ int f16_exponent(uint32_t top)
+{
+    const int e = static_cast<int>(top >> 23) - 127 - 14;
+    return e < -100 ? -100 : e;
+}
+
 // Sequences with more than `few` rows per KV head (tokens times query heads), on the tensor cores.
 size_t chunk_ws_bytes(int g, int Hkv, int n_seqs, int n_rows, int max_rows);
 cudaError_t launch_chunks(const AttendView& a, const CacheView& c, bool e4m3, const BatchView& b, int few, int sms,

@@ -28,8 +28,10 @@ namespace scale {
 namespace {
 
 constexpr int kTile = 128;            // keys of a tile, rows of a query tile
-constexpr int kPlanThreads = 1024;
-constexpr int kCuts = 3;              // pieces per SM that the plan considers, at most
+constexpr int kPlanThreads = 512;     // at least 2 kMaxSms
+constexpr int kCuts = 3;              // pieces per SM, at most, beyond one per item
+constexpr int kPieces = 8;            // pieces of an item that the plan considers
+constexpr int kCandidates = kPieces + kCuts;
 constexpr int kPieceTiles = 6;        // what a CTA's start and end take, in key tiles
 
 // A CTA's work. Rows [row0, row0 + ntok) of the row tensors are tokens pos ..; key tiles
@@ -97,7 +99,7 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* s_warp, int64_
     if (lane == 31) s_warp[warp] = incl;
     __syncthreads();
     if (warp == 0) {
-        int64_t v = lane < static_cast<int>(blockDim.x) / 32 ? s_warp[lane] : 0;
+        int64_t v = lane < kPlanThreads / 32 ? s_warp[lane] : 0;
         for (int o = 1; o < 32; o <<= 1) {
             const int64_t y = __shfl_up_sync(0xFFFFFFFFu, v, o);
             if (lane >= o) v += y;
@@ -111,13 +113,15 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* s_warp, int64_
 
 // The list of jobs: one CTA. Items are (sequence, KV head, pair of query tiles), a KV head's pairs from the
 // last (the one with most keys) to the first, so that the CTAs running at a time share the keys of few heads.
-// Fewer than two items per SM are cut along their keys into pieces of at most C tiles: C is the one of W
-// / (f SMs), f = 1 .. kCuts, and "whole" for which ceil(pieces / SMs) rounds of C + kPieceTiles end first.
+// As many items as fill the SMs a whole number of times run whole; the rest (all of them, when there are
+// fewer than two per SM) are cut along their keys into pieces of at most C tiles. C is one of longest / 1 .. longest
+// / kPieces and W / SMs .. W / (kCuts SMs), W the rest's key tiles: the one for which ceil(pieces / SMs) rounds of
+// C + kPieceTiles end first.
 __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_constant__ ChunkArgs a)
 {
     __shared__ int s_before[kMaxSeqs + 1];  // items (of one KV head) of the sequences before
     __shared__ int64_t s_warp[32];
-    __shared__ int s_pieces[kCuts + 1], s_longest;
+    __shared__ int s_pieces[kCandidates], s_longest;
     __shared__ unsigned long long s_work;
     pdl_enter();
     const int tid = threadIdx.x;
@@ -145,7 +149,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_consta
         s_before[a.b.n_seqs] = static_cast<int>(all);
         s_work = 0;
         s_longest = 0;
-        for (int f = 0; f <= kCuts; ++f) s_pieces[f] = 0;
+        for (int f = 0; f < kCandidates; ++f) s_pieces[f] = 0;
     }
     __syncthreads();
     // item x: sequences outermost, then KV heads, then pairs from the last
@@ -170,52 +174,49 @@ __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_consta
         jb->k1 = t->n;
         jb->slot = -1;
     };
-    if (items > 2 * a.sms || items == 0) {
-        for (int64_t x = tid; x < items; x += kPlanThreads) {
-            ChunkJob jb;
-            Tiles t;
-            item(x, &jb, &t);
-            a.p.jobs[x] = jb;
-        }
-        if (tid == 0) {
-            a.p.counts[0] = static_cast<int>(items);
-            a.p.counts[1] = 0;
-        }
-        return;
+    const int64_t whole = items > 2 * a.sms ? items - items % a.sms : 0;
+    const int rest = static_cast<int>(items - whole);
+    for (int64_t x = tid; x < whole; x += kPlanThreads) {
+        ChunkJob jb;
+        Tiles t;
+        item(x, &jb, &t);
+        a.p.jobs[x] = jb;
     }
-    // at most 2 kMaxSms items: one per thread
+    // the rest, at most 2 kMaxSms: one per thread
     ChunkJob jb{};
     Tiles t{};
-    if (tid < items) {
-        item(tid, &jb, &t);
+    if (tid < rest) {
+        item(whole + tid, &jb, &t);
         atomicAdd(&s_work, static_cast<unsigned long long>(t.n));
         atomicMax(&s_longest, t.n);
     }
     __syncthreads();
-    int cut[kCuts + 1];
-    cut[0] = s_longest;
-    for (int f = 1; f <= kCuts; ++f) {
-        const int64_t len = (static_cast<int64_t>(s_work) + static_cast<int64_t>(f) * a.sms - 1) / (static_cast<int64_t>(f) * a.sms);
-        cut[f] = len < 2 ? 2 : static_cast<int>(len);
+    auto longest_piece = [&](int f) {  // of candidate f
+        const int c = f < kPieces ? (s_longest + f) / (f + 1) : static_cast<int>(static_cast<float>(s_work) / static_cast<float>((f - kPieces + 1) * a.sms)) + 1;
+        return c < 2 ? 2 : c;
+    };
+    auto pieces_of = [&](int f) { return (t.n + longest_piece(f) - 1) / longest_piece(f); };
+    for (int f = 0; f < kCandidates; ++f) {
+        const int n = __reduce_add_sync(0xFFFFFFFFu, tid < rest ? pieces_of(f) : 0);
+        if ((tid & 31) == 0 && n) atomicAdd(&s_pieces[f], n);
     }
-    if (tid < items)
-        for (int f = 0; f <= kCuts; ++f) atomicAdd(&s_pieces[f], (t.n + cut[f] - 1) / cut[f]);
     __syncthreads();
-    int best = 0;
-    int64_t best_time = 0;
-    for (int f = 0; f <= kCuts; ++f) {
-        const int64_t rounds = (s_pieces[f] + a.sms - 1) / a.sms;
-        const int64_t time = rounds * (cut[f] + kPieceTiles);
-        if (f == 0 || time < best_time) {
+    int best = 0, best_time = 0x7FFFFFFF;
+    for (int f = 0; f < kCandidates; ++f) {
+        const int rounds = (s_pieces[f] + a.sms - 1) / a.sms;
+        const int time = rounds * (longest_piece(f) + kPieceTiles);
+        if (time < best_time && (f == 0 || s_pieces[f] <= rest + kCuts * a.sms)) {
             best = f;
             best_time = time;
         }
     }
-    const int pieces = tid < items ? (t.n + cut[best] - 1) / cut[best] : 0;
-    int64_t jobs, slots, merges;
-    const int64_t at = block_scan(pieces, s_warp, &jobs);
-    const int64_t slot = block_scan(pieces > 1 ? pieces : 0, s_warp, &slots);
-    const int64_t merge = block_scan(pieces > 1 ? 1 : 0, s_warp, &merges);
+    const int pieces = tid < rest ? pieces_of(best) : 0;
+    // jobs, partial results and merges before this item, one scan of 21 bits each
+    int64_t sums;
+    const int64_t mask = (1 << 21) - 1;
+    const int64_t before = block_scan(pieces > 1 ? pieces | static_cast<int64_t>(pieces) << 21 | 1ll << 42 : pieces, s_warp, &sums);
+    const int64_t at = whole + (before & mask), slot = (before >> 21) & mask, merge = before >> 42;
+    const int64_t jobs = whole + (sums & mask), slots = (sums >> 21) & mask, merges = sums >> 42;
     if (jobs > a.p.max_jobs || slots > a.p.max_slots || merges > a.p.max_merges) {  // as above
         if (tid == 0) {
             record_status(a.status, SCALE_ERR_DEVICE);
@@ -243,14 +244,27 @@ constexpr uint32_t kOffK = kOffQ + 2 * kTileBytes;
 constexpr uint32_t kOffV = kOffK + 2 * kTileBytes;
 constexpr uint32_t kOffRaw = kOffV + 2 * kTileBytes;  // 8-bit: codes of a K tile, then of a V tile
 constexpr uint32_t kRawBytes = kTile * kHeadDim;
-__host__ __device__ constexpr uint32_t chunk_smem(bool e4m3) { return kOffRaw + (e4m3 ? 2 * kRawBytes : 0) + 1024; }
-
 struct RawBarriers {
     uint64_t full[2], empty[2];  // codes of K, of V: landed; turned
+    uint64_t q_ready;            // Q is f16
 };
 
+// Behind the tiles. The 8-bit kernel's tiles leave 3 KB of the 227.
+struct ChunkShared {
+    Barriers bars;
+    RawBarriers raw;
+    float kscale[4][kTile];    // tile t & 3: what a key's products are multiplied by
+    uint8_t vscale[4][kTile];  // scale bytes of its values
+    uint32_t q_top;            // largest finite |q| of the CTA's rows, as bits
+    uint32_t tmem_slot;
+    volatile int abort_flag;
+};
+__host__ __device__ constexpr uint32_t off_shared(bool e4m3) { return kOffRaw + (e4m3 ? 2 * kRawBytes : 0); }
+__host__ __device__ constexpr uint32_t chunk_smem(bool e4m3) { return off_shared(e4m3) + sizeof(ChunkShared); }
+static_assert(chunk_smem(true) <= 227 * 1024, "shared memory of a CTA");
+
 // Threads: warps 0-7 softmax, 8 producer, 9 MMA; 8-bit: 12-15 turn codes into bf16 (10 and 11 idle, for whole
-// groups of four warps in the register split: 2 x 128 x 200 + 2 x 128 x 56 = 512 x 128).
+// groups of four warps in the register split: 2 x 128 x 192 + 2 x 128 x 64 = 512 x 128).
 __host__ __device__ constexpr int chunk_threads(bool e4m3) { return e4m3 ? 512 : 320; }
 
 template <bool E4M3>
@@ -258,14 +272,16 @@ __global__ void __launch_bounds__(chunk_threads(E4M3), 1)
 k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
         const __grid_constant__ CUtensorMap tv, const __grid_constant__ ChunkArgs a)
 {
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ Barriers bars;
-    __shared__ RawBarriers raw;
-    __shared__ uint32_t tmem_slot;
-    __shared__ volatile int abort_flag;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    ChunkShared& sh = *reinterpret_cast<ChunkShared*>(smem + off_shared(E4M3));
+    Barriers& bars = sh.bars;
+    RawBarriers& raw = sh.raw;
+    volatile int& abort_flag = sh.abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
         abort_flag = 0;
+        sh.q_top = 0;
+        mbar_init(&raw.q_ready, 128);
         mbar_init(&bars.q_full, 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bars.kv_full[i], E4M3 ? 128 : 1);
@@ -305,9 +321,12 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
     // whether some key of the tile at t0 is seen by no row: not seen(t) = t > last or (t < lo and t >= n_sink)
     auto has_unseen = [&](int t0) { return t0 + kTile - 1 > last || (t0 < lo && t0 + kTile - 1 >= a.a.n_sink); };
 
-    uint8_t* smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+    if (smem_addr(smem) & 1023u) {  // the swizzle goes by the address
+        if (tid == 0) record_status(a.status, SCALE_ERR_DEVICE);
+        return;
+    }
     if (warp == 9) {
-        tmem_alloc(&tmem_slot, 512);
+        tmem_alloc(&sh.tmem_slot, 512);
         tmem_relinquish();
     }
     // rows of a query tile past its g tt: zeros
@@ -322,10 +341,10 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = sh.tmem_slot;
 
     if (warp >= 8) {
-        if (E4M3) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (E4M3) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 8) {
             // ------------------------------------------------------------ producer: a lane per box
             const int boxes = kTile / a.box;
@@ -401,9 +420,9 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
         } else if (warp == 9) {
             // ------------------------------------------------------------ MMA issuer
             if (lane == 0) {
-                const uint32_t id_qk = idesc_bf16_f32(128, 128, 0);
+                const uint32_t id_qk = E4M3 ? idesc_f16_f32(128, 128, 0) : idesc_bf16_f32(128, 128, 0);
                 const uint32_t id_pv = idesc_bf16_f32(128, 128, 1);
-                bool ok = mbar_wait_bounded(&bars.q_full, 0, a.timeout_ns, &abort_flag);
+                bool ok = mbar_wait_bounded(E4M3 ? &raw.q_ready : &bars.q_full, 0, a.timeout_ns, &abort_flag);
                 const uint64_t qdesc0 = sdesc_sw128(smem_addr(smem + kOffQ), 16, 1024);
                 const uint64_t kdesc0 = sdesc_sw128(smem_addr(smem + kOffK), 16, 1024);
                 const uint64_t vdesc0 = sdesc_sw128(smem_addr(smem + kOffV), kHalf, 1024);
@@ -421,73 +440,87 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 }
             }
         } else if (E4M3 && warp >= 12) {
-            // ------------------------------------------------------------ codes to bf16
-            // Eight lanes take a row, 16 codes each; 16 rows of a pass lie in one page. The two 16-byte
-            // pieces of bf16 go to the swizzled place, the lanes of the second half in the other order, so that
-            // eight lanes write 128 bytes of different banks.
+            // ------------------------------------------------------------ codes to f16 keys and bf16 values
+            // Eight lanes take a row, 16 codes each. The two 16-byte pieces they become go to the swizzled
+            // place, the lanes of the second half in the other order, so that eight lanes write 128 bytes of
+            // different banks. Thread x also looks after the scales of row x, one tile ahead.
             const int x = tid - 384, sub = x & 7, r16 = x >> 3;
-            bool ok = true;
-            uint32_t vscale[2] = {0, 0};  // scale bytes of the V rows of tile t - 1 (passes 0-3, 4-7)
+            const int c0 = 2 * (sub & 3), late = sub >> 2;
             uint64_t* const s_last = bars.s_full[nq - 1];
+            uint32_t ks = 0, vs = 0;
+            auto load_scales = [&](int t) {
+                const int place = cache_row(a.c, a.b, job.b, token_of(t) + x);
+                ks = vs = 127;
+                if (place >= 0) {
+                    const int page = place / a.c.page_size;
+                    const int64_t at = (static_cast<int64_t>(page) * a.c.Hkv + job.j) * a.c.page_size + place - page * a.c.page_size;
+                    ks = a.c.ks[at];
+                    vs = a.c.vs[at];
+                }
+            };
+            load_scales(0);
+            bool ok = mbar_wait_bounded(&raw.q_ready, 0, a.timeout_ns, &abort_flag);
+            const float q_scale = a.a.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 + f16_exponent(sh.q_top)) << 23);
             for (int t = 0; t <= T && ok; ++t) {
                 const int st = t & 1;
-                uint32_t kscale[2] = {0, 0}, vnext[2] = {0, 0};
-                if (t < T) {
-                    const int t0 = token_of(t);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int place = cache_row(a.c, a.b, job.b, t0 + 16 * i);
-                        uint32_t ks = 0, vs = 0;
-                        if (place >= 0) {
-                            const int page = place / a.c.page_size;
-                            const int64_t at = (static_cast<int64_t>(page) * a.c.Hkv + job.j) * a.c.page_size + place - page * a.c.page_size + r16;
-                            ks = a.c.ks[at];
-                            vs = a.c.vs[at];
-                        }
-                        kscale[i >> 2] |= ks << (8 * (i & 3));
-                        vnext[i >> 2] |= vs << (8 * (i & 3));
-                    }
-                }
-                // the bf16 tiles of this step were last read by MMAs of step t - 2
+                // the tiles of this step were last read by MMAs of step t - 2, the scales' places by the softmax of tile t - 4
                 if (t >= 2) ok = mbar_wait_bounded(&s_last[st], ((t - 2) >> 1) & 1, a.timeout_ns, &abort_flag);
-                for (int kv = 1; kv >= 0 && ok; --kv) {
-                    if (kv ? t == 0 : t == T) continue;
-                    const int u = kv ? t - 1 : t;
-                    ok = mbar_wait_bounded(&raw.full[kv], u & 1, a.timeout_ns, &abort_flag);
+                if (!ok) break;
+                if (t < T) {
+                    sh.kscale[t & 3][x] = fmaxf(scale_value(ks) * q_scale, 1e-37f);  // not 0: hidden logits stay -inf
+                    sh.vscale[t & 3][x] = static_cast<uint8_t>(vs);
+                    if (t + 1 < T) load_scales(t + 1);
+                }
+                if (t > 0) {
+                    const int u = t - 1;
+                    // (step u: every thread wrote its row's scales)
+                    ok = mbar_wait_bounded(&bars.kv_full[u & 1], (u >> 1) & 1, a.timeout_ns, &abort_flag) &&
+                         mbar_wait_bounded(&raw.full[1], u & 1, a.timeout_ns, &abort_flag);
                     if (!ok) break;
-                    const uint8_t* from = smem + kOffRaw + kv * kRawBytes;
-                    uint8_t* to = smem + (kv ? kOffV : kOffK) + (u & 1) * kTileBytes + (sub >> 2) * kHalf;
+                    const uint8_t* from = smem + kOffRaw + kRawBytes + r16 * kHeadDim + sub * 16;
+                    uint8_t* to = smem + kOffV + (u & 1) * kTileBytes + (sub >> 2) * kHalf + r16 * 128;
                     const int t0 = token_of(u);
-                    const bool unseen = kv && has_unseen(t0);
-#pragma unroll 2
+                    const bool unseen = has_unseen(t0);
+#pragma unroll 4
                     for (int i = 0; i < 8; ++i) {
-                        const int row = 16 * i + r16;
-                        const uint4 w = *reinterpret_cast<const uint4*>(from + row * kHeadDim + sub * 16);
-                        const float s = scale_value(((kv ? vscale[i >> 2] : kscale[i >> 2]) >> (8 * (i & 3))) & 255u);
-                        const uint2 y0 = e4m3x4_to_bf16(w.x, s), y1 = e4m3x4_to_bf16(w.y, s);
-                        const uint2 y2 = e4m3x4_to_bf16(w.z, s), y3 = e4m3x4_to_bf16(w.w, s);
+                        const uint4 w = *reinterpret_cast<const uint4*>(from + i * 16 * kHeadDim);
+                        const float f = scale_value(sh.vscale[u & 3][16 * i + r16]);
+                        const uint2 y0 = e4m3x4_to_bf16(w.x, f), y1 = e4m3x4_to_bf16(w.y, f);
+                        const uint2 y2 = e4m3x4_to_bf16(w.z, f), y3 = e4m3x4_to_bf16(w.w, f);
                         uint4 p = make_uint4(y0.x, y0.y, y1.x, y1.y), q = make_uint4(y2.x, y2.y, y3.x, y3.y);
                         if (unseen) {
-                            const int tok = t0 + row;
+                            const int tok = t0 + 16 * i + r16;
                             if (tok > last || (tok < lo && tok >= a.a.n_sink)) p = q = make_uint4(0, 0, 0, 0);
                         }
-                        const int c0 = 2 * (sub & 3), late = sub >> 2;
-                        uint8_t* dst = to + row * 128;
-                        *reinterpret_cast<uint4*>(dst + (((c0 + late) ^ (row & 7)) << 4)) = late ? q : p;
-                        *reinterpret_cast<uint4*>(dst + (((c0 + 1 - late) ^ (row & 7)) << 4)) = late ? p : q;
+                        uint8_t* dst = to + i * 16 * 128;  // row 16 i + r16: r16 & 7 decides the swizzle
+                        *reinterpret_cast<uint4*>(dst + (((c0 + late) ^ (r16 & 7)) << 4)) = late ? q : p;
+                        *reinterpret_cast<uint4*>(dst + (((c0 + 1 - late) ^ (r16 & 7)) << 4)) = late ? p : q;
                     }
-                    mbar_arrive(&raw.empty[kv]);
+                    mbar_arrive(&raw.empty[1]);
                 }
-                if (!ok) break;
+                if (t < T) {
+                    ok = mbar_wait_bounded(&raw.full[0], t & 1, a.timeout_ns, &abort_flag);
+                    if (!ok) break;
+                    const uint8_t* from = smem + kOffRaw + r16 * kHeadDim + sub * 16;
+                    uint8_t* to = smem + kOffK + st * kTileBytes + (sub >> 2) * kHalf + r16 * 128;
+#pragma unroll 4
+                    for (int i = 0; i < 8; ++i) {
+                        const uint4 w = *reinterpret_cast<const uint4*>(from + i * 16 * kHeadDim);
+                        const uint4 p = make_uint4(e4m3x2_to_f16x2(w.x), e4m3x2_to_f16x2(w.x >> 16), e4m3x2_to_f16x2(w.y), e4m3x2_to_f16x2(w.y >> 16));
+                        const uint4 q = make_uint4(e4m3x2_to_f16x2(w.z), e4m3x2_to_f16x2(w.z >> 16), e4m3x2_to_f16x2(w.w), e4m3x2_to_f16x2(w.w >> 16));
+                        uint8_t* dst = to + i * 16 * 128;
+                        *reinterpret_cast<uint4*>(dst + (((c0 + late) ^ (r16 & 7)) << 4)) = late ? q : p;
+                        *reinterpret_cast<uint4*>(dst + (((c0 + 1 - late) ^ (r16 & 7)) << 4)) = late ? p : q;
+                    }
+                    mbar_arrive(&raw.empty[0]);
+                }
                 fence_proxy_async_smem();
                 mbar_arrive(&bars.kv_full[st]);
-                vscale[0] = vnext[0];
-                vscale[1] = vnext[1];
             }
             if (!ok) fail(&abort_flag, a.status);
         }
     } else {
-        if (E4M3) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+        if (E4M3) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
         if ((warp >> 2) < nq) {
             // ------------------------------------------------------------ softmax + epilogue
             const int qt = warp >> 2;
@@ -502,6 +535,39 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
             const uint32_t o_addr = s_addr + 128;
             float m_run = -INFINITY, l_run = 0.f;
             bool ok = true;
+            if (E4M3) {
+                // Q to f16, by one power of two for all rows of the CTA: with the largest finite |q| brought to
+                // 2^14 .. 2^15, what the rows' smaller values lose is 2^-39 of it.
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.q_full, 0, a.timeout_ns, &abort_flag));
+                uint8_t* row = smem + kOffQ + qt * kTileBytes + r * 128;
+                uint32_t top = 0;
+                if (r < (qt + 1 == nq ? job.ntok - qt * tt : tt) * g) {
+#pragma unroll 4
+                    for (int i = 0; i < 16; ++i) {
+                        const uint4 w = *reinterpret_cast<const uint4*>(row + (i >> 3) * kHalf + (((i & 7) ^ (r & 7)) << 4));
+                        const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t x = (v[e] << 16) & 0x7FFFFFFFu, y = v[e] & 0x7FFF0000u;
+                            top = max(top, max(x >= 0x7F800000u ? 0u : x, y >= 0x7F800000u ? 0u : y));
+                        }
+                    }
+                }
+                top = __reduce_max_sync(0xFFFFFFFFu, top);
+                if (lane == 0) atomicMax(&sh.q_top, top);
+                named_barrier(2, 128 * nq);
+                const float down = __uint_as_float(static_cast<uint32_t>(127 - f16_exponent(sh.q_top)) << 23);
+#pragma unroll 4
+                for (int i = 0; i < 16; ++i) {
+                    uint4* at = reinterpret_cast<uint4*>(row + (i >> 3) * kHalf + (((i & 7) ^ (r & 7)) << 4));
+                    const uint4 w = *at;
+                    auto half = [&](uint32_t v) { return pack_f16x2(__uint_as_float(v << 16) * down, __uint_as_float(v & 0xFFFF0000u) * down); };
+                    *at = make_uint4(half(w.x), half(w.y), half(w.z), half(w.w));
+                }
+                fence_proxy_async_smem();
+                named_barrier(2, 128 * nq);
+                if (qt == 0) mbar_arrive(&raw.q_ready);
+            }
             // S row of a tile; columns [lim, 128) and [gap, low) are not seen
             auto load_s = [&](uint32_t (&sr)[128], bool masked, int lim, int gap, int low) {
 #pragma unroll
@@ -515,12 +581,14 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 }
             };
             // p = 2^(s scale - m) of keys [64 h, 64 h + 64) as bf16 pairs; returns their sum
-            auto exp_half = [&](const float* s, int h, float neg_m, uint32_t (&pk)[32]) {
+            // (8-bit: scale 2^e of each key, from shared memory)
+            auto exp_half = [&](const float* s, const float* ks, int h, float neg_m, uint32_t (&pk)[32]) {
                 float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
                     float x0, x1;
-                    ffma2(x0, x1, s[h * 64 + 2 * i], s[h * 64 + 2 * i + 1], a.a.scale_log2, a.a.scale_log2, neg_m, neg_m);
+                    const float2 f = E4M3 ? *reinterpret_cast<const float2*>(ks + h * 64 + 2 * i) : make_float2(a.a.scale_log2, a.a.scale_log2);
+                    ffma2(x0, x1, s[h * 64 + 2 * i], s[h * 64 + 2 * i + 1], f.x, f.y, neg_m, neg_m);
                     x0 = ex2(x0);
                     x1 = ex2(x1);
                     const int jj = (i & 3) * 2;
@@ -536,6 +604,12 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                     break;
                 }
                 tc_fence_after();
+                // (complete: the products were made of it) orders the reads of the tile's scales after their writes
+                if (E4M3 && !__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.kv_full[t & 1], (t >> 1) & 1, a.timeout_ns, &abort_flag))) {
+                    ok = false;
+                    break;
+                }
+                const float* ks = sh.kscale[t & 3];
                 const int t0 = token_of(t);
                 const bool masked = t0 + kTile - 1 > pos_first ||
                                     (a.a.n_local >= 0 && pos_last - t0 > a.a.n_local && t0 + kTile - 1 >= a.a.n_sink);
@@ -553,15 +627,18 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                     if (exact) {
                         float mx8[8];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) mx8[i] = s[i];
+                        for (int i = 0; i < 8; ++i) mx8[i] = E4M3 ? s[i] * ks[i] : s[i];
 #pragma unroll
                         for (int c = 8; c < 120; c += 16)
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) mx8[i] = fmax3(mx8[i], s[c + 2 * i], s[c + 2 * i + 1]);
+                            for (int i = 0; i < 8; ++i) {
+                                const int x = c + 2 * i;
+                                mx8[i] = E4M3 ? fmax3(mx8[i], s[x] * ks[x], s[x + 1] * ks[x + 1]) : fmax3(mx8[i], s[x], s[x + 1]);
+                            }
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) mx8[i] = fmaxf(mx8[i], s[120 + i]);
+                        for (int i = 0; i < 8; ++i) mx8[i] = fmaxf(mx8[i], E4M3 ? s[120 + i] * ks[120 + i] : s[120 + i]);
                         const float mx = fmax3(fmax3(mx8[0], mx8[1], mx8[2]), fmax3(mx8[3], mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7]));
-                        const float m_new = fmaxf(m_run, mx * a.a.scale_log2);
+                        const float m_new = fmaxf(m_run, E4M3 ? mx : mx * a.a.scale_log2);
                         const bool raise = m_new > m_run + kRescaleThreshold;
                         // the O rescale is warp-collective: taken by the whole warp when any row needs it
                         if (__any_sync(0xFFFFFFFFu, raise)) {
@@ -583,8 +660,8 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                     }
                     const float neg_m = (m_run == -INFINITY) ? 0.f : -m_run;
                     uint32_t pk[2][32];
-                    sum = exp_half(s, 0, neg_m, pk[0]);
-                    sum += exp_half(s, 1, neg_m, pk[1]);
+                    sum = exp_half(s, ks, 0, neg_m, pk[0]);
+                    sum += exp_half(s, ks, 1, neg_m, pk[1]);
                     if (!exact && __any_sync(0xFFFFFFFFu, !(sum <= kFastSumLimit))) {
                         exact = true;
                         continue;
@@ -747,7 +824,7 @@ ChunkWs chunk_layout(int g, int Hkv, int n_seqs, int n_rows, int max_rows)
     const int64_t cut = items < 2 * kMaxSms ? items : 2 * kMaxSms;  // items that may be cut
     const int64_t slots = cut + kCuts * kMaxSms;
     w.max_merges = static_cast<int>(cut);
-    w.max_jobs = static_cast<int>(items > slots ? items : slots);
+    w.max_jobs = static_cast<int>(items + kCuts * kMaxSms);
     w.max_slots = static_cast<int>(slots);
     w.part_rows = max_rows > tt ? 2 * kTile : kTile;
     w.counts = take(2 * sizeof(int32_t));

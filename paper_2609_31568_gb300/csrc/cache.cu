@@ -38,6 +38,25 @@ struct PlaceArgs {
     uint8_t axis[64];
 };
 
+// f radians as a fraction of a turn, times 2^64, modulo 2^64. In integers: the 53 significant bits of f times
+// 2^64 / (2 pi), shifted to their place (64-bit floating point products would take 152 SMs' warps
+// longer than the rows of a small call).
+__device__ __forceinline__ uint64_t turns_of(double f)
+{
+    constexpr uint64_t kPerRadian = 2935890503282001226ull;  // 2^64 / (2 pi), rounded
+    const uint64_t bits = static_cast<uint64_t>(__double_as_longlong(f));
+    const int e = static_cast<int>((bits >> 52) & 0x7FF);
+    const uint64_t m = (bits & 0xFFFFFFFFFFFFFull) | (e ? 1ull << 52 : 0ull);
+    const uint64_t hi = __umul64hi(m, kPerRadian), lo = m * kPerRadian;
+    const int right = 1075 - (e ? e : 1);  // f = m 2^-right
+    uint64_t t;
+    if (right >= 128) t = 0;
+    else if (right >= 64) t = hi >> (right - 64);
+    else if (right > 0) t = lo >> right | hi << (64 - right);
+    else t = right > -64 ? lo << -right : 0;
+    return bits >> 63 ? 0 - t : t;
+}
+
 // cos and sin of `turn` / 2^64 of a turn. The turn is split into the nearest quarter and an angle of at
 // most an eighth, so the angle in fp32 is off by 2^-25 of an eighth at most.
 __device__ __forceinline__ float2 cos_sin_of_turn(uint64_t turn)
@@ -78,8 +97,7 @@ __global__ void __launch_bounds__(kPlaceThreads) k_place(const __grid_constant__
     if (ORDER) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const double turns = a.inv_freq[lane + 32 * i] * 0.15915494309189535;  // 1 / (2 pi)
-            freq[i] = static_cast<uint64_t>((turns - floor(turns)) * 18446744073709551616.0);
+            freq[i] = turns_of(a.inv_freq[lane + 32 * i]);
             ax[i] = a.axis[lane + 32 * i];
         }
     }

@@ -369,6 +369,12 @@ __host__ __device__ constexpr uint32_t idesc_bf16_f32(uint32_t M, uint32_t N, ui
            | ((M >> 4) << 24);       // M / 16
 }
 
+// idesc_bf16_f32 with f16 operands.
+__host__ __device__ constexpr uint32_t idesc_f16_f32(uint32_t M, uint32_t N, uint32_t b_mn_major)
+{
+    return idesc_bf16_f32(M, N, b_mn_major) & ~((1u << 7) | (1u << 10));
+}
+
 // Shared-memory matrix descriptor, 128-byte swizzle. Addresses and offsets in
 // bytes; `lbo` and `sbo` are the leading / stride byte offsets of the
 // canonical layouts (ignored lbo for K-major swizzled operands).
@@ -513,6 +519,14 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi)
 {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// Two floats to packed f16x2, round to nearest even; `lo` lands in bits 0-15.
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
 
