@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_rows(const __grid_constant_
         for (int i = i0; i < i1; ++i) {
             const Seq s = seq_of(a, bt, i);
             before[i] = sum;
-            if (s.rows > 0 && few_rows(s, a.g)) sum += steps_of(a, s).n;
+            if (s.rows > 0) sum += steps_of(a, s).n;
         }
         int64_t incl = sum;
         for (int o = 1; o < 32; o <<= 1) {
@@ -628,11 +628,9 @@ cudaError_t launch_attend(const AttendView& a, const CacheView& c, bool e4m3, co
                reinterpret_cast<float2*>(ws + lay.part_ml), lay.part_rows};
     const int64_t rows = static_cast<int64_t>(b.max_rows) * a.g;
     if (rows > kRowsMax) {
-        // One sequence that may have many rows: whatever it has goes there. A batch is split by what its
-        // sequences have, which only the device knows.
-        const int few = b.n_seqs == 1 ? 0 : kRowsMax;
-        e = launch_chunks(a, c, e4m3, b, few, sms, reinterpret_cast<int32_t*>(ws + kStatusOffset), ws + lay.chunks, timeout_ns, st);
-        if (e != cudaSuccess || few == 0) return e;
+        // Batches with longer pieces go there whole: a sequence of few rows takes its share of that kernel's
+        // jobs, at the pace of its keys, and no second route follows.
+        return launch_chunks(a, c, e4m3, b, sms, reinterpret_cast<int32_t*>(ws + kStatusOffset), ws + lay.chunks, timeout_ns, st);
     }
     if (rows <= 8) return e4m3 ? run_rows<1, true>(r, sms, st) : run_rows<1, false>(r, sms, st);
     return e4m3 ? run_rows<2, true>(r, sms, st) : run_rows<2, false>(r, sms, st);

@@ -6,7 +6,7 @@
 
 namespace scale {
 
-constexpr int kRowsMax = 16;  // (token, query head) rows of a KV head that k_rows takes
+constexpr int kRowsMax = 16;  // (token, query head) rows of a KV head up to which a call's sequences go to k_rows
 constexpr int kMaxSms = 160;  // SMs that a call uses at most
 
 // Rows and keys of sequence b. Its computed rows are [row0, row0 + rows), tokens
@@ -30,9 +30,6 @@ __device__ __forceinline__ Seq seq_of(const AttendView& a, const BatchView& b, i
     return s;
 }
 
-// Whether k_rows takes the sequence (when its call has that route).
-__device__ __forceinline__ bool few_rows(const Seq& s, int g) { return s.rows <= kRowsMax && s.rows * g <= kRowsMax; }
-
 // Exponent of the power of two that brings values of at most `top` (fp32 bits, finite) below 2^15, inside f16;
 // it and its negative are exponents of normal fp32 values.
 __device__ __forceinline__ int f16_exponent(uint32_t top)
@@ -41,9 +38,9 @@ __device__ __forceinline__ int f16_exponent(uint32_t top)
     return e < -100 ? -100 : e;
 }
 
-// Sequences with more than `few` rows per KV head (tokens times query heads), on the tensor cores.
+// Calls whose sequences may have more than kRowsMax rows per KV head: tcgen05, 128 rows at a time.
 size_t chunk_ws_bytes(int g, int Hkv, int n_seqs, int n_rows, int max_rows);
-cudaError_t launch_chunks(const AttendView& a, const CacheView& c, bool e4m3, const BatchView& b, int few, int sms,
+cudaError_t launch_chunks(const AttendView& a, const CacheView& c, bool e4m3, const BatchView& b, int sms,
                           int32_t* status, uint8_t* ws, uint64_t timeout_ns, cudaStream_t st);
 
 }  // namespace scale

@@ -1,6 +1,6 @@
 // attend_chunk.cu -- attention of many new tokens of a sequence over its paged
-// cache, on the tensor cores (scale_cache_attend's route for more than kRowsMax
-// rows per KV head).
+// cache, on the tensor cores (scale_cache_attend's route for calls whose sequences
+// may have more than kRowsMax rows per KV head).
 //
 // A query tile is 128 rows (token, query head) of one KV head: 128 / g tokens with
 // the g query heads that share its keys, which one TMA box of g heads lays down in
@@ -11,9 +11,9 @@
 //  - a key tile is gathered from pages of any multiple of 16 tokens, in boxes of
 //    the largest power of two that divides the page, one lane of the producer's
 //    warp per box;
-//  - 8-bit keys and values land as codes and four further warps turn them into the
-//    bf16 tiles, exactly, scales and all, so the products are those of a bf16 cache
-//    that holds the same values;
+//  - 8-bit keys are multiplied as the codes they are, by Q in two e4m3 parts (twice the
+//    products at twice the rate), and their scales join the logits; 8-bit values land as
+//    codes and four further warps turn them into bf16 tiles, exactly, scales and all;
 //  - k_chunk_plan lays out the work: the query tiles of all sequences, and where those
 //    are fewer than the SMs keep busy, each cut along its keys, with (O, reference,
 //    sum) of the pieces merged by k_chunk_merge.
@@ -59,7 +59,6 @@ struct ChunkArgs {
     CacheView c;
     BatchView b;
     ChunkPlan p;
-    int few;           // sequences of at most so many rows per KV head are not ours
     int sms;
     int tile_tokens;   // tokens of a query tile
     int box;           // tokens of a TMA box: divides the page and the key tile
@@ -132,7 +131,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_consta
     for (int i = i0; i < i1; ++i) {
         const Seq s = seq_of(a.a, a.b, i);
         s_before[i] = static_cast<int>(mine);
-        if (s.rows > 0 && static_cast<int64_t>(s.rows) * a.a.g > a.few) mine += (s.rows + per_item - 1) / per_item;
+        if (s.rows > 0) mine += (s.rows + per_item - 1) / per_item;
     }
     int64_t all;
     const int64_t base = block_scan(mine, s_warp, &all);
@@ -238,34 +237,100 @@ __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_consta
     }
 }
 
-// Dynamic shared memory (offsets from the 1024-aligned base).
+// Dynamic shared memory (offsets from its 1024-aligned base): Q, then K and V in two stages each. 8-bit:
+// Q as its two parts, K and V as codes, then V as bf16.
+constexpr uint32_t kCodeBytes = kTile * kHeadDim;  // one 128 x 128 tile of codes
 constexpr uint32_t kOffQ = 0;
 constexpr uint32_t kOffK = kOffQ + 2 * kTileBytes;
-constexpr uint32_t kOffV = kOffK + 2 * kTileBytes;
-constexpr uint32_t kOffRaw = kOffV + 2 * kTileBytes;  // 8-bit: codes of a K tile, then of a V tile
-constexpr uint32_t kRawBytes = kTile * kHeadDim;
-struct RawBarriers {
-    uint64_t full[2], empty[2];  // codes of K, of V: landed; turned
-    uint64_t q_ready;            // Q is f16
-};
+__host__ __device__ constexpr uint32_t off_raw(bool e4m3) { return kOffK + 2 * (e4m3 ? kCodeBytes : kTileBytes); }
+__host__ __device__ constexpr uint32_t off_v(bool e4m3) { return off_raw(e4m3) + (e4m3 ? 2 * kCodeBytes : 0); }
+__host__ __device__ constexpr uint32_t off_shared(bool e4m3) { return off_v(e4m3) + 2 * kTileBytes; }
 
-// Behind the tiles. The 8-bit kernel's tiles leave 3 KB of the 227.
 struct ChunkShared {
     Barriers bars;
-    RawBarriers raw;
-    float kscale[4][kTile];    // tile t & 3: what a key's products are multiplied by
-    uint8_t vscale[4][kTile];  // scale bytes of its values
-    uint32_t q_top;            // largest finite |q| of the CTA's rows, as bits
+    // 8-bit only
+    uint64_t q_ready;                    // Q is in its parts
+    uint64_t raw_full[2], raw_empty[2];  // codes of V: landed; turned
+    uint64_t v_full[2];                  // V is bf16
+    float kscale[8][kTile];              // per softmax warp: what the products with each key of its tile are multiplied by
+    uint32_t q_top;                      // largest finite |q| of the CTA's rows, as bits
     uint32_t tmem_slot;
     volatile int abort_flag;
 };
-__host__ __device__ constexpr uint32_t off_shared(bool e4m3) { return kOffRaw + (e4m3 ? 2 * kRawBytes : 0); }
 __host__ __device__ constexpr uint32_t chunk_smem(bool e4m3) { return off_shared(e4m3) + sizeof(ChunkShared); }
-static_assert(chunk_smem(true) <= 227 * 1024, "shared memory of a CTA");
+static_assert(chunk_smem(true) <= 227 * 1024 && chunk_smem(false) <= 227 * 1024, "shared memory of a CTA");
 
-// Threads: warps 0-7 softmax, 8 producer, 9 MMA; 8-bit: 12-15 turn codes into bf16 (10 and 11 idle, for whole
+// Threads: warps 0-7 softmax, 8 producer, 9 MMA; 8-bit: 12-15 turn V into bf16 (10 and 11 idle, for whole
 // groups of four warps in the register split: 2 x 128 x 192 + 2 x 128 x 64 = 512 x 128).
 __host__ __device__ constexpr int chunk_threads(bool e4m3) { return e4m3 ? 512 : 320; }
+
+// A CTA's job as its roles see it; T = 0: none.
+struct JobView {
+    ChunkJob job;
+    Tiles tiles;
+    int nq, last, lo, T, n_sink;
+    // first token of the job's key tile t
+    __device__ __forceinline__ int token_of(int t) const
+    {
+        const int i = job.k0 + t;
+        return (i < tiles.sinks ? i : tiles.first + i - tiles.sinks) * kTile;
+    }
+    // whether no row sees token t
+    __device__ __forceinline__ bool unseen(int t) const { return t > last || (t < lo && t >= n_sink); }
+    // whether that holds for a token of the tile at t0
+    __device__ __forceinline__ bool has_unseen(int t0) const { return t0 + kTile - 1 > last || (t0 < lo && t0 + kTile - 1 >= n_sink); }
+};
+
+// Waits for the plan, then reads the job of this CTA.
+__device__ __forceinline__ JobView load_job(const ChunkArgs& a)
+{
+    pdl_enter();
+    JobView v;
+    const int n_jobs = a.p.counts[0];
+    const int4 x = reinterpret_cast<const int4*>(a.p.jobs + blockIdx.x)[0], y = reinterpret_cast<const int4*>(a.p.jobs + blockIdx.x)[1];
+    v.job = ChunkJob{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+    v.nq = v.job.ntok > a.tile_tokens ? 2 : 1;
+    v.last = v.job.pos + v.job.ntok - 1;
+    v.lo = a.a.n_local >= 0 && v.job.pos > a.a.n_local ? v.job.pos - a.a.n_local : 0;
+    v.n_sink = a.a.n_sink;
+    v.tiles = tiles_of(a.a, v.job.pos, v.job.ntok);
+    v.T = static_cast<int>(blockIdx.x) < n_jobs ? v.job.k1 - v.job.k0 : 0;
+    return v;
+}
+
+// mma_iteration and mma_issue_loop (attn_mma.cuh) for 8-bit keys: S = Q1 K^T + Q2 K^T on codes, K and V behind
+// barriers of their own.
+template <int NQ>
+__device__ __forceinline__ bool mma_issue_codes(ChunkShared& sh, uint32_t tmem, uint64_t qdesc0, uint64_t kdesc0, uint64_t vdesc0,
+                                                int T, bool skip_last, uint64_t timeout_ns)
+{
+    constexpr uint64_t kStageStep = kTileBytes >> 4, kCodeStep = kCodeBytes >> 4;
+    constexpr uint32_t id_qk = idesc_e4m3_f32(128, 128), id_pv = idesc_bf16_f32(128, 128, 1);
+    Barriers& bars = sh.bars;
+    const volatile int* abort_flag = &sh.abort_flag;
+    for (int t = 0; t <= T; ++t) {
+        const int st = t & 1, sv = st ^ 1;
+        if (t < T && !mbar_wait_bounded(&bars.kv_full[st], (t >> 1) & 1, timeout_ns, abort_flag)) return false;
+        if (t > 0 && !mbar_wait_bounded(&sh.v_full[sv], ((t - 1) >> 1) & 1, timeout_ns, abort_flag)) return false;
+        if (t == 0) tc_fence_after();
+#pragma unroll
+        for (int qt = 0; qt < NQ; ++qt) {
+            if (t > 0) {
+                if (!mbar_wait_bounded(&bars.p_full[qt], (t - 1) & 1, timeout_ns, abort_flag)) return false;
+                tc_fence_after();
+                if (!(NQ == 2 && qt == 0 && t == T && skip_last))
+                    mma_ts_k128<2048>(tmem + qt * 256 + 128, tmem + qt * 256, vdesc0 + sv * kStageStep, id_pv, t > 1 ? 1u : 0u);
+            }
+            if (t < T) {
+                mma_e4m3_k128(tmem + qt * 256, qdesc0 + qt * kStageStep, kdesc0 + st * kCodeStep, id_qk, 0u);
+                mma_e4m3_k128(tmem + qt * 256, qdesc0 + qt * kStageStep + kCodeStep, kdesc0 + st * kCodeStep, id_qk, 1u);
+                mma_commit(&bars.s_full[qt][st]);
+            }
+        }
+    }
+    mma_commit(&bars.o_full);
+    return true;
+}
 
 template <bool E4M3>
 __global__ void __launch_bounds__(chunk_threads(E4M3), 1)
@@ -275,21 +340,33 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
     extern __shared__ __align__(1024) uint8_t smem[];
     ChunkShared& sh = *reinterpret_cast<ChunkShared*>(smem + off_shared(E4M3));
     Barriers& bars = sh.bars;
-    RawBarriers& raw = sh.raw;
     volatile int& abort_flag = sh.abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tt = a.tile_tokens, g = a.a.g;
+    // CTAs of the first wave set up, and run the softmax code once, while the plan is made
+    const bool first_wave = static_cast<int>(blockIdx.x) < a.sms;
+    if (!first_wave) {
+        pdl_enter();
+        if (static_cast<int>(blockIdx.x) >= a.p.counts[0]) return;
+    }
+    if (smem_addr(smem) & 1023u) {  // the swizzle goes by the address
+        pdl_enter();
+        if (tid == 0) record_status(a.status, SCALE_ERR_DEVICE);
+        return;
+    }
     if (tid == 0) {
         abort_flag = 0;
         sh.q_top = 0;
-        mbar_init(&raw.q_ready, 128);
         mbar_init(&bars.q_full, 1);
+        mbar_init(&sh.q_ready, 128);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&bars.kv_full[i], E4M3 ? 128 : 1);
+            mbar_init(&bars.kv_full[i], 1);
             mbar_init(&bars.s_full[i][0], 1);
             mbar_init(&bars.s_full[i][1], 1);
             mbar_init(&bars.p_full[i], 128);
-            mbar_init(&raw.full[i], 1);
-            mbar_init(&raw.empty[i], 128);
+            mbar_init(&sh.raw_full[i], 1);
+            mbar_init(&sh.raw_empty[i], 128);
+            mbar_init(&sh.v_full[i], 128);
         }
         mbar_init(&bars.o_full, 1);
         mbar_init(&bars.drain, 1);
@@ -299,31 +376,6 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
         tma_prefetch_desc(&tq);
         tma_prefetch_desc(&tk);
         tma_prefetch_desc(&tv);
-    }
-    __syncthreads();
-    pdl_enter();
-    const int n_jobs = a.p.counts[0];
-    const int4 j0 = reinterpret_cast<const int4*>(a.p.jobs + blockIdx.x)[0];
-    const int4 j1 = reinterpret_cast<const int4*>(a.p.jobs + blockIdx.x)[1];
-    if (static_cast<int>(blockIdx.x) >= n_jobs) return;
-    const ChunkJob job{j0.x, j0.y, j0.z, j0.w, j1.x, j1.y, j1.z, j1.w};
-    const int tt = a.tile_tokens, g = a.a.g;
-    const int nq = job.ntok > tt ? 2 : 1;
-    const int last = job.pos + job.ntok - 1;  // token of the last row
-    const int lo = a.a.n_local >= 0 && job.pos > a.a.n_local ? job.pos - a.a.n_local : 0;
-    const Tiles tiles = tiles_of(a.a, job.pos, job.ntok);
-    const int T = job.k1 - job.k0;
-    // first token of the job's key tile t
-    auto token_of = [&](int t) {
-        const int i = job.k0 + t;
-        return (i < tiles.sinks ? i : tiles.first + i - tiles.sinks) * kTile;
-    };
-    // whether some key of the tile at t0 is seen by no row: not seen(t) = t > last or (t < lo and t >= n_sink)
-    auto has_unseen = [&](int t0) { return t0 + kTile - 1 > last || (t0 < lo && t0 + kTile - 1 >= a.a.n_sink); };
-
-    if (smem_addr(smem) & 1023u) {  // the swizzle goes by the address
-        if (tid == 0) record_status(a.status, SCALE_ERR_DEVICE);
-        return;
     }
     if (warp == 9) {
         tmem_alloc(&sh.tmem_slot, 512);
@@ -345,12 +397,15 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
 
     if (warp >= 8) {
         if (E4M3) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        if (warp == 8) {
+        const JobView jv = load_job(a);
+        const ChunkJob& job = jv.job;
+        const int T = jv.T, nq = jv.nq;
+        if (T == 0) {
+        } else if (warp == 8) {
             // ------------------------------------------------------------ producer: a lane per box
-            const int boxes = kTile / a.box;
-            const int halves = E4M3 ? 1 : 2;
-            const int bx = lane / halves, hf = lane - bx * halves;  // 8 boxes of 16 tokens at most: 16 lanes
-            const bool mine = bx < boxes;
+            constexpr int kHalves = E4M3 ? 1 : 2;
+            const int bx = lane / kHalves, hf = lane - bx * kHalves;  // 8 boxes of 16 tokens at most: 16 lanes
+            const bool mine = bx < kTile / a.box;
             const int32_t pool_rows = a.c.num_pages * a.c.page_size;
             if (lane == 0) {
                 mbar_arrive_expect_tx(&bars.q_full, static_cast<uint32_t>(nq * 2 * g * tt * 128));
@@ -360,47 +415,43 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                                     job.row0 + qt * tt);
             }
             uint64_t* const s_last = bars.s_full[nq - 1];
-            int steps = 0, issued_k = 0, issued_v = 0;
+            int steps = 0, steps_v = 0;
             int32_t row_v = 0;  // pool row of this lane's box in tile t - 1
             auto row_of = [&](int t) {
-                const int r = mine ? cache_row(a.c, a.b, job.b, token_of(t) + bx * a.box) : 0;
+                const int r = mine ? cache_row(a.c, a.b, job.b, jv.token_of(t) + bx * a.box) : 0;
                 return r < 0 ? pool_rows : r;  // past the end: zeros
             };
-            int32_t row_k = T > 0 ? row_of(0) : 0;
-            for (int t = 0; t <= T; ++t) {
+            int32_t row_k = row_of(0);
+            // bf16: step t loads K(t) and V(t - 1) behind one barrier; 8-bit: K(t), and V(t) for the warps that turn it
+            for (int t = 0; t < T + (E4M3 ? 0 : 1); ++t) {
                 const int st = t & 1;
-                bool ok = true;
-                if (E4M3) {
-                    // K(t) into the raw K tile, V(t - 1) into the raw V tile, once the tile before was turned
-                    for (int kv = 1; kv >= 0; --kv) {
-                        if (kv ? t == 0 : t == T) continue;
-                        const int u = kv ? t - 1 : t;
-                        if (u > 0 && !mbar_wait_bounded(&raw.empty[kv], (u - 1) & 1, a.timeout_ns, &abort_flag)) ok = false;
-                        ok = __all_sync(0xFFFFFFFFu, ok);
-                        if (!ok) break;
-                        if (lane == 0) mbar_arrive_expect_tx(&raw.full[kv], kRawBytes);
-                        if (kv) ++issued_v;
-                        else ++issued_k;
-                        __syncwarp();
-                        if (mine)
-                            tma_load_3d(smem + kOffRaw + kv * kRawBytes + bx * a.box * kHeadDim, kv ? &tv : &tk, &raw.full[kv], 0,
-                                        job.j, kv ? row_v : row_k);
-                    }
-                } else {
-                    if (t >= 2 && !mbar_wait_bounded(&s_last[st], ((t - 2) >> 1) & 1, a.timeout_ns, &abort_flag)) ok = false;
+                bool ok = t < 2 || mbar_wait_bounded(&s_last[st], ((t - 2) >> 1) & 1, a.timeout_ns, &abort_flag);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (ok && E4M3) {
+                    if (lane == 0) mbar_arrive_expect_tx(&bars.kv_full[st], kCodeBytes);
+                    ++steps;
+                    __syncwarp();
+                    const uint32_t to = st * kCodeBytes + bx * a.box * kHeadDim;
+                    if (mine) tma_load_3d(smem + kOffK + to, &tk, &bars.kv_full[st], 0, job.j, row_k);
+                    ok = t < 2 || mbar_wait_bounded(&sh.raw_empty[st], ((t - 2) >> 1) & 1, a.timeout_ns, &abort_flag);
                     ok = __all_sync(0xFFFFFFFFu, ok);
                     if (ok) {
-                        const bool has_k = t < T, has_v = t >= 1;
-                        if (lane == 0)
-                            mbar_arrive_expect_tx(&bars.kv_full[st], (has_k ? kTileBytes : 0u) + (has_v ? kTileBytes : 0u));
-                        ++steps;
+                        if (lane == 0) mbar_arrive_expect_tx(&sh.raw_full[st], kCodeBytes);
+                        ++steps_v;
                         __syncwarp();
-                        const uint32_t to = hf * kHalf + bx * a.box * 128;
-                        if (mine && has_v)
-                            tma_load_3d(smem + kOffV + ((t - 1) & 1) * kTileBytes + to, &tv, &bars.kv_full[st], hf * 64, job.j, row_v);
-                        if (mine && has_k)
-                            tma_load_3d(smem + kOffK + st * kTileBytes + to, &tk, &bars.kv_full[st], hf * 64, job.j, row_k);
+                        if (mine) tma_load_3d(smem + off_raw(true) + to, &tv, &sh.raw_full[st], 0, job.j, row_k);
                     }
+                } else if (ok) {
+                    const bool has_k = t < T, has_v = t >= 1;
+                    if (lane == 0)
+                        mbar_arrive_expect_tx(&bars.kv_full[st], (has_k ? kTileBytes : 0u) + (has_v ? kTileBytes : 0u));
+                    ++steps;
+                    __syncwarp();
+                    const uint32_t to = hf * kHalf + bx * a.box * 128;
+                    if (mine && has_v)
+                        tma_load_3d(smem + off_v(false) + ((t - 1) & 1) * kTileBytes + to, &tv, &bars.kv_full[st], hf * 64, job.j, row_v);
+                    if (mine && has_k)
+                        tma_load_3d(smem + kOffK + st * kTileBytes + to, &tk, &bars.kv_full[st], hf * 64, job.j, row_k);
                 }
                 if (!ok) {
                     if (lane == 0) fail(&abort_flag, a.status);
@@ -413,26 +464,32 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
             if (abort_flag && lane == 0) {
                 // every copy in flight lands before the CTA ends
                 mbar_wait_bounded(&bars.q_full, 0, a.timeout_ns, nullptr);
-                const int n0 = E4M3 ? issued_k : (steps + 1) / 2, n1 = E4M3 ? issued_v : steps / 2;
-                if (n0) mbar_wait_bounded(E4M3 ? &raw.full[0] : &bars.kv_full[0], (n0 - 1) & 1, a.timeout_ns, nullptr);
-                if (n1) mbar_wait_bounded(E4M3 ? &raw.full[1] : &bars.kv_full[1], (n1 - 1) & 1, a.timeout_ns, nullptr);
+                for (int i = 0; i < 2; ++i) {
+                    const int n = (steps + 1 - i) / 2, nv = (steps_v + 1 - i) / 2;  // copies into stage i
+                    if (n) mbar_wait_bounded(&bars.kv_full[i], (n - 1) & 1, a.timeout_ns, nullptr);
+                    if (E4M3 && nv) mbar_wait_bounded(&sh.raw_full[i], (nv - 1) & 1, a.timeout_ns, nullptr);
+                }
             }
         } else if (warp == 9) {
             // ------------------------------------------------------------ MMA issuer
             if (lane == 0) {
-                const uint32_t id_qk = E4M3 ? idesc_f16_f32(128, 128, 0) : idesc_bf16_f32(128, 128, 0);
-                const uint32_t id_pv = idesc_bf16_f32(128, 128, 1);
-                bool ok = mbar_wait_bounded(E4M3 ? &raw.q_ready : &bars.q_full, 0, a.timeout_ns, &abort_flag);
+                bool ok = mbar_wait_bounded(E4M3 ? &sh.q_ready : &bars.q_full, 0, a.timeout_ns, &abort_flag);
                 const uint64_t qdesc0 = sdesc_sw128(smem_addr(smem + kOffQ), 16, 1024);
                 const uint64_t kdesc0 = sdesc_sw128(smem_addr(smem + kOffK), 16, 1024);
-                const uint64_t vdesc0 = sdesc_sw128(smem_addr(smem + kOffV), kHalf, 1024);
+                const uint64_t vdesc0 = sdesc_sw128(smem_addr(smem + off_v(E4M3)), kHalf, 1024);
                 // the last key tile may lie after every row of the first query tile
-                const bool skip_last = T > 1 && token_of(T - 1) > job.pos + tt - 1;
-                if (ok)
+                const bool skip_last = T > 1 && jv.token_of(T - 1) > job.pos + tt - 1;
+                if (ok && E4M3) {
+                    ok = nq == 2 ? mma_issue_codes<2>(sh, tmem, qdesc0, kdesc0, vdesc0, T, skip_last, a.timeout_ns)
+                                 : mma_issue_codes<1>(sh, tmem, qdesc0, kdesc0, vdesc0, T, false, a.timeout_ns);
+                } else if (ok) {
+                    const uint32_t id_qk = idesc_bf16_f32(128, 128, 0);
+                    const uint32_t id_pv = idesc_bf16_f32(128, 128, 1);
                     ok = nq == 2 ? mma_issue_loop<2>(&bars, tmem, qdesc0, kdesc0, vdesc0, id_qk, id_pv, T, skip_last,
                                                      a.timeout_ns, &abort_flag)
                                  : mma_issue_loop<1>(&bars, tmem, qdesc0, kdesc0, vdesc0, id_qk, id_pv, T, false,
                                                      a.timeout_ns, &abort_flag);
+                }
                 if (!ok) {
                     fail(&abort_flag, a.status);
                     mma_commit(&bars.drain);
@@ -440,265 +497,297 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 }
             }
         } else if (E4M3 && warp >= 12) {
-            // ------------------------------------------------------------ codes to f16 keys and bf16 values
-            // Eight lanes take a row, 16 codes each. The two 16-byte pieces they become go to the swizzled
-            // place, the lanes of the second half in the other order, so that eight lanes write 128 bytes of
-            // different banks. Thread x also looks after the scales of row x, one tile ahead.
+            // ------------------------------------------------------------ V: codes to bf16
+            // Eight lanes take a row, 16 codes each; a warp takes four rows of every 16. The two 16-byte pieces
+            // that 16 codes become go to the swizzled place, the lanes of the second half in the other order, so
+            // that eight lanes write 128 bytes of different banks. Lane x keeps the scale of the warp's row x, looked
+            // up two tiles ahead (the page) and one ahead (the byte).
             const int x = tid - 384, sub = x & 7, r16 = x >> 3;
             const int c0 = 2 * (sub & 3), late = sub >> 2;
+            const int my_row = 16 * (lane >> 2) + 4 * (warp - 12) + (lane & 3);
             uint64_t* const s_last = bars.s_full[nq - 1];
-            uint32_t ks = 0, vs = 0;
-            auto load_scales = [&](int t) {
-                const int place = cache_row(a.c, a.b, job.b, token_of(t) + x);
-                ks = vs = 127;
-                if (place >= 0) {
-                    const int page = place / a.c.page_size;
-                    const int64_t at = (static_cast<int64_t>(page) * a.c.Hkv + job.j) * a.c.page_size + place - page * a.c.page_size;
-                    ks = a.c.ks[at];
-                    vs = a.c.vs[at];
-                }
+            auto place_of = [&](int t) { return t < T ? cache_row(a.c, a.b, job.b, jv.token_of(t) + my_row) : -1; };
+            auto byte_of = [&](int place) -> uint32_t {
+                if (place < 0) return 127u;
+                const int page = place / a.c.page_size;
+                return a.c.vs[(static_cast<int64_t>(page) * a.c.Hkv + job.j) * a.c.page_size + place - page * a.c.page_size];
             };
-            load_scales(0);
-            bool ok = mbar_wait_bounded(&raw.q_ready, 0, a.timeout_ns, &abort_flag);
-            const float q_scale = a.a.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 + f16_exponent(sh.q_top)) << 23);
-            for (int t = 0; t <= T && ok; ++t) {
+            uint32_t next_scale = byte_of(place_of(0));
+            int next_place = place_of(1);
+            bool ok = true;
+            for (int t = 0; t < T; ++t) {
                 const int st = t & 1;
-                // the tiles of this step were last read by MMAs of step t - 2, the scales' places by the softmax of tile t - 4
-                if (t >= 2) ok = mbar_wait_bounded(&s_last[st], ((t - 2) >> 1) & 1, a.timeout_ns, &abort_flag);
+                const uint32_t scale = next_scale;
+                next_scale = byte_of(next_place);
+                next_place = place_of(t + 2);
+                // the bf16 stage was last read by the product with V(t - 2), which S(t - 1) was issued after
+                ok = (t < 2 || mbar_wait_bounded(&s_last[st ^ 1], ((t - 1) >> 1) & 1, a.timeout_ns, &abort_flag)) &&
+                     mbar_wait_bounded(&sh.raw_full[st], (t >> 1) & 1, a.timeout_ns, &abort_flag);
+                ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
-                if (t < T) {
-                    sh.kscale[t & 3][x] = fmaxf(scale_value(ks) * q_scale, 1e-37f);  // not 0: hidden logits stay -inf
-                    sh.vscale[t & 3][x] = static_cast<uint8_t>(vs);
-                    if (t + 1 < T) load_scales(t + 1);
-                }
-                if (t > 0) {
-                    const int u = t - 1;
-                    // (step u: every thread wrote its row's scales)
-                    ok = mbar_wait_bounded(&bars.kv_full[u & 1], (u >> 1) & 1, a.timeout_ns, &abort_flag) &&
-                         mbar_wait_bounded(&raw.full[1], u & 1, a.timeout_ns, &abort_flag);
-                    if (!ok) break;
-                    const uint8_t* from = smem + kOffRaw + kRawBytes + r16 * kHeadDim + sub * 16;
-                    uint8_t* to = smem + kOffV + (u & 1) * kTileBytes + (sub >> 2) * kHalf + r16 * 128;
-                    const int t0 = token_of(u);
-                    const bool unseen = has_unseen(t0);
+                const uint8_t* from = smem + off_raw(true) + st * kCodeBytes + r16 * kHeadDim + sub * 16;
+                uint8_t* to = smem + off_v(true) + st * kTileBytes + (sub >> 2) * kHalf + r16 * 128;
+                uint8_t* const to0 = to + (((c0 + late) ^ (r16 & 7)) << 4);
+                uint8_t* const to1 = to + (((c0 + 1 - late) ^ (r16 & 7)) << 4);
+                const int t0 = jv.token_of(t);
+                const bool unseen = jv.has_unseen(t0);
 #pragma unroll 4
-                    for (int i = 0; i < 8; ++i) {
-                        const uint4 w = *reinterpret_cast<const uint4*>(from + i * 16 * kHeadDim);
-                        const float f = scale_value(sh.vscale[u & 3][16 * i + r16]);
-                        const uint2 y0 = e4m3x4_to_bf16(w.x, f), y1 = e4m3x4_to_bf16(w.y, f);
-                        const uint2 y2 = e4m3x4_to_bf16(w.z, f), y3 = e4m3x4_to_bf16(w.w, f);
-                        uint4 p = make_uint4(y0.x, y0.y, y1.x, y1.y), q = make_uint4(y2.x, y2.y, y3.x, y3.y);
-                        if (unseen) {
-                            const int tok = t0 + 16 * i + r16;
-                            if (tok > last || (tok < lo && tok >= a.a.n_sink)) p = q = make_uint4(0, 0, 0, 0);
-                        }
-                        uint8_t* dst = to + i * 16 * 128;  // row 16 i + r16: r16 & 7 decides the swizzle
-                        *reinterpret_cast<uint4*>(dst + (((c0 + late) ^ (r16 & 7)) << 4)) = late ? q : p;
-                        *reinterpret_cast<uint4*>(dst + (((c0 + 1 - late) ^ (r16 & 7)) << 4)) = late ? p : q;
-                    }
-                    mbar_arrive(&raw.empty[1]);
+                for (int i = 0; i < 8; ++i) {
+                    const uint4 w = *reinterpret_cast<const uint4*>(from + i * 16 * kHeadDim);
+                    const float f = scale_value(__shfl_sync(0xFFFFFFFFu, scale, 4 * i + (lane >> 3)));
+                    const uint2 y0 = e4m3x4_to_bf16(w.x, f), y1 = e4m3x4_to_bf16(w.y, f);
+                    const uint2 y2 = e4m3x4_to_bf16(w.z, f), y3 = e4m3x4_to_bf16(w.w, f);
+                    uint4 p = make_uint4(y0.x, y0.y, y1.x, y1.y), q = make_uint4(y2.x, y2.y, y3.x, y3.y);
+                    if (unseen && jv.unseen(t0 + 16 * i + r16)) p = q = make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4*>(to0 + i * 16 * 128) = late ? q : p;
+                    *reinterpret_cast<uint4*>(to1 + i * 16 * 128) = late ? p : q;
                 }
-                if (t < T) {
-                    ok = mbar_wait_bounded(&raw.full[0], t & 1, a.timeout_ns, &abort_flag);
-                    if (!ok) break;
-                    const uint8_t* from = smem + kOffRaw + r16 * kHeadDim + sub * 16;
-                    uint8_t* to = smem + kOffK + st * kTileBytes + (sub >> 2) * kHalf + r16 * 128;
-#pragma unroll 4
-                    for (int i = 0; i < 8; ++i) {
-                        const uint4 w = *reinterpret_cast<const uint4*>(from + i * 16 * kHeadDim);
-                        const uint4 p = make_uint4(e4m3x2_to_f16x2(w.x), e4m3x2_to_f16x2(w.x >> 16), e4m3x2_to_f16x2(w.y), e4m3x2_to_f16x2(w.y >> 16));
-                        const uint4 q = make_uint4(e4m3x2_to_f16x2(w.z), e4m3x2_to_f16x2(w.z >> 16), e4m3x2_to_f16x2(w.w), e4m3x2_to_f16x2(w.w >> 16));
-                        uint8_t* dst = to + i * 16 * 128;
-                        *reinterpret_cast<uint4*>(dst + (((c0 + late) ^ (r16 & 7)) << 4)) = late ? q : p;
-                        *reinterpret_cast<uint4*>(dst + (((c0 + 1 - late) ^ (r16 & 7)) << 4)) = late ? p : q;
-                    }
-                    mbar_arrive(&raw.empty[0]);
-                }
+                mbar_arrive(&sh.raw_empty[st]);
                 fence_proxy_async_smem();
-                mbar_arrive(&bars.kv_full[st]);
+                mbar_arrive(&sh.v_full[st]);
             }
             if (!ok) fail(&abort_flag, a.status);
         }
     } else {
         if (E4M3) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
-        if ((warp >> 2) < nq) {
-            // ------------------------------------------------------------ softmax + epilogue
-            const int qt = warp >> 2;
-            const int quarter = warp & 3;
-            const int r = quarter * 32 + lane;
-            const int pos_first = job.pos + qt * tt;                      // tokens of the tile
-            const int pos_last = qt + 1 == nq ? last : pos_first + tt - 1;
-            int p = pos_first + r / g;
-            p = p < pos_last ? p : pos_last;  // rows past the tile's end see what its last row sees
-            const uint32_t lane_base = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
-            const uint32_t s_addr = lane_base + qt * 256;
-            const uint32_t o_addr = s_addr + 128;
-            float m_run = -INFINITY, l_run = 0.f;
-            bool ok = true;
-            if (E4M3) {
-                // Q to f16, by one power of two for all rows of the CTA: with the largest finite |q| brought to
-                // 2^14 .. 2^15, what the rows' smaller values lose is 2^-39 of it.
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.q_full, 0, a.timeout_ns, &abort_flag));
-                uint8_t* row = smem + kOffQ + qt * kTileBytes + r * 128;
-                uint32_t top = 0;
-                if (r < (qt + 1 == nq ? job.ntok - qt * tt : tt) * g) {
-#pragma unroll 4
-                    for (int i = 0; i < 16; ++i) {
-                        const uint4 w = *reinterpret_cast<const uint4*>(row + (i >> 3) * kHalf + (((i & 7) ^ (r & 7)) << 4));
-                        const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+        // ------------------------------------------------------------ softmax + epilogue
+        const int qt = warp >> 2;
+        const int quarter = warp & 3;
+        const int r = quarter * 32 + lane;
+        const uint32_t lane_base = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+        const uint32_t s_addr = lane_base + qt * 256;
+        const uint32_t o_addr = s_addr + 128;
+        float* const ks = sh.kscale[warp];
+        // S row of a tile; columns [lim, 128) and [gap, low) are not seen
+        auto load_s = [&](uint32_t (&sr)[128], bool masked, int lim, int gap, int low) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint32_t x = (v[e] << 16) & 0x7FFFFFFFu, y = v[e] & 0x7FFF0000u;
-                            top = max(top, max(x >= 0x7F800000u ? 0u : x, y >= 0x7F800000u ? 0u : y));
-                        }
-                    }
-                }
-                top = __reduce_max_sync(0xFFFFFFFFu, top);
-                if (lane == 0) atomicMax(&sh.q_top, top);
-                named_barrier(2, 128 * nq);
-                const float down = __uint_as_float(static_cast<uint32_t>(127 - f16_exponent(sh.q_top)) << 23);
-#pragma unroll 4
-                for (int i = 0; i < 16; ++i) {
-                    uint4* at = reinterpret_cast<uint4*>(row + (i >> 3) * kHalf + (((i & 7) ^ (r & 7)) << 4));
-                    const uint4 w = *at;
-                    auto half = [&](uint32_t v) { return pack_f16x2(__uint_as_float(v << 16) * down, __uint_as_float(v & 0xFFFF0000u) * down); };
-                    *at = make_uint4(half(w.x), half(w.y), half(w.z), half(w.w));
-                }
-                fence_proxy_async_smem();
-                named_barrier(2, 128 * nq);
-                if (qt == 0) mbar_arrive(&raw.q_ready);
+            for (int c = 0; c < 4; ++c)
+                tmem_ld32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[c * 32]));
+            tmem_ld_wait();
+            if (masked) {
+#pragma unroll
+                for (int c = 0; c < 128; ++c)
+                    if (c >= lim || (c >= gap && c < low)) sr[c] = 0xFF800000u;
             }
-            // S row of a tile; columns [lim, 128) and [gap, low) are not seen
-            auto load_s = [&](uint32_t (&sr)[128], bool masked, int lim, int gap, int low) {
+        };
+        // p = 2^(s scale - m) of keys [64 h, 64 h + 64) as bf16 pairs; returns their sum
+        // (8-bit: a scale for each key, from shared memory)
+        auto exp_half = [&](const float* s, int h, float neg_m, uint32_t (&pk)[32]) {
+            float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    tmem_ld32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[c * 32]));
-                tmem_ld_wait();
-                if (masked) {
+            for (int i = 0; i < 32; i += 2) {
+                const float4 f = E4M3 ? *reinterpret_cast<const float4*>(ks + h * 64 + 2 * i)
+                                      : make_float4(a.a.scale_log2, a.a.scale_log2, a.a.scale_log2, a.a.scale_log2);
 #pragma unroll
-                    for (int c = 0; c < 128; ++c)
-                        if (c >= lim || (c >= gap && c < low)) sr[c] = 0xFF800000u;
-                }
-            };
-            // p = 2^(s scale - m) of keys [64 h, 64 h + 64) as bf16 pairs; returns their sum
-            // (8-bit: scale 2^e of each key, from shared memory)
-            auto exp_half = [&](const float* s, const float* ks, int h, float neg_m, uint32_t (&pk)[32]) {
-                float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
+                for (int k = 0; k < 2; ++k) {
                     float x0, x1;
-                    const float2 f = E4M3 ? *reinterpret_cast<const float2*>(ks + h * 64 + 2 * i) : make_float2(a.a.scale_log2, a.a.scale_log2);
-                    ffma2(x0, x1, s[h * 64 + 2 * i], s[h * 64 + 2 * i + 1], f.x, f.y, neg_m, neg_m);
+                    ffma2(x0, x1, s[h * 64 + 2 * (i + k)], s[h * 64 + 2 * (i + k) + 1], k ? f.z : f.x, k ? f.w : f.y, neg_m, neg_m);
                     x0 = ex2(x0);
                     x1 = ex2(x1);
-                    const int jj = (i & 3) * 2;
+                    const int jj = ((i + k) & 3) * 2;
                     fadd2(acc[jj], acc[jj + 1], acc[jj], acc[jj + 1], x0, x1);
-                    pk[i] = pack_bf16x2(x0, x1);
+                    pk[i + k] = pack_bf16x2(x0, x1);
                 }
-                return ((acc[0] + acc[1]) + (acc[2] + acc[3])) + ((acc[4] + acc[5]) + (acc[6] + acc[7]));
-            };
-            for (int t = 0; t < T; ++t) {
+            }
+            return ((acc[0] + acc[1]) + (acc[2] + acc[3])) + ((acc[4] + acc[5]) + (acc[6] + acc[7]));
+        };
+        float m_run = -INFINITY, l_run = 0.f;
+        bool ok = true;
+        JobView jv{};
+        int T = 0, pos_first = 0, pos_last = 0, p = 0;
+        // 8-bit: lane x looks up the scales of the keys 4 x .. 4 x + 3 of a tile, its page two tiles ahead, the bytes one ahead
+        int next_place = -1;
+        uint32_t next_scales = 0x7F7F7F7Fu;
+        float q_scale = 0.f;
+        auto place_of = [&](int t) { return t < T ? cache_row(a.c, a.b, jv.job.b, jv.token_of(t) + 4 * lane) : -1; };
+        auto scales_of = [&](int place) -> uint32_t {
+            if (place < 0) return 0x7F7F7F7Fu;
+            const int page = place / a.c.page_size;
+            return *reinterpret_cast<const uint32_t*>(a.c.ks + (static_cast<int64_t>(page) * a.c.Hkv + jv.job.j) * a.c.page_size + place - page * a.c.page_size);
+        };
+        // Tile -1 is whatever TMEM and shared memory hold: its softmax brings the code into the instruction cache
+        // while the CTA waits for the plan (the first tile of a call took 10,000 to 20,000 cycles for that).
+#pragma unroll 1
+        for (int t = first_wave ? -1 : 0;; ++t) {
+            if (t == 0) {
+                jv = load_job(a);
+                T = qt < jv.nq ? jv.T : 0;
+                pos_first = jv.job.pos + qt * tt;  // tokens of the tile
+                pos_last = qt + 1 == jv.nq ? jv.last : pos_first + tt - 1;
+                p = pos_first + r / g;
+                p = p < pos_last ? p : pos_last;  // rows past the tile's end see what its last row sees
+                m_run = -INFINITY;
+                l_run = 0.f;
+                if (E4M3 && T > 0) {
+                    next_scales = scales_of(place_of(0));
+                    next_place = place_of(1);
+                    // Q to two e4m3 parts, Q = Q1 + Q2, by one power of two for all rows of the CTA that brings the
+                    // largest finite |q| to 2^7 .. 2^8. Q1 takes four of the eight significant bits, Q2 the rest;
+                    // what is below 2^-10, 2^-18 of the largest, is lost.
+                    ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.q_full, 0, a.timeout_ns, &abort_flag));
+                    uint8_t* row = smem + kOffQ + qt * kTileBytes + r * 128;
+                    uint4 w[16];  // dimensions 8 i .. 8 i + 7
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) w[i] = *reinterpret_cast<const uint4*>(row + (i >> 3) * kHalf + (((i & 7) ^ (r & 7)) << 4));
+                    uint32_t top = 0;
+                    if (r < (qt + 1 == jv.nq ? jv.job.ntok - qt * tt : tt) * g) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const uint32_t x = (v[e] << 16) & 0x7FFFFFFFu, y = v[e] & 0x7FFF0000u;
+                                top = max(top, max(x >= 0x7F800000u ? 0u : x, y >= 0x7F800000u ? 0u : y));
+                            }
+                        }
+                    }
+                    top = __reduce_max_sync(0xFFFFFFFFu, top);
+                    if (lane == 0) atomicMax(&sh.q_top, top);
+                    named_barrier(2, 128 * jv.nq);
+                    const int e = f16_exponent(sh.q_top) + 7;
+                    const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+                    q_scale = a.a.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {  // 16 dimensions: one 16-byte piece of each part
+                        const uint32_t v[8] = {w[2 * i].x, w[2 * i].y, w[2 * i].z, w[2 * i].w, w[2 * i + 1].x, w[2 * i + 1].y, w[2 * i + 1].z, w[2 * i + 1].w};
+                        uint32_t hi[4], lo[4];
+#pragma unroll
+                        for (int e4 = 0; e4 < 4; ++e4) {
+                            hi[e4] = lo[e4] = 0;
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                const float x = __uint_as_float(v[2 * e4 + k] << 16) * down, y = __uint_as_float(v[2 * e4 + k] & 0xFFFF0000u) * down;
+                                const uint32_t h = f32_to_e4m3x2(x, y);
+                                const float2 back = f16x2_to_f32(e4m3x2_to_f16x2(h));
+                                hi[e4] |= h << (16 * k);
+                                lo[e4] |= f32_to_e4m3x2(x - back.x, y - back.y) << (16 * k);
+                            }
+                        }
+                        uint8_t* at = row + ((i ^ (r & 7)) << 4);
+                        *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                        *reinterpret_cast<uint4*>(at + kCodeBytes) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                    }
+                    fence_proxy_async_smem();
+                    named_barrier(2, 128 * jv.nq);
+                    if (qt == 0) mbar_arrive(&sh.q_ready);
+                }
+            }
+            if (t >= T && t >= 0) break;
+            if (t >= 0) {
                 const bool got = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.s_full[qt][t & 1], (t >> 1) & 1, a.timeout_ns, &abort_flag));
                 if (!got) {
                     ok = false;
                     break;
                 }
-                tc_fence_after();
-                // (complete: the products were made of it) orders the reads of the tile's scales after their writes
-                if (E4M3 && !__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.kv_full[t & 1], (t >> 1) & 1, a.timeout_ns, &abort_flag))) {
+            }
+            tc_fence_after();
+            if (E4M3) {
+                // not 0: hidden logits stay -inf
+                const float4 f = make_float4(fmaxf(scale_value(next_scales & 255u) * q_scale, 1e-37f),
+                                             fmaxf(scale_value((next_scales >> 8) & 255u) * q_scale, 1e-37f),
+                                             fmaxf(scale_value((next_scales >> 16) & 255u) * q_scale, 1e-37f),
+                                             fmaxf(scale_value(next_scales >> 24) * q_scale, 1e-37f));
+                __syncwarp();  // the tile before is read
+                *reinterpret_cast<float4*>(ks + 4 * lane) = f;
+                __syncwarp();
+                next_scales = scales_of(next_place);
+                next_place = place_of(t + 2);
+            }
+            const int t0 = jv.token_of(t);
+            const bool masked = t < 0 || t0 + kTile - 1 > pos_first ||
+                                (a.a.n_local >= 0 && pos_last - t0 > a.a.n_local && t0 + kTile - 1 >= a.a.n_sink);
+            const int lim = p - t0 + 1;  // keys t0 + c with c >= lim are in the future
+            const int gap = a.a.n_sink - t0, low = a.a.n_local >= 0 && p - t0 > a.a.n_local ? p - t0 - a.a.n_local : 0;
+            // The fast and the exact path of k_sparse_attn: exponentials against the reference as it
+            // stands unless the tile's sum shows a logit far above it.
+            bool exact = !__all_sync(0xFFFFFFFFu, m_run != -INFINITY);
+            float sum;
+#pragma unroll 1
+            for (;;) {
+                uint32_t sr[128];
+                load_s(sr, masked, lim, gap, low);
+                const float* s = reinterpret_cast<const float*>(sr);
+                if (exact) {
+                    float mx8[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) mx8[i] = E4M3 ? s[i] * ks[i] : s[i];
+#pragma unroll
+                    for (int c = 8; c < 120; c += 16)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int x = c + 2 * i;
+                            mx8[i] = E4M3 ? fmax3(mx8[i], s[x] * ks[x], s[x + 1] * ks[x + 1]) : fmax3(mx8[i], s[x], s[x + 1]);
+                        }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) mx8[i] = fmaxf(mx8[i], E4M3 ? s[120 + i] * ks[120 + i] : s[120 + i]);
+                    const float mx = fmax3(fmax3(mx8[0], mx8[1], mx8[2]), fmax3(mx8[3], mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7]));
+                    const float m_new = fmaxf(m_run, E4M3 ? mx : mx * a.a.scale_log2);
+                    const bool raise = m_new > m_run + kRescaleThreshold;
+                    // the O rescale is warp-collective: taken by the whole warp when any row needs it
+                    if (__any_sync(0xFFFFFFFFu, raise)) {
+                        const float alpha = raise ? ex2(m_run - m_new) : 1.0f;
+                        l_run *= alpha;
+                        if (t > 0) {
+#pragma unroll 1
+                            for (int c = 0; c < 8; ++c) {
+                                uint32_t v[16];
+                                tmem_ld16(o_addr + c * 16, v);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
+                                tmem_st16(o_addr + c * 16, v);
+                            }
+                        }
+                        if (raise) m_run = m_new;
+                    }
+                }
+                const float neg_m = (m_run == -INFINITY) ? 0.f : -m_run;
+                uint32_t pk[2][32];
+                sum = exp_half(s, 0, neg_m, pk[0]);
+                sum += exp_half(s, 1, neg_m, pk[1]);
+                if (!exact && __any_sync(0xFFFFFFFFu, !(sum <= kFastSumLimit))) {
+                    exact = true;
+                    continue;
+                }
+                if (t >= 0) {  // (the first products may be on their way)
+                    tmem_st32(s_addr, pk[0]);
+                    tmem_st32(s_addr + 32, pk[1]);
+                } else {
+                    sum += __uint_as_float(pk[0][0] ^ pk[1][31]);  // tile -1: keeps the code
+                }
+                break;
+            }
+            l_run += sum;
+            if (t < 0) continue;
+            tmem_st_wait();
+            if (!E4M3 && qt == 0 && jv.has_unseen(t0)) {
+                // value rows that no row of the CTA sees: 0 times what lies there may be NaN. The MMA thread
+                // waits for this group before either tile's product with them.
+                const bool landed = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.kv_full[(t + 1) & 1], ((t + 1) >> 1) & 1, a.timeout_ns, &abort_flag));
+                if (!landed) {
                     ok = false;
                     break;
                 }
-                const float* ks = sh.kscale[t & 3];
-                const int t0 = token_of(t);
-                const bool masked = t0 + kTile - 1 > pos_first ||
-                                    (a.a.n_local >= 0 && pos_last - t0 > a.a.n_local && t0 + kTile - 1 >= a.a.n_sink);
-                const int lim = p - t0 + 1;  // keys t0 + c with c >= lim are in the future
-                const int gap = a.a.n_sink - t0, low = a.a.n_local >= 0 && p - t0 > a.a.n_local ? p - t0 - a.a.n_local : 0;
-                // The fast and the exact path of k_sparse_attn: exponentials against the reference as it
-                // stands unless the tile's sum shows a logit far above it.
-                bool exact = !__all_sync(0xFFFFFFFFu, m_run != -INFINITY);
-                float sum;
-#pragma unroll 1
-                for (;;) {
-                    uint32_t sr[128];
-                    load_s(sr, masked, lim, gap, low);
-                    const float* s = reinterpret_cast<const float*>(sr);
-                    if (exact) {
-                        float mx8[8];
+                if (jv.unseen(t0 + r)) {
+                    uint8_t* row = smem + off_v(false) + (t & 1) * kTileBytes + r * 128;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) mx8[i] = E4M3 ? s[i] * ks[i] : s[i];
-#pragma unroll
-                        for (int c = 8; c < 120; c += 16)
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                const int x = c + 2 * i;
-                                mx8[i] = E4M3 ? fmax3(mx8[i], s[x] * ks[x], s[x + 1] * ks[x + 1]) : fmax3(mx8[i], s[x], s[x + 1]);
-                            }
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) mx8[i] = fmaxf(mx8[i], E4M3 ? s[120 + i] * ks[120 + i] : s[120 + i]);
-                        const float mx = fmax3(fmax3(mx8[0], mx8[1], mx8[2]), fmax3(mx8[3], mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7]));
-                        const float m_new = fmaxf(m_run, E4M3 ? mx : mx * a.a.scale_log2);
-                        const bool raise = m_new > m_run + kRescaleThreshold;
-                        // the O rescale is warp-collective: taken by the whole warp when any row needs it
-                        if (__any_sync(0xFFFFFFFFu, raise)) {
-                            const float alpha = raise ? ex2(m_run - m_new) : 1.0f;
-                            l_run *= alpha;
-                            if (t > 0) {
-#pragma unroll 1
-                                for (int c = 0; c < 8; ++c) {
-                                    uint32_t v[16];
-                                    tmem_ld16(o_addr + c * 16, v);
-                                    tmem_ld_wait();
-#pragma unroll
-                                    for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
-                                    tmem_st16(o_addr + c * 16, v);
-                                }
-                            }
-                            if (raise) m_run = m_new;
-                        }
-                    }
-                    const float neg_m = (m_run == -INFINITY) ? 0.f : -m_run;
-                    uint32_t pk[2][32];
-                    sum = exp_half(s, ks, 0, neg_m, pk[0]);
-                    sum += exp_half(s, ks, 1, neg_m, pk[1]);
-                    if (!exact && __any_sync(0xFFFFFFFFu, !(sum <= kFastSumLimit))) {
-                        exact = true;
-                        continue;
-                    }
-                    tmem_st32(s_addr, pk[0]);
-                    tmem_st32(s_addr + 32, pk[1]);
-                    break;
+                    for (int i = 0; i < 16; ++i)
+                        *reinterpret_cast<uint4*>(row + (i >> 3) * kHalf + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
                 }
-                l_run += sum;
-                tmem_st_wait();
-                if (!E4M3 && qt == 0 && has_unseen(t0)) {
-                    // value rows that no row of the CTA sees: 0 times what lies there may be NaN. The MMA thread
-                    // waits for this group before either tile's product with them.
-                    const bool landed = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.kv_full[(t + 1) & 1], ((t + 1) >> 1) & 1, a.timeout_ns, &abort_flag));
-                    if (!landed) {
-                        ok = false;
-                        break;
-                    }
-                    const int tok = t0 + r;
-                    if (tok > last || (tok < lo && tok >= a.a.n_sink)) {
-                        uint8_t* row = smem + kOffV + (t & 1) * kTileBytes + r * 128;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            *reinterpret_cast<uint4*>(row + (i >> 3) * kHalf + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
-                    }
-                    fence_proxy_async_smem();
-                }
-                tc_fence_before();
-                mbar_arrive(&bars.p_full[qt]);
+                fence_proxy_async_smem();
             }
+            tc_fence_before();
+            mbar_arrive(&bars.p_full[qt]);
+        }
+        if (T > 0) {
+            const ChunkJob& job = jv.job;
             bool go = __all_sync(0xFFFFFFFFu, ok && !abort_flag);
             if (go) go = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.o_full, 0, a.timeout_ns, &abort_flag));
             if (go) {
                 tc_fence_after();
                 // Every MMA is done and every copy landed, so the tiles in shared memory are free: a warp
                 // stages its 32 output rows there and stores whole rows.
-                const int rows = (qt + 1 == nq ? job.ntok - qt * tt : tt) * g - quarter * 32;  // of this warp, if more than 0
+                const int rows = (qt + 1 == jv.nq ? job.ntok - qt * tt : tt) * g - quarter * 32;  // of this warp, if more than 0
                 if (job.slot < 0) {
                     const float inv_l = l_run > 0.f ? 1.0f / l_run : 0.f;
                     uint32_t v[128];
@@ -731,7 +820,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                         a.a.lse[static_cast<int64_t>(job.row0 + qt * tt + r / g) * a.a.Hq + job.j * g + r % g] =
                             l_run == 0.f ? -INFINITY : (m_run + __log2f(l_run)) * 0.6931471805599453f;
                 } else {
-                    uint8_t* stage = smem + warp * 32 * 512;  // 128 KB: the Q and K tiles
+                    uint8_t* stage = smem + warp * 32 * 512;  // 128 KB of tiles
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         uint32_t v[32];
@@ -744,9 +833,10 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                     }
                     __syncwarp();
                     const int64_t at = static_cast<int64_t>(job.slot) * a.part_rows + qt * kTile + quarter * 32;
-                    for (int x = 0; x < 32 && x < rows; ++x)
-                        reinterpret_cast<uint4*>(a.part_o + (at + x) * kHeadDim)[lane] =
-                            *reinterpret_cast<const uint4*>(stage + x * 512 + ((lane ^ x) << 4));
+                    uint4* dst = reinterpret_cast<uint4*>(a.part_o + at * kHeadDim) + lane;
+#pragma unroll 8
+                    for (int x = 0; x < 32; ++x)
+                        if (x < rows) dst[x * (kHeadDim / 4)] = *reinterpret_cast<const uint4*>(stage + x * 512 + ((lane ^ x) << 4));
                     if (lane < rows) a.part_ml[at + lane] = make_float2(m_run, l_run);
                 }
             } else {
@@ -843,8 +933,8 @@ cudaError_t run_chunks(const ChunkArgs& a, cudaStream_t st)
     const uint64_t pool = static_cast<uint64_t>(a.c.num_pages) * a.c.page_size;
     bool ok = scale_host::make_rows_map(&tq, a.a.q, kHeadDim, a.a.Hq, a.a.q_stride, a.b.n_rows, a.a.g, a.tile_tokens);
     if (E4M3)
-        ok = ok && scale_host::make_byte_rows_map(&tk, a.c.k, kHeadDim, a.c.Hkv, pool, a.box) &&
-             scale_host::make_byte_rows_map(&tv, a.c.v, kHeadDim, a.c.Hkv, pool, a.box);
+        ok = ok && scale_host::make_byte_rows_map(&tk, a.c.k, kHeadDim, a.c.Hkv, pool, a.box, true) &&
+             scale_host::make_byte_rows_map(&tv, a.c.v, kHeadDim, a.c.Hkv, pool, a.box, false);
     else
         ok = ok && scale_host::make_token_major_map(&tk, a.c.k, kHeadDim, a.c.Hkv, pool, 64, a.box) &&
              scale_host::make_token_major_map(&tv, a.c.v, kHeadDim, a.c.Hkv, pool, 64, a.box);
@@ -864,7 +954,7 @@ size_t chunk_ws_bytes(int g, int Hkv, int n_seqs, int n_rows, int max_rows)
     return chunk_layout(g, Hkv, n_seqs, n_rows, max_rows).end;
 }
 
-cudaError_t launch_chunks(const AttendView& a, const CacheView& c, bool e4m3, const BatchView& b, int few, int sms,
+cudaError_t launch_chunks(const AttendView& a, const CacheView& c, bool e4m3, const BatchView& b, int sms,
                           int32_t* status, uint8_t* ws, uint64_t timeout_ns, cudaStream_t st)
 {
     const ChunkWs w = chunk_layout(a.g, c.Hkv, b.n_seqs, b.n_rows, b.max_rows);
@@ -874,7 +964,6 @@ cudaError_t launch_chunks(const AttendView& a, const CacheView& c, bool e4m3, co
     x.b = b;
     x.p = ChunkPlan{reinterpret_cast<int32_t*>(ws + w.counts), reinterpret_cast<ChunkJob*>(ws + w.jobs),
                     reinterpret_cast<ChunkMerge*>(ws + w.merges), w.max_jobs, w.max_merges, w.max_slots};
-    x.few = few;
     x.sms = sms;
     x.tile_tokens = kTile / a.g;
     x.box = 16;

@@ -369,10 +369,31 @@ __host__ __device__ constexpr uint32_t idesc_bf16_f32(uint32_t M, uint32_t N, ui
            | ((M >> 4) << 24);       // M / 16
 }
 
-// idesc_bf16_f32 with f16 operands.
-__host__ __device__ constexpr uint32_t idesc_f16_f32(uint32_t M, uint32_t N, uint32_t b_mn_major)
+// Instruction descriptor, kind::f8f6f4: fp32 accumulator, e4m3 A and B, both K-major, shape M x N.
+__host__ __device__ constexpr uint32_t idesc_e4m3_f32(uint32_t M, uint32_t N)
 {
-    return idesc_bf16_f32(M, N, b_mn_major) & ~((1u << 7) | (1u << 10));
+    return (1u << 4)  // D format: f32 (A and B format 0: e4m3)
+           | ((N >> 3) << 17) | ((M >> 4) << 24);
+}
+
+// Four MMAs D (+)= A_j * B_j over one 128-deep K range of e4m3 held as 128-byte rows of 128-byte-swizzled
+// K-major tiles: the descriptors advance by 32 bytes per 32-element K step.
+__device__ __forceinline__ void mma_e4m3_k128(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                              uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 a, b;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 q, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t"
+        "add.s64 a, %1, 2;\n\tadd.s64 b, %2, 2;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %3, q;\n\t"
+        "add.s64 a, %1, 4;\n\tadd.s64 b, %2, 4;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %3, q;\n\t"
+        "add.s64 a, %1, 6;\n\tadd.s64 b, %2, 6;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %3, q;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(1u)
+        : "memory");
 }
 
 // Shared-memory matrix descriptor, 128-byte swizzle. Addresses and offsets in

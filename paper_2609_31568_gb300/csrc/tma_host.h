@@ -88,10 +88,10 @@ inline bool make_rows_map(CUtensorMap* map, const void* base, uint64_t head_dim,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// A 3-D map over 8-bit rows [n_rows][n_heads][head_dim] with a box of one head of box_t rows, not
-// swizzled, zeros outside. Returns false on failure.
+// A 3-D map over 8-bit rows [n_rows][n_heads][head_dim] (head_dim 128) with a box of one head of box_t rows,
+// 128-byte swizzle or none, zeros outside. Returns false on failure.
 inline bool make_byte_rows_map(CUtensorMap* map, const void* base, uint64_t head_dim, uint64_t n_heads, uint64_t n_rows,
-                               uint32_t box_t)
+                               uint32_t box_t, bool swizzle)
 {
     auto enc = tensor_map_encoder();
     if (!enc) return false;
@@ -100,7 +100,7 @@ inline bool make_byte_rows_map(CUtensorMap* map, const void* base, uint64_t head
     const cuuint32_t box[3] = {static_cast<cuuint32_t>(head_dim), 1, box_t};
     const cuuint32_t estr[3] = {1, 1, 1};
     return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estr,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
