@@ -14,16 +14,19 @@ using namespace scale_ptx;
 
 // ---------------------------------------------------------------- few rows: decode
 
-constexpr int kStep = 16;       // keys of a step; a page holds whole steps
-constexpr int kRowsWarps = 8;
-constexpr int kRowsThreads = 32 * kRowsWarps;
-constexpr int kMaxParts = 2 * kMaxSms * kRowsWarps;  // partial results
-constexpr int kMinSteps = 2;    // steps of a warp before another one helps
-constexpr float kRaise = 8.0f;  // log2 units by which a logit may pass the reference
+constexpr int kStep = 16;          // keys of a step; a page holds whole steps
+constexpr int kMaxRowsWarps = 16;
+constexpr int kMaxParts = 2 * kMaxSms * kMaxRowsWarps;  // partial results
+constexpr int kMinSteps = 8;       // steps of a CTA before another one helps
+constexpr float kRaise = 8.0f;     // log2 units by which a logit may pass the reference
 
-__host__ __device__ constexpr int rows_stages(bool e4m3) { return e4m3 ? 6 : 3; }
+// Warps of a CTA and stages of a warp's ring. 8-bit rows of few query rows take half the copies and 1.3 times the
+// instructions per byte: sixteen warps hide what eight with twice the stages left open (128K tokens 64 us).
+__host__ __device__ constexpr int rows_warps(int nt, bool e4m3) { return e4m3 && nt == 1 ? 16 : 8; }
+__host__ __device__ constexpr int rows_stages(int nt, bool e4m3) { return e4m3 && nt > 1 ? 6 : 3; }
 __host__ __device__ constexpr int rows_step_bytes(bool e4m3) { return e4m3 ? 2 * kStep * kHeadDim + 2 * kStep : 4 * kStep * kHeadDim; }
-__host__ __device__ constexpr int rows_ring_bytes(bool e4m3) { return kRowsWarps * rows_stages(e4m3) * rows_step_bytes(e4m3); }
+__host__ __device__ constexpr int rows_warp_bytes(int nt, bool e4m3) { return rows_stages(nt, e4m3) * rows_step_bytes(e4m3); }
+__host__ __device__ constexpr int rows_ring_bytes(int nt, bool e4m3) { return rows_warps(nt, e4m3) * rows_warp_bytes(nt, e4m3); }
 
 // Steps of a sequence: those of the sinks, then those from the window's first.
 struct Steps {
@@ -51,19 +54,30 @@ struct RowsArgs {
     int part_rows;
 };
 
-// Steps of a run when `warps` warps share the work; the last runs may be shorter or none.
-__device__ __forceinline__ int64_t run_steps(int64_t work, int64_t warps)
-{
-    const int64_t n = work >> 32 ? (work + warps - 1) / warps
-                                 : (static_cast<uint32_t>(work) + static_cast<uint32_t>(warps) - 1) / static_cast<uint32_t>(warps);
-    return n < kMinSteps ? kMinSteps : n;
-}
-
 // x / n, mostly of 32-bit numbers.
-__device__ __forceinline__ int64_t run_of(int64_t x, int64_t n)
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t n)
 {
     return (x | n) >> 32 ? x / n : static_cast<uint32_t>(x) / static_cast<uint32_t>(n);
 }
+
+// How the steps are shared out: CTA c has the steps [c per_cta, (c + 1) per_cta), its warp w the run of per_warp of them
+// from w per_warp on.
+struct Runs {
+    int64_t work, per_cta, per_warp;
+    __device__ __forceinline__ Runs(int64_t n, int ctas, int warps) : work(n)
+    {
+        per_cta = quotient(n + ctas - 1, ctas);
+        per_cta = per_cta < kMinSteps ? kMinSteps : per_cta;
+        per_warp = quotient(per_cta + warps - 1, warps);
+    }
+    __device__ __forceinline__ int64_t cta_end(int64_t c) const { return (c + 1) * per_cta < work ? (c + 1) * per_cta : work; }
+    __device__ __forceinline__ int64_t start(int64_t c, int64_t w) const { return c * per_cta + w * per_warp; }
+    __device__ __forceinline__ int64_t end(int64_t c, int64_t w) const
+    {
+        const int64_t x = start(c, w + 1), y = cta_end(c);
+        return x < y ? x : y;
+    }
+};
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool real)
 {
@@ -123,7 +137,8 @@ struct Item {
 //
 // The work is one list of 16-key steps, sequence by sequence and KV head by KV head, cut into equal runs, one
 // per warp, whatever the lengths: a warp walks its run with a ring of its own in shared memory, so nothing in
-// the loop waits for another warp and the copies run on across items. The rows are the N side of the
+// the loop waits for another warp and the copies run on across items. What the warps of a CTA have of the same item
+// at the ends of their runs is added up there. The rows are the N side of the
 // products: S^T = K Q^T with the step's 16 keys as M, O^T += V^T P^T with 16 dimensions as M, so rows are
 // padded to 8 and not to 16 and a thread keeps the same two rows in both; P changes sides by a register
 // transpose. The reference of a row's exponentials is raised only when a logit passes it by 2^8, so a step
@@ -137,18 +152,18 @@ struct Item {
 // Keys that no row sees are not read: their places are filled with zeros, so nothing that lies there
 // reaches a sum. Bound by HBM: K and V once.
 template <int NT, bool E4M3>
-__global__ void __launch_bounds__(kRowsThreads, 1) k_rows(const __grid_constant__ RowsArgs args)
+__global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __grid_constant__ RowsArgs args)
 {
-    constexpr int kStages = rows_stages(E4M3);
+    constexpr int kStages = rows_stages(NT, E4M3), kWarps = rows_warps(NT, E4M3), kRowsThreads = 32 * kWarps;
     constexpr int kRow = E4M3 ? kHeadDim : 2 * kHeadDim;  // bytes of a held row
     constexpr int kTile = kStep * kRow;
     constexpr int kChunks = kRow / 16;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ int64_t s_sum[kRowsWarps];
+    __shared__ int64_t s_sum[kWarps];  // then the item that a warp's run ends in
     const AttendView& a = args.a;
     const CacheView& c = args.c;
     const BatchView& bt = args.b;
-    int64_t* before = reinterpret_cast<int64_t*>(smem + rows_ring_bytes(E4M3));
+    int64_t* before = reinterpret_cast<int64_t*>(smem + rows_ring_bytes(NT, E4M3));
     pdl_enter();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int quad = lane & 3, oct = lane >> 2;
@@ -178,15 +193,13 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_rows(const __grid_constant_
         if (blockIdx.x == 0)
             for (int i = tid; i <= bt.n_seqs; i += kRowsThreads) args.before[i] = before[i];
     }
-    const int64_t work = before[bt.n_seqs] * c.Hkv;
-    const int64_t per_run = run_steps(work, static_cast<int64_t>(gridDim.x) * kRowsWarps);
-    const int64_t run = static_cast<int64_t>(warp) * gridDim.x + blockIdx.x;  // the first runs on different SMs
-    const int64_t x0 = run * per_run;
-    if (x0 >= work) return;
-    const int64_t n = work - x0 < per_run ? work - x0 : per_run;
+    const Runs runs(before[bt.n_seqs] * c.Hkv, gridDim.x, kWarps);
+    const int64_t run = static_cast<int64_t>(blockIdx.x) * kWarps + warp;
+    const int64_t x0 = runs.start(blockIdx.x, warp), n = runs.end(blockIdx.x, warp) - x0;  // n <= 0: none
+    const uint32_t ring = smem_addr(smem) + warp * rows_warp_bytes(NT, E4M3);
+    int64_t open = -1;  // item that the run ends inside of
 
-    const uint32_t ring = smem_addr(smem) + warp * kStages * rows_step_bytes(E4M3);
-
+    if (n > 0) {
     auto enter = [&](Item& it, int b) {  // the first sequence from b on that has steps
         while (before[b + 1] == before[b]) ++b;
         it.b = b;
@@ -194,6 +207,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_rows(const __grid_constant_
         it.x = steps_of(a, it.s);
     };
     Item load, use;
+    int lp = 0, slot = 0, page = -1;  // where the step to load lies: page of the table, row in it, page of the pool
+    auto look_up = [&]() { page = lp < bt.stride ? bt.table[static_cast<int64_t>(load.b) * bt.stride + lp] : -1; };
     {
         int lo = 0, hi = bt.n_seqs;  // the last sequence whose steps start at or before x0
         while (hi - lo > 1) {
@@ -203,7 +218,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_rows(const __grid_constant_
         }
         enter(load, lo);
         const int64_t rem = x0 - before[load.b] * c.Hkv;
-        load.j = static_cast<int>(run_of(rem, load.x.n));
+        load.j = static_cast<int>(quotient(rem, load.x.n));
         load.step = static_cast<int>(rem - static_cast<int64_t>(load.j) * load.x.n);
         use = load;
     }
@@ -216,26 +231,52 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_rows(const __grid_constant_
         it.j = 0;
         if (it.b + 1 < bt.n_seqs && before[it.b + 1] < before[bt.n_seqs]) enter(it, it.b + 1);
     };
-    // The keys of a step that some row sees, as bits: seen(t) = t <= last and (t >= lo or t < n_sink)
-    auto copy_step = [&](int stage, int place) {
+    auto find_page = [&]() {
+        const int t = token_of(load, load.step);
+        lp = static_cast<int>(static_cast<uint32_t>(t) / static_cast<uint32_t>(c.page_size));
+        slot = t - lp * c.page_size;
+        look_up();
+    };
+    auto advance_load = [&]() {
+        const int it_step = load.step;
+        advance(load);
+        if (load.step == it_step + 1 && load.step != load.x.sinks) {  // the next 16 keys
+            slot += kStep;
+            if (slot >= c.page_size) {
+                slot = 0;
+                ++lp;
+                look_up();
+            }
+        } else {
+            find_page();
+        }
+    };
+    constexpr int kRowsAtOnce = 32 / kChunks;  // rows that the warp's 16-byte copies cover
+    const int my_row = lane / kChunks, my_chunk = lane % kChunks;
+    const int64_t pitch = static_cast<int64_t>(c.Hkv) * kRow;
+    auto copy_step = [&](int stage) {
         const int t0 = token_of(load, load.step);
         const int last = load.s.pos0 + load.s.rows - 1;
         const uint32_t dst = ring + stage * rows_step_bytes(E4M3);
-        const int64_t first = place < 0 ? 0 : place;
+        const bool in_pool = static_cast<uint32_t>(page) < static_cast<uint32_t>(c.num_pages);
+        const int64_t first = in_pool ? static_cast<int64_t>(page) * c.page_size + slot : 0;
+        const int64_t at = (first * c.Hkv + load.j) * kRow + my_row * pitch + my_chunk * 16;
+        const uint8_t *k = c.k + at, *v = c.v + at;
+        // the keys that some row sees: t <= last and (t >= lo or t < n_sink)
+        const bool all = in_pool && t0 + kStep - 1 <= last && (t0 >= load.s.lo || t0 + kStep - 1 < a.n_sink);
 #pragma unroll
         for (int i = 0; i < kTile / 512; ++i) {
-            const int id = i * 32 + lane, row = id / kChunks, ch = id % kChunks;
-            const int t = t0 + row;
-            const bool real = place >= 0 && t <= last && (t >= load.s.lo || t < a.n_sink);
-            const int64_t at = ((real ? first + row : 0) * c.Hkv + load.j) * kRow + ch * 16;
-            const uint32_t to = dst + row * kRow + ((ch ^ (row & 7)) << 4);
-            cp_async16(to, c.k + at, real);
-            cp_async16(to + kTile, c.v + at, real);
+            const int row = i * kRowsAtOnce + my_row, t = t0 + row;
+            const bool real = all || (in_pool && t <= last && (t >= load.s.lo || t < a.n_sink));
+            const uint32_t to = dst + row * kRow + ((my_chunk ^ (row & 7)) << 4);
+            cp_async16(to, real ? k : c.k, real);
+            cp_async16(to + kTile, real ? v : c.v, real);
+            k += kRowsAtOnce * pitch;
+            v += kRowsAtOnce * pitch;
         }
         if (E4M3 && lane < 2) {  // the step's 16 scales lie in one page
-            const int64_t page = first / c.page_size;
-            const int64_t at = (page * c.Hkv + load.j) * c.page_size + (first - page * c.page_size);
-            cp_async16(dst + 2 * kTile + lane * kStep, (lane ? c.vs : c.ks) + at, place >= 0);
+            const int64_t sc = in_pool ? (static_cast<int64_t>(page) * c.Hkv + load.j) * c.page_size + slot : 0;
+            cp_async16(dst + 2 * kTile + lane * kStep, (lane ? c.vs : c.ks) + sc, in_pool);
         }
     };
 
@@ -294,10 +335,18 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_rows(const __grid_constant_
             l[nt][0] = l[nt][1] = 0.f;
         }
     };
-    // (O, reference, sum) of the item's steps [from, to) to the output, or to this run's partial results.
-    auto end_item = [&](int from, int to) {
+    // (O, reference, sum) of the item's steps [from, to): to the output when that is all of them, else to the warp's
+    // ring at the run's end, else to the run's place for an item that ended inside it.
+    auto end_item = [&](int from, int to, bool at_end) {
         const bool whole = from == 0 && to == use.x.n;
-        const int64_t slot = 2 * run + (from == 0);
+        float* const part = at_end ? reinterpret_cast<float*>(smem + warp * rows_warp_bytes(NT, E4M3))
+                                   : args.part_o + 2 * run * args.part_rows * kHeadDim;
+        float2* const part_ml = at_end ? reinterpret_cast<float2*>(part + NT * 8 * kHeadDim) : args.part_ml + 2 * run * args.part_rows;
+        if (at_end && !whole) {
+            cp_async_wait<0>();
+            __syncwarp();
+            open = static_cast<int64_t>(use.b) * c.Hkv + use.j;
+        }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -326,23 +375,21 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_rows(const __grid_constant_
                     if (a.lse && oct == 0)
                         a.lse[row * a.Hq + h] = sum > 0.f ? (m[nt][e] + __log2f(sum)) * 0.6931471805599453f : -INFINITY;
                 } else {
-                    float* part = args.part_o + (slot * args.part_rows + r) * kHeadDim;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        part[16 * i + (E4M3 ? 2 * oct : oct)] = o[i][nt][e];
-                        part[16 * i + (E4M3 ? 2 * oct + 1 : 8 + oct)] = o[i][nt][2 + e];
+                        part[r * kHeadDim + 16 * i + (E4M3 ? 2 * oct : oct)] = o[i][nt][e];
+                        part[r * kHeadDim + 16 * i + (E4M3 ? 2 * oct + 1 : 8 + oct)] = o[i][nt][2 + e];
                     }
-                    if (oct == 0) args.part_ml[slot * args.part_rows + r] = make_float2(m[nt][e], sum);
+                    if (oct == 0) part_ml[r] = make_float2(m[nt][e], sum);
                 }
             }
     };
 
-    int next = cache_row(c, bt, load.b, token_of(load, load.step));  // the next step to load
+    find_page();
     auto load_next = [&](int64_t i, int stage) {
         if (i < n) {
-            copy_step(stage, next);
-            advance(load);
-            if (i + 1 < n) next = cache_row(c, bt, load.b, token_of(load, load.step));
+            copy_step(stage);
+            if (i + 1 < n) advance_load();
         }
         cp_async_commit();
     };
@@ -498,7 +545,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_rows(const __grid_constant_
         }
         stage = stage + 1 == kStages ? 0 : stage + 1;
         if (use.step + 1 == use.x.n || i + 1 == n) {
-            end_item(from, use.step + 1);
+            end_item(from, use.step + 1, i + 1 == n);
             if (i + 1 < n) {
                 advance(use);
                 begin_item();
@@ -509,66 +556,93 @@ __global__ void __launch_bounds__(kRowsThreads, 1) k_rows(const __grid_constant_
         }
     }
     cp_async_wait<0>();
+    }
+    // ---- the pieces at the runs' ends, item by item: a warp takes every kWarps-th row
+    if (lane == 0) s_sum[warp] = open;
+    __syncthreads();
+    for (int r = warp; r < NT * 8; r += kWarps) {
+        for (int w = 0; w < kWarps;) {
+            const int64_t item = s_sum[w];
+            int end = w + 1;
+            while (end < kWarps && s_sum[end] == item) ++end;
+            if (item >= 0) {
+                auto piece = [&](int x) { return reinterpret_cast<const float*>(smem + x * rows_warp_bytes(NT, E4M3)); };
+                auto piece_ml = [&](int x) { return reinterpret_cast<const float2*>(piece(x) + NT * 8 * kHeadDim)[r]; };
+                float top = -INFINITY, sum = 0.f;
+                for (int x = w; x < end; ++x) top = fmaxf(top, piece_ml(x).x);
+                const float base = top == -INFINITY ? 0.f : top;
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int x = w; x < end; ++x) {
+                    const float4 y = reinterpret_cast<const float4*>(piece(x) + r * kHeadDim)[lane];
+                    const float2 ml = piece_ml(x);
+                    const float f = ex2(ml.x - base);
+                    sum = fmaf(ml.y, f, sum);
+                    acc.x = fmaf(y.x, f, acc.x);
+                    acc.y = fmaf(y.y, f, acc.y);
+                    acc.z = fmaf(y.z, f, acc.z);
+                    acc.w = fmaf(y.w, f, acc.w);
+                }
+                const int64_t at = (2 * (static_cast<int64_t>(blockIdx.x) * kWarps + w) + 1) * args.part_rows + r;
+                reinterpret_cast<float4*>(args.part_o + at * kHeadDim)[lane] = acc;
+                if (lane == 0) args.part_ml[at] = make_float2(top, sum);
+            }
+            w = end;
+        }
+    }
 }
 
-// Items that several runs of k_rows share: CTA (item, row), a warp for every eighth run, four dimensions a lane.
-__global__ void __launch_bounds__(256) k_rows_merge(const __grid_constant__ RowsArgs args, int64_t warps)
+// Items that several CTAs or warps of k_rows share: a CTA per item, a warp per row, four dimensions a lane. A CTA of k_rows
+// left one piece of the item, under the first of its runs that has a part of it, and where the item ends inside a
+// run, that run another one.
+__global__ void __launch_bounds__(256) k_rows_merge(const __grid_constant__ RowsArgs args, int ctas, int warps)
 {
-    __shared__ float s_o[8][kHeadDim], s_l[8], s_m[8];
     pdl_enter();
     const AttendView& a = args.a;
-    const int b = blockIdx.x / args.c.Hkv, j = blockIdx.x - b * args.c.Hkv, r = blockIdx.y;
-    const int64_t n = args.before[b + 1] - args.before[b];
-    if (n == 0) return;
-    const int64_t per_run = run_steps(args.before[args.b.n_seqs] * args.c.Hkv, warps);
-    const int64_t x0 = args.before[b] * args.c.Hkv + n * j;
-    const int64_t w0 = run_of(x0, per_run), w1 = run_of(x0 + n - 1, per_run);
-    if (w0 == w1) return;
+    const int b = blockIdx.x / args.c.Hkv, j = blockIdx.x - b * args.c.Hkv;
+    const int lane = threadIdx.x & 31;
+    const int64_t first = args.before[b], n = args.before[b + 1] - first, total = args.before[args.b.n_seqs];
     const Seq s = seq_of(a, args.b, b);
-    if (r >= s.rows * a.g) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    auto part = [&](int64_t w) { return (2 * w + (w == w0)) * args.part_rows + r; };
-    // the reference of all runs, then each warp's sums against it
-    float top = -INFINITY;
-    for (int64_t w = w0 + threadIdx.x; w <= w1; w += 256) top = fmaxf(top, __ldcg(&args.part_ml[part(w)]).x);
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    if (lane == 0) s_m[warp] = top;
-    __syncthreads();
-    for (int i = 0; i < 8; ++i) top = fmaxf(top, s_m[i]);
-    const float base = top == -INFINITY ? 0.f : top;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
+    if (n == 0) return;
+    const Runs runs(total * args.c.Hkv, ctas, warps);
+    const int64_t x0 = first * args.c.Hkv + n * j, x1 = x0 + n;
+    const int64_t c0 = quotient(x0, runs.per_cta), c1 = quotient(x1 - 1, runs.per_cta);
+    const int64_t w0 = quotient(x0 - c0 * runs.per_cta, runs.per_warp), w1 = quotient(x1 - 1 - c1 * runs.per_cta, runs.per_warp);
+    if (c0 == c1 && w0 == w1) return;
+    const bool at_end = runs.end(c1, w1) == x1;              // the last run's part is one of the CTA's pieces
+    const bool c1_piece = at_end || w1 > (c0 == c1 ? w0 : 0);  // the last CTA has one
+    const int pieces = static_cast<int>(c1 - c0) + c1_piece + !at_end;
+    auto place = [&](int i) -> int64_t {
+        const int64_t c = c0 + i;
+        if (c < c1 || (c == c1 && c1_piece)) return 2 * (c * warps + (i == 0 ? w0 : 0)) + 1;
+        return 2 * (c1 * warps + w1);
+    };
+    for (int r = threadIdx.x >> 5; r < s.rows * a.g; r += 8) {
+        float top = -INFINITY;
+        for (int i = lane; i < pieces; i += 32) top = fmaxf(top, __ldcg(&args.part_ml[place(i) * args.part_rows + r]).x);
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        const float base = top == -INFINITY ? 0.f : top;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        float sum = 0.f;
 #pragma unroll 8
-    for (int64_t w = w0 + warp; w <= w1; w += 8) {
-        const float2 ml = __ldcg(&args.part_ml[part(w)]);
-        const float4 x = __ldcg(reinterpret_cast<const float4*>(args.part_o + part(w) * kHeadDim) + lane);
-        const float f = ex2(ml.x - base);
-        sum = fmaf(ml.y, f, sum);
-        acc.x = fmaf(x.x, f, acc.x);
-        acc.y = fmaf(x.y, f, acc.y);
-        acc.z = fmaf(x.z, f, acc.z);
-        acc.w = fmaf(x.w, f, acc.w);
+        for (int i = 0; i < pieces; ++i) {
+            const int64_t at = place(i) * args.part_rows + r;
+            const float2 ml = __ldcg(&args.part_ml[at]);
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(args.part_o + at * kHeadDim) + lane);
+            const float f = ex2(ml.x - base);
+            sum = fmaf(ml.y, f, sum);
+            acc.x = fmaf(x.x, f, acc.x);
+            acc.y = fmaf(x.y, f, acc.y);
+            acc.z = fmaf(x.z, f, acc.z);
+            acc.w = fmaf(x.w, f, acc.w);
+        }
+        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+        const int64_t row = s.row0 + r / a.g;
+        const int h = j * a.g + r % a.g;
+        auto* out = static_cast<__nv_bfloat16*>(a.out) + row * a.out_stride + h * kHeadDim;
+        reinterpret_cast<uint2*>(out)[lane] = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+        if (a.lse && lane == 0) a.lse[row * a.Hq + h] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * 0.6931471805599453f;
     }
-    *reinterpret_cast<float4*>(&s_o[warp][4 * lane]) = acc;
-    if (lane == 0) s_l[warp] = sum;
-    __syncthreads();
-    if (threadIdx.x >= kHeadDim) return;
-    float y = 0.f, total = 0.f;
-    for (int i = 0; i < 8; ++i) {
-        y += s_o[i][threadIdx.x];
-        total += s_l[i];
-    }
-    const int64_t row = s.row0 + r / a.g;
-    const int h = j * a.g + r % a.g;
-    static_cast<__nv_bfloat16*>(a.out)[row * a.out_stride + h * kHeadDim + threadIdx.x] =
-        __float2bfloat16_rn(total > 0.f ? y / total : 0.f);
-    if (a.lse && threadIdx.x == 0)
-        a.lse[row * a.Hq + h] = total > 0.f ? (top + __log2f(total)) * 0.6931471805599453f : -INFINITY;
 }
-
-}  // namespace
-
-namespace {
 
 // Workspace regions (byte offsets); the status word comes first.
 struct AttendWs {
@@ -598,15 +672,14 @@ AttendWs attend_layout(int Hq, int Hkv, int n_seqs, int n_rows, int max_rows)
 template <int NT, bool E4M3>
 cudaError_t run_rows(const RowsArgs& r, int sms, cudaStream_t st)
 {
+    constexpr int kWarps = rows_warps(NT, E4M3);
     auto kern = k_rows<NT, E4M3>;
-    const size_t smem = rows_ring_bytes(E4M3) + (static_cast<size_t>(r.b.n_seqs) + 1) * sizeof(int64_t);
+    const size_t smem = rows_ring_bytes(NT, E4M3) + (static_cast<size_t>(r.b.n_seqs) + 1) * sizeof(int64_t);
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
-    e = launch_after(st, dim3(sms), kRowsThreads, smem, 1, kern, r);
+    e = launch_after(st, dim3(sms), 32 * kWarps, smem, 1, kern, r);
     if (e != cudaSuccess) return e;
-    const int64_t rows = static_cast<int64_t>(r.b.max_rows) * r.a.g;
-    return launch_after(st, dim3(r.b.n_seqs * r.c.Hkv, static_cast<unsigned>(rows < r.part_rows ? rows : r.part_rows)), 256, 0, 1,
-                        k_rows_merge, r, static_cast<int64_t>(sms) * kRowsWarps);
+    return launch_after(st, dim3(r.b.n_seqs * r.c.Hkv), 256, 0, 1, k_rows_merge, r, sms, kWarps);
 }
 
 }  // namespace

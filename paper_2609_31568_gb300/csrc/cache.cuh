@@ -39,25 +39,19 @@ __device__ __forceinline__ int cache_row(const CacheView& c, const BatchView& bt
     return page * c.page_size + (t - lp * c.page_size);
 }
 
-// Sequence and token of row r, by the whole warp (r the same in every lane): the
-// last sequence that starts at or before r, 32 starts compared at a time. Returns
-// the sequence, or -1 for a row that belongs to none.
-__device__ __forceinline__ int seq_of_row(const BatchView& bt, int r, int* token)
+// Row of the pool of row r of the batch: -1 when its token has no place, -2 when r belongs to no sequence. The
+// last sequence that starts at or before r is found by bisection.
+__device__ __forceinline__ int place_of_row(const CacheView& c, const BatchView& bt, int r)
 {
-    const int lane = threadIdx.x & 31;
-    int lo = 0, n = bt.n_seqs;
-    while (n > 1) {
-        const int step = (n + 31) / 32, i = lane * step;
-        const bool at = i < n && bt.row_start[lo + i] <= r;
-        const int k = __popc(__ballot_sync(0xFFFFFFFFu, at)) - 1;
-        if (k < 0) return -1;
-        lo += k * step;
-        n = n - k * step < step ? n - k * step : step;
+    int lo = 0, hi = bt.n_seqs;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (bt.row_start[mid] <= r) lo = mid;
+        else hi = mid;
     }
-    const int first = bt.row_start[lo], end = bt.row_start[lo + 1];
-    if (r < first || r >= end) return -1;
-    *token = bt.kv_len[lo] - (end - r);
-    return lo;
+    const int end = bt.row_start[lo + 1], len = bt.kv_len[lo];
+    if (r < bt.row_start[lo] || r >= end) return -2;
+    return cache_row(c, bt, lo, len - (end - r));
 }
 
 // Two e4m3 codes (the low 16 bits of x) as f16, exact.

@@ -509,6 +509,16 @@ __device__ __forceinline__ void fadd2(float& d0, float& d1, float a0, float a1, 
         : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
 }
 
+// (d0, d1) = (a0 * b0, a1 * b1) as one packed fp32x2 product.
+__device__ __forceinline__ void fmul2(float& d0, float& d1, float a0, float a1, float b0, float b1)
+{
+    asm("{\n\t.reg .b64 x, y;\n\t"
+        "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+        "mul.rn.ftz.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d0), "=f"(d1)
+        : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+
 // (2^x0, 2^x1) on the FMA pipe, for softmax weights that are rounded to bf16
 // afterwards. Cody-Waite style split x = j + f with j = round(x) (adding
 // 1.5 * 2^23 rounds to an integer held in the low mantissa bits) and
