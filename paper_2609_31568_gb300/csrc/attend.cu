@@ -284,7 +284,7 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
     float q_scale[NT][2];             // 8-bit: the power of two that Q's row was divided by
     float o[8][NT][4];                // O^T: 16 dimensions at a time
     float m[NT][2], l[NT][2];         // per row: reference (log2 units, a warp's), sum of this lane's keys
-    auto begin_item = [&]() {
+    auto load_q = [&]() {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int r = nt * 8 + oct;  // this lane's row of Q
@@ -303,6 +303,11 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
                     qf[nt][i][1] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 8 + 2 * quad) : 0u;
                 }
             }
+        }
+    };
+    auto begin_item = [&]() {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
             if (E4M3) {
                 uint32_t top = 0;
 #pragma unroll
@@ -386,6 +391,7 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
     };
 
     find_page();
+    load_q();  // ahead of the copies
     auto load_next = [&](int64_t i, int stage) {
         if (i < n) {
             copy_step(stage);
@@ -548,6 +554,7 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
             end_item(from, use.step + 1, i + 1 == n);
             if (i + 1 < n) {
                 advance(use);
+                load_q();
                 begin_item();
                 from = 0;
             }
@@ -591,15 +598,18 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
     }
 }
 
-// Items that several CTAs or warps of k_rows share: a CTA per item, a warp per row, four dimensions a lane. A CTA of k_rows
-// left one piece of the item, under the first of its runs that has a part of it, and where the item ends inside a
-// run, that run another one.
+// Items that several CTAs or warps of k_rows share: a CTA per item, four dimensions a lane, one warp to eight for a row by
+// how many rows there are. A CTA of k_rows left one piece of the item, under the first of its runs that has a part of it, and
+// where the item ends inside a run, that run another one. Bound by latency: a lane looks a piece up and weighs it, then
+// the rows of eight pieces are in flight at a time.
 __global__ void __launch_bounds__(256) k_rows_merge(const __grid_constant__ RowsArgs args, int ctas, int warps)
 {
+    __shared__ float4 s_o[8][32];
+    __shared__ float2 s_ml[8];
     pdl_enter();
     const AttendView& a = args.a;
     const int b = blockIdx.x / args.c.Hkv, j = blockIdx.x - b * args.c.Hkv;
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t first = args.before[b], n = args.before[b + 1] - first, total = args.before[args.b.n_seqs];
     const Seq s = seq_of(a, args.b, b);
     if (n == 0) return;
@@ -616,31 +626,81 @@ __global__ void __launch_bounds__(256) k_rows_merge(const __grid_constant__ Rows
         if (c < c1 || (c == c1 && c1_piece)) return 2 * (c * warps + (i == 0 ? w0 : 0)) + 1;
         return 2 * (c1 * warps + w1);
     };
-    for (int r = threadIdx.x >> 5; r < s.rows * a.g; r += 8) {
-        float top = -INFINITY;
-        for (int i = lane; i < pieces; i += 32) top = fmaxf(top, __ldcg(&args.part_ml[place(i) * args.part_rows + r]).x);
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        const float base = top == -INFINITY ? 0.f : top;
+    const int rows = s.rows * a.g;
+    const int share = rows > 4 ? 1 : rows > 2 ? 2 : rows > 1 ? 4 : 8;  // warps of a row
+    for (int r0 = 0; r0 < rows; r0 += 8 / share) {
+        const int r = r0 + warp / share, sub = warp % share;
+        const bool live = r < rows;
+        float top = -INFINITY, sum = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        float sum = 0.f;
-#pragma unroll 8
-        for (int i = 0; i < pieces; ++i) {
-            const int64_t at = place(i) * args.part_rows + r;
-            const float2 ml = __ldcg(&args.part_ml[at]);
-            const float4 x = __ldcg(reinterpret_cast<const float4*>(args.part_o + at * kHeadDim) + lane);
-            const float f = ex2(ml.x - base);
-            sum = fmaf(ml.y, f, sum);
-            acc.x = fmaf(x.x, f, acc.x);
-            acc.y = fmaf(x.y, f, acc.y);
-            acc.z = fmaf(x.z, f, acc.z);
-            acc.w = fmaf(x.w, f, acc.w);
+#pragma unroll 1
+        for (int i0 = sub; live && i0 < pieces; i0 += 32 * share) {  // this warp's next 32 pieces, one per lane
+            const int i = i0 + lane * share;
+            int64_t at = 0;
+            float2 ml = make_float2(-INFINITY, 0.f);
+            if (i < pieces) {
+                at = place(i) * args.part_rows + r;
+                ml = __ldcg(&args.part_ml[at]);
+            }
+            float m = ml.x;
+            for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+            m = fmaxf(m, top);
+            const float base = m == -INFINITY ? 0.f : m;
+            const float alpha = ex2(top - base), w = ex2(ml.x - base);
+            float l = ml.y * w;
+            for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
+            sum = fmaf(sum, alpha, l);
+            acc = make_float4(acc.x * alpha, acc.y * alpha, acc.z * alpha, acc.w * alpha);
+            top = m;
+            const int n_in = (pieces - i0 + share - 1) / share < 32 ? (pieces - i0 + share - 1) / share : 32;
+#pragma unroll 1
+            for (int u0 = 0; u0 < n_in; u0 += 8) {
+                float4 x[8];
+                float f[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const int64_t from = __shfl_sync(0xFFFFFFFFu, at, u0 + u);
+                    f[u] = __shfl_sync(0xFFFFFFFFu, w, u0 + u);
+                    x[u] = u0 + u < n_in ? __ldcg(reinterpret_cast<const float4*>(args.part_o + from * kHeadDim) + lane)
+                                         : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    acc.x = fmaf(x[u].x, f[u], acc.x);
+                    acc.y = fmaf(x[u].y, f[u], acc.y);
+                    acc.z = fmaf(x[u].z, f[u], acc.z);
+                    acc.w = fmaf(x[u].w, f[u], acc.w);
+                }
+            }
         }
-        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-        const int64_t row = s.row0 + r / a.g;
-        const int h = j * a.g + r % a.g;
-        auto* out = static_cast<__nv_bfloat16*>(a.out) + row * a.out_stride + h * kHeadDim;
-        reinterpret_cast<uint2*>(out)[lane] = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
-        if (a.lse && lane == 0) a.lse[row * a.Hq + h] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * 0.6931471805599453f;
+        if (share > 1) {  // the row's warps, in order
+            s_o[warp][lane] = acc;
+            if (lane == 0) s_ml[warp] = make_float2(top, sum);
+            __syncthreads();
+            if (sub == 0) {
+                for (int x = 1; x < share; ++x) top = fmaxf(top, s_ml[warp + x].x);
+                const float base = top == -INFINITY ? 0.f : top;
+                sum = 0.f;
+                acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int x = 0; x < share; ++x) {
+                    const float f = ex2(s_ml[warp + x].x - base);
+                    const float4 y = s_o[warp + x][lane];
+                    sum = fmaf(s_ml[warp + x].y, f, sum);
+                    acc.x = fmaf(y.x, f, acc.x);
+                    acc.y = fmaf(y.y, f, acc.y);
+                    acc.z = fmaf(y.z, f, acc.z);
+                    acc.w = fmaf(y.w, f, acc.w);
+                }
+            }
+        }
+        if (live && sub == 0) {
+            const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+            const int64_t row = s.row0 + r / a.g;
+            const int h = j * a.g + r % a.g;
+            auto* out = static_cast<__nv_bfloat16*>(a.out) + row * a.out_stride + h * kHeadDim;
+            reinterpret_cast<uint2*>(out)[lane] = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+            if (a.lse && lane == 0) a.lse[row * a.Hq + h] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * 0.6931471805599453f;
+        }
     }
 }
 
