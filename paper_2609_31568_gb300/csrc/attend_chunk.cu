@@ -32,7 +32,8 @@ constexpr int kPlanThreads = 512;     // at least 2 kMaxSms
 constexpr int kCuts = 3;              // pieces per SM, at most, beyond one per item
 constexpr int kPieces = 8;            // pieces of an item that the plan considers
 constexpr int kCandidates = kPieces + kCuts;
-constexpr int kPieceTiles = 6;        // what a CTA's start and end take, in key tiles
+constexpr int kPieceTiles = 5;        // what a CTA's start and end take, in key tiles
+constexpr int kMergeTiles = 4;        // what writing and merging one piece per SM takes
 
 // A CTA's work. Rows [row0, row0 + ntok) of the row tensors are tokens pos ..; key tiles
 // [k0, k1) of those the job's rows see; slot >= 0: partial results there.
@@ -115,23 +116,25 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* s_warp, int64_
 // As many items as fill the SMs a whole number of times run whole; the rest (all of them, when there are
 // fewer than two per SM) are cut along their keys into pieces of at most C tiles. C is one of longest / 1 .. longest
 // / kPieces and W / SMs .. W / (kCuts SMs), W the rest's key tiles: the one for which ceil(pieces / SMs) rounds of
-// C + kPieceTiles end first.
+// C + kPieceTiles, and the merge of the pieces, end first.
 __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_constant__ ChunkArgs a)
 {
     __shared__ int s_before[kMaxSeqs + 1];  // items (of one KV head) of the sequences before
     __shared__ int64_t s_warp[32];
-    __shared__ int s_pieces[kCandidates], s_longest;
+    __shared__ int s_longest, s_pieces[32], s_cut;
     __shared__ unsigned long long s_work;
-    pdl_enter();
-    const int tid = threadIdx.x;
+    pdl_trigger();  // k_chunk's first CTAs set up meanwhile
+    pdl_wait();
+    const int tid = threadIdx.x, lane = tid & 31;
     const int per_item = 2 * a.tile_tokens;
     const int per = (a.b.n_seqs + kPlanThreads - 1) / kPlanThreads;
     const int i0 = tid * per < a.b.n_seqs ? tid * per : a.b.n_seqs, i1 = i0 + per < a.b.n_seqs ? i0 + per : a.b.n_seqs;
     int64_t mine = 0;
+#pragma unroll 1
     for (int i = i0; i < i1; ++i) {
         const Seq s = seq_of(a.a, a.b, i);
         s_before[i] = static_cast<int>(mine);
-        if (s.rows > 0) mine += (s.rows + per_item - 1) / per_item;
+        if (s.rows > 0) mine += static_cast<uint32_t>(s.rows + per_item - 1) / static_cast<uint32_t>(per_item);
     }
     int64_t all;
     const int64_t base = block_scan(mine, s_warp, &all);
@@ -143,79 +146,94 @@ __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_consta
         }
         return;
     }
+#pragma unroll 1
     for (int i = i0; i < i1; ++i) s_before[i] += static_cast<int>(base);
     if (tid == 0) {
         s_before[a.b.n_seqs] = static_cast<int>(all);
         s_work = 0;
         s_longest = 0;
-        for (int f = 0; f < kCandidates; ++f) s_pieces[f] = 0;
     }
+    if (tid < 32) s_pieces[tid] = 0;
     __syncthreads();
     // item x: sequences outermost, then KV heads, then pairs from the last
-    auto item = [&](int64_t x, ChunkJob* jb, Tiles* t) {
+    auto item = [&](int x, ChunkJob* jb) {
         int lo = 0, hi = a.b.n_seqs;
+#pragma unroll 1
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (static_cast<int64_t>(s_before[mid]) * a.c.Hkv <= x) lo = mid;
+            if (s_before[mid] * a.c.Hkv <= x) lo = mid;
             else hi = mid;
         }
         const int n = s_before[lo + 1] - s_before[lo];
-        const int rem = static_cast<int>(x - static_cast<int64_t>(s_before[lo]) * a.c.Hkv);
+        const int rem = x - s_before[lo] * a.c.Hkv;
         const Seq s = seq_of(a.a, a.b, lo);
         jb->b = lo;
-        jb->j = rem / n;
+        jb->j = static_cast<int>(static_cast<uint32_t>(rem) / static_cast<uint32_t>(n));
         const int first = (n - 1 - (rem - jb->j * n)) * per_item;
         jb->row0 = s.row0 + first;
         jb->ntok = s.rows - first < per_item ? s.rows - first : per_item;
         jb->pos = s.pos0 + first;
-        *t = tiles_of(a.a, jb->pos, jb->ntok);
         jb->k0 = 0;
-        jb->k1 = t->n;
+        jb->k1 = tiles_of(a.a, jb->pos, jb->ntok).n;
         jb->slot = -1;
     };
-    const int64_t whole = items > 2 * a.sms ? items - items % a.sms : 0;
-    const int rest = static_cast<int>(items - whole);
-    for (int64_t x = tid; x < whole; x += kPlanThreads) {
+    const int whole = items > 2 * a.sms ? static_cast<int>(items) / a.sms * a.sms : 0;
+    const int rest = static_cast<int>(items) - whole;  // at most 2 kMaxSms: one per thread
+#pragma unroll 1
+    for (int x = tid; x < whole; x += kPlanThreads) {
         ChunkJob jb;
-        Tiles t;
-        item(x, &jb, &t);
+        item(x, &jb);
         a.p.jobs[x] = jb;
     }
-    // the rest, at most 2 kMaxSms: one per thread
     ChunkJob jb{};
-    Tiles t{};
-    if (tid < rest) {
-        item(whole + tid, &jb, &t);
-        atomicAdd(&s_work, static_cast<unsigned long long>(t.n));
-        atomicMax(&s_longest, t.n);
+    if (tid < rest) item(whole + tid, &jb);
+    if ((tid & ~31) < rest) {
+        const uint32_t sum = __reduce_add_sync(0xFFFFFFFFu, static_cast<uint32_t>(jb.k1)), top = __reduce_max_sync(0xFFFFFFFFu, jb.k1);
+        if (lane == 0) {
+            atomicAdd(&s_work, static_cast<unsigned long long>(sum));
+            atomicMax(&s_longest, static_cast<int>(top));
+        }
     }
     __syncthreads();
-    auto longest_piece = [&](int f) {  // of candidate f
+    // the longest piece of candidate f, and the pieces of n tiles then
+    auto cut_of = [&](int f) {
         const int c = f < kPieces ? (s_longest + f) / (f + 1) : static_cast<int>(static_cast<float>(s_work) / static_cast<float>((f - kPieces + 1) * a.sms)) + 1;
         return c < 2 ? 2 : c;
     };
-    auto pieces_of = [&](int f) { return (t.n + longest_piece(f) - 1) / longest_piece(f); };
-    for (int f = 0; f < kCandidates; ++f) {
-        const int n = __reduce_add_sync(0xFFFFFFFFu, tid < rest ? pieces_of(f) : 0);
-        if ((tid & 31) == 0 && n) atomicAdd(&s_pieces[f], n);
+    auto pieces_of = [&](int n, int cut, float inv) {  // ceil(n / cut)
+        int q = static_cast<int>(static_cast<float>(n + cut - 1) * inv);
+        q += q * cut < n;
+        return q - ((q - 1) * cut >= n);
+    };
+    const int my_cut = lane < kCandidates ? cut_of(lane) : 2;  // lane f: candidate f
+    if ((tid & ~31) < rest) {
+        const float inv = 1.0f / static_cast<float>(my_cut);
+        int n = 0;
+#pragma unroll 4
+        for (int i = 0; i < 32; ++i) {  // the warp's items
+            const int k1 = __shfl_sync(0xFFFFFFFFu, jb.k1, i);
+            if (k1 > 0) n += pieces_of(k1, my_cut, inv);
+        }
+        if (lane < kCandidates) atomicAdd(&s_pieces[lane], n);
     }
     __syncthreads();
-    int best = 0, best_time = 0x7FFFFFFF;
-    for (int f = 0; f < kCandidates; ++f) {
-        const int rounds = (s_pieces[f] + a.sms - 1) / a.sms;
-        const int time = rounds * (longest_piece(f) + kPieceTiles);
-        if (time < best_time && (f == 0 || s_pieces[f] <= rest + kCuts * a.sms)) {
-            best = f;
-            best_time = time;
-        }
+    if (tid < 32) {
+        const int n = s_pieces[lane];
+        const uint32_t time = static_cast<uint32_t>(n + a.sms - 1) / static_cast<uint32_t>(a.sms) * static_cast<uint32_t>(my_cut + kPieceTiles) +
+                              (n > rest ? static_cast<uint32_t>(kMergeTiles * n) / static_cast<uint32_t>(a.sms) : 0u);
+        const bool open = lane < kCandidates && (lane == 0 || n <= rest + kCuts * a.sms);
+        const uint32_t best = __reduce_min_sync(0xFFFFFFFFu, open ? time : 0xFFFFFFFFu);
+        const int f = __ffs(__ballot_sync(0xFFFFFFFFu, open && time == best)) - 1;
+        if (lane == f) s_cut = my_cut;
     }
-    const int pieces = tid < rest ? pieces_of(best) : 0;
+    __syncthreads();
+    const int pieces = tid < rest ? pieces_of(jb.k1, s_cut, 1.0f / static_cast<float>(s_cut)) : 0;
     // jobs, partial results and merges before this item, one scan of 21 bits each
     int64_t sums;
     const int64_t mask = (1 << 21) - 1;
     const int64_t before = block_scan(pieces > 1 ? pieces | static_cast<int64_t>(pieces) << 21 | 1ll << 42 : pieces, s_warp, &sums);
-    const int64_t at = whole + (before & mask), slot = (before >> 21) & mask, merge = before >> 42;
-    const int64_t jobs = whole + (sums & mask), slots = (sums >> 21) & mask, merges = sums >> 42;
+    const int at = whole + static_cast<int>(before & mask), slot = static_cast<int>((before >> 21) & mask), merge = static_cast<int>(before >> 42);
+    const int jobs = whole + static_cast<int>(sums & mask), slots = static_cast<int>((sums >> 21) & mask), merges = static_cast<int>(sums >> 42);
     if (jobs > a.p.max_jobs || slots > a.p.max_slots || merges > a.p.max_merges) {  // as above
         if (tid == 0) {
             record_status(a.status, SCALE_ERR_DEVICE);
@@ -223,17 +241,22 @@ __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_consta
         }
         return;
     }
-    for (int i = 0; i < pieces; ++i) {
+    const int n = jb.k1;
+    const int each = pieces > 1 ? static_cast<int>(static_cast<uint32_t>(n) / static_cast<uint32_t>(pieces)) : n, more = n - each * pieces;
+#pragma unroll 1
+    for (int i = 0; i < pieces; ++i) {  // the first `more` pieces have one tile more
         ChunkJob x = jb;
-        x.k0 = static_cast<int>(static_cast<int64_t>(t.n) * i / pieces);
-        x.k1 = static_cast<int>(static_cast<int64_t>(t.n) * (i + 1) / pieces);
-        x.slot = pieces > 1 ? static_cast<int>(slot) + i : -1;
-        a.p.jobs[at + i] = x;
+        x.k0 = each * i + (i < more ? i : more);
+        x.k1 = x.k0 + each + (i < more);
+        x.slot = pieces > 1 ? slot + i : -1;
+        int4* to = reinterpret_cast<int4*>(a.p.jobs + at + i);
+        to[0] = make_int4(x.b, x.j, x.row0, x.ntok);
+        to[1] = make_int4(x.pos, x.k0, x.k1, x.slot);
     }
-    if (pieces > 1) a.p.merges[merge] = ChunkMerge{jb.j, jb.row0, jb.ntok, static_cast<int>(slot), pieces, {0, 0, 0}};
+    if (pieces > 1) a.p.merges[merge] = ChunkMerge{jb.j, jb.row0, jb.ntok, slot, pieces, {0, 0, 0}};
     if (tid == 0) {
-        a.p.counts[0] = static_cast<int>(jobs);
-        a.p.counts[1] = static_cast<int>(merges);
+        a.p.counts[0] = jobs;
+        a.p.counts[1] = merges;
     }
 }
 
@@ -252,17 +275,28 @@ struct ChunkShared {
     uint64_t q_ready;                    // Q is in its parts
     uint64_t raw_full[2], raw_empty[2];  // codes of V: landed; turned
     uint64_t v_full[2];                  // V is bf16
-    float kscale[8][kTile];              // per softmax warp: what the products with each key of its tile are multiplied by
+    alignas(16) float kscale[8][kTile];  // per softmax warp: what the products with each key of its tile are multiplied by
     uint32_t q_top;                      // largest finite |q| of the CTA's rows, as bits
     uint32_t tmem_slot;
     volatile int abort_flag;
 };
 __host__ __device__ constexpr uint32_t chunk_smem(bool e4m3) { return off_shared(e4m3) + sizeof(ChunkShared); }
+static_assert(offsetof(ChunkShared, kscale) % 16 == 0 && off_shared(true) % 16 == 0 && off_shared(false) % 16 == 0, "16-byte reads");
 static_assert(chunk_smem(true) <= 227 * 1024 && chunk_smem(false) <= 227 * 1024, "shared memory of a CTA");
 
-// Threads: warps 0-7 softmax, 8 producer, 9 MMA; 8-bit: 12-15 turn V into bf16 (10 and 11 idle, for whole
-// groups of four warps in the register split: 2 x 128 x 192 + 2 x 128 x 64 = 512 x 128).
+// Threads: warps 0-7 softmax, 8 producer, 9 MMA; 8-bit: 12-15 turn V into bf16 (10 and 11 idle,
+// for whole groups of four warps in the register split: 2 x 128 x 192 + 2 x 128 x 64 = 512 x 128).
 __host__ __device__ constexpr int chunk_threads(bool e4m3) { return e4m3 ? 512 : 320; }
+
+// The lowest n bits, 0 <= n <= 32 or beyond either end.
+__device__ __forceinline__ uint32_t ones_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1u; }
+
+__device__ __forceinline__ float4 lds_f4(uint32_t addr)
+{
+    float4 r;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(r.x), "=f"(r.y), "=f"(r.z), "=f"(r.w) : "r"(addr));
+    return r;
+}
 
 // A CTA's job as its roles see it; T = 0: none.
 struct JobView {
@@ -566,27 +600,42 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
             tmem_ld_wait();
             if (masked) {
 #pragma unroll
-                for (int c = 0; c < 128; ++c)
-                    if (c >= lim || (c >= gap && c < low)) sr[c] = 0xFF800000u;
+                for (int c = 0; c < 4; ++c) {  // a bit per column: columns below x of these 32 are ones_below(x - 32 c)
+                    const uint32_t seen = ones_below(lim - 32 * c) & ~(ones_below(low - 32 * c) & ~ones_below(gap - 32 * c));
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (!((seen >> i) & 1u)) sr[32 * c + i] = 0xFF800000u;
+                }
             }
         };
         // p = 2^(s scale - m) of keys [64 h, 64 h + 64) as bf16 pairs; returns their sum
         // (8-bit: a scale for each key, from shared memory)
+        // The scales are loaded sixteen keys ahead: read where they are used, 32 waits for shared memory, which the
+        // products keep busy, took a tile's softmax from 1,250 to 3,000 cycles.
+        const uint32_t ks_at = smem_addr(ks);
+        auto load_scales = [&](float4 (&f)[4], int c) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i] = lds_f4(ks_at + (c + 4 * i) * 4);
+        };
         auto exp_half = [&](const float* s, int h, float neg_m, uint32_t (&pk)[32]) {
             float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            float4 f[2][4];
+            if (E4M3) load_scales(f[0], h * 64);
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-                const float4 f = E4M3 ? *reinterpret_cast<const float4*>(ks + h * 64 + 2 * i)
-                                      : make_float4(a.a.scale_log2, a.a.scale_log2, a.a.scale_log2, a.a.scale_log2);
+            for (int b = 0; b < 4; ++b) {  // sixteen keys
+                if (E4M3 && b < 3) load_scales(f[(b + 1) & 1], h * 64 + 16 * (b + 1));
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
+                for (int k = 0; k < 8; ++k) {
+                    const int i = 8 * b + k;
+                    const float4 q = f[b & 1][k >> 1];
+                    const float f0 = E4M3 ? (k & 1 ? q.z : q.x) : a.a.scale_log2, f1 = E4M3 ? (k & 1 ? q.w : q.y) : a.a.scale_log2;
                     float x0, x1;
-                    ffma2(x0, x1, s[h * 64 + 2 * (i + k)], s[h * 64 + 2 * (i + k) + 1], k ? f.z : f.x, k ? f.w : f.y, neg_m, neg_m);
+                    ffma2(x0, x1, s[h * 64 + 2 * i], s[h * 64 + 2 * i + 1], f0, f1, neg_m, neg_m);
                     x0 = ex2(x0);
                     x1 = ex2(x1);
-                    const int jj = ((i + k) & 3) * 2;
+                    const int jj = (i & 3) * 2;
                     fadd2(acc[jj], acc[jj + 1], acc[jj], acc[jj + 1], x0, x1);
-                    pk[i + k] = pack_bf16x2(x0, x1);
+                    pk[i] = pack_bf16x2(x0, x1);
                 }
             }
             return ((acc[0] + acc[1]) + (acc[2] + acc[3])) + ((acc[4] + acc[5]) + (acc[6] + acc[7]));
@@ -595,7 +644,8 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
         bool ok = true;
         JobView jv{};
         int T = 0, pos_first = 0, pos_last = 0, p = 0;
-        // 8-bit: lane x looks up the scales of the keys 4 x .. 4 x + 3 of a tile, its page two tiles ahead, the bytes one ahead
+        // 8-bit: lane x looks up the scales of the keys 4 x .. 4 x + 3 of a tile, its page two tiles ahead, the bytes one
+        // ahead. (A warp that did it for both query tiles came late: 600 cycles a tile.)
         int next_place = -1;
         uint32_t next_scales = 0x7F7F7F7Fu;
         float q_scale = 0.f;
@@ -604,6 +654,13 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
             if (place < 0) return 0x7F7F7F7Fu;
             const int page = place / a.c.page_size;
             return *reinterpret_cast<const uint32_t*>(a.c.ks + (static_cast<int64_t>(page) * a.c.Hkv + jv.job.j) * a.c.page_size + place - page * a.c.page_size);
+        };
+        auto write_scales = [&]() {  // not 0: hidden logits stay -inf
+            *reinterpret_cast<float4*>(ks + 4 * lane) = make_float4(fmaxf(scale_value(next_scales & 255u) * q_scale, 1e-37f),
+                                                                    fmaxf(scale_value((next_scales >> 8) & 255u) * q_scale, 1e-37f),
+                                                                    fmaxf(scale_value((next_scales >> 16) & 255u) * q_scale, 1e-37f),
+                                                                    fmaxf(scale_value(next_scales >> 24) * q_scale, 1e-37f));
+            __syncwarp();
         };
         // Tile -1 is whatever TMEM and shared memory hold: its softmax brings the code into the instruction cache
         // while the CTA waits for the plan (the first tile of a call took 10,000 to 20,000 cycles for that).
@@ -673,6 +730,11 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 }
             }
             if (t >= T && t >= 0) break;
+            if (E4M3) {  // while the products are made
+                write_scales();
+                next_scales = scales_of(next_place);
+                next_place = place_of(t + 2);
+            }
             if (t >= 0) {
                 const bool got = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.s_full[qt][t & 1], (t >> 1) & 1, a.timeout_ns, &abort_flag));
                 if (!got) {
@@ -681,18 +743,6 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 }
             }
             tc_fence_after();
-            if (E4M3) {
-                // not 0: hidden logits stay -inf
-                const float4 f = make_float4(fmaxf(scale_value(next_scales & 255u) * q_scale, 1e-37f),
-                                             fmaxf(scale_value((next_scales >> 8) & 255u) * q_scale, 1e-37f),
-                                             fmaxf(scale_value((next_scales >> 16) & 255u) * q_scale, 1e-37f),
-                                             fmaxf(scale_value(next_scales >> 24) * q_scale, 1e-37f));
-                __syncwarp();  // the tile before is read
-                *reinterpret_cast<float4*>(ks + 4 * lane) = f;
-                __syncwarp();
-                next_scales = scales_of(next_place);
-                next_place = place_of(t + 2);
-            }
             const int t0 = jv.token_of(t);
             const bool masked = t < 0 || t0 + kTile - 1 > pos_first ||
                                 (a.a.n_local >= 0 && pos_last - t0 > a.a.n_local && t0 + kTile - 1 >= a.a.n_sink);
@@ -758,6 +808,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 break;
             }
             l_run += sum;
+            if (E4M3) __syncwarp();  // the tile's scales are read
             if (t < 0) continue;
             tmem_st_wait();
             if (!E4M3 && qt == 0 && jv.has_unseen(t0)) {
@@ -853,41 +904,46 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
     }
 }
 
-// Pieces of a query tile pair put together: a warp per row, four dimensions a lane.
+// Pieces of a query tile pair put together: a warp per row, four dimensions a lane. A grid of what the SMs hold walks
+// the rows: one CTA for eight of every row that could be cut took 12 us, most of it for CTAs without a row.
 __global__ void __launch_bounds__(256) k_chunk_merge(const __grid_constant__ ChunkArgs a)
 {
     pdl_enter();
-    if (static_cast<int>(blockIdx.x) >= a.p.counts[1]) return;
-    const ChunkMerge& mg = a.p.merges[blockIdx.x];
     const int lane = threadIdx.x & 31, per_tile = a.tile_tokens * a.a.g;
-    const int x = blockIdx.y * 8 + (threadIdx.x >> 5);  // live row of the pair
-    if (x >= mg.ntok * a.a.g) return;
-    const int r = x < per_tile ? x : kTile + x - per_tile;  // its row of the tiles
-    float top = -INFINITY;
-    for (int i = lane; i < mg.pieces; i += 32)
-        top = fmaxf(top, __ldcg(&a.part_ml[static_cast<int64_t>(mg.slot + i) * a.part_rows + r]).x);
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    const float base = top == -INFINITY ? 0.f : top;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
+    const int merges = a.p.counts[1];
+    const int step = gridDim.x * 8;
+#pragma unroll 1
+    for (int w = blockIdx.x * 8 + (threadIdx.x >> 5); w < merges * a.part_rows; w += step) {
+        const int r = w % a.part_rows;                   // row of the pair's tiles
+        const int x = r < kTile ? r : per_tile + r - kTile;  // and which of its live rows that is
+        const ChunkMerge mg = a.p.merges[w / a.part_rows];
+        if ((r < kTile ? r >= per_tile : false) || x >= mg.ntok * a.a.g) continue;
+        float top = -INFINITY;
+        for (int i = lane; i < mg.pieces; i += 32)
+            top = fmaxf(top, __ldcg(&a.part_ml[static_cast<int64_t>(mg.slot + i) * a.part_rows + r]).x);
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        const float base = top == -INFINITY ? 0.f : top;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        float sum = 0.f;
 #pragma unroll 4
-    for (int i = 0; i < mg.pieces; ++i) {
-        const int64_t at = static_cast<int64_t>(mg.slot + i) * a.part_rows + r;
-        const float2 ml = __ldcg(&a.part_ml[at]);
-        const float4 o = __ldcg(reinterpret_cast<const float4*>(a.part_o + at * kHeadDim) + lane);
-        const float f = ex2(ml.x - base);
-        sum = fmaf(ml.y, f, sum);
-        acc.x = fmaf(o.x, f, acc.x);
-        acc.y = fmaf(o.y, f, acc.y);
-        acc.z = fmaf(o.z, f, acc.z);
-        acc.w = fmaf(o.w, f, acc.w);
+        for (int i = 0; i < mg.pieces; ++i) {
+            const int64_t at = static_cast<int64_t>(mg.slot + i) * a.part_rows + r;
+            const float2 ml = __ldcg(&a.part_ml[at]);
+            const float4 o = __ldcg(reinterpret_cast<const float4*>(a.part_o + at * kHeadDim) + lane);
+            const float f = ex2(ml.x - base);
+            sum = fmaf(ml.y, f, sum);
+            acc.x = fmaf(o.x, f, acc.x);
+            acc.y = fmaf(o.y, f, acc.y);
+            acc.z = fmaf(o.z, f, acc.z);
+            acc.w = fmaf(o.w, f, acc.w);
+        }
+        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+        const int64_t row = mg.row0 + x / a.a.g;
+        const int h = mg.j * a.a.g + x % a.a.g;
+        auto* out = static_cast<__nv_bfloat16*>(a.a.out) + row * a.a.out_stride + h * kHeadDim;
+        reinterpret_cast<uint2*>(out)[lane] = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+        if (a.a.lse && lane == 0) a.a.lse[row * a.a.Hq + h] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * 0.6931471805599453f;
     }
-    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-    const int64_t row = mg.row0 + x / a.a.g;
-    const int h = mg.j * a.a.g + x % a.a.g;
-    auto* out = static_cast<__nv_bfloat16*>(a.a.out) + row * a.a.out_stride + h * kHeadDim;
-    reinterpret_cast<uint2*>(out)[lane] = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
-    if (a.a.lse && lane == 0) a.a.lse[row * a.a.Hq + h] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * 0.6931471805599453f;
 }
 
 // Workspace regions (byte offsets from the route's part of the workspace).
@@ -943,7 +999,8 @@ cudaError_t run_chunks(const ChunkArgs& a, cudaStream_t st)
     if (e == cudaSuccess) e = launch_after(st, dim3(1), kPlanThreads, 0, 1, k_chunk_plan, a);
     if (e == cudaSuccess)
         e = launch_after(st, dim3(a.p.max_jobs), chunk_threads(E4M3), chunk_smem(E4M3), 1, k_chunk<E4M3>, tq, tk, tv, a);
-    if (e == cudaSuccess) e = launch_after(st, dim3(a.p.max_merges, a.part_rows / 8), 256, 0, 1, k_chunk_merge, a);
+    const int merge_ctas = a.p.max_merges * (a.part_rows / 8), most = a.sms * 8;
+    if (e == cudaSuccess) e = launch_after(st, dim3(merge_ctas < most ? merge_ctas : most), 256, 0, 1, k_chunk_merge, a);
     return e;
 }
 
