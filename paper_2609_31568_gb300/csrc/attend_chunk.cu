@@ -260,8 +260,8 @@ __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_consta
     }
 }
 
-// Dynamic shared memory (offsets from its 1024-aligned base): Q, then K and V in two stages each. 8-bit:
-// Q as its two parts, K and V as codes, then V as bf16.
+// Dynamic shared memory (offsets from its 1024-aligned base): Q, then K and V in two stages each. 8-bit: Q as its two
+// parts, K and V as codes, then V as bf16.
 constexpr uint32_t kCodeBytes = kTile * kHeadDim;  // one 128 x 128 tile of codes
 constexpr uint32_t kOffQ = 0;
 constexpr uint32_t kOffK = kOffQ + 2 * kTileBytes;
@@ -271,17 +271,18 @@ __host__ __device__ constexpr uint32_t off_shared(bool e4m3) { return off_v(e4m3
 
 struct ChunkShared {
     Barriers bars;
+    uint32_t tmem_slot;
+    volatile int abort_flag;
     // 8-bit only
     uint64_t q_ready;                    // Q is in its parts
     uint64_t raw_full[2], raw_empty[2];  // codes of V: landed; turned
     uint64_t v_full[2];                  // V is bf16
-    alignas(16) float kscale[8][kTile];  // per softmax warp: what the products with each key of its tile are multiplied by
     uint32_t q_top;                      // largest finite |q| of the CTA's rows, as bits
-    uint32_t tmem_slot;
-    volatile int abort_flag;
 };
-__host__ __device__ constexpr uint32_t chunk_smem(bool e4m3) { return off_shared(e4m3) + sizeof(ChunkShared); }
-static_assert(offsetof(ChunkShared, kscale) % 16 == 0 && off_shared(true) % 16 == 0 && off_shared(false) % 16 == 0, "16-byte reads");
+// 8-bit: per softmax warp, what the products with each key of its tile are multiplied by
+__host__ __device__ constexpr uint32_t off_scales(bool e4m3) { return off_shared(e4m3) + 256; }
+__host__ __device__ constexpr uint32_t chunk_smem(bool e4m3) { return off_scales(e4m3) + (e4m3 ? 8 * kTile * 4 : 0); }
+static_assert(sizeof(ChunkShared) <= 256 && off_scales(true) % 16 == 0, "scales are read four at a time");
 static_assert(chunk_smem(true) <= 227 * 1024 && chunk_smem(false) <= 227 * 1024, "shared memory of a CTA");
 
 // Threads: warps 0-7 softmax, 8 producer, 9 MMA; 8-bit: 12-15 turn V into bf16 (10 and 11 idle,
@@ -332,35 +333,64 @@ __device__ __forceinline__ JobView load_job(const ChunkArgs& a)
     return v;
 }
 
-// mma_iteration and mma_issue_loop (attn_mma.cuh) for 8-bit keys: S = Q1 K^T + Q2 K^T on codes, K and V behind
-// barriers of their own.
+// S = Q1 K^T + Q2 K^T on codes, and the commit.
+__device__ __forceinline__ void mma_codes(ChunkShared& sh, uint32_t tmem, uint64_t qdesc0, uint64_t kdesc, int qt, int st)
+{
+    constexpr uint64_t kTileStep = kTileBytes >> 4, kCodeStep = kCodeBytes >> 4;
+    constexpr uint32_t id = idesc_e4m3_f32(128, 128);
+    mma_e4m3_k128(tmem + qt * 256, qdesc0 + qt * kTileStep, kdesc, id, 0u);
+    mma_e4m3_k128(tmem + qt * 256, qdesc0 + qt * kTileStep + kCodeStep, kdesc, id, 1u);
+    mma_commit(&sh.bars.s_full[qt][st]);
+}
+
+// Iteration t > 0 (t & 1 = ST) of mma_issue_codes.
+template <int NQ, int ST>
+__device__ __forceinline__ bool mma_codes_step(ChunkShared& sh, uint32_t tmem, uint64_t qdesc0, uint64_t kdesc0, uint64_t vdesc0,
+                                               int t, uint64_t timeout_ns)
+{
+    Barriers& bars = sh.bars;
+    const volatile int* abort_flag = &sh.abort_flag;
+    if (!mbar_wait_bounded(&bars.kv_full[ST], (t >> 1) & 1, timeout_ns, abort_flag)) return false;
+    if (!mbar_wait_bounded(&sh.v_full[ST ^ 1], ((t - 1) >> 1) & 1, timeout_ns, abort_flag)) return false;
+#pragma unroll
+    for (int qt = 0; qt < NQ; ++qt) {
+        if (!mbar_wait_bounded(&bars.p_full[qt], ST ^ 1, timeout_ns, abort_flag)) return false;
+        tc_fence_after();
+        mma_ts_k128<2048>(tmem + qt * 256 + 128, tmem + qt * 256, vdesc0 + (ST ^ 1) * (kTileBytes >> 4),
+                          idesc_bf16_f32(128, 128, 1), t > 1 ? 1u : 0u);
+        mma_codes(sh, tmem, qdesc0, kdesc0 + ST * (kCodeBytes >> 4), qt, ST);
+    }
+    return true;
+}
+
+// mma_issue_loop (attn_mma.cuh) for 8-bit keys, whose K and V have barriers of their own. (What this loop and the softmax
+// run per key tile has to stay in the SM's instruction cache: with six iterations unrolled the requests to the next level
+// tripled and the products took a fifth longer.)
 template <int NQ>
 __device__ __forceinline__ bool mma_issue_codes(ChunkShared& sh, uint32_t tmem, uint64_t qdesc0, uint64_t kdesc0, uint64_t vdesc0,
                                                 int T, bool skip_last, uint64_t timeout_ns)
 {
-    constexpr uint64_t kStageStep = kTileBytes >> 4, kCodeStep = kCodeBytes >> 4;
-    constexpr uint32_t id_qk = idesc_e4m3_f32(128, 128), id_pv = idesc_bf16_f32(128, 128, 1);
     Barriers& bars = sh.bars;
     const volatile int* abort_flag = &sh.abort_flag;
-    for (int t = 0; t <= T; ++t) {
-        const int st = t & 1, sv = st ^ 1;
-        if (t < T && !mbar_wait_bounded(&bars.kv_full[st], (t >> 1) & 1, timeout_ns, abort_flag)) return false;
-        if (t > 0 && !mbar_wait_bounded(&sh.v_full[sv], ((t - 1) >> 1) & 1, timeout_ns, abort_flag)) return false;
-        if (t == 0) tc_fence_after();
-#pragma unroll
-        for (int qt = 0; qt < NQ; ++qt) {
-            if (t > 0) {
-                if (!mbar_wait_bounded(&bars.p_full[qt], (t - 1) & 1, timeout_ns, abort_flag)) return false;
-                tc_fence_after();
-                if (!(NQ == 2 && qt == 0 && t == T && skip_last))
-                    mma_ts_k128<2048>(tmem + qt * 256 + 128, tmem + qt * 256, vdesc0 + sv * kStageStep, id_pv, t > 1 ? 1u : 0u);
-            }
-            if (t < T) {
-                mma_e4m3_k128(tmem + qt * 256, qdesc0 + qt * kStageStep, kdesc0 + st * kCodeStep, id_qk, 0u);
-                mma_e4m3_k128(tmem + qt * 256, qdesc0 + qt * kStageStep + kCodeStep, kdesc0 + st * kCodeStep, id_qk, 1u);
-                mma_commit(&bars.s_full[qt][st]);
-            }
-        }
+    if (!mbar_wait_bounded(&bars.kv_full[0], 0, timeout_ns, abort_flag)) return false;
+    tc_fence_after();
+#pragma unroll 1
+    for (int qt = 0; qt < NQ; ++qt) mma_codes(sh, tmem, qdesc0, kdesc0, qt, 0);
+    for (int t = 1; t < T;) {
+        if (!mma_codes_step<NQ, 1>(sh, tmem, qdesc0, kdesc0, vdesc0, t, timeout_ns)) return false;
+        if (++t >= T) break;
+        if (!mma_codes_step<NQ, 0>(sh, tmem, qdesc0, kdesc0, vdesc0, t, timeout_ns)) return false;
+        ++t;
+    }
+    const int sv = (T - 1) & 1;
+    if (!mbar_wait_bounded(&sh.v_full[sv], ((T - 1) >> 1) & 1, timeout_ns, abort_flag)) return false;
+#pragma unroll 1
+    for (int qt = 0; qt < NQ; ++qt) {
+        if (!mbar_wait_bounded(&bars.p_full[qt], sv, timeout_ns, abort_flag)) return false;
+        tc_fence_after();
+        if (NQ == 2 && qt == 0 && skip_last) continue;
+        mma_ts_k128<2048>(tmem + qt * 256 + 128, tmem + qt * 256, vdesc0 + sv * (kTileBytes >> 4), idesc_bf16_f32(128, 128, 1),
+                          T > 1 ? 1u : 0u);
     }
     mma_commit(&bars.o_full);
     return true;
@@ -450,13 +480,13 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
             }
             uint64_t* const s_last = bars.s_full[nq - 1];
             int steps = 0, steps_v = 0;
-            int32_t row_v = 0;  // pool row of this lane's box in tile t - 1
             auto row_of = [&](int t) {
                 const int r = mine ? cache_row(a.c, a.b, job.b, jv.token_of(t) + bx * a.box) : 0;
                 return r < 0 ? pool_rows : r;  // past the end: zeros
             };
-            int32_t row_k = row_of(0);
-            // bf16: step t loads K(t) and V(t - 1) behind one barrier; 8-bit: K(t), and V(t) for the warps that turn it
+            int32_t row_k = row_of(0), row_v = 0;  // pool rows of this lane's box in tiles t and t - 1
+            // Step t: bf16 loads K(t) and V(t - 1) behind one barrier; 8-bit K(t), and V(t) for the warps that turn it. The stages
+            // were last read by products of iteration t - 2, which the commit of its last S covers.
             for (int t = 0; t < T + (E4M3 ? 0 : 1); ++t) {
                 const int st = t & 1;
                 bool ok = t < 2 || mbar_wait_bounded(&s_last[st], ((t - 2) >> 1) & 1, a.timeout_ns, &abort_flag);
@@ -483,7 +513,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                     __syncwarp();
                     const uint32_t to = hf * kHalf + bx * a.box * 128;
                     if (mine && has_v)
-                        tma_load_3d(smem + off_v(false) + ((t - 1) & 1) * kTileBytes + to, &tv, &bars.kv_full[st], hf * 64, job.j, row_v);
+                        tma_load_3d(smem + off_v(false) + (st ^ 1) * kTileBytes + to, &tv, &bars.kv_full[st], hf * 64, job.j, row_v);
                     if (mine && has_k)
                         tma_load_3d(smem + kOffK + st * kTileBytes + to, &tk, &bars.kv_full[st], hf * 64, job.j, row_k);
                 }
@@ -517,8 +547,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                     ok = nq == 2 ? mma_issue_codes<2>(sh, tmem, qdesc0, kdesc0, vdesc0, T, skip_last, a.timeout_ns)
                                  : mma_issue_codes<1>(sh, tmem, qdesc0, kdesc0, vdesc0, T, false, a.timeout_ns);
                 } else if (ok) {
-                    const uint32_t id_qk = idesc_bf16_f32(128, 128, 0);
-                    const uint32_t id_pv = idesc_bf16_f32(128, 128, 1);
+                    const uint32_t id_qk = idesc_bf16_f32(128, 128, 0), id_pv = idesc_bf16_f32(128, 128, 1);
                     ok = nq == 2 ? mma_issue_loop<2>(&bars, tmem, qdesc0, kdesc0, vdesc0, id_qk, id_pv, T, skip_last,
                                                      a.timeout_ns, &abort_flag)
                                  : mma_issue_loop<1>(&bars, tmem, qdesc0, kdesc0, vdesc0, id_qk, id_pv, T, false,
@@ -591,23 +620,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
         const uint32_t lane_base = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
         const uint32_t s_addr = lane_base + qt * 256;
         const uint32_t o_addr = s_addr + 128;
-        float* const ks = sh.kscale[warp];
-        // S row of a tile; columns [lim, 128) and [gap, low) are not seen
-        auto load_s = [&](uint32_t (&sr)[128], bool masked, int lim, int gap, int low) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-                tmem_ld32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[c * 32]));
-            tmem_ld_wait();
-            if (masked) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {  // a bit per column: columns below x of these 32 are ones_below(x - 32 c)
-                    const uint32_t seen = ones_below(lim - 32 * c) & ~(ones_below(low - 32 * c) & ~ones_below(gap - 32 * c));
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (!((seen >> i) & 1u)) sr[32 * c + i] = 0xFF800000u;
-                }
-            }
-        };
+        float* const ks = reinterpret_cast<float*>(smem + off_scales(E4M3)) + warp * kTile;
         // p = 2^(s scale - m) of keys [64 h, 64 h + 64) as bf16 pairs; returns their sum
         // (8-bit: a scale for each key, from shared memory)
         // The scales are loaded sixteen keys ahead: read where they are used, 32 waits for shared memory, which the
@@ -642,18 +655,21 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
         };
         float m_run = -INFINITY, l_run = 0.f;
         bool ok = true;
-        JobView jv{};
-        int T = 0, pos_first = 0, pos_last = 0, p = 0;
+        // What the loop keeps of the job: its key tiles from k0 on, those from `sinks` on `past` further; the row's token p,
+        // the tile's first, and the first token from which the window hides nothing of the tile; the CTA's last token
+        int T = 0, k0 = 0, sinks = 0, past = 0, p = 0, pos_first = 0, open_from = 0, last = 0;
+        int seq = 0, kvh = 0;
+        auto token_of = [&](int t) { return (k0 + t < sinks ? k0 + t : k0 + t + past) * kTile; };
         // 8-bit: lane x looks up the scales of the keys 4 x .. 4 x + 3 of a tile, its page two tiles ahead, the bytes one
         // ahead. (A warp that did it for both query tiles came late: 600 cycles a tile.)
         int next_place = -1;
         uint32_t next_scales = 0x7F7F7F7Fu;
         float q_scale = 0.f;
-        auto place_of = [&](int t) { return t < T ? cache_row(a.c, a.b, jv.job.b, jv.token_of(t) + 4 * lane) : -1; };
+        auto place_of = [&](int t) { return t < T ? cache_row(a.c, a.b, seq, token_of(t) + 4 * lane) : -1; };
         auto scales_of = [&](int place) -> uint32_t {
             if (place < 0) return 0x7F7F7F7Fu;
             const int page = place / a.c.page_size;
-            return *reinterpret_cast<const uint32_t*>(a.c.ks + (static_cast<int64_t>(page) * a.c.Hkv + jv.job.j) * a.c.page_size + place - page * a.c.page_size);
+            return *reinterpret_cast<const uint32_t*>(a.c.ks + (static_cast<int64_t>(page) * a.c.Hkv + kvh) * a.c.page_size + place - page * a.c.page_size);
         };
         auto write_scales = [&]() {  // not 0: hidden logits stay -inf
             *reinterpret_cast<float4*>(ks + 4 * lane) = make_float4(fmaxf(scale_value(next_scales & 255u) * q_scale, 1e-37f),
@@ -667,12 +683,19 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
 #pragma unroll 1
         for (int t = first_wave ? -1 : 0;; ++t) {
             if (t == 0) {
-                jv = load_job(a);
+                const JobView jv = load_job(a);
                 T = qt < jv.nq ? jv.T : 0;
-                pos_first = jv.job.pos + qt * tt;  // tokens of the tile
-                pos_last = qt + 1 == jv.nq ? jv.last : pos_first + tt - 1;
+                k0 = jv.job.k0;
+                sinks = jv.tiles.sinks;
+                past = jv.tiles.first - jv.tiles.sinks;
+                seq = jv.job.b;
+                kvh = jv.job.j;
+                last = jv.last;
+                pos_first = jv.job.pos + qt * tt;
+                const int pos_last = qt + 1 == jv.nq ? jv.last : pos_first + tt - 1;
                 p = pos_first + r / g;
                 p = p < pos_last ? p : pos_last;  // rows past the tile's end see what its last row sees
+                open_from = a.a.n_local >= 0 && pos_last > a.a.n_local ? pos_last - a.a.n_local : 0;
                 m_run = -INFINITY;
                 l_run = 0.f;
                 if (E4M3 && T > 0) {
@@ -743,83 +766,114 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 }
             }
             tc_fence_after();
-            const int t0 = jv.token_of(t);
-            const bool masked = t < 0 || t0 + kTile - 1 > pos_first ||
-                                (a.a.n_local >= 0 && pos_last - t0 > a.a.n_local && t0 + kTile - 1 >= a.a.n_sink);
+            const int t0 = token_of(t);
+            const bool masked = t < 0 || t0 + kTile - 1 > pos_first || (t0 < open_from && t0 + kTile - 1 >= a.a.n_sink);
             const int lim = p - t0 + 1;  // keys t0 + c with c >= lim are in the future
             const int gap = a.a.n_sink - t0, low = a.a.n_local >= 0 && p - t0 > a.a.n_local ? p - t0 - a.a.n_local : 0;
-            // The fast and the exact path of k_sparse_attn: exponentials against the reference as it
-            // stands unless the tile's sum shows a logit far above it.
-            bool exact = !__all_sync(0xFFFFFFFFu, m_run != -INFINITY);
-            float sum;
-#pragma unroll 1
-            for (;;) {
-                uint32_t sr[128];
-                load_s(sr, masked, lim, gap, low);
+            // Fast: exponentials against the reference as it stands, all of the row at once, unless something is hidden or
+            // the sum shows a logit far above the reference (the limits of k_sparse_attn). Slow: the maximum first, and 32
+            // columns at a time in loops, so that its instructions leave the fast path's in the cache (4,096 tokens
+            // over 64K: 2,730 us with both paths unrolled).
+            bool slow = masked || !__all_sync(0xFFFFFFFFu, m_run != -INFINITY);
+            float sum = 0.f;
+            if (!slow || t < 0) {
+                uint32_t sr[128], pk[2][32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[c * 32]));
+                tmem_ld_wait();
                 const float* s = reinterpret_cast<const float*>(sr);
-                if (exact) {
-                    float mx8[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) mx8[i] = E4M3 ? s[i] * ks[i] : s[i];
-#pragma unroll
-                    for (int c = 8; c < 120; c += 16)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int x = c + 2 * i;
-                            mx8[i] = E4M3 ? fmax3(mx8[i], s[x] * ks[x], s[x + 1] * ks[x + 1]) : fmax3(mx8[i], s[x], s[x + 1]);
-                        }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) mx8[i] = fmaxf(mx8[i], E4M3 ? s[120 + i] * ks[120 + i] : s[120 + i]);
-                    const float mx = fmax3(fmax3(mx8[0], mx8[1], mx8[2]), fmax3(mx8[3], mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7]));
-                    const float m_new = fmaxf(m_run, E4M3 ? mx : mx * a.a.scale_log2);
-                    const bool raise = m_new > m_run + kRescaleThreshold;
-                    // the O rescale is warp-collective: taken by the whole warp when any row needs it
-                    if (__any_sync(0xFFFFFFFFu, raise)) {
-                        const float alpha = raise ? ex2(m_run - m_new) : 1.0f;
-                        l_run *= alpha;
-                        if (t > 0) {
-#pragma unroll 1
-                            for (int c = 0; c < 8; ++c) {
-                                uint32_t v[16];
-                                tmem_ld16(o_addr + c * 16, v);
-                                tmem_ld_wait();
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
-                                tmem_st16(o_addr + c * 16, v);
-                            }
-                        }
-                        if (raise) m_run = m_new;
-                    }
-                }
-                const float neg_m = (m_run == -INFINITY) ? 0.f : -m_run;
-                uint32_t pk[2][32];
-                sum = exp_half(s, 0, neg_m, pk[0]);
-                sum += exp_half(s, 1, neg_m, pk[1]);
-                if (!exact && __any_sync(0xFFFFFFFFu, !(sum <= kFastSumLimit))) {
-                    exact = true;
-                    continue;
-                }
-                if (t >= 0) {  // (the first products may be on their way)
+                sum = exp_half(s, 0, -m_run, pk[0]);
+                sum += exp_half(s, 1, -m_run, pk[1]);
+                slow = slow || __any_sync(0xFFFFFFFFu, !(sum <= kFastSumLimit));
+                if (!slow) {
                     tmem_st32(s_addr, pk[0]);
                     tmem_st32(s_addr + 32, pk[1]);
-                } else {
-                    sum += __uint_as_float(pk[0][0] ^ pk[1][31]);  // tile -1: keeps the code
                 }
-                break;
+            }
+            if (slow) {
+                // a bit per column: columns below x of these 32 are ones_below(x - 32 c)
+                auto load_32 = [&](uint32_t (&sr)[32], int c) {
+                    tmem_ld32(s_addr + c * 32, sr);
+                    const uint32_t seen = masked ? ones_below(lim - 32 * c) & ~(ones_below(low - 32 * c) & ~ones_below(gap - 32 * c)) : 0xFFFFFFFFu;
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (!((seen >> i) & 1u)) sr[i] = 0xFF800000u;
+                };
+                float mx = -INFINITY;
+#pragma unroll 1
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t sr[32];
+                    load_32(sr, c);
+                    const float* s = reinterpret_cast<const float*>(sr);
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        const float4 f = E4M3 ? lds_f4(ks_at + (32 * c + i) * 4) : make_float4(1.f, 1.f, 1.f, 1.f);
+                        mx = E4M3 ? fmax3(mx, s[i] * f.x, s[i + 1] * f.y) : fmax3(mx, s[i], s[i + 1]);
+                        mx = E4M3 ? fmax3(mx, s[i + 2] * f.z, s[i + 3] * f.w) : fmax3(mx, s[i + 2], s[i + 3]);
+                    }
+                }
+                const float m_new = fmaxf(m_run, E4M3 ? mx : mx * a.a.scale_log2);
+                const bool raise = m_new > m_run + kRescaleThreshold;
+                // the O rescale is warp-collective: taken by the whole warp when any row needs it
+                if (__any_sync(0xFFFFFFFFu, raise)) {
+                    const float alpha = raise ? ex2(m_run - m_new) : 1.0f;
+                    l_run *= alpha;
+                    if (t > 0) {
+#pragma unroll 1
+                        for (int c = 0; c < 8; ++c) {
+                            uint32_t v[16];
+                            tmem_ld16(o_addr + c * 16, v);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
+                            tmem_st16(o_addr + c * 16, v);
+                        }
+                    }
+                    if (raise) m_run = m_new;
+                }
+                const float neg_m = (m_run == -INFINITY) ? 0.f : -m_run;
+                sum = 0.f;
+#pragma unroll 1
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t sr[32], pk[16];
+                    load_32(sr, c);
+                    const float* s = reinterpret_cast<const float*>(sr);
+                    float acc0 = 0.f, acc1 = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        const float4 f = E4M3 ? lds_f4(ks_at + (32 * c + i) * 4) : make_float4(a.a.scale_log2, a.a.scale_log2, a.a.scale_log2, a.a.scale_log2);
+                        float x0, x1, x2, x3;
+                        ffma2(x0, x1, s[i], s[i + 1], f.x, f.y, neg_m, neg_m);
+                        ffma2(x2, x3, s[i + 2], s[i + 3], f.z, f.w, neg_m, neg_m);
+                        x0 = ex2(x0);
+                        x1 = ex2(x1);
+                        x2 = ex2(x2);
+                        x3 = ex2(x3);
+                        fadd2(acc0, acc1, acc0, acc1, x0, x1);
+                        fadd2(acc0, acc1, acc0, acc1, x2, x3);
+                        pk[i / 2] = pack_bf16x2(x0, x1);
+                        pk[i / 2 + 1] = pack_bf16x2(x2, x3);
+                    }
+                    sum += acc0 + acc1;
+                    if (t >= 0) tmem_st16(s_addr + 16 * c, pk);  // over columns that are read; in tile -1 the first products may be on their way
+                    else sum += __uint_as_float(pk[15]);         // keeps the code
+                }
             }
             l_run += sum;
             if (E4M3) __syncwarp();  // the tile's scales are read
             if (t < 0) continue;
             tmem_st_wait();
-            if (!E4M3 && qt == 0 && jv.has_unseen(t0)) {
-                // value rows that no row of the CTA sees: 0 times what lies there may be NaN. The MMA thread
-                // waits for this group before either tile's product with them.
+            if (!E4M3 && qt == 0 && masked) {
+                // value rows that no row of the CTA sees: 0 times what lies there may be NaN. The MMA thread waits for this
+                // group before either query tile's product with them; the next load into the stage waits for those.
                 const bool landed = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.kv_full[(t + 1) & 1], ((t + 1) >> 1) & 1, a.timeout_ns, &abort_flag));
                 if (!landed) {
                     ok = false;
                     break;
                 }
-                if (jv.unseen(t0 + r)) {
+                const int tok = t0 + r, lo = a.a.n_local >= 0 && pos_first > a.a.n_local ? pos_first - a.a.n_local : 0;
+                if (tok > last || (tok < lo && tok >= a.a.n_sink)) {
                     uint8_t* row = smem + off_v(false) + (t & 1) * kTileBytes + r * 128;
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
@@ -831,6 +885,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
             mbar_arrive(&bars.p_full[qt]);
         }
         if (T > 0) {
+            const JobView jv = load_job(a);  // (again: nothing of it is kept through the loop)
             const ChunkJob& job = jv.job;
             bool go = __all_sync(0xFFFFFFFFu, ok && !abort_flag);
             if (go) go = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.o_full, 0, a.timeout_ns, &abort_flag));
