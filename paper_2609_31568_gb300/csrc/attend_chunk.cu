@@ -343,52 +343,49 @@ __device__ __forceinline__ void mma_codes(ChunkShared& sh, uint32_t tmem, uint64
     mma_commit(&sh.bars.s_full[qt][st]);
 }
 
-// Iteration t > 0 (t & 1 = ST) of mma_issue_codes.
-template <int NQ, int ST>
+// Iteration t > 0 of mma_issue_codes.
 __device__ __forceinline__ bool mma_codes_step(ChunkShared& sh, uint32_t tmem, uint64_t qdesc0, uint64_t kdesc0, uint64_t vdesc0,
-                                               int t, uint64_t timeout_ns)
+                                               int nq, int t, uint64_t timeout_ns)
 {
+    const int st = t & 1;
     Barriers& bars = sh.bars;
     const volatile int* abort_flag = &sh.abort_flag;
-    if (!mbar_wait_bounded(&bars.kv_full[ST], (t >> 1) & 1, timeout_ns, abort_flag)) return false;
-    if (!mbar_wait_bounded(&sh.v_full[ST ^ 1], ((t - 1) >> 1) & 1, timeout_ns, abort_flag)) return false;
-#pragma unroll
-    for (int qt = 0; qt < NQ; ++qt) {
-        if (!mbar_wait_bounded(&bars.p_full[qt], ST ^ 1, timeout_ns, abort_flag)) return false;
+    if (!mbar_wait_bounded(&bars.kv_full[st], (t >> 1) & 1, timeout_ns, abort_flag)) return false;
+    if (!mbar_wait_bounded(&sh.v_full[st ^ 1], ((t - 1) >> 1) & 1, timeout_ns, abort_flag)) return false;
+#pragma unroll 1
+    for (int qt = 0; qt < nq; ++qt) {
+        if (!mbar_wait_bounded(&bars.p_full[qt], st ^ 1, timeout_ns, abort_flag)) return false;
         tc_fence_after();
-        mma_ts_k128<2048>(tmem + qt * 256 + 128, tmem + qt * 256, vdesc0 + (ST ^ 1) * (kTileBytes >> 4),
+        mma_ts_k128<2048>(tmem + qt * 256 + 128, tmem + qt * 256, vdesc0 + (st ^ 1) * (kTileBytes >> 4),
                           idesc_bf16_f32(128, 128, 1), t > 1 ? 1u : 0u);
-        mma_codes(sh, tmem, qdesc0, kdesc0 + ST * (kCodeBytes >> 4), qt, ST);
+        mma_codes(sh, tmem, qdesc0, kdesc0 + st * (kCodeBytes >> 4), qt, st);
     }
     return true;
 }
 
-// mma_issue_loop (attn_mma.cuh) for 8-bit keys, whose K and V have barriers of their own. (What this loop and the softmax
-// run per key tile has to stay in the SM's instruction cache: with six iterations unrolled the requests to the next level
-// tripled and the products took a fifth longer.)
-template <int NQ>
+// mma_issue_loop (attn_mma.cuh) for 8-bit keys, whose K and V have barriers of their own. Rolled: what all roles run per
+// key tile has to stay in the SM's instruction cache. (4,096 tokens over 64K, 8-bit: 3,535 us; 3,730 us with two
+// iterations of this loop and four of the values' conversion unrolled, when requests for instructions took 64% of
+// what the next level answers, and 16% now.)
 __device__ __forceinline__ bool mma_issue_codes(ChunkShared& sh, uint32_t tmem, uint64_t qdesc0, uint64_t kdesc0, uint64_t vdesc0,
-                                                int T, bool skip_last, uint64_t timeout_ns)
+                                                int nq, int T, bool skip_last, uint64_t timeout_ns)
 {
     Barriers& bars = sh.bars;
     const volatile int* abort_flag = &sh.abort_flag;
     if (!mbar_wait_bounded(&bars.kv_full[0], 0, timeout_ns, abort_flag)) return false;
     tc_fence_after();
 #pragma unroll 1
-    for (int qt = 0; qt < NQ; ++qt) mma_codes(sh, tmem, qdesc0, kdesc0, qt, 0);
-    for (int t = 1; t < T;) {
-        if (!mma_codes_step<NQ, 1>(sh, tmem, qdesc0, kdesc0, vdesc0, t, timeout_ns)) return false;
-        if (++t >= T) break;
-        if (!mma_codes_step<NQ, 0>(sh, tmem, qdesc0, kdesc0, vdesc0, t, timeout_ns)) return false;
-        ++t;
-    }
+    for (int qt = 0; qt < nq; ++qt) mma_codes(sh, tmem, qdesc0, kdesc0, qt, 0);
+#pragma unroll 1
+    for (int t = 1; t < T; ++t)
+        if (!mma_codes_step(sh, tmem, qdesc0, kdesc0, vdesc0, nq, t, timeout_ns)) return false;
     const int sv = (T - 1) & 1;
     if (!mbar_wait_bounded(&sh.v_full[sv], ((T - 1) >> 1) & 1, timeout_ns, abort_flag)) return false;
 #pragma unroll 1
-    for (int qt = 0; qt < NQ; ++qt) {
+    for (int qt = 0; qt < nq; ++qt) {
         if (!mbar_wait_bounded(&bars.p_full[qt], sv, timeout_ns, abort_flag)) return false;
         tc_fence_after();
-        if (NQ == 2 && qt == 0 && skip_last) continue;
+        if (nq == 2 && qt == 0 && skip_last) continue;
         mma_ts_k128<2048>(tmem + qt * 256 + 128, tmem + qt * 256, vdesc0 + sv * (kTileBytes >> 4), idesc_bf16_f32(128, 128, 1),
                           T > 1 ? 1u : 0u);
     }
@@ -544,8 +541,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 // the last key tile may lie after every row of the first query tile
                 const bool skip_last = T > 1 && jv.token_of(T - 1) > job.pos + tt - 1;
                 if (ok && E4M3) {
-                    ok = nq == 2 ? mma_issue_codes<2>(sh, tmem, qdesc0, kdesc0, vdesc0, T, skip_last, a.timeout_ns)
-                                 : mma_issue_codes<1>(sh, tmem, qdesc0, kdesc0, vdesc0, T, false, a.timeout_ns);
+                    ok = mma_issue_codes(sh, tmem, qdesc0, kdesc0, vdesc0, nq, T, skip_last, a.timeout_ns);
                 } else if (ok) {
                     const uint32_t id_qk = idesc_bf16_f32(128, 128, 0), id_pv = idesc_bf16_f32(128, 128, 1);
                     ok = nq == 2 ? mma_issue_loop<2>(&bars, tmem, qdesc0, kdesc0, vdesc0, id_qk, id_pv, T, skip_last,
@@ -594,7 +590,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 uint8_t* const to1 = to + (((c0 + 1 - late) ^ (r16 & 7)) << 4);
                 const int t0 = jv.token_of(t);
                 const bool unseen = jv.has_unseen(t0);
-#pragma unroll 4
+#pragma unroll 1  // (the instruction cache: see mma_issue_codes)
                 for (int i = 0; i < 8; ++i) {
                     const uint4 w = *reinterpret_cast<const uint4*>(from + i * 16 * kHeadDim);
                     const float f = scale_value(__shfl_sync(0xFFFFFFFFu, scale, 4 * i + (lane >> 3)));
@@ -959,45 +955,82 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
     }
 }
 
-// Pieces of a query tile pair put together: a warp per row, four dimensions a lane. A grid of what the SMs hold walks
-// the rows: one CTA for eight of every row that could be cut took 12 us, most of it for CTAs without a row.
-__global__ void __launch_bounds__(256) k_chunk_merge(const __grid_constant__ ChunkArgs a)
+// Pieces of a query tile pair put together: a warp takes four rows, four dimensions a lane, and eight pieces at a time,
+// whose references and sums the lanes hold (lane 8 i + p: row i, piece p). Bound by the latency of its loads, which
+// depend on nothing but the list: eight rows are on their way at a time. 9 sequences of 1 to 700 new tokens, 8 KV heads,
+// 176 pairs in two or three pieces: the call takes 129 us, and 134 with a warp per row that looks the weights up piece by
+// piece. A grid of what the SMs hold walks the rows: one CTA for eight of every row that could be cut took 12 us, most of
+// it for CTAs without a row.
+constexpr int kMergeCtas = 4;  // per SM, of 256 threads
+
+__global__ void __launch_bounds__(256, kMergeCtas) k_chunk_merge(const __grid_constant__ ChunkArgs a)
 {
     pdl_enter();
     const int lane = threadIdx.x & 31, per_tile = a.tile_tokens * a.a.g;
-    const int merges = a.p.counts[1];
+    const int total = a.p.counts[1] * (a.part_rows / 4);  // at most 2 kMaxSms pairs of 64
     const int step = gridDim.x * 8;
 #pragma unroll 1
-    for (int w = blockIdx.x * 8 + (threadIdx.x >> 5); w < merges * a.part_rows; w += step) {
-        const int r = w % a.part_rows;                   // row of the pair's tiles
-        const int x = r < kTile ? r : per_tile + r - kTile;  // and which of its live rows that is
-        const ChunkMerge mg = a.p.merges[w / a.part_rows];
-        if ((r < kTile ? r >= per_tile : false) || x >= mg.ntok * a.a.g) continue;
-        float top = -INFINITY;
-        for (int i = lane; i < mg.pieces; i += 32)
-            top = fmaxf(top, __ldcg(&a.part_ml[static_cast<int64_t>(mg.slot + i) * a.part_rows + r]).x);
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        const float base = top == -INFINITY ? 0.f : top;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        float sum = 0.f;
-#pragma unroll 4
-        for (int i = 0; i < mg.pieces; ++i) {
-            const int64_t at = static_cast<int64_t>(mg.slot + i) * a.part_rows + r;
-            const float2 ml = __ldcg(&a.part_ml[at]);
-            const float4 o = __ldcg(reinterpret_cast<const float4*>(a.part_o + at * kHeadDim) + lane);
+    for (int w = blockIdx.x * 8 + (threadIdx.x >> 5); w < total; w += step) {
+        const int m = w / (a.part_rows / 4);
+        const int r = (w - m * (a.part_rows / 4)) * 4;       // first row of the pair's tiles
+        const int4 y0 = reinterpret_cast<const int4*>(a.p.merges + m)[0];  // KV head, first row, tokens, slot
+        const int pieces = a.p.merges[m].pieces;
+        // live rows: those of the first tile below per_tile, then those of the second
+        auto live_row = [&](int rr) { return rr < kTile ? (rr < per_tile ? rr : y0.z * a.a.g) : per_tile + rr - kTile; };
+        if (live_row(r) >= y0.z * a.a.g) continue;
+        const float* from = a.part_o + (static_cast<int64_t>(y0.w) * a.part_rows + r) * kHeadDim + lane * 4;
+        const float2* ml_at = a.part_ml + static_cast<int64_t>(y0.w) * a.part_rows + r + (lane >> 3);
+        float top = -INFINITY, sum = 0.f;  // of row lane >> 3, the same in its eight lanes
+        float4 acc[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (int p0 = 0; p0 < pieces; p0 += 8) {
+            const int p = p0 + (lane & 7);
+            const float2 ml = p < pieces ? __ldcg(ml_at + static_cast<int64_t>(p) * a.part_rows) : make_float2(-INFINITY, 0.f);
+            float mx = ml.x;
+            for (int o = 4; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, o));
+            const float now = fmaxf(top, mx), base = now == -INFINITY ? 0.f : now;
+            const float old = ex2(top - base);  // 0 for the first eight
             const float f = ex2(ml.x - base);
-            sum = fmaf(ml.y, f, sum);
-            acc.x = fmaf(o.x, f, acc.x);
-            acc.y = fmaf(o.y, f, acc.y);
-            acc.z = fmaf(o.z, f, acc.z);
-            acc.w = fmaf(o.w, f, acc.w);
+            float part = ml.y * f;
+            for (int o = 4; o > 0; o >>= 1) part += __shfl_xor_sync(0xFFFFFFFFu, part, o);
+            sum = fmaf(sum, old, part);
+            top = now;
+            if (p0 > 0) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float x = __shfl_sync(0xFFFFFFFFu, old, 8 * i);
+                    acc[i] = make_float4(acc[i].x * x, acc[i].y * x, acc[i].z * x, acc[i].w * x);
+                }
+            }
+            const int n = pieces - p0 < 8 ? pieces - p0 : 8;
+#pragma unroll 2
+            for (int q = 0; q < n; ++q) {
+                const float* row = from + static_cast<int64_t>(p0 + q) * a.part_rows * kHeadDim;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float4 o = __ldcg(reinterpret_cast<const float4*>(row + i * kHeadDim));
+                    const float x = __shfl_sync(0xFFFFFFFFu, f, 8 * i + q);
+                    acc[i].x = fmaf(o.x, x, acc[i].x);
+                    acc[i].y = fmaf(o.y, x, acc[i].y);
+                    acc[i].z = fmaf(o.z, x, acc[i].z);
+                    acc[i].w = fmaf(o.w, x, acc[i].w);
+                }
+            }
         }
-        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-        const int64_t row = mg.row0 + x / a.a.g;
-        const int h = mg.j * a.a.g + x % a.a.g;
-        auto* out = static_cast<__nv_bfloat16*>(a.a.out) + row * a.a.out_stride + h * kHeadDim;
-        reinterpret_cast<uint2*>(out)[lane] = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
-        if (a.a.lse && lane == 0) a.a.lse[row * a.a.Hq + h] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * 0.6931471805599453f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float l = __shfl_sync(0xFFFFFFFFu, sum, 8 * i), mx = __shfl_sync(0xFFFFFFFFu, top, 8 * i);
+            const int x = live_row(r + i);
+            if (x >= y0.z * a.a.g) continue;
+            const float inv = l == 0.f ? 0.f : 1.0f / l;
+            const int64_t row = y0.y + x / a.a.g;
+            const int h = y0.x * a.a.g + x % a.a.g;
+            auto* out = static_cast<__nv_bfloat16*>(a.a.out) + row * a.a.out_stride + h * kHeadDim;
+            reinterpret_cast<uint2*>(out)[lane] = make_uint2(pack_bf16x2(acc[i].x * inv, acc[i].y * inv), pack_bf16x2(acc[i].z * inv, acc[i].w * inv));
+            if (a.a.lse && lane == 0) a.a.lse[row * a.a.Hq + h] = l == 0.f ? -INFINITY : (mx + __log2f(l)) * 0.6931471805599453f;
+        }
     }
 }
 
@@ -1054,7 +1087,7 @@ cudaError_t run_chunks(const ChunkArgs& a, cudaStream_t st)
     if (e == cudaSuccess) e = launch_after(st, dim3(1), kPlanThreads, 0, 1, k_chunk_plan, a);
     if (e == cudaSuccess)
         e = launch_after(st, dim3(a.p.max_jobs), chunk_threads(E4M3), chunk_smem(E4M3), 1, k_chunk<E4M3>, tq, tk, tv, a);
-    const int merge_ctas = a.p.max_merges * (a.part_rows / 8), most = a.sms * 8;
+    const int merge_ctas = a.p.max_merges * (a.part_rows / 32), most = a.sms * kMergeCtas;
     if (e == cudaSuccess) e = launch_after(st, dim3(merge_ctas < most ? merge_ctas : most), 256, 0, 1, k_chunk_merge, a);
     return e;
 }
