@@ -29,9 +29,13 @@ namespace {
 
 constexpr int kTile = 128;            // keys of a tile, rows of a query tile
 constexpr int kPlanThreads = 512;     // at least 2 kMaxSms
-constexpr int kCuts = 3;              // pieces per SM, at most, beyond one per item
+constexpr int kCuts = 3;              // pieces per SM, at most, beyond one per item;
+constexpr int kCutsRest = 2;          // of the rest of more items than 2 kMaxSms
 constexpr int kPieces = 8;            // pieces of an item that the plan considers
-constexpr int kCandidates = kPieces + kCuts;
+constexpr int kUniform = kPieces + kCuts;  // ways to cut that the plan considers: all alike,
+constexpr int kTails = 3, kTailCuts = 4;   // and the last half, quarter or eighth of the work shorter
+constexpr int kCandidates = kUniform + kTails * kTailCuts;
+static_assert(kCandidates <= 32, "a lane for each");
 constexpr int kPieceTiles = 5;        // what a CTA's start and end take, in key tiles
 constexpr int kMergeTiles = 4;        // what writing and merging one piece per SM takes
 
@@ -113,15 +117,22 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* s_warp, int64_
 
 // The list of jobs: one CTA. Items are (sequence, KV head, pair of query tiles), a KV head's pairs from the
 // last (the one with most keys) to the first, so that the CTAs running at a time share the keys of few heads.
-// As many items as fill the SMs a whole number of times run whole; the rest (all of them, when there are
-// fewer than two per SM) are cut along their keys into pieces of at most C tiles. C is one of longest / 1 .. longest
-// / kPieces and W / SMs .. W / (kCuts SMs), W the rest's key tiles: the one for which ceil(pieces / SMs) rounds of
-// C + kPieceTiles, and the merge of the pieces, end first.
+// No job has more than an even share of all key tiles (64 sequences of 5 tokens, bf16, one at 131072 and the others
+// at 1,000: 172 us, and 1,328 with the long one's 8 items whole). Calls of more items than 2 kMaxSms run as many as fill
+// the SMs a whole number of times so; how the rest are cut (all of them, in other calls) is one of kCandidates: into
+// pieces of at most C tiles, C one of
+// longest / 1 .. longest / kPieces and R / SMs .. R / (kCuts SMs), R the rest's key tiles; or only the items that hold
+// the last half, quarter or eighth of R, T tiles, into pieces of T / SMs .. T / (kTailCuts SMs), which fill up what the
+// jobs before them leave uneven. The one is taken that ends first, by the rounds of the SMs or by what jobs taken in
+// order can be late at most, kPieceTiles for each job and the merge of the pieces included. (9 sequences of 1 to 700
+// tokens, 200 items, 8-bit: 113 us, and 129 with all cut alike. 4,096 tokens over 64K: 512 items, 208 of them cut.)
+// The plan takes 7 to 8 us, most of it latency: lengths from memory, scans, the lists' way back.
 __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_constant__ ChunkArgs a)
 {
     __shared__ int s_before[kMaxSeqs + 1];  // items (of one KV head) of the sequences before
     __shared__ int64_t s_warp[32];
-    __shared__ int s_longest, s_pieces[32], s_cut;
+    __shared__ int s_longest, s_long[32], s_tail[32], s_split[32], s_cut;
+    __shared__ float s_cut_tail;
     __shared__ unsigned long long s_work;
     pdl_trigger();  // k_chunk's first CTAs set up meanwhile
     pdl_wait();
@@ -153,7 +164,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_consta
         s_work = 0;
         s_longest = 0;
     }
-    if (tid < 32) s_pieces[tid] = 0;
+    if (tid < 32) s_long[tid] = s_tail[tid] = s_split[tid] = 0;
     __syncthreads();
     // item x: sequences outermost, then KV heads, then pairs from the last
     auto item = [&](int x, ChunkJob* jb) {
@@ -177,86 +188,125 @@ __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_consta
         jb->k1 = tiles_of(a.a, jb->pos, jb->ntok).n;
         jb->slot = -1;
     };
-    const int whole = items > 2 * a.sms ? static_cast<int>(items) / a.sms * a.sms : 0;
+    const int whole = items > 2 * kMaxSms ? static_cast<int>(items) / a.sms * a.sms : 0;
     const int rest = static_cast<int>(items) - whole;  // at most 2 kMaxSms: one per thread
+    int64_t work = 0;
 #pragma unroll 1
     for (int x = tid; x < whole; x += kPlanThreads) {
-        ChunkJob jb;
-        item(x, &jb);
-        a.p.jobs[x] = jb;
+        ChunkJob jw;
+        item(x, &jw);
+        work += jw.k1;
+    }
+    if (whole > 0) {
+        for (int o = 16; o > 0; o >>= 1) work += __shfl_xor_sync(0xFFFFFFFFu, work, o);
+        if (lane == 0) atomicAdd(&s_work, static_cast<unsigned long long>(work));
     }
     ChunkJob jb{};
     if (tid < rest) item(whole + tid, &jb);
     if ((tid & ~31) < rest) {
-        const uint32_t sum = __reduce_add_sync(0xFFFFFFFFu, static_cast<uint32_t>(jb.k1)), top = __reduce_max_sync(0xFFFFFFFFu, jb.k1);
-        if (lane == 0) {
-            atomicAdd(&s_work, static_cast<unsigned long long>(sum));
-            atomicMax(&s_longest, static_cast<int>(top));
-        }
+        const int top = __reduce_max_sync(0xFFFFFFFFu, jb.k1);
+        if (lane == 0) atomicMax(&s_longest, top);
     }
-    __syncthreads();
-    // the longest piece of candidate f, and the pieces of n tiles then
-    auto cut_of = [&](int f) {
-        const int c = f < kPieces ? (s_longest + f) / (f + 1) : static_cast<int>(static_cast<float>(s_work) / static_cast<float>((f - kPieces + 1) * a.sms)) + 1;
-        return c < 2 ? 2 : c;
-    };
+    int64_t rest_work;
+    const int64_t work_before = block_scan(jb.k1, s_warp, &rest_work);
+    const float R = static_cast<float>(rest_work), per_sm = 1.0f / static_cast<float>(a.sms);
+    const float share = fminf((static_cast<float>(s_work) + R) * per_sm, 1e9f);
+    const int cut_long = static_cast<int>(share) + 1 < 2 ? 2 : static_cast<int>(share) + 1;
     auto pieces_of = [&](int n, int cut, float inv) {  // ceil(n / cut)
         int q = static_cast<int>(static_cast<float>(n + cut - 1) * inv);
         q += q * cut < n;
         return q - ((q - 1) * cut >= n);
     };
-    const int my_cut = lane < kCandidates ? cut_of(lane) : 2;  // lane f: candidate f
+    // lane f: candidate f. Items of which no more than my_tail is left are cut at my_cut, those before at cut_long.
+    const float inv_long = 1.0f / static_cast<float>(cut_long);
+    const int f2 = lane - kUniform;
+    const float my_tail = f2 < 0 ? R : R / static_cast<float>(2 << f2 / kTailCuts);
+    const int parts = f2 < 0 ? lane - kPieces + 1 : f2 % kTailCuts + 1;
+    int my_cut = lane < kPieces ? (s_longest + lane) / (lane + 1) : static_cast<int>(fminf(my_tail * per_sm / static_cast<float>(parts), 1e9f)) + 1;
+    if (my_cut < 2) my_cut = 2;
+    const float sfx = static_cast<float>(rest_work - work_before);  // key tiles from this item on
     if ((tid & ~31) < rest) {
         const float inv = 1.0f / static_cast<float>(my_cut);
-        int n = 0;
+        const int mine = rest - (tid & ~31) < 32 ? rest - (tid & ~31) : 32;
+        int n_long = 0, n_tail = 0, n_cut = 0;
 #pragma unroll 4
-        for (int i = 0; i < 32; ++i) {  // the warp's items
+        for (int i = 0; i < mine; ++i) {  // the warp's items
             const int k1 = __shfl_sync(0xFFFFFFFFu, jb.k1, i);
-            if (k1 > 0) n += pieces_of(k1, my_cut, inv);
+            const bool tail = __shfl_sync(0xFFFFFFFFu, sfx, i) <= my_tail;
+            const int q = pieces_of(k1, tail ? my_cut : cut_long, tail ? inv : inv_long);
+            (tail ? n_tail : n_long) += q;
+            n_cut += q > 1 ? q : 0;
         }
-        if (lane < kCandidates) atomicAdd(&s_pieces[lane], n);
+        if (lane < kCandidates) {
+            atomicAdd(&s_long[lane], n_long);
+            atomicAdd(&s_tail[lane], n_tail);
+            atomicAdd(&s_split[lane], n_cut);
+        }
     }
     __syncthreads();
     if (tid < 32) {
-        const int n = s_pieces[lane];
-        const uint32_t time = static_cast<uint32_t>(n + a.sms - 1) / static_cast<uint32_t>(a.sms) * static_cast<uint32_t>(my_cut + kPieceTiles) +
-                              (n > rest ? static_cast<uint32_t>(kMergeTiles * n) / static_cast<uint32_t>(a.sms) : 0u);
-        const bool open = lane < kCandidates && (lane == 0 || n <= rest + kCuts * a.sms);
-        const uint32_t best = __reduce_min_sync(0xFFFFFFFFu, open ? time : 0xFFFFFFFFu);
-        const int f = __ffs(__ballot_sync(0xFFFFFFFFu, open && time == best)) - 1;
-        if (lane == f) s_cut = my_cut;
+        const int n_long = s_long[lane], n = n_long + s_tail[lane];
+        auto rounds = [&](int jobs) { return ceilf(static_cast<float>(jobs) * per_sm); };
+        float time;
+        if (f2 < 0) {
+            time = rounds(n) * static_cast<float>(my_cut + kPieceTiles);
+        } else {
+            const float top = static_cast<float>((s_longest < cut_long ? s_longest : cut_long) + kPieceTiles);
+            const float first = fminf(rounds(n_long) * top, (R - my_tail + static_cast<float>(n_long * kPieceTiles)) * per_sm + top);
+            time = fmaxf(first, (R + static_cast<float>(n * kPieceTiles)) * per_sm + static_cast<float>(my_cut + kPieceTiles));
+        }
+        time += static_cast<float>(kMergeTiles * s_split[lane]) * per_sm;
+        // candidate kPieces: at most `rest` pieces and one per SM, whatever the lengths
+        const bool open = lane < kCandidates && (lane == kPieces || n <= rest + (whole ? kCutsRest : kCuts) * a.sms);
+        const uint32_t bits = open ? __float_as_uint(time) : 0xFFFFFFFFu;
+        const uint32_t best = __reduce_min_sync(0xFFFFFFFFu, bits);
+        if (lane == __ffs(__ballot_sync(0xFFFFFFFFu, bits == best)) - 1) {
+            s_cut = my_cut;
+            s_cut_tail = my_tail;
+        }
     }
     __syncthreads();
-    const int pieces = tid < rest ? pieces_of(jb.k1, s_cut, 1.0f / static_cast<float>(s_cut)) : 0;
-    // jobs, partial results and merges before this item, one scan of 21 bits each
-    int64_t sums;
-    const int64_t mask = (1 << 21) - 1;
-    const int64_t before = block_scan(pieces > 1 ? pieces | static_cast<int64_t>(pieces) << 21 | 1ll << 42 : pieces, s_warp, &sums);
-    const int at = whole + static_cast<int>(before & mask), slot = static_cast<int>((before >> 21) & mask), merge = static_cast<int>(before >> 42);
-    const int jobs = whole + static_cast<int>(sums & mask), slots = static_cast<int>((sums >> 21) & mask), merges = static_cast<int>(sums >> 42);
-    if (jobs > a.p.max_jobs || slots > a.p.max_slots || merges > a.p.max_merges) {  // as above
-        if (tid == 0) {
-            record_status(a.status, SCALE_ERR_DEVICE);
-            a.p.counts[0] = a.p.counts[1] = 0;
-        }
-        return;
-    }
-    const int n = jb.k1;
-    const int each = pieces > 1 ? static_cast<int>(static_cast<uint32_t>(n) / static_cast<uint32_t>(pieces)) : n, more = n - each * pieces;
+    // Jobs, a block of items at a time; at, slot and merge count jobs, partial results and merges so far.
+    int at = 0, slot = 0, merge = 0;
 #pragma unroll 1
-    for (int i = 0; i < pieces; ++i) {  // the first `more` pieces have one tile more
+    for (int x0 = 0;; x0 += kPlanThreads) {
+        const bool done = x0 >= whole;
         ChunkJob x = jb;
-        x.k0 = each * i + (i < more ? i : more);
-        x.k1 = x.k0 + each + (i < more);
-        x.slot = pieces > 1 ? slot + i : -1;
-        int4* to = reinterpret_cast<int4*>(a.p.jobs + at + i);
-        to[0] = make_int4(x.b, x.j, x.row0, x.ntok);
-        to[1] = make_int4(x.pos, x.k0, x.k1, x.slot);
+        if (!done) {
+            x.k1 = 0;
+            if (x0 + tid < whole) item(x0 + tid, &x);
+        }
+        const int cut = done && sfx <= s_cut_tail ? s_cut : cut_long;
+        const int n = x.k1, pieces = n > 0 ? pieces_of(n, cut, 1.0f / static_cast<float>(cut)) : 0;
+        // jobs, partial results and merges before this item, one scan of 21 bits each
+        int64_t sums;
+        const int64_t mask = (1 << 21) - 1;
+        const int64_t before = block_scan(pieces > 1 ? pieces | static_cast<int64_t>(pieces) << 21 | 1ll << 42 : pieces, s_warp, &sums);
+        const int my_at = at + static_cast<int>(before & mask), my_slot = slot + static_cast<int>((before >> 21) & mask), my_merge = merge + static_cast<int>(before >> 42);
+        at += static_cast<int>(sums & mask);
+        slot += static_cast<int>((sums >> 21) & mask);
+        merge += static_cast<int>(sums >> 42);
+        if (at > a.p.max_jobs || slot > a.p.max_slots || merge > a.p.max_merges) {  // as above
+            if (tid == 0) {
+                record_status(a.status, SCALE_ERR_DEVICE);
+                a.p.counts[0] = a.p.counts[1] = 0;
+            }
+            return;
+        }
+        const int each = pieces > 1 ? static_cast<int>(static_cast<uint32_t>(n) / static_cast<uint32_t>(pieces)) : n, more = n - each * pieces;
+#pragma unroll 1
+        for (int i = 0; i < pieces; ++i) {  // the first `more` pieces have one tile more
+            const int k0 = each * i + (i < more ? i : more);
+            int4* to = reinterpret_cast<int4*>(a.p.jobs + my_at + i);
+            to[0] = make_int4(x.b, x.j, x.row0, x.ntok);
+            to[1] = make_int4(x.pos, k0, k0 + each + (i < more), pieces > 1 ? my_slot + i : -1);
+        }
+        if (pieces > 1) a.p.merges[my_merge] = ChunkMerge{x.j, x.row0, x.ntok, my_slot, pieces, {0, 0, 0}};
+        if (done) break;
     }
-    if (pieces > 1) a.p.merges[merge] = ChunkMerge{jb.j, jb.row0, jb.ntok, slot, pieces, {0, 0, 0}};
     if (tid == 0) {
-        a.p.counts[0] = jobs;
-        a.p.counts[1] = merges;
+        a.p.counts[0] = at;
+        a.p.counts[1] = merge;
     }
 }
 
@@ -1055,9 +1105,13 @@ ChunkWs chunk_layout(int g, int Hkv, int n_seqs, int n_rows, int max_rows)
     const int64_t each = (static_cast<int64_t>(max_rows) + 2 * tt - 1) / (2 * tt);
     if (pairs > each * n_seqs) pairs = each * n_seqs;
     const int64_t items = pairs * Hkv;
-    const int64_t cut = items < 2 * kMaxSms ? items : 2 * kMaxSms;  // items that may be cut
-    const int64_t slots = cut + kCuts * kMaxSms;
-    w.max_merges = static_cast<int>(cut);
+    // What is cut: all items of a call of few, an item and kCuts pieces per SM; of many, the rest (kCutsRest) and of the others
+    // those longer than an SM's share, a job for each SM more at most, which is two pieces. The actual number of items may
+    // be below this bound and count as few.
+    const int64_t few = items < 2 * kMaxSms ? items : 2 * kMaxSms;
+    static_assert(kCuts >= kCutsRest + 1, "jobs of either kind of call");
+    const int64_t slots = few + kCuts * kMaxSms;
+    w.max_merges = static_cast<int>(few);
     w.max_jobs = static_cast<int>(items + kCuts * kMaxSms);
     w.max_slots = static_cast<int>(slots);
     w.part_rows = max_rows > tt ? 2 * kTile : kTile;

@@ -531,3 +531,23 @@ def test_serving_run(hq, hkv, e4m3):
     S.scale_build_reps(p, q0, kb[: total[0]], buf.reps, buf.fingerprints, buf.unit_start, buf.n_units, buf.ws)
     means = torch.stack([kb[: total[0]].double()[i: i + 32].mean(0) for i in range(0, total[0], 32)]).transpose(0, 1)
     assert (buf.reps.double() - means).abs().max() < 1e-5
+
+
+# ---------------------------------------------------------------- how work is divided
+
+
+@pytest.mark.parametrize("long_at", [0, 20, 47])
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_a_long_sequence_among_many_short(long_at, e4m3):
+    """More query tiles than the SMs hold twice, one sequence of fifty times the keys of the others."""
+    lens = [40 + 37 * i % 300 for i in range(48)]
+    lens[long_at] = 19999
+    check_attend(Batch([5] * 48, lens, hq=32, hkv=8, page=64, e4m3=e4m3))
+
+
+@pytest.mark.parametrize("n_sink,n_local", [(0, -1), (64, 1500)])
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_more_query_tiles_than_sms(n_sink, n_local, e4m3):
+    """Between one query tile pair per SM and two: some whole, the last ones in pieces that fill up the SMs."""
+    check_attend(Batch([64 * 7, 1, 300, 64 * 9], [3000, 777, 2900, 3100], hq=16, hkv=8, page=32, e4m3=e4m3), n_sink=n_sink,
+                 n_local=n_local)
