@@ -115,14 +115,15 @@ def kv_cache(k_pages, v_pages, k_scales=None, v_scales=None) -> ScaleCache:
     if k_pages.dtype != v_pages.dtype or (k_scales is None) != (v_scales is None):
         raise ValueError("keys and values of a cache have the same type")
     if k_scales is None:
-        if k_pages.itemsize != 2 or not k_pages.is_floating_point():
+        if k_pages.dtype is not _imported_torch().bfloat16:
             raise ValueError("a cache without scales holds bf16 rows")
         dtype = SCALE_CACHE_BF16
     else:
-        if k_pages.itemsize != 1:
-            raise ValueError("a cache with scales holds 8-bit rows")
+        torch = _imported_torch()
+        if k_pages.dtype not in (torch.uint8, torch.float8_e4m3fn):
+            raise ValueError("a cache with scales holds e4m3 rows (uint8 or float8_e4m3fn)")
         for s in (k_scales, v_scales):
-            if tuple(s.shape) != (pages, heads, page) or s.itemsize != 1:
+            if tuple(s.shape) != (pages, heads, page) or s.dtype is not torch.uint8:
                 raise ValueError("scales are uint8 [num_pages][num_kv_heads][page_size]")
         dtype = SCALE_CACHE_E4M3
     c = ScaleCache(_ptr(k_pages), _ptr(v_pages), _ptr(k_scales), _ptr(v_scales), dtype, heads, page, pages)
@@ -260,6 +261,18 @@ def load() -> ctypes.CDLL:
         return lib
 
 
+_torch = None  # the torch module, once a call has needed it
+
+
+def _imported_torch():
+    global _torch
+    if _torch is None:
+        import torch
+
+        _torch = torch
+    return _torch
+
+
 def _ptr(x) -> int | None:
     """Device or host address of a tensor / array / int (None for None)."""
     if x is None or isinstance(x, int):
@@ -288,7 +301,7 @@ def _rows(x, n_rows: int, heads: int | None = None) -> tuple:
     shape, stride = x.shape, x.stride()
     if len(shape) != 3 or shape[2] != 128 or shape[0] < n_rows or (heads is not None and shape[1] != heads):
         raise ValueError(f"expected a row tensor [{n_rows}][{'heads' if heads is None else heads}][128], got {tuple(shape)}")
-    if x.itemsize != 2 or not x.is_floating_point():
+    if x.dtype is not _imported_torch().bfloat16:
         raise ValueError("row tensors are bf16")
     if stride[2] != 1 or (shape[1] > 1 and stride[1] != 128):
         raise ValueError("the heads of a row must be contiguous")
@@ -299,21 +312,14 @@ def _nbytes(x) -> int:
     return int(x.nbytes)
 
 
-_torch = None  # the torch module, once a call has needed its current stream
-
-
 def _stream(stream) -> int | None:
     if stream is None:
-        global _torch
-        if _torch is None:
-            import torch
-
-            _torch = torch
+        torch = _imported_torch()
         # the handle alone, where this torch gives it: 0.3 us, against 3 us for a torch.cuda.Stream object
-        raw = getattr(_torch._C, "_cuda_getCurrentRawStream", None)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         if raw is None:
-            return _torch.cuda.current_stream().cuda_stream
-        return raw(_torch.cuda.current_device())
+            return torch.cuda.current_stream().cuda_stream
+        return raw(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -520,7 +526,7 @@ def scale_cache_attend(attend: ScaleAttend, cache: ScaleCache, batch: ScaleBatch
     """Attention of the batch's rows over their sequences in the cache; lse fp32 [n_rows][H_q] or None."""
     qp, qs, _ = _rows(q, batch.n_rows, attend.num_q_heads)
     op, os_, _ = _rows(out, batch.n_rows, attend.num_q_heads)
-    if lse is not None and (lse.numel() < batch.n_rows * attend.num_q_heads or lse.itemsize != 4):
+    if lse is not None and (lse.numel() < batch.n_rows * attend.num_q_heads or lse.itemsize != 4 or not lse.is_floating_point()):
         raise ValueError("lse is fp32 [n_rows][num_q_heads]")
     _check("scale_cache_attend", load().scale_cache_attend(
         ctypes.byref(attend), ctypes.byref(cache), ctypes.byref(batch), qp, qs, op, os_, _ptr(lse), _ptr(ws),

@@ -198,3 +198,19 @@ def test_e4m3_reference_against_torch():
     assert got[1, 5] == 126 and got[2, 7] == 127 and e[0] == 27
     top = x.double().abs().nan_to_num(nan=0, posinf=0).amax(-1)
     assert bool((top <= 448 / scale[:, 0]).all()) and bool((top[1:] > 224 / scale[1:, 0]).all())
+
+
+def test_binding_refuses_other_types_of_the_same_size():
+    half = torch.zeros(3, 16, 2, 128, dtype=torch.float16)
+    codes, scales = torch.zeros(3, 16, 2, 128, dtype=torch.uint8), torch.zeros(3, 2, 16, dtype=torch.uint8)
+    assert S.kv_cache(*(codes.view(torch.float8_e4m3fn) for _ in range(2)), scales, scales).dtype == S.SCALE_CACHE_E4M3
+    for bad in (lambda: S.kv_cache(half, half), lambda: S._rows(half[0], 16), lambda: S._rows(half[0].view(torch.int16), 16),
+                lambda: S.kv_cache(*(codes.view(torch.float8_e5m2) for _ in range(2)), scales, scales),
+                lambda: S.kv_cache(*(codes.view(torch.int8) for _ in range(2)), scales, scales),
+                lambda: S.kv_cache(codes, codes, scales.view(torch.int8), scales)):
+        with pytest.raises(ValueError):
+            bad()
+    rows, ints = torch.zeros(2, 4, 128, dtype=torch.bfloat16), torch.zeros(8, dtype=torch.int32)
+    b = S.kv_batch(ints[:3], ints[:2], ints.view(2, 4), 2, 1)
+    with pytest.raises(ValueError):
+        S.scale_cache_attend(S.attend_params(num_q_heads=4), S.kv_cache(codes, codes, scales, scales), b, rows, rows.clone(), ints, ints)
