@@ -365,7 +365,7 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
                 const int64_t row = use.s.row0 + r / a.g;
                 const int h = use.j * a.g + r % a.g;
                 if (whole) {
-                    const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+                    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
                     auto* out = static_cast<__nv_bfloat16*>(a.out) + row * a.out_stride + h * kHeadDim;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -378,7 +378,7 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
                         }
                     }
                     if (a.lse && oct == 0)
-                        a.lse[row * a.Hq + h] = sum > 0.f ? (m[nt][e] + __log2f(sum)) * 0.6931471805599453f : -INFINITY;
+                        a.lse[row * a.Hq + h] = sum == 0.f ? -INFINITY : (m[nt][e] + __log2f(sum)) * 0.6931471805599453f;
                 } else {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {

@@ -327,7 +327,6 @@ struct ChunkShared {
     uint64_t q_ready;                    // Q is in its parts
     uint64_t raw_full[2], raw_empty[2];  // codes of V: landed; turned
     uint64_t v_full[2];                  // V is bf16
-    uint32_t q_top;                      // largest finite |q| of the CTA's rows, as bits
 };
 // 8-bit: per softmax warp, what the products with each key of its tile are multiplied by
 __host__ __device__ constexpr uint32_t off_scales(bool e4m3) { return off_shared(e4m3) + 256; }
@@ -467,7 +466,6 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
     }
     if (tid == 0) {
         abort_flag = 0;
-        sh.q_top = 0;
         mbar_init(&bars.q_full, 1);
         mbar_init(&sh.q_ready, 128);
         for (int i = 0; i < 2; ++i) {
@@ -747,9 +745,10 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 if (E4M3 && T > 0) {
                     next_scales = scales_of(place_of(0));
                     next_place = place_of(1);
-                    // Q to two e4m3 parts, Q = Q1 + Q2, by one power of two for all rows of the CTA that brings the
+                    // Q to two e4m3 parts, Q = Q1 + Q2, by one power of two for the warp's rows that brings their
                     // largest finite |q| to 2^7 .. 2^8. Q1 takes four of the eight significant bits, Q2 the rest;
-                    // what is below 2^-10, 2^-18 of the largest, is lost.
+                    // what is below 2^-10, 2^-18 of the largest, is lost. (One for each row would be a product more per
+                    // logit: the key's scale, which is the warp's, takes this one along.) Not finite becomes NaN.
                     ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.q_full, 0, a.timeout_ns, &abort_flag));
                     uint8_t* row = smem + kOffQ + qt * kTileBytes + r * 128;
                     uint4 w[16];  // dimensions 8 i .. 8 i + 7
@@ -768,9 +767,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                         }
                     }
                     top = __reduce_max_sync(0xFFFFFFFFu, top);
-                    if (lane == 0) atomicMax(&sh.q_top, top);
-                    named_barrier(2, 128 * jv.nq);
-                    const int e = f16_exponent(sh.q_top) + 7;
+                    const int e = f16_exponent(top) + 7;
                     const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
                     q_scale = a.a.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
 #pragma unroll
@@ -786,7 +783,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                                 const uint32_t h = f32_to_e4m3x2(x, y);
                                 const float2 back = f16x2_to_f32(e4m3x2_to_f16x2(h));
                                 hi[e4] |= h << (16 * k);
-                                lo[e4] |= f32_to_e4m3x2(x - back.x, y - back.y) << (16 * k);
+                                lo[e4] |= f32_to_e4m3x2(fmaf(x, 0.f, x - back.x), fmaf(y, 0.f, y - back.y)) << (16 * k);  // infinity * 0 = NaN
                             }
                         }
                         uint8_t* at = row + ((i ^ (r & 7)) << 4);

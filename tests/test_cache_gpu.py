@@ -551,3 +551,30 @@ def test_more_query_tiles_than_sms(n_sink, n_local, e4m3):
     """Between one query tile pair per SM and two: some whole, the last ones in pieces that fill up the SMs."""
     check_attend(Batch([64 * 7, 1, 300, 64 * 9], [3000, 777, 2900, 3100], hq=16, hkv=8, page=32, e4m3=e4m3), n_sink=n_sink,
                  n_local=n_local)
+
+
+# ---------------------------------------------------------------- queries of every kind
+
+
+@pytest.mark.parametrize("news,lens", [([1, 2], [300, 70]), ([100, 3], [500, 90])])
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_queries_that_are_not_finite(news, lens, e4m3):
+    """A head with NaN or infinity in its query gets NaN; the rows beside it are as if it held zeros."""
+    bt = Batch(news, lens, hq=8, hkv=2, page=16, e4m3=e4m3)
+    bt.q[1, 2, 5], bt.q[-1, 6, 127], bt.q[0, 1, 0] = math.nan, math.inf, -math.inf
+    out, lse = attend(bt)
+    bad = torch.zeros(bt.rows, 8, dtype=torch.bool, device="cuda")
+    bad[1, 2] = bad[-1, 6] = bad[0, 1] = True
+    assert out[bad].isnan().all() and lse[bad].isnan().all()
+    want, want_l, tol, tol_l = attend64(bt, torch.where(bad[..., None], 0.0, bt.q))
+    within(out[~bad], want[~bad], tol[~bad], "out")
+    within(lse[~bad].double(), want_l[~bad], tol_l[~bad], "lse")
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_queries_of_every_size(e4m3):
+    """Blocks of 32 (token, query head) rows whose queries are 2^18 apart, each as exact as alone."""
+    bt = Batch([100], [500], hq=8, hkv=2, page=16, e4m3=e4m3)
+    size = torch.tensor([-12.0, 6.0, -3.0, 0.0], device="cuda")[torch.arange(100, device="cuda") // 8 % 4]
+    bt.q *= torch.exp2(size)[:, None, None].bfloat16()
+    check_attend(bt)
