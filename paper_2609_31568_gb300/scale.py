@@ -299,13 +299,11 @@ def _rows(x, n_rows: int, heads: int | None = None) -> tuple:
     if x is None:
         return None, 0, 0
     shape, stride = x.shape, x.stride()
-    if len(shape) != 3 or shape[2] != 128 or shape[0] < n_rows or (heads is not None and shape[1] != heads):
-        raise ValueError(f"expected a row tensor [{n_rows}][{'heads' if heads is None else heads}][128], got {tuple(shape)}")
-    if x.dtype is not _imported_torch().bfloat16:
-        raise ValueError("row tensors are bf16")
-    if stride[2] != 1 or (shape[1] > 1 and stride[1] != 128):
-        raise ValueError("the heads of a row must be contiguous")
-    return x.data_ptr(), stride[0] if shape[0] > 1 else max(stride[0], shape[1] * 128), shape[1]
+    if (len(shape) == 3 and shape[2] == 128 and shape[0] >= n_rows and (heads is None or shape[1] == heads)
+            and x.dtype is _imported_torch().bfloat16 and stride[2] == 1 and (stride[1] == 128 or shape[1] == 1)):
+        return x.data_ptr(), stride[0] if shape[0] > 1 else max(stride[0], shape[1] * 128), shape[1]
+    raise ValueError(f"expected bf16 rows [{n_rows}][{'heads' if heads is None else heads}][128], the heads of a row "
+                     f"contiguous; got {x.dtype} {tuple(shape)} with strides {tuple(stride)}")
 
 
 def _nbytes(x) -> int:
