@@ -152,9 +152,13 @@ def key_counts(w, unit_start, n_units, sel, cnt, per_subchunk):
 
 def kernel_source_hash(path: str) -> str:
     """sha256[:16] of a CUDA source with its comments and blank lines removed:
-    a change to the code changes it, a change to a comment does not."""
+    a change to the code changes it, a change to a comment does not. The MMA
+    loop that it includes (attn_mma.cuh, beside it) counts as part of it."""
     with open(path) as f:
         txt = f.read()
+    for name in re.findall(r'#include "(attn_mma\.cuh)"', txt):
+        with open(os.path.join(os.path.dirname(path), name)) as f:
+            txt += f.read()
     txt = re.sub(r"/\*.*?\*/", "", txt, flags=re.S)
     txt = re.sub(r"//[^\n]*", "", txt)
     code = "\n".join(ln.rstrip() for ln in txt.splitlines() if ln.strip())

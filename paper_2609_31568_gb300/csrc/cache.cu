@@ -86,8 +86,8 @@ __device__ __forceinline__ float2 cos_sin_of_turn(uint64_t turn)
 // warp's lanes share the 64 angles of the row through shared memory; a frequency is kept as a 64-bit
 // fraction of a turn, so that position * frequency modulo 1 is one integer product.
 // Bound by HBM and, with an 8-bit cache, nearly as much by issue (1,700 instructions a row of 48 heads): 32,709 tokens
-// turned (536 MB) in 86 us, an 8,192-token chunk into an 8-bit cache (185 MB) in 36 us. Two CTAs per SM with three groups
-// in flight; three with fewer registers took 97 and 42 us.
+// turned (536 MB) in 86 us, an 8,192-token chunk into an 8-bit cache (185 MB) in 34 us. Two CTAs per SM with three groups
+// in flight; three with fewer registers took 97 us for the first, and a sixth longer for the second.
 template <int ORDER, int CACHE>
 __global__ void __launch_bounds__(kPlaceThreads, kPlaceCtas) k_place(const __grid_constant__ PlaceArgs a)
 {
@@ -275,13 +275,17 @@ __global__ void __launch_bounds__(kPlaceThreads, kPlaceCtas) k_place(const __gri
         }
     };
     // One step ahead: the loads of the next groups (of this task or the next) are in flight while a step's heads are
-    // worked on.
+    // worked on. Two steps unrolled, a buffer each, have two steps' loads in flight while a warp waits; the code for 8-bit rows
+    // is so long that it does not stay in the instruction cache then (54% of the next level's requests), and its
+    // loads are copied from one buffer to the other instead (8,192 tokens appended 34.3 and 38.3 us; turned rows, the other
+    // way, 87.7 and 85.6 us).
+    constexpr bool kCopy = CACHE == 2;
     open_task();
     if (task < tasks) load(0);
 #pragma unroll 1
     while (task < tasks) {
 #pragma unroll
-        for (int buf = 0; buf < 2; ++buf) {
+        for (int buf = 0; buf < (kCopy ? 1 : 2); ++buf) {
             if (task >= tasks) break;
             const int row0 = row, place0 = place, g0 = g, end0 = g1, p0 = pos[0], p1 = pos[1];
             const bool begins0 = begins;
@@ -294,6 +298,11 @@ __global__ void __launch_bounds__(kPlaceThreads, kPlaceCtas) k_place(const __gri
             }
             if (task < tasks) load(buf ^ 1);
             work(buf, row0, place0, g0, end0, begins0, p0, p1);
+#pragma unroll
+            for (int u = 0; kCopy && u < kInFlight; ++u) {
+                data[0][u][0] = data[1][u][0];
+                data[0][u][1] = data[1][u][1];
+            }
         }
     }
 }
