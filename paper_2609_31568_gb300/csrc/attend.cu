@@ -740,7 +740,10 @@ cudaError_t run_rows(const RowsArgs& r, int sms, cudaStream_t st)
     constexpr int kWarps = rows_warps(NT, E4M3);
     auto kern = k_rows<NT, E4M3>;
     const size_t smem = rows_ring_bytes(NT, E4M3) + (static_cast<size_t>(r.b.n_seqs) + 1) * sizeof(int64_t);
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    // the largest call's, whatever this one's: calls from several threads set the same
+    constexpr size_t kMost = rows_ring_bytes(NT, E4M3) + (kMaxSeqs + 1) * sizeof(int64_t);
+    static_assert(kMost <= 226 * 1024, "shared memory of a CTA");
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMost));
     if (e != cudaSuccess) return e;
     e = launch_after(st, dim3(sms), 32 * kWarps, smem, 1, kern, r);
     if (e != cudaSuccess) return e;
