@@ -18,10 +18,12 @@
 //    are fewer than the SMs keep busy, each cut along its keys, with (O, reference,
 //    sum) of the pieces merged by k_chunk_merge.
 // 32 query heads on 8, 4,096 tokens over 64K, bf16: 2,710 us, 1.58 PFLOP/s under the power limit, where k_sparse_attn is
-// too (2,535 us on a cool GPU). 8-bit: 3,535 us, bound by no one unit (tensor pipe half busy, issue 53%,
-// shared memory 30%): a tile's softmax takes the keys' scales from shared memory besides, and the four warps that
-// turn V share its issue slots. Few query tiles are bound by the plan (7 to 8 us), a CTA's start
-// and end (kPieceTiles tiles) and the unevenness of the last round.
+// too (2,535 us on a cool GPU). 8-bit: 3,535 us, bound by shared memory: a key tile takes 4,100 cycles (bf16 2,820), in
+// which the operands of the products are 1,540 reads of 128 bytes, the keys' scales 1,020 (four each for 32
+// lanes), the turning of V 380 and the copies 260; the MMA pipe has work all the time and is half busy. Scales
+// as 16-bit halves put together by a byte permutation are half the reads and 3,855 us: the softmax's chain is next.
+// Few query tiles are bound by the plan (7 to 8 us), a CTA's start and end (kPieceTiles tiles) and the
+// unevenness of the last wave.
 #include <cuda_bf16.h>
 
 #include "attend.cuh"
