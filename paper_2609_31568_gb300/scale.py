@@ -261,15 +261,15 @@ def load() -> ctypes.CDLL:
         return lib
 
 
-_torch = None  # the torch module, once a call has needed it
+_torch = _bf16 = None  # the torch module and its bf16 type, once a call has needed them
 
 
 def _imported_torch():
-    global _torch
+    global _torch, _bf16
     if _torch is None:
         import torch
 
-        _torch = torch
+        _torch, _bf16 = torch, torch.bfloat16
     return _torch
 
 
@@ -298,10 +298,14 @@ def _rows(x, n_rows: int, heads: int | None = None) -> tuple:
     lie apart; (None, 0, 0) for None."""
     if x is None:
         return None, 0, 0
+    if _bf16 is None:
+        _imported_torch()
     shape, stride = x.shape, x.stride()
-    if (len(shape) == 3 and shape[2] == 128 and shape[0] >= n_rows and (heads is None or shape[1] == heads)
-            and x.dtype is _imported_torch().bfloat16 and stride[2] == 1 and (stride[1] == 128 or shape[1] == 1)):
-        return x.data_ptr(), stride[0] if shape[0] > 1 else max(stride[0], shape[1] * 128), shape[1]
+    if len(shape) == 3:
+        (n, h, d), (across, along, step) = shape, stride
+        if (d == 128 and n >= n_rows and (heads is None or h == heads) and x.dtype is _bf16 and step == 1
+                and (along == 128 or h == 1)):
+            return x.data_ptr(), across if n > 1 else max(across, h * 128), h
     raise ValueError(f"expected bf16 rows [{n_rows}][{'heads' if heads is None else heads}][128], the heads of a row "
                      f"contiguous; got {x.dtype} {tuple(shape)} with strides {tuple(stride)}")
 
@@ -312,7 +316,7 @@ def _nbytes(x) -> int:
 
 def _stream(stream) -> int | None:
     if stream is None:
-        torch = _imported_torch()
+        torch = _torch or _imported_torch()
         # the handle alone, where this torch gives it: 0.3 us, against 3 us for a torch.cuda.Stream object
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         if raw is None:
