@@ -17,7 +17,7 @@ using namespace scale_ptx;
 constexpr int kStep = 16;          // keys of a step; a page holds whole steps
 constexpr int kMaxRowsWarps = 16;
 constexpr int kMaxParts = 2 * kMaxSms * kMaxRowsWarps;  // partial results
-constexpr int kMinSteps = 8;       // steps of a CTA before another one helps
+constexpr int kMinSteps = 8;       // steps of a CTA before another one helps (one token at 4K, 4 heads: 8.7 us, 9.5 with 4, 9.9 with 32)
 constexpr float kRaise = 8.0f;     // log2 units by which a logit may pass the reference
 
 // Warps of a CTA and stages of a warp's ring. 8-bit rows of few query rows take half the copies and 1.3 times the

@@ -319,15 +319,12 @@ cudaError_t run_place(PlaceArgs& a, cudaStream_t st)
     int sms = 0;
     cudaError_t e = device_sms(&sms);
     if (e != cudaSuccess) return e;
-    // Few rows: their heads are shared out, down to one group of four heads a warp; and as long as that leaves a warp
-    // less than kRounds tasks, in tasks of the groups that a warp has in flight, whose rounds end together.
-    constexpr int kRounds = 2;
+    // Few rows: their heads are shared out, down to one group of four heads a warp. (Rows cut further, so that a warp's rounds
+    // end together, gain 0.4 us at 1,500 rows of 36 heads and lose 0.8 at 1,000.)
     const int groups = (a.v.end + 3) / 4;
     const int64_t warps = static_cast<int64_t>(sms) * kPlaceWarps * kPlaceCtas;
     const int64_t share = warps / a.n_rows;
-    const int batches = (groups + kInFlight - 1) / kInFlight;
     a.parts = static_cast<int>(share > groups ? groups : share > 1 ? share : 1);
-    if (a.parts < batches && static_cast<int64_t>(a.n_rows) * batches < warps * kRounds) a.parts = batches;
     const int64_t ctas = (static_cast<int64_t>(a.n_rows) * a.parts + kPlaceWarps - 1) / kPlaceWarps;
     const int64_t most = static_cast<int64_t>(sms) * kPlaceCtas;
     return launch_after(st, dim3(static_cast<unsigned>(ctas < most ? ctas : most)), kPlaceThreads, 0, 1, k_place<ORDER, CACHE>, a);
