@@ -425,7 +425,7 @@ int scale_cache_read(const scale_cache_t *cache, const scale_batch_t *batch, voi
  * the rows that see it not finite, and may make so rows of the same call up to
  * 256 tokens before it. A query that is not finite makes its row and head NaN. Beside
  * 8-bit keys a query is rounded to 2^-18 of the largest |q| of its row, or, in calls with
- * more than 16 (row, head of a KV head) pairs to a sequence, of 32 neighbouring pairs.
+ * more than 24 (row, head of a KV head) pairs to a sequence, of 32 neighbouring pairs.
  *   q, out bf16 [n_rows][num_q_heads][128];  lse fp32 [n_rows][num_q_heads] or NULL
  *   ws     scale_cache_attend_workspace_size() bytes, initialised once with
  *          scale_workspace_init(); a device problem is recorded in its status word.

@@ -133,7 +133,7 @@ struct Item {
     Steps x;
 };
 
-// Attention of sequences with at most kRowsMax rows (new tokens times query heads of a KV head).
+// Attention of sequences with at most rows_max rows (new tokens times query heads of a KV head).
 //
 // The work is one list of 16-key steps, sequence by sequence and KV head by KV head, cut into equal runs, one
 // per warp, whatever the lengths: a warp walks its run with a ring of its own in shared memory, so nothing in
@@ -160,6 +160,7 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
     constexpr int kRow = E4M3 ? kHeadDim : 2 * kHeadDim;  // bytes of a held row
     constexpr int kTile = kStep * kRow;
     constexpr int kChunks = kRow / 16;
+    static_assert(NT * 8 * (kHeadDim * 4 + 8) <= rows_warp_bytes(NT, E4M3), "a run's last piece lies in its ring");
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ int64_t s_sum[kWarps];  // then the item that a warp's run ends in
     const AttendView& a = args.a;
@@ -755,7 +756,7 @@ struct AttendWs {
     int part_rows;
 };
 
-AttendWs attend_layout(int Hq, int Hkv, int n_seqs, int n_rows, int max_rows)
+AttendWs attend_layout(int Hq, int Hkv, bool e4m3, int n_seqs, int n_rows, int max_rows)
 {
     AttendWs w{};
     size_t off = 256;
@@ -765,8 +766,8 @@ AttendWs attend_layout(int Hq, int Hkv, int n_seqs, int n_rows, int max_rows)
         return at;
     };
     const int64_t rows = static_cast<int64_t>(max_rows) * (Hq / Hkv);
-    w.part_rows = rows <= 8 ? 8 : kRowsMax;
-    if (rows > kRowsMax) {
+    w.part_rows = static_cast<int>((rows + 7) / 8 * 8);
+    if (rows > rows_max(e4m3)) {
         w.chunks = take(chunk_ws_bytes(Hq / Hkv, Hkv, n_seqs, n_rows, max_rows));
     } else {
         w.before = take((static_cast<size_t>(n_seqs) + 1) * sizeof(int64_t));
@@ -795,9 +796,9 @@ cudaError_t run_rows(const RowsArgs& r, int sms, cudaStream_t st)
 
 }  // namespace
 
-size_t attend_ws_bytes(int Hq, int Hkv, int n_seqs, int n_rows, int max_rows)
+size_t attend_ws_bytes(int Hq, int Hkv, bool e4m3, int n_seqs, int n_rows, int max_rows)
 {
-    return attend_layout(Hq, Hkv, n_seqs, n_rows, max_rows).end;
+    return attend_layout(Hq, Hkv, e4m3, n_seqs, n_rows, max_rows).end;
 }
 
 cudaError_t launch_attend(const AttendView& a, const CacheView& c, bool e4m3, const BatchView& b, uint8_t* ws,
@@ -807,9 +808,9 @@ cudaError_t launch_attend(const AttendView& a, const CacheView& c, bool e4m3, co
     cudaError_t e = device_sms(&sms);
     if (e != cudaSuccess) return e;
     sms = sms < kMaxSms ? sms : kMaxSms;
-    const AttendWs lay = attend_layout(a.Hq, c.Hkv, b.n_seqs, b.n_rows, b.max_rows);
+    const AttendWs lay = attend_layout(a.Hq, c.Hkv, e4m3, b.n_seqs, b.n_rows, b.max_rows);
     const int64_t rows = static_cast<int64_t>(b.max_rows) * a.g;
-    if (rows > kRowsMax) {
+    if (rows > rows_max(e4m3)) {
         // Batches with longer pieces go there whole, and no second route follows: a sequence of few rows takes its share of
         // that kernel's jobs, at the pace of its keys (17 tokens at 128K, 537 MB of bf16: 103 us, 5.2 TB/s).
         return launch_chunks(a, c, e4m3, b, sms, reinterpret_cast<int32_t*>(ws + kStatusOffset), ws + lay.chunks, timeout_ns, st);
@@ -817,7 +818,8 @@ cudaError_t launch_attend(const AttendView& a, const CacheView& c, bool e4m3, co
     const RowsArgs r{a, c, b, reinterpret_cast<int64_t*>(ws + lay.before), reinterpret_cast<float*>(ws + lay.part_o),
                      reinterpret_cast<float2*>(ws + lay.part_ml), lay.part_rows};
     if (rows <= 8) return e4m3 ? run_rows<1, true>(r, sms, st) : run_rows<1, false>(r, sms, st);
-    return e4m3 ? run_rows<2, true>(r, sms, st) : run_rows<2, false>(r, sms, st);
+    if (rows <= 16) return e4m3 ? run_rows<2, true>(r, sms, st) : run_rows<2, false>(r, sms, st);
+    return run_rows<3, true>(r, sms, st);
 }
 
 }  // namespace scale

@@ -6,10 +6,11 @@
 
 namespace scale {
 
-// (token, query head) rows of a KV head up to which a call's sequences go to k_rows, whose registers hold no more. 16 sequences
-// of 4 tokens at 8,192, 32 query heads on 8: 96 us there and 102 by the tensor cores' route, 8-bit 72 and 128; one of 2
-// tokens at 4,096 12 and 23, 14 and 26.
-constexpr int kRowsMax = 16;
+// (token, query head) rows of a KV head up to which a call's sequences go to k_rows, whose registers hold no more. 32 query
+// heads on 8: one sequence of 2 tokens at 4,096 12 us there and 23 by the tensor cores' route, 16 of 4 at 8,192 96
+// and 102. 8-bit: 14 and 26, 72 and 128; 24 rows, 16 of 6 at 8,192 86 and 129, one of 6 at 4,096 25 and 24; 32 rows,
+// which spill, 124 and 130, 34 and 25.
+__host__ __device__ constexpr int rows_max(bool e4m3) { return e4m3 ? 24 : 16; }
 constexpr int kMaxSms = 160;  // SMs that a call uses at most
 
 // Rows and keys of sequence b. Its computed rows are [row0, row0 + rows), tokens
@@ -41,7 +42,7 @@ __device__ __forceinline__ int f16_exponent(uint32_t top)
     return e < -100 ? -100 : e;
 }
 
-// Calls whose sequences may have more than kRowsMax rows per KV head: tcgen05, 128 rows at a time.
+// Calls whose sequences may have more than rows_max rows per KV head: tcgen05, 128 rows at a time.
 size_t chunk_ws_bytes(int g, int Hkv, int n_seqs, int n_rows, int max_rows);
 cudaError_t launch_chunks(const AttendView& a, const CacheView& c, bool e4m3, const BatchView& b, int sms,
                           int32_t* status, uint8_t* ws, uint64_t timeout_ns, cudaStream_t st);

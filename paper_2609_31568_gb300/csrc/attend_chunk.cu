@@ -1,6 +1,6 @@
 // attend_chunk.cu -- attention of many new tokens of a sequence over its paged
 // cache, on the tensor cores (scale_cache_attend's route for calls whose sequences
-// may have more than kRowsMax rows per KV head).
+// may have more than rows_max rows per KV head).
 //
 // A query tile is 128 rows (token, query head) of one KV head: 128 / g tokens with
 // the g query heads that share its keys, which one TMA box of g heads lays down in

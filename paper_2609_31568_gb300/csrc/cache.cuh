@@ -119,7 +119,7 @@ struct AttendView {
     int64_t out_stride;
     float* lse;
 };
-size_t attend_ws_bytes(int Hq, int Hkv, int n_seqs, int n_rows, int max_rows);
+size_t attend_ws_bytes(int Hq, int Hkv, bool e4m3, int n_seqs, int n_rows, int max_rows);
 cudaError_t launch_attend(const AttendView& a, const CacheView& c, bool e4m3, const BatchView& b, uint8_t* ws,
                           uint64_t timeout_ns, cudaStream_t st);
 

@@ -234,7 +234,7 @@ int scale_cache_attend_workspace_size(const scale_attend_t* attend, const scale_
     if ((rc = check_batch(batch, &b))) return rc;
     if ((rc = check_attend(attend, c, b))) return rc;
     if (!bytes) return SCALE_ERR_INVALID_ARG;
-    *bytes = attend_ws_bytes(attend->num_q_heads, c.Hkv, b.n_seqs, b.n_rows, b.max_rows);
+    *bytes = attend_ws_bytes(attend->num_q_heads, c.Hkv, e4m3, b.n_seqs, b.n_rows, b.max_rows);
     return SCALE_OK;
 }
 
@@ -261,7 +261,7 @@ int scale_cache_attend(const scale_attend_t* attend, const scale_cache_t* cache,
     if (lse) p.need(lse, 4);
     p.need(ws, 256);
     if (!p.ok) return SCALE_ERR_INVALID_ARG;
-    if (ws_bytes < attend_ws_bytes(Hq, c.Hkv, b.n_seqs, b.n_rows, b.max_rows)) return SCALE_ERR_WORKSPACE;
+    if (ws_bytes < attend_ws_bytes(Hq, c.Hkv, e4m3, b.n_seqs, b.n_rows, b.max_rows)) return SCALE_ERR_WORKSPACE;
     if (b.max_rows == 0) return SCALE_OK;
     const float scale = attend->attn_scale > 0.f ? attend->attn_scale : 1.0f / std::sqrt(static_cast<float>(kHeadDim));
     const AttendView a{Hq, Hq / c.Hkv, attend->n_sink, attend->n_local, scale * 1.4426950408889634f,

@@ -674,3 +674,12 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     for (bt, ws, outs), (out, _) in zip(work, want):
         assert S.scale_get_device_status(ws) == S.SCALE_OK and all(same_bits(x, out) for x in outs)
+
+
+@pytest.mark.parametrize("hq,hkv,new", [(17, 1, 1), (8, 1, 3), (24, 4, 4), (32, 8, 6), (32, 8, 5), (25, 1, 1)])
+@pytest.mark.parametrize("n_sink,n_local", [(0, -1), (20, 90)])
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_around_the_rows_of_one_route(hq, hkv, new, n_sink, n_local, e4m3):
+    """17 to 25 (token, query head) rows of a KV head: the last that the route of few rows takes, and the first that it leaves."""
+    check_attend(Batch([new, 1, new], [700, 33, new], hq=hq, hkv=hkv, page=16, e4m3=e4m3, n_rows=2 * new + 3), n_sink=n_sink,
+                 n_local=n_local)
