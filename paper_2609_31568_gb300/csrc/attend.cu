@@ -747,6 +747,7 @@ __global__ void __launch_bounds__(256) k_rows_merge(const __grid_constant__ Rows
                 if (a.lse && lane == 0) a.lse[row * a.Hq + h] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * 0.6931471805599453f;
             }
         }
+        if (!real) __syncthreads();  // the dry pass has read what the next one writes
     }
 }
 
