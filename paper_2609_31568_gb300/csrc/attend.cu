@@ -615,16 +615,19 @@ __global__ void __launch_bounds__(256) k_rows_merge(const __grid_constant__ Rows
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     // Steps of the sequences before this one, its own and all, from the batch's lists while k_rows still runs: every CTA of
     // k_rows is past its own wait when this kernel starts, so what wrote the lists is complete, and k_rows writes
-    // none. (One token at 4K 9.5 -> 9.0 us, at 128K 62.1 -> 61.4.) More sequences than threads: what k_rows left, after
-    // the wait, and as long.
+    // none; the loads are ld_relaxed, which see it. (One token at 4K 9.5 -> 9.0 us, at 128K 62.1 -> 61.4.) More sequences
+    // than threads: what k_rows left, after the wait, and as long.
     int64_t first = 0, n, total = 0;
-    const Seq s = seq_of(a, args.b, b);
+    auto read_seq = [&](int i) {
+        return seq_of(a, args.b, ld_relaxed(args.b.row_start + i), ld_relaxed(args.b.row_start + i + 1), ld_relaxed(args.b.kv_len + i));
+    };
+    const Seq s = read_seq(b);
     const bool early = args.b.n_seqs <= 256;
     if (early) {
         const int i = threadIdx.x;
         int64_t mine = 0;
         if (i < args.b.n_seqs) {
-            const Seq x = seq_of(a, args.b, i);
+            const Seq x = read_seq(i);
             mine = x.rows > 0 ? steps_of(a, x).n : 0;
         }
         int64_t lower = i < b ? mine : 0;

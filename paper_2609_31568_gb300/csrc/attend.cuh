@@ -20,18 +20,21 @@ struct Seq {
     int pos0, lo;
 };
 
-__device__ __forceinline__ Seq seq_of(const AttendView& a, const BatchView& b, int i)
+__device__ __forceinline__ Seq seq_of(const AttendView& a, const BatchView& b, int row0, int end, int len)
 {
     Seq s;
-    s.row0 = b.row_start[i];
-    const int end = b.row_start[i + 1];
+    s.row0 = row0;
     const int n = s.row0 < 0 || end <= s.row0 ? 0 : end - s.row0;
     s.rows = n < b.max_rows ? n : b.max_rows;
     if (s.rows > b.n_rows - s.row0) s.rows = b.n_rows - s.row0 > 0 ? b.n_rows - s.row0 : 0;
-    const int len = b.kv_len[i];
     s.pos0 = (len > 0 ? len : 0) - n;
     s.lo = a.n_local >= 0 && s.pos0 > a.n_local ? s.pos0 - a.n_local : 0;
     return s;
+}
+
+__device__ __forceinline__ Seq seq_of(const AttendView& a, const BatchView& b, int i)
+{
+    return seq_of(a, b, b.row_start[i], b.row_start[i + 1], b.kv_len[i]);
 }
 
 // Exponent of the power of two that brings values of at most `top` (fp32 bits, finite) below 2^15, inside f16;

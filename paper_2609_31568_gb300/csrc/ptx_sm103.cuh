@@ -150,9 +150,9 @@ __device__ __forceinline__ void named_barrier(uint32_t id, uint32_t count)
 
 // A kernel launched by launch_after() may start while the kernel before it on
 // the stream still runs: pdl_wait() returns once that one has completed and its
-// writes are visible. Every thread calls it before any access to global memory,
-// and no thread returns before it, so a kernel never completes before those
-// ahead of it.
+// writes are visible. Every thread calls it before any access to global memory (but
+// those of ld_relaxed), and no thread returns before it, so a kernel never completes
+// before those ahead of it.
 __device__ __forceinline__ void pdl_wait()
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -170,6 +170,16 @@ __device__ __forceinline__ void pdl_enter()
 {
     pdl_wait();
     pdl_trigger();
+}
+
+// A load ahead of pdl_wait(), of what no kernel in flight writes: where the kernel ahead has passed its own wait in
+// every CTA, what the kernels before that one wrote is complete. A relaxed load at device scope takes it from L2, where
+// they left it; a weak one might take a line that the SM's first-level cache held before.
+__device__ __forceinline__ int32_t ld_relaxed(const int32_t* p)
+{
+    int32_t r;
+    asm volatile("ld.relaxed.gpu.global.s32 %0, [%1];" : "=r"(r) : "l"(p) : "memory");
+    return r;
 }
 
 // ------------------------------------------------------------------ clusters
