@@ -146,8 +146,11 @@ struct Item {
 //
 // 8-bit rows stay codes up to the registers and become f16 there (exact, one conversion per two values);
 // a key's scale multiplies its logit, a value's scale 2^e moves into the exponent, w' = 2^(s + e - m), and the sum
-// takes w' 2^-e. Q is brought to f16 by a power of two per row. P is rounded to bf16 beside bf16 values, to
-// f16 (11 bits) beside codes.
+// takes w' 2^-e. Q is brought to f16 by a power of two per row.
+//
+// P is two bf16 parts (16 bits) beside bf16 values and f16 (11 bits) beside codes. The second product costs nothing that
+// was measured, since the tensor pipe stood at 8 %: 48 tokens of 130 to 30,000, 16 of 4 tokens at 8,192 (16 rows) and one at
+// 4K take as long with it as with one part of 8 bits.
 //
 // Keys that no row sees are not read: their places are filled with zeros, so nothing that lies there
 // reaches a sum. Bound by HBM: K and V once. With 32 query heads on 8 and 28 on 4: one token at 128K, 8-bit (272 MB), 60 us
@@ -508,8 +511,8 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
                     }
                 }
         }
-        // ---- weights, and P^T
-        uint32_t pf[NT][2];
+        // ---- weights, and P^T; beside bf16 values in two parts, of which the second is what the first leaves of a weight
+        uint32_t pf[NT][2], pf2[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             float w[4];
@@ -523,8 +526,12 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
                 }
             }
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
-                pf[nt][x] = transpose8x8(E4M3 ? pack_f16x2(w[2 * x], w[2 * x + 1]) : pack_bf16x2(w[2 * x], w[2 * x + 1]));
+            for (int x = 0; x < 2; ++x) {
+                const uint32_t p = E4M3 ? pack_f16x2(w[2 * x], w[2 * x + 1]) : pack_bf16x2(w[2 * x], w[2 * x + 1]);
+                pf[nt][x] = transpose8x8(p);
+                if (!E4M3)
+                    pf2[nt][x] = transpose8x8(pack_bf16x2(w[2 * x] - __uint_as_float(p << 16), w[2 * x + 1] - __uint_as_float(p & 0xFFFF0000u)));
+            }
         }
         // ---- O^T += V^T P^T
         if (E4M3) {
@@ -549,7 +556,10 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
                 const int row = (lane & 7) + (lane >> 4) * 8, ch = 2 * h + ((lane >> 3) & 1);
                 ldsm4_t(r, vt + row * kRow + ((ch ^ (row & 7)) << 4));
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma16816<false>(o[h][nt], r, pf[nt][0], pf[nt][1]);
+                for (int nt = 0; nt < NT; ++nt) {
+                    mma16816<false>(o[h][nt], r, pf[nt][0], pf[nt][1]);
+                    mma16816<false>(o[h][nt], r, pf2[nt][0], pf2[nt][1]);
+                }
             }
         }
         stage = stage + 1 == kStages ? 0 : stage + 1;
