@@ -424,11 +424,10 @@ int scale_cache_read(const scale_cache_t *cache, const scale_batch_t *batch, voi
  * a sequence's call sees may hold anything. A value row that is not finite makes
  * the rows that see it not finite, and may make so rows of the same call up to
  * 256 tokens before it. A query that is not finite makes its row and head NaN. Beside
- * 8-bit keys a query is rounded to 2^-18 of the largest |q| of its row, or, in calls with
- * more than 24 (row, head of a KV head) pairs to a sequence, of 32 neighbouring pairs.
+ * 8-bit keys a query is rounded to 2^-12 of the largest |q| of its row and head or less.
  * Logits, softmax statistics and sums are fp32. A weight is rounded before it multiplies its value row: to 16
- * bits beside bf16 values and 11 (f16) beside 8-bit ones in calls with at most 16 (8-bit: 24) such pairs to a
- * sequence (max_rows of them per KV head), to bf16 in others.
+ * bits beside bf16 values and 11 (f16) beside 8-bit ones in calls with at most 16 (8-bit: 24) pairs of a row
+ * and a query head of one KV head to a sequence (by max_rows), to bf16 in others.
  *   q, out bf16 [n_rows][num_q_heads][128];  lse fp32 [n_rows][num_q_heads] or NULL
  *   ws     scale_cache_attend_workspace_size() bytes, initialised once with
  *          scale_workspace_init(); a device problem is recorded in its status word.

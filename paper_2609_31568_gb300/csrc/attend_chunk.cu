@@ -44,6 +44,7 @@ constexpr int kTails = 3, kTailCuts = 4;   // and the last half, quarter or eigh
 constexpr int kCandidates = kUniform + kTails * kTailCuts;
 static_assert(kCandidates <= 32, "a lane for each");
 constexpr int kPieceTiles = 5;        // what a CTA's start and end take, in key tiles
+constexpr int kRowsApart = 5;         // 8-bit: log2 of the sizes of queries that share a power of two
 constexpr int kMergeTiles = 4;        // what writing and merging one piece per SM takes
 
 // A CTA's work. Rows [row0, row0 + ntok) of the row tensors are tokens pos ..; key tiles
@@ -707,15 +708,16 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
         float m_run = -INFINITY, l_run = 0.f;
         bool ok = true;
         // What the loop keeps of the job: its key tiles from k0 on, those from `sinks` on `past` further; the row's token p,
-        // the tile's first, and the first token from which the window hides nothing of the tile; the CTA's last token
-        int T = 0, k0 = 0, sinks = 0, past = 0, p = 0, pos_first = 0, open_from = 0, last = 0;
+        // the tile's first, which is also the last that all of the tile's rows see (8-bit: or -1, to mask every tile), and the
+        // first from which the window hides nothing of the tile; the CTA's last token
+        int T = 0, k0 = 0, sinks = 0, past = 0, p = 0, pos_first = 0, plain_to = 0, open_from = 0, last = 0;
         int seq = 0, kvh = 0;
         auto token_of = [&](int t) { return (k0 + t < sinks ? k0 + t : k0 + t + past) * kTile; };
         // 8-bit: lane x looks up the scales of the keys 4 x .. 4 x + 3 of a tile, its page two tiles ahead, the bytes one
         // ahead. (A warp that did it for both query tiles came late: 600 cycles a tile.)
         int next_place = -1;
         uint32_t next_scales = 0x7F7F7F7Fu;
-        float q_scale = 0.f;
+        float q_scale = 0.f, row_scale = 1.f;  // of the warp's logits, beside its keys' scales; of this row's besides
         auto place_of = [&](int t) { return t < T ? cache_row(a.c, a.b, seq, token_of(t) + 4 * lane) : -1; };
         auto scales_of = [&](int place) -> uint32_t {
             if (place < 0) return 0x7F7F7F7Fu;
@@ -742,7 +744,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 seq = jv.job.b;
                 kvh = jv.job.j;
                 last = jv.last;
-                pos_first = jv.job.pos + qt * tt;
+                pos_first = plain_to = jv.job.pos + qt * tt;
                 const int pos_last = qt + 1 == jv.nq ? jv.last : pos_first + tt - 1;
                 p = pos_first + r / g;
                 p = p < pos_last ? p : pos_last;  // rows past the tile's end see what its last row sees
@@ -752,10 +754,11 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 if (E4M3 && T > 0) {
                     next_scales = scales_of(place_of(0));
                     next_place = place_of(1);
-                    // Q to two e4m3 parts, Q = Q1 + Q2, by one power of two for the warp's rows that brings their
-                    // largest finite |q| to 2^7 .. 2^8. Q1 takes four of the eight significant bits, Q2 the rest;
-                    // what is below 2^-10, 2^-18 of the largest, is lost. (One for each row would be a product more per
-                    // logit: the key's scale, which is the warp's, takes this one along.) Not finite becomes NaN.
+                    // Q to two e4m3 parts, Q = Q1 + Q2, by a power of two that brings the largest finite |q| to 2^7 .. 2^8. Q1
+                    // takes four of the eight significant bits, Q2 the rest; half of Q2's least step, 2^-10 or 2^-17 of the
+                    // largest, is lost at most. The power is one for the warp's rows, which the keys' scales (the warp's)
+                    // take along, unless a row is more than 2^kRowsApart below the largest: then each row has its own, and all
+                    // tiles take the slow path, which multiplies its logits by it. Not finite becomes NaN.
                     ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.q_full, 0, a.timeout_ns, &abort_flag));
                     uint8_t* row = smem + kOffQ + qt * kTileBytes + r * 128;
                     uint4 w[16];  // dimensions 8 i .. 8 i + 7
@@ -773,10 +776,14 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                             }
                         }
                     }
-                    top = __reduce_max_sync(0xFFFFFFFFu, top);
-                    const int e = f16_exponent(top) + 7;
+                    const int e_row = f16_exponent(top) + 7, e_warp = f16_exponent(__reduce_max_sync(0xFFFFFFFFu, top)) + 7;
+                    const bool rows_apart = __any_sync(0xFFFFFFFFu, top != 0 && e_row < e_warp - kRowsApart);
+                    const int e = rows_apart ? e_row : e_warp;
                     const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-                    q_scale = a.a.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+                    const float up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+                    row_scale = rows_apart ? up : 1.f;
+                    if (rows_apart) plain_to = -1;
+                    q_scale = rows_apart ? a.a.scale_log2 : a.a.scale_log2 * up;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {  // 16 dimensions: one 16-byte piece of each part
                         const uint32_t v[8] = {w[2 * i].x, w[2 * i].y, w[2 * i].z, w[2 * i].w, w[2 * i + 1].x, w[2 * i + 1].y, w[2 * i + 1].z, w[2 * i + 1].w};
@@ -817,7 +824,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
             }
             tc_fence_after();
             const int t0 = token_of(t);
-            const bool masked = t < 0 || t0 + kTile - 1 > pos_first || (t0 < open_from && t0 + kTile - 1 >= a.a.n_sink);
+            const bool masked = t < 0 || t0 + kTile - 1 > plain_to || (t0 < open_from && t0 + kTile - 1 >= a.a.n_sink);
             const int lim = p - t0 + 1;  // keys t0 + c with c >= lim are in the future
             const int gap = a.a.n_sink - t0, low = a.a.n_local >= 0 && p - t0 > a.a.n_local ? p - t0 - a.a.n_local : 0;
             // Fast: exponentials against the reference as it stands, all of the row at once, unless something is hidden or
@@ -847,8 +854,10 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                     const uint32_t seen = masked ? ones_below(lim - 32 * c) & ~(ones_below(low - 32 * c) & ~ones_below(gap - 32 * c)) : 0xFFFFFFFFu;
                     tmem_ld_wait();
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
+                    for (int i = 0; i < 32; ++i) {
+                        if (E4M3) sr[i] = __float_as_uint(__uint_as_float(sr[i]) * row_scale);
                         if (!((seen >> i) & 1u)) sr[i] = 0xFF800000u;
+                    }
                 };
                 float mx = -INFINITY;
 #pragma unroll 1

@@ -7,9 +7,9 @@ import pytest
 import torch
 
 import paper_2609_31568_gb300 as pkg
-from _cache import Batch
+from _cache import Batch, attend64
 from paper_2609_31568_gb300 import scale as S
-from test_cache_gpu import attend, within
+from test_cache_gpu import attend, check_attend, within
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +52,60 @@ def test_weights_beside_bf16_values(hq, hkv, news, most):
         # the output in bf16; the weights (and their sum) off by `off`, their products by 2^-16, n sums in fp32
         tol = 2.0 ** -8 * want.abs() + (2.0 ** -16 + 2 * off[..., None] + 2 * n * 2.0 ** -24) * size
         within(out[news * b: news * (b + 1)], want, tol, f"{n} keys")
+
+
+def own_logits(q, k, k_values, hq, rows):
+    """lse of rows that see their own key only, which is its logit: (attend's, fp64, A = sum |q_i k_i| scale)."""
+    bt = Batch([rows], [rows], hq=hq, hkv=1, page=16, e4m3=True)
+    bt.q[:] = q
+    bt.values[0][0] = bt._put(0, 0, k)
+    assert torch.equal(bt.values[0][0], k_values)
+    _, lse = attend(bt, n_sink=0, n_local=0)
+    x, y = bt.q.double(), k_values.repeat_interleave(hq, 1)
+    return lse.double(), (x * y).sum(-1) / math.sqrt(128), (x * y).abs().sum(-1) / math.sqrt(128)
+
+
+@pytest.mark.parametrize("hq,rows", [(1, 100), (4, 33), (8, 60), (7, 41), (8, 2), (24, 1)])
+@pytest.mark.parametrize("apart", [0, 1, 40])
+def test_queries_beside_8bit_keys_keep_their_bits(hq, rows, apart):
+    """A query is off by at most 2^-12 of the largest |q| of its own row, whatever the rows beside it (2^-17 where all
+    of a warp's rows are of one size): keys that are zero where the row is largest show the rest of it."""
+    gen = torch.Generator(device="cuda").manual_seed(hq + rows + apart)
+    rand = lambda *n: torch.rand(*n, generator=gen, device="cuda")  # noqa: E731
+    # the others from 2^-6 to 2^-22 of the largest, which is just above a power of two
+    q = torch.exp2(-6 - 16 * rand(rows, hq, 128)) * torch.sign(rand(rows, hq, 128) - 0.5)
+    q[..., 5] = 1 + 2.0 ** -7
+    q = (q * torch.exp2((apart * (rand(rows, hq, 1) - 0.5)).round())).bfloat16()
+    k = torch.where(rand(rows, 1, 128) < 0.5, -1.0, 1.0).double()
+    k[..., 5] = 0
+    got, want, size = own_logits(q, k * 256, k * 256, hq, rows)
+    top = q.double().abs().amax(-1)
+    lost = 2.0 ** (-17 if apart == 0 else -12) * top * 127 * 256 / math.sqrt(128)
+    # and 2^-20, however small the logit: beside few rows the exponent of its value, 16 at most here, joins it in fp32 and
+    # leaves it again (two roundings of half a step of 2^-20, times ln 2), and the sum's log2 is off by 2^-22
+    within(got, want, lost + 2 * 128 * 2.0 ** -24 * size + 2.0 ** -21 * want.abs() + 2.0 ** -20)
+
+
+@pytest.mark.parametrize("hq,hkv", [(8, 2), (7, 1), (32, 1)])
+@pytest.mark.parametrize("sizes", [(-3.0, 0.0, 3.0, 4.0), (-12.0, 6.0, -3.0, 0.0), (0.0, 9.0, 11.0, 1.0)])
+def test_neighbours_of_other_sizes(hq, hkv, sizes):
+    """Rows of sizes up to 2^18 apart side by side, each as exact as alone."""
+    bt = Batch([100, 30], [500, 90], hq=hq, hkv=hkv, page=16, e4m3=True)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    size = torch.tensor(sizes, device="cuda")[torch.randint(0, 4, (bt.rows, hq), generator=gen, device="cuda")]
+    bt.q *= torch.exp2(size)[..., None].bfloat16()
+    check_attend(bt)
+
+
+@pytest.mark.parametrize("zero", [0.0, math.nan, math.inf])
+def test_neighbours_that_are_zero_or_not_finite(zero):
+    """They count for nothing in the size of the rows beside them."""
+    bt = Batch([100], [300], hq=8, hkv=2, page=16, e4m3=True)
+    bt.q[::3, ::2] = zero
+    bad = torch.zeros(bt.rows, 8, dtype=torch.bool, device="cuda")
+    bad[::3, ::2] = zero != 0.0
+    out, lse = attend(bt)
+    assert out[bad].isnan().all() and lse[bad].isnan().all()
+    want, want_l, tol, tol_l = attend64(bt, torch.where(bad[..., None], 0.0, bt.q))
+    within(out[~bad], want[~bad], tol[~bad], "out")
+    within(lse[~bad].double(), want_l[~bad], tol_l[~bad], "lse")
