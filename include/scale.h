@@ -426,7 +426,8 @@ int scale_cache_read(const scale_cache_t *cache, const scale_batch_t *batch, voi
  * 256 tokens before it. A query that is not finite makes its row and head NaN. Beside
  * 8-bit keys a query is rounded to 2^-12 of the largest |q| of its row and head or less.
  * Logits, softmax statistics and sums are fp32. A weight is rounded before it multiplies its value row: to 16
- * bits beside bf16 values and 11 (f16) beside 8-bit ones in calls with at most 16 (8-bit: 24) pairs of a row
+ * bits beside bf16 values and 11 (f16) beside 8-bit ones (weights times value scales below 2^-20 of a row's largest to
+ * 2^-31 of it) in calls with at most 16 (8-bit: 24) pairs of a row
  * and a query head of one KV head to a sequence (by max_rows), to bf16 in others.
  *   q, out bf16 [n_rows][num_q_heads][128];  lse fp32 [n_rows][num_q_heads] or NULL
  *   ws     scale_cache_attend_workspace_size() bytes, initialised once with

@@ -19,6 +19,7 @@ constexpr int kMaxRowsWarps = 16;
 constexpr int kMaxParts = 2 * kMaxSms * kMaxRowsWarps;  // partial results
 constexpr int kMinSteps = 8;       // steps of a CTA before another one helps (one token at 4K, 4 heads: 8.7 us, 9.5 with 4, 9.9 with 32)
 constexpr float kRaise = 8.0f;     // log2 units by which a logit may pass the reference
+constexpr float kLift = 6.0f;      // 8-bit: log2 units that a new reference lies below the largest logit
 
 // Warps of a CTA and stages of a warp's ring. 8-bit rows of few query rows take half the copies and 1.3 times the
 // instructions per byte: sixteen warps hide what eight with twice the stages left open (128K tokens 64 us).
@@ -148,7 +149,9 @@ struct Item {
 // a key's scale multiplies its logit, a value's scale 2^e moves into the exponent, w' = 2^(s + e - m), and the sum
 // takes w' 2^-e. Q is brought to f16 by a power of two per row.
 //
-// P is two bf16 parts (16 bits) beside bf16 values and f16 (11 bits) beside codes. The second product costs nothing that
+// P is two bf16 parts (16 bits) beside bf16 values and f16 (11 bits) beside codes, where the reference is set kLift below
+// the largest logit: f16 keeps its 11 bits down to 2^-14, so weights do down to 2^-20 of a run's largest, and to 2^-31 of it
+// beyond. (w' stays below 2^kRaise either way.) The second product costs nothing that
 // was measured, since the tensor pipe stood at 8 %: 48 tokens of 130 to 30,000, 16 of 4 tokens at 8,192 (16 rows) and one at
 // 4K take as long with it as with one part of 8 bits.
 //
@@ -500,7 +503,7 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
                     top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
                     top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
                     top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
-                    top = fmaxf(top, m[nt][e]);
+                    top = fmaxf(top - (E4M3 ? kLift : 0.f), m[nt][e]);
                     const float alpha = top == -INFINITY ? 1.f : ex2(m[nt][e] - top);
                     m[nt][e] = top;
                     l[nt][e] *= alpha;

@@ -109,3 +109,29 @@ def test_neighbours_that_are_zero_or_not_finite(zero):
     want, want_l, tol, tol_l = attend64(bt, torch.where(bad[..., None], 0.0, bt.q))
     within(out[~bad], want[~bad], tol[~bad], "out")
     within(lse[~bad].double(), want_l[~bad], tol_l[~bad], "lse")
+
+
+@pytest.mark.parametrize("hq,news", [(8, 1), (4, 3), (24, 1)])
+@pytest.mark.parametrize("gap", [10, 15, 19])
+def test_small_weights_beside_8bit_values(hq, news, gap):
+    """Few rows: weights of 2^-gap of a row's largest keep the 11 bits of f16, down to 2^-20, for the dimensions where
+    the largest one's value is zero."""
+    n = 40
+    bt = Batch([news] * 5, [n] * 5, hq=hq, hkv=1, page=16, e4m3=True, seed=gap)
+    for b in range(5):
+        k, v = bt.values[0][b] * 0, bt.values[1][b].clone()
+        k[0, :, 0] = 1.0
+        v[0, :, 1:], v[1:, :, 0], v[:, :, 0] = 0, 0, 1.0
+        v[1:] = v[1:] / v[1:].abs().amax(-1, keepdim=True) * 1.5  # scales alike
+        bt.values[0][b], bt.values[1][b] = bt._put(0, b, k.bfloat16().double()), bt._put(1, b, v.bfloat16().double())
+    bt.q[:] = 0
+    gaps = gap + 0.9 * torch.rand(bt.q.shape[:2], generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    bt.q[..., 0] = gaps * math.log(2) * math.sqrt(128)  # key 0's logit; all others' are 0
+    out, _ = attend(bt)
+    for b in range(5):
+        w, off = weights64(bt, b, news * b)
+        assert 0.45 < float(w[0, 0, 1] / w[0, 0, 0]) * 2.0 ** gap < 1.05
+        v = bt.values[1][b].repeat_interleave(hq, 1)
+        want, size = torch.einsum("rhn,nhd->rhd", w, v), torch.einsum("rhn,nhd->rhd", w, v.abs())
+        tol = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2 * off[..., None] + 2 * n * 2.0 ** -24) * size
+        within(out[news * b: news * (b + 1)], want, tol)
