@@ -440,8 +440,9 @@ typedef struct {
     float attn_scale;  /* 0 means 1/sqrt(128)                                              */
 } scale_attend_t;
 
-/* Workspace of scale_cache_attend for these heads and this batch's n_seqs, n_rows and
- * max_rows (no pointer of either struct is looked at). Synchronous, host only. */
+/* Workspace of scale_cache_attend for these heads, a cache of this type and number of heads, and
+ * batches of at most this one's n_seqs, n_rows and max_rows: the size for the largest batch
+ * does for all of them (no pointer of either struct is looked at). Synchronous, host only. */
 int scale_cache_attend_workspace_size(const scale_attend_t *attend, const scale_cache_t *cache,
                                       const scale_batch_t *batch, size_t *bytes);
 int scale_cache_attend(const scale_attend_t *attend, const scale_cache_t *cache, const scale_batch_t *batch,

@@ -15,8 +15,6 @@ using namespace scale_ptx;
 // ---------------------------------------------------------------- few rows: decode
 
 constexpr int kStep = 16;          // keys of a step; a page holds whole steps
-constexpr int kMaxRowsWarps = 16;
-constexpr int kMaxParts = 2 * kMaxSms * kMaxRowsWarps;  // partial results
 constexpr int kMinSteps = 8;       // steps of a CTA before another one helps (one token at 4K, 4 heads: 8.7 us, 9.5 with 4, 9.9 with 32)
 constexpr float kRaise = 8.0f;     // log2 units by which a logit may pass the reference
 constexpr float kLift = 6.0f;      // 8-bit: log2 units that a new reference lies below the largest logit
@@ -50,8 +48,8 @@ struct RowsArgs {
     CacheView c;
     BatchView b;
     int64_t* before;   // [n_seqs + 1] steps (of one KV head) of the sequences before, for k_rows_merge
-    float* part_o;     // [kMaxParts][rows][128]
-    float2* part_ml;   // [kMaxParts][rows] (reference, sum)
+    float* part_o;     // [2 of each run][rows][128]
+    float2* part_ml;   // [2 of each run][rows] (reference, sum)
     int part_rows;
 };
 
@@ -783,13 +781,15 @@ AttendWs attend_layout(int Hq, int Hkv, bool e4m3, int n_seqs, int n_rows, int m
         return at;
     };
     const int64_t rows = static_cast<int64_t>(max_rows) * (Hq / Hkv);
-    w.part_rows = static_cast<int>((rows + 7) / 8 * 8);
     if (rows > rows_max(e4m3)) {
         w.chunks = take(chunk_ws_bytes(Hq / Hkv, Hkv, n_seqs, n_rows, max_rows));
     } else {
+        const int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 3;
+        const size_t parts = 2 * kMaxSms * rows_warps(nt, e4m3);  // two of a run
+        w.part_rows = 8 * nt;
         w.before = take((static_cast<size_t>(n_seqs) + 1) * sizeof(int64_t));
-        w.part_ml = take(static_cast<size_t>(kMaxParts) * w.part_rows * sizeof(float2));
-        w.part_o = take(static_cast<size_t>(kMaxParts) * w.part_rows * kHeadDim * sizeof(float));
+        w.part_ml = take(parts * w.part_rows * sizeof(float2));
+        w.part_o = take(parts * w.part_rows * kHeadDim * sizeof(float));
     }
     w.end = off;
     return w;
@@ -813,9 +813,15 @@ cudaError_t run_rows(const RowsArgs& r, int sms, cudaStream_t st)
 
 }  // namespace
 
+// Either route's size does not fall with any of its numbers, so what a batch of fewer may need is the route of few rows
+// at its most, where that is not the batch's own.
 size_t attend_ws_bytes(int Hq, int Hkv, bool e4m3, int n_seqs, int n_rows, int max_rows)
 {
-    return attend_layout(Hq, Hkv, e4m3, n_seqs, n_rows, max_rows).end;
+    const size_t own = attend_layout(Hq, Hkv, e4m3, n_seqs, n_rows, max_rows).end;
+    const int most = rows_max(e4m3) / (Hq / Hkv);
+    if (max_rows <= most) return own;
+    const size_t few = attend_layout(Hq, Hkv, e4m3, n_seqs, n_rows, most).end;
+    return own > few ? own : few;
 }
 
 cudaError_t launch_attend(const AttendView& a, const CacheView& c, bool e4m3, const BatchView& b, uint8_t* ws,

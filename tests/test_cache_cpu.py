@@ -214,3 +214,30 @@ def test_binding_refuses_other_types_of_the_same_size():
     b = S.kv_batch(ints[:3], ints[:2], ints.view(2, 4), 2, 1)
     with pytest.raises(ValueError):
         S.scale_cache_attend(S.attend_params(num_q_heads=4), S.kv_cache(codes, codes, scales, scales), b, rows, rows.clone(), ints, ints)
+
+
+def _attend_size(lib, hq, hkv, e4m3, n_seqs, n_rows, max_rows):
+    n = ctypes.c_size_t()
+    c = _cache(dtype=S.SCALE_CACHE_E4M3 if e4m3 else S.SCALE_CACHE_BF16, num_kv_heads=hkv)
+    assert lib.scale_cache_attend_workspace_size(ctypes.byref(S.ScaleAttend(hq, 0, -1, 0.0)), ctypes.byref(c),
+                                                 ctypes.byref(_batch(n_seqs=n_seqs, n_rows=n_rows, max_rows=max_rows)),
+                                                 ctypes.byref(n)) == S.SCALE_OK
+    return n.value
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 8), (32, 8), (28, 4), (17, 1), (25, 1), (64, 2), (64, 64)])
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_a_workspace_for_the_largest_batch_does_for_all(lib, hq, hkv, e4m3):
+    """The size of a batch is at least that of every batch of no more sequences, rows and rows of a sequence."""
+    sizes = {(s, r, m): _attend_size(lib, hq, hkv, e4m3, s, r, m)
+             for s in (1, 7, 4096) for r in (1, 17, 40000) for m in (0, 1, 2, 3, 5, 16, 17, 24, 25, 129, 40000)}
+    for x, big in sizes.items():
+        for y, small in sizes.items():
+            assert small <= big or any(a > b for a, b in zip(y, x)), (y, small, x, big)
+
+
+def test_the_workspace_of_a_decode_step_follows_its_route(lib):
+    """Partial results of as many warps as the route has: two of 520 bytes a row for each of 160 SMs' warps."""
+    assert _attend_size(lib, 4, 1, False, 1, 1, 1) <= 2 * 160 * 8 * 8 * 520 + 4096
+    assert _attend_size(lib, 32, 8, True, 64, 64, 1) <= 2 * 160 * 16 * 8 * 520 + 4096
+    assert _attend_size(lib, 16, 1, False, 1, 1, 1) <= 2 * 160 * 8 * 16 * 520 + 4096

@@ -217,6 +217,23 @@ def test_the_selection_path_reads_a_pool_that_was_appended_to(page, block):
         assert same_bits(paged.out, flat.out)
 
 
+# ---------------------------------------------------------------- one workspace for batches of many sizes
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (4, 1), (8, 2)])
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_the_largest_batch_sizes_the_workspace(hq, hkv, e4m3):
+    """Batches of 25 rows of a sequence down to one, either route, in a workspace of the first's size."""
+    bts = [Batch([n] * 3, [900, 30, 200], hq=hq, hkv=hkv, page=16, e4m3=e4m3) for n in (25, 24, 17, 16, 6, 4, 2, 1)]
+    a = S.attend_params(num_q_heads=hq)
+    ws = torch.empty(S.scale_cache_attend_workspace_size(a, bts[0].cache, bts[0].batch), dtype=torch.uint8, device="cuda")
+    S.scale_workspace_init(ws)
+    for bt in bts:
+        want, want_l = attend(bt)
+        out, lse = attend(bt, ws=ws)
+        assert same_bits(out, want) and same_bits(lse, want_l)
+
+
 # ---------------------------------------------------------------- threads
 
 
