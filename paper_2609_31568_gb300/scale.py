@@ -71,9 +71,16 @@ class ScaleKvPages(ctypes.Structure):
 
 
 def kv_pages(k_pages, v_pages, page_table, page_size: int) -> ScaleKvPages:
-    """Descriptor of torch tensors k_pages / v_pages [num_pages][page_size][H_kv][128]
-    and page_table (int32) on the device."""
-    return ScaleKvPages(_ptr(k_pages), _ptr(v_pages), _ptr(page_table), page_size, k_pages.shape[0])
+    """Descriptor of torch tensors k_pages / v_pages bf16 [num_pages][page_size][H_kv][128]
+    and page_table (int32) on the device. It keeps the tensors alive."""
+    bf16 = _imported_torch().bfloat16
+    if k_pages.dtype is not bf16 or v_pages.dtype is not bf16 or k_pages.dim() != 4 or k_pages.shape != v_pages.shape \
+            or k_pages.shape[1] != page_size or k_pages.shape[3] != 128:
+        raise ValueError(f"pages are bf16 [num_pages][{page_size}][num_kv_heads][128], the same for keys and values")
+    _int32(page_table)
+    kv = ScaleKvPages(_ptr(k_pages), _ptr(v_pages), _ptr(page_table), page_size, k_pages.shape[0])
+    kv.tensors = (k_pages, v_pages, page_table)
+    return kv
 
 
 class ScaleCache(ctypes.Structure):

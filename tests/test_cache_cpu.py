@@ -241,3 +241,16 @@ def test_the_workspace_of_a_decode_step_follows_its_route(lib):
     assert _attend_size(lib, 4, 1, False, 1, 1, 1) <= 2 * 160 * 8 * 8 * 520 + 4096
     assert _attend_size(lib, 32, 8, True, 64, 64, 1) <= 2 * 160 * 16 * 8 * 520 + 4096
     assert _attend_size(lib, 16, 1, False, 1, 1, 1) <= 2 * 160 * 8 * 16 * 520 + 4096
+
+
+def test_pages_of_the_selection_path_are_checked():
+    """Its kernels read bf16 pages of 128 values and do not see their type: an 8-bit cache's pages, half as large, are refused."""
+    pages, table = torch.zeros(3, 64, 2, 128, dtype=torch.bfloat16), torch.zeros(5, dtype=torch.int32)
+    kv = S.kv_pages(pages, pages.clone(), table.clone(), 64)
+    assert (kv.page_size, kv.num_pages) == (64, 3) and kv.tensors[2].data_ptr() == kv.page_table  # kept alive
+    codes = torch.zeros(3, 64, 2, 128, dtype=torch.uint8)
+    for bad in ((codes, codes, table, 64), (pages, codes, table, 64), (pages.half(), pages.half(), table, 64),
+                (pages, pages[:2], table, 64), (pages[..., :64].contiguous(), pages[..., :64].contiguous(), table, 64),
+                (pages, pages, table, 128), (pages[0], pages[0], table, 64), (pages, pages, table.long(), 64)):
+        with pytest.raises(ValueError):
+            S.kv_pages(*bad)
