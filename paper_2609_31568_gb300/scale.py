@@ -157,6 +157,7 @@ def kv_batch(row_start, kv_len, page_table, n_rows: int, max_rows: int) -> Scale
     if kv_len.dim() != 1 or tuple(row_start.shape) != (n + 1,) or page_table.dim() != 2 or page_table.shape[0] != n:
         raise ValueError("a batch has row_start [n_seqs + 1], kv_len [n_seqs] and page_table [n_seqs][pages]")
     _int32(row_start, kv_len, page_table)
+    _in_int32(n_rows=n_rows, max_rows=max_rows)
     b = ScaleBatch(_ptr(row_start), _ptr(kv_len), _ptr(page_table), n, page_table.shape[1], n_rows, max_rows)
     b.tensors = (row_start, kv_len, page_table)
     return b
@@ -179,6 +180,7 @@ def rope_axes(inv_freq, positions, axis=None, adjacent: bool = False) -> ScaleRo
 
 
 def attend_params(*, num_q_heads: int, n_sink: int = 0, n_local: int = -1, attn_scale: float = 0.0) -> ScaleAttend:
+    _in_int32(num_q_heads=num_q_heads, n_sink=n_sink, n_local=n_local)
     return ScaleAttend(num_q_heads, n_sink, n_local, attn_scale)
 
 
@@ -298,6 +300,13 @@ def _int32(*tensors) -> None:
     for x in tensors:
         if x.itemsize != 4 or x.is_floating_point():
             raise ValueError("expected int32 tensors")
+
+
+def _in_int32(**numbers) -> None:
+    """ctypes would cut them to their low 32 bits."""
+    for name, x in numbers.items():
+        if not -2 ** 31 <= x < 2 ** 31:
+            raise ValueError(f"{name} = {x} does not fit 32 bits")
 
 
 def _rows(x, n_rows: int, heads: int | None = None) -> tuple:

@@ -254,3 +254,15 @@ def test_pages_of_the_selection_path_are_checked():
                 (pages, pages, table, 128), (pages[0], pages[0], table, 64), (pages, pages, table.long(), 64)):
         with pytest.raises(ValueError):
             S.kv_pages(*bad)
+
+
+def test_numbers_beyond_32_bits_are_refused():
+    """Not cut to their low bits: a window of 2^32 tokens would be one of none."""
+    ints = torch.zeros(8, dtype=torch.int32)
+    assert S.attend_params(num_q_heads=8, n_sink=2 ** 31 - 1, n_local=2 ** 31 - 1).n_local == 2 ** 31 - 1
+    for bad in (lambda: S.attend_params(num_q_heads=8, n_local=2 ** 32), lambda: S.attend_params(num_q_heads=8, n_sink=2 ** 31),
+                lambda: S.attend_params(num_q_heads=2 ** 32 + 8), lambda: S.attend_params(num_q_heads=8, n_local=-2 ** 31 - 1),
+                lambda: S.kv_batch(ints[:3], ints[:2], ints.view(2, 4), 2 ** 32 + 2, 1),
+                lambda: S.kv_batch(ints[:3], ints[:2], ints.view(2, 4), 2, 2 ** 32)):
+        with pytest.raises(ValueError):
+            bad()
