@@ -333,7 +333,7 @@ int scale_decode_step(const scale_params_t *p, int64_t t, const void *q_t, const
  * pointer is a device pointer of the current device, row tensors and pages
  * 16-byte aligned. Inputs and outputs must not overlap, except that scale_rope
  * and scale_cache_append may write their rotated rows in place (same pointer
- * and stride). n_rows = 0 enqueues nothing. */
+ * and stride). n_rows = 0 enqueues nothing and needs no row tensors. */
 
 /* How the cache holds a row of 128 values. */
 typedef enum {

@@ -99,10 +99,10 @@ int check_rope(const scale_rope_t* r)
     return SCALE_OK;
 }
 
-// Heads and strides of a row tensor that is turned from x into y; 0 heads: none.
+// Heads and strides of a row tensor that is turned from x into y; 0 heads: none. Without rows there need be no tensors.
 int check_turned(int heads, int most, const void* x, int64_t xs, const void* y, int64_t ys, int64_t rows)
 {
-    if (heads < 0 || (heads == 0) != (x == nullptr) || (heads == 0) != (y == nullptr)) return SCALE_ERR_INVALID_ARG;
+    if (heads < 0 || (rows > 0 && ((heads == 0) != (x == nullptr) || (heads == 0) != (y == nullptr)))) return SCALE_ERR_INVALID_ARG;
     if (heads == 0) return SCALE_OK;
     if (heads > most) return SCALE_ERR_UNSUPPORTED;
     if (!stride_ok(xs, heads) || !stride_ok(ys, heads)) return SCALE_ERR_INVALID_ARG;
@@ -208,7 +208,7 @@ int scale_cache_read(const scale_cache_t* cache, const scale_batch_t* batch, voi
     int rc = check_cache(cache, &c, &e4m3);
     if (rc) return rc;
     if ((rc = check_batch(batch, &b))) return rc;
-    if (!k_out && !v_out) return SCALE_ERR_INVALID_ARG;
+    if (b.n_rows && !k_out && !v_out) return SCALE_ERR_INVALID_ARG;
     if ((k_out && !stride_ok(k_out_stride, c.Hkv)) || (v_out && !stride_ok(v_out_stride, c.Hkv)))
         return SCALE_ERR_INVALID_ARG;
     if (k_out && v_out && b.n_rows && overlap(k_out, k_out_stride, c.Hkv, v_out, v_out_stride, c.Hkv, b.n_rows))

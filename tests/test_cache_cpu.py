@@ -266,3 +266,23 @@ def test_numbers_beyond_32_bits_are_refused():
                 lambda: S.kv_batch(ints[:3], ints[:2], ints.view(2, 4), 2, 2 ** 32)):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_a_step_without_rows_enqueues_nothing(lib):
+    """Empty tensors, whose address torch gives as 0, through every call of the binding."""
+    pages, ints = torch.zeros(3, 16, 2, 128, dtype=torch.bfloat16), torch.zeros(8, dtype=torch.int32)
+    cache, batch = S.kv_cache(pages, pages.clone()), S.kv_batch(ints[:3], ints[:2], ints.view(2, 4), 0, 1)
+    rope = S.rope_axes(torch.zeros(64).double(), torch.zeros(1, 0, dtype=torch.int32))
+    q, k = torch.zeros(0, 4, 128, dtype=torch.bfloat16), torch.zeros(0, 2, 128, dtype=torch.bfloat16)
+    S.scale_rope(rope, q, k, q, k, stream=0)
+    S.scale_rope(rope, q, None, q, None, stream=0)
+    S.scale_cache_append(cache, batch, k, k, stream=0)
+    S.scale_cache_append(cache, batch, k, k, rope, q, q, stream=0)
+    S.scale_cache_read(cache, batch, k, k, stream=0)
+    S.scale_cache_read(cache, batch, None, k, stream=0)
+    S.scale_cache_attend(S.attend_params(num_q_heads=4), cache, batch, q, q, None, ints, stream=0)
+    # what is wrong without rows too
+    at, ref = 1 << 30, ctypes.byref
+    assert lib.scale_rope(ref(_rope()), 0, 257, at, 65536, at, 65536, 0, None, 0, None, 0, None) == S.SCALE_ERR_UNSUPPORTED
+    assert lib.scale_rope(ref(_rope()), 0, 8, None, 1000, None, 1024, 0, None, 0, None, 0, None) == S.SCALE_ERR_INVALID_ARG
+    assert lib.scale_cache_read(ref(_cache()), ref(_batch(n_rows=0)), at, 8, None, 0, None) == S.SCALE_ERR_INVALID_ARG
