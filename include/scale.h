@@ -342,7 +342,12 @@ typedef enum {
 } scale_cache_dtype_t;
 
 /* A paged cache of keys and values. The value of an 8-bit row is code * 2^e
- * with e = scale byte - 127; every such value is exact in bf16. */
+ * with e = scale byte - 127; scale_cache_append writes bytes 27 to 247 (e of -100 to
+ * 120), whose values are exact in bf16, and rows that are read hold no others.
+ * A bf16 cache's pages are also those of scale_kv_pages_t (a sequence's row of
+ * page_table is its table), under that one's rules: pages of a multiple of 64
+ * tokens, and finite rows behind token N - 1 in the last one, which stay what they
+ * were before tokens were written. */
 typedef struct {
     void *k_pages;         /* bf16 or e4m3 [num_pages][page_size][H_kv][128]                 */
     void *v_pages;
