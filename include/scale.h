@@ -344,8 +344,8 @@ typedef enum {
 /* A paged cache of keys and values. The value of an 8-bit row is code * 2^e
  * with e = scale byte - 127; scale_cache_append writes bytes 27 to 247 (e of -100 to
  * 120), whose values are exact in bf16, and rows that are read hold no others.
- * A bf16 cache's pages are also those of scale_kv_pages_t (a sequence's row of
- * page_table is its table), under that one's rules: pages of a multiple of 64
+ * A bf16 cache's pages do for scale_kv_pages_t too, with a sequence's row of
+ * page_table as its table and under that one's rules: pages of a multiple of 64
  * tokens, and finite rows behind token N - 1 in the last one, which stay what they
  * were before tokens were written. */
 typedef struct {
