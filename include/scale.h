@@ -407,8 +407,8 @@ int scale_rope(const scale_rope_t *rope, int32_t n_rows, int32_t num_q_heads, co
  * launch; a turned key goes into an 8-bit cache from fp32, rounded once. Without
  * `rope` q must be NULL.
  * An 8-bit row gets e = the least exponent, at least -100, with max |x| <= 448 * 2^e
- * over its finite values, and codes e4m3(x / 2^e), rounded to nearest even;
- * infinities become the largest code, NaN stays NaN. */
+ * over its finite values, and codes e4m3(x / 2^e), rounded to nearest even (256 * 2^120,
+ * beyond bf16, becomes 240 * 2^120); infinities become the largest code, NaN stays NaN. */
 int scale_cache_append(const scale_cache_t *cache, const scale_batch_t *batch, const void *k, int64_t k_stride,
                        const void *v, int64_t v_stride, const scale_rope_t *rope, int32_t num_q_heads,
                        const void *q, int64_t q_stride, void *q_out, int64_t q_out_stride, scale_stream_t stream);

@@ -253,6 +253,10 @@ __global__ void __launch_bounds__(kPlaceThreads, kPlaceCtas) k_place(const __gri
                         fmul2(z[2], z[3], x[4 * i + 2], x[4 * i + 3], inv, inv);
                         y[i] = f32_to_e4m3x2(z[0], z[1]) | f32_to_e4m3x2(z[2], z[3]) << 16;
                     }
+                    if (e > 119) {  // 256 2^120 is beyond bf16: the code below it
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) y[i] -= __vcmpeq4(y[i] & 0x7F7F7F7Fu, 0x78787878u) & 0x01010101u;
+                    }
                     uint8_t* dst = (is_k ? out_k : out_v) + h * kHeadDim;
                     *reinterpret_cast<uint2*>(dst) = make_uint2(y[0], y[1]);
                     *reinterpret_cast<uint2*>(dst + 64) = make_uint2(y[2], y[3]);

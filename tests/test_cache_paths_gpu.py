@@ -292,3 +292,27 @@ def test_first_calls_of_a_process_come_from_threads():
     run = subprocess.run([sys.executable, "-c", FIRST_CALLS % (ROOT, os.path.join(ROOT, "tests"))], capture_output=True, text=True,
                          timeout=300)
     assert run.returncode == 0, run.stderr[-3000:]
+
+
+# ---------------------------------------------------------------- the largest values
+
+
+def test_8bit_rows_at_the_end_of_bf16():
+    """Rows whose largest value lies above 448 * 2^119: what rounds to 256 * 2^120, beyond bf16, is held as 240 * 2^120."""
+    n = 8
+    bt = Batch([n], [n], hq=1, hkv=1, page=16, e4m3=True, fill=False)
+    big = 2.0 ** 127
+    x = torch.randn(n, 1, 128, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").bfloat16()
+    for i, f in enumerate((1.9921875, 1.9375, 1.9296875, 1.890625, 1.8125, 1.7578125, 1.75, 1.0)):
+        x[i, 0, 3], x[i, 0, 90] = f * big, -f * big
+    x[0, 0, 50], x[1, 0, 51] = math.nan, math.inf
+    S.scale_cache_append(bt.cache, bt.batch, x, x)
+    out = [torch.empty_like(x) for _ in range(2)]
+    S.scale_cache_read(bt.cache, bt.batch, *out)
+    want = torch.tensor([240.0, 240, 240, 240, 224, 224, 224, 128], dtype=torch.float64, device="cuda") * 2.0 ** 120
+    for y in out:
+        assert torch.equal(y[:, 0, 3].double(), want) and torch.equal(y[:, 0, 90].double(), -want)
+        assert y[0, 0, 50].isnan() and y[1, 0, 51].isinf()  # the largest code, 448, times 2^120
+        assert torch.isfinite(y).sum() == n * 128 - 2
+    page_of, slot = bt.table[0].long()[torch.arange(n, device="cuda") // 16], torch.arange(n, device="cuda") % 16
+    assert bt.scales[0].transpose(1, 2)[page_of, slot][:, 0].tolist() == [247] * 6 + [246, 246]
