@@ -15,7 +15,7 @@ using namespace scale_ptx;
 // ---------------------------------------------------------------- few rows: decode
 
 constexpr int kStep = 16;          // keys of a step; a page holds whole steps
-constexpr int kMinSteps = 8;       // steps of a CTA before another one helps (one token at 4K, 4 heads: 8.7 us, 9.5 with 4, 9.9 with 32)
+constexpr int kMinSteps = 8;       // steps of a CTA before another one helps (one token at 4K, 4 heads: 8.3 us; 8.7, 9.5 with 4 and 9.9 with 32 when it was chosen)
 constexpr float kRaise = 8.0f;     // log2 units by which a logit may pass the reference
 constexpr float kLift = 6.0f;      // 8-bit: log2 units that a new reference lies below the largest logit
 
@@ -154,9 +154,9 @@ struct Item {
 // 4K take as long with it as with one part of 8 bits.
 //
 // Keys that no row sees are not read: their places are filled with zeros, so nothing that lies there
-// reaches a sum. Bound by HBM: K and V once. With 32 query heads on 8 and 28 on 4: one token at 128K, 8-bit (272 MB), 60 us
-// with the merge, 6.3 TB/s between a start of 6 us (launch, lengths, pages, first rows) and the merge of
-// 6 us; 48 tokens of 130 to 30,000, bf16 (560 MB), 94 us, 7 TB/s in the loop; one at 4K 8.7 us, all latency.
+// reaches a sum. Bound by HBM: K and V once. With 32 query heads on 8 and 28 on 4: one token at 128K, 8-bit (272 MB), 55 us
+// with the merge (60 and 61 on other GPUs), 6.3 TB/s between a start of 6 us (launch, lengths, pages, first rows) and the
+// merge of 6 us; 48 tokens of 130 to 30,000, bf16 (560 MB), 92 us, 7 TB/s in the loop; one at 4K 8.3 us, all latency.
 template <int NT, bool E4M3>
 __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __grid_constant__ RowsArgs args)
 {

@@ -44,8 +44,13 @@ constexpr int kTails = 3, kTailCuts = 4;   // and the last half, quarter or eigh
 constexpr int kCandidates = kUniform + kTails * kTailCuts;
 static_assert(kCandidates <= 32, "a lane for each");
 constexpr int kPieceTiles = 5;        // what a CTA's start and end take, in key tiles
-constexpr int kRowsApart = 5;         // 8-bit: log2 of the sizes of queries that share a power of two
 constexpr int kMergeTiles = 4;        // what writing and merging one piece per SM takes
+
+// 8-bit: log2 of the sizes of queries that share a power of two. At most 2^-12 of a row's largest |q| is lost so, 2^-4 of what
+// bf16 itself leaves of that value. Rows of sizes up to 2^12 apart, each with its own power, take 1.33 times as long
+// (4,096 tokens over 64K: 6,620 us, and 4,990 with one power and the small rows' bits lost); of sizes 1 to 8, which share
+// it, 332 and 329 us at 1,024 over 16K (476 where they did not, with a limit of 2^3).
+constexpr int kRowsApart = 5;
 
 // A CTA's work. Rows [row0, row0 + ntok) of the row tensors are tokens pos ..; key tiles
 // [k0, k1) of those the job's rows see; slot >= 0: partial results there.
@@ -133,7 +138,7 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* s_warp, int64_
 // the last half, quarter or eighth of R, T tiles, into pieces of T / SMs .. T / (kTailCuts SMs), which fill up what the
 // jobs before them leave uneven. The one is taken that ends first, by the rounds of the SMs or by what jobs taken in
 // order can be late at most, kPieceTiles for each job and the merge of the pieces included. (9 sequences of 1 to 700
-// tokens, 200 items, 8-bit: 113 us, and 129 with all cut alike. 4,096 tokens over 64K: 512 items, 208 of them cut.)
+// tokens, 200 items, 8-bit: 116 us; 113, and 129 with all cut alike, when the choice was made. 4,096 tokens over 64K: 512 items, 208 of them cut.)
 // The plan takes 7 to 8 us, most of it latency: lengths from memory, scans, the lists' way back.
 __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_constant__ ChunkArgs a)
 {
