@@ -15,7 +15,8 @@ using namespace scale_ptx;
 // ---------------------------------------------------------------- few rows: decode
 
 constexpr int kStep = 16;          // keys of a step; a page holds whole steps
-constexpr int kMinSteps = 8;       // steps of a CTA before another one helps (one token at 4K, 4 heads: 8.3 us; 8.7, 9.5 with 4 and 9.9 with 32 when it was chosen)
+// Steps of a CTA before another one helps: one token at 4K, 4 heads, 8.3 us (8.7, 9.5 with 4 and 9.9 with 32, when it was chosen)
+constexpr int kMinSteps = 8;
 constexpr float kRaise = 8.0f;     // log2 units by which a logit may pass the reference
 constexpr float kLift = 6.0f;      // 8-bit: log2 units that a new reference lies below the largest logit
 

@@ -138,7 +138,8 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* s_warp, int64_
 // the last half, quarter or eighth of R, T tiles, into pieces of T / SMs .. T / (kTailCuts SMs), which fill up what the
 // jobs before them leave uneven. The one is taken that ends first, by the rounds of the SMs or by what jobs taken in
 // order can be late at most, kPieceTiles for each job and the merge of the pieces included. (9 sequences of 1 to 700
-// tokens, 200 items, 8-bit: 116 us; 113, and 129 with all cut alike, when the choice was made. 4,096 tokens over 64K: 512 items, 208 of them cut.)
+// tokens, 200 items, 8-bit: 116 us; 113, and 129 with all cut alike, when the choice was made. 4,096 tokens over 64K: 512
+// items, 208 of them cut.)
 // The plan takes 7 to 8 us, most of it latency: lengths from memory, scans, the lists' way back.
 __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_constant__ ChunkArgs a)
 {
