@@ -454,6 +454,131 @@ int scale_cache_attend(const scale_attend_t *attend, const scale_cache_t *cache,
                        const void *q, int64_t q_stride, void *out, int64_t out_stride, float *lse, void *ws,
                        size_t ws_bytes, scale_stream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Several continuations of a sequence over its paged cache: drafted trees that
+ * the model verifies in one pass, and beams. The conventions are those of the
+ * calls above.
+ *
+ * A step with drafted trees: scale_tree_plan, then in every layer scale_cache_append with
+ * the plan's positions and scale_cache_attend_tree; from the last layer's logits the model's
+ * token after each node (scale_beam_select with one beam and n_best 1, or a sampler);
+ * scale_tree_accept, and scale_cache_move over the caches of all layers. The caches then
+ * hold what they would, had the accepted tokens come one by one.
+ *
+ * A step of beam search: scale_cache_append and scale_cache_attend with a sequence for
+ * each beam, scale_beam_select, scale_beam_reorder, and scale_cache_move over all layers. */
+
+/* Drafted trees. The rows of a sequence of a scale_batch_t are its tree's nodes (or several trees'):
+ * node c of sequence b is row row_start[b] + c, and its key and value are the cache's token
+ * base + c, base = kv_len[b] less the sequence's rows. */
+typedef struct {
+    const int32_t *parents; /* [n_rows]: an earlier node of the sequence; -1: none, the node follows
+                               token base - 1; anything else: the row is no node (padding).
+                               scale_cache_attend_tree does not use it                         */
+    int32_t *positions;     /* [n_rows]: base + the number of ancestors; -1: no node             */
+    uint32_t *masks;        /* [n_rows][mask_words]: bit c % 32 of word c / 32: node c is seen   */
+    int32_t mask_words;     /* 32 mask_words >= max_rows; at most 32                             */
+} scale_tree_t;
+
+/* Positions and masks of the batch's nodes from their parents: a node sees itself and its
+ * ancestors (n_local >= 0: those at most n_local above it, and those at positions below
+ * n_sink, as if its path were the sequence). A row that is no node, all below it, and every
+ * row of a sequence whose kv_len is less than its rows, get position -1 and an empty mask. The
+ * positions do for scale_rope_t with one axis. max_rows is at most 1024 (SCALE_ERR_UNSUPPORTED);
+ * rows of a sequence past it are left as they were. page_table is not used. */
+int scale_tree_plan(const scale_tree_t *tree, const scale_batch_t *batch, int32_t n_sink, int32_t n_local,
+                    scale_stream_t stream);
+
+/* scale_cache_attend for the nodes of drafted trees. Row r of sequence b, p = max(positions[r], base):
+ *   keys {t < base : t < n_sink or t >= p - n_local} (n_local < 0: all t < base) and
+ *        {base + c : the bit of node c in masks[r] is set}, whatever n_sink and n_local.
+ * A row with a negative position, or whose own token is negative, has no keys. Any masks do: a row may see
+ * later nodes, or not itself; bits of nodes past the sequence's rows or max_rows are ignored.
+ * Nodes that no row of their sequence sees, and tokens that a window ending at `base` hides, may hold anything; a value row
+ * that is not finite makes the rows that see it not finite and may make so the other rows of its sequence. Heads, NaN queries, lse,
+ * precision and the workspace (its size too) are as there. max_rows is at most 1024. */
+int scale_cache_attend_tree(const scale_attend_t *attend, const scale_tree_t *tree, const scale_cache_t *cache,
+                            const scale_batch_t *batch, const void *q, int64_t q_stride, void *out,
+                            int64_t out_stride, float *lse, void *ws, size_t ws_bytes, scale_stream_t stream);
+
+/* Rows that move within a cache: a move copies row src of the pool (page * page_size + place in the page), keys
+ * and values of all heads, to row dst; with either outside the pool (-1) it is none. A row that a move writes may
+ * be read by an earlier move of its group, but not by a later one; no two moves write the same row, and no
+ * move reads or writes a row that one of another group writes. */
+typedef struct {
+    int32_t *src, *dst;   /* [n_moves]                                                              */
+    const int32_t *start; /* [n_groups + 1], ascending: group g has the moves [start[g], start[g + 1])
+                             (those within n_moves); NULL: n_moves / n_groups moves each            */
+    int32_t n_groups;     /* 1..4096                                                                */
+    int32_t n_moves;
+} scale_moves_t;
+
+/* The moves in each of n_caches caches (1..1024; the layers' of one batch: all of the same type,
+ * heads, page size and number of pages), which must not share memory. */
+int scale_cache_move(const scale_cache_t *caches, int32_t n_caches, const scale_moves_t *moves, scale_stream_t stream);
+
+/* Greedy verification of drafted trees. The walk down sequence b's tree begins with the token first[b], which
+ * the model chose after token base - 1: of the nodes without a parent the lowest that holds it is accepted;
+ * then of that node's children the lowest that holds the model's choice after it, and so on.
+ *   tokens     int32 [n_rows]  tokens of the nodes
+ *   choices    int32 [n_rows]  the model's token after each node
+ *   first      int32 [n_seqs], or NULL: the lowest node without a parent is accepted whatever it holds
+ *   n_accepted int32 [n_seqs]  out: nodes accepted
+ *   path       int32 [n_rows]  out: the accepted nodes of sequence b at row_start[b] .., then -1
+ *   next       int32 [n_seqs]  out: the model's choice after the last accepted node (none accepted: first[b], or -1):
+ *                              the next step's first[b], whose tree has it as its root
+ *   new_len    int32 [n_seqs]  out: base + n_accepted; kv_len of the next append is this and its rows
+ *   moves      src and dst [n_rows] out: the moves of the accepted nodes' rows to tokens base .., for
+ *              scale_cache_move with start = row_start; n_groups is n_seqs and n_moves n_rows
+ * A sequence without rows, or with kv_len less than its rows, accepts none and keeps kv_len. `cache` says the
+ * page size and the number of pages; its pages are not touched. max_rows is at most 1024; rows past it are no nodes,
+ * and what is written for rows is left as it was there. */
+int scale_tree_accept(const scale_tree_t *tree, const scale_cache_t *cache, const scale_batch_t *batch,
+                      const int32_t *tokens, const int32_t *choices, const int32_t *first, int32_t *n_accepted,
+                      int32_t *path, int32_t *next, int32_t *new_len, const scale_moves_t *moves, scale_stream_t stream);
+
+/* Type of logits. */
+typedef enum { SCALE_LOGITS_BF16 = 0, SCALE_LOGITS_FP32 = 1 } scale_logits_dtype_t;
+
+/* Groups of beams that are searched together. */
+typedef struct {
+    int32_t n_groups; /* n_groups * n_beams at most 4096                                            */
+    int32_t n_beams;  /* beams of a group, 1..32                                                    */
+    int32_t vocab;    /* 1..2^24                                                                    */
+    int32_t n_best;   /* continuations kept of a group: 1..64, at most n_beams * vocab              */
+    int32_t dtype;    /* scale_logits_dtype_t                                                       */
+} scale_beam_t;
+
+/* The best continuations of each group of beams. Token v after beam i of a group scores
+ *   scores[i] + log softmax(logits of the beam)[v],
+ * in 64 bits from sums in 32 that are kept to 2^-22 of them; the n_best largest are written in descending order, equal ones
+ * by the lower beam, then the lower token. A NaN logit counts as -inf; every continuation of a beam whose score
+ * is not finite, or whose logits have no finite maximum, scores -inf and is taken in its turn like any other.
+ *   logits      [n_groups * n_beams][vocab], rows logits_stride elements apart (at least vocab), aligned to their type
+ *   scores      fp32 [n_groups][n_beams]
+ *   best_scores fp32 [n_groups][n_best], best_beams int32 (0..n_beams - 1), best_tokens int32: out
+ *   ws          scale_beam_workspace_size() bytes, 256-byte aligned, not initialised */
+int scale_beam_workspace_size(const scale_beam_t *beam, size_t *bytes);
+int scale_beam_select(const scale_beam_t *beam, const void *logits, int64_t logits_stride, const float *scores,
+                      float *best_scores, int32_t *best_beams, int32_t *best_tokens, void *ws, size_t ws_bytes,
+                      scale_stream_t stream);
+
+/* Beams go on from others: beam i of a group (sequence n_beams * group + i of the page table) goes on from beam
+ * parents[i] of its group (a number outside 0..n_beams - 1: from itself). The beams of a group have the length of
+ * its first (kv_len, tokens in the cache). Complete pages are shared: the new rows of the table have those of
+ * the beams they go on from. The page that is being filled, and the table's entries behind it, stay one beam's: of the
+ * beams that go on from the same one, that one itself, or else the lowest, keeps them; the others get, in
+ * their order, those of the beams that none goes on from, into which the rows so far are copied by
+ * `moves`. So no page is needed, and pages that no table names any more stay the caller's.
+ *   page_table int32 [n_groups * n_beams][table_stride]; table_out the same, or page_table itself
+ *   parents    int32 [n_groups][n_beams];  kv_len int32 [n_groups * n_beams]
+ *   moves      src and dst [n_groups * n_beams][page_size] out, for scale_cache_move with start = NULL;
+ *              n_groups is the number of beams in all and n_moves that times page_size
+ * n_beams is 1..32, n_groups * n_beams at most 4096. `cache` says the page size and number of pages. */
+int scale_beam_reorder(const scale_cache_t *cache, int32_t n_groups, int32_t n_beams, const int32_t *parents,
+                       const int32_t *kv_len, const int32_t *page_table, int32_t table_stride, int32_t *table_out,
+                       const scale_moves_t *moves, scale_stream_t stream);
+
 /* Synchronous: waits for `stream`, then reads the device status word of `ws`
  * into *status (SCALE_OK, SCALE_ERR_TIMEOUT or SCALE_ERR_DEVICE). The word is
  * sticky until scale_workspace_init(). */

@@ -158,7 +158,11 @@ struct Item {
 // reaches a sum. Bound by HBM: K and V once. With 32 query heads on 8 and 28 on 4: one token at 128K, 8-bit (272 MB), 55 us
 // with the merge (60 and 61 on other GPUs), 6.3 TB/s between a start of 6 us (launch, lengths, pages, first rows) and the
 // merge of 6 us; 48 tokens of 130 to 30,000, bf16 (560 MB), 92 us, 7 TB/s in the loop; one at 4K 8.3 us, all latency.
-template <int NT, bool E4M3>
+//
+// TREE: the new tokens are nodes of drafted trees, and a row's mask says which of them it sees. Only steps that hold new
+// tokens (and those of a window, whose end goes by the rows' positions) look at masks; the nodes that none of the item's
+// rows sees are filled with zeros like other hidden keys.
+template <int NT, bool E4M3, bool TREE>
 __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __grid_constant__ RowsArgs args)
 {
     constexpr int kStages = rows_stages(NT, E4M3), kWarps = rows_warps(NT, E4M3), kRowsThreads = 32 * kWarps;
@@ -270,12 +274,17 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
         const int64_t first = in_pool ? static_cast<int64_t>(page) * c.page_size + slot : 0;
         const int64_t at = (first * c.Hkv + load.j) * kRow + my_row * pitch + my_chunk * 16;
         const uint8_t *k = c.k + at, *v = c.v + at;
-        // the keys that some row sees: t <= last and (t >= lo or t < n_sink)
-        const bool all = in_pool && t0 + kStep - 1 <= last && (t0 >= load.s.lo || t0 + kStep - 1 < a.n_sink);
+        // the keys that some row sees: t <= last and (t >= lo or t < n_sink), and of drafted nodes those of its rows' masks
+        bool all = in_pool && t0 + kStep - 1 <= last && (t0 >= load.s.lo || t0 + kStep - 1 < a.n_sink);
+        uint32_t nodes = 0xFFFFFFFFu;
+        if (TREE && t0 + kStep - 1 >= load.s.pos0) {
+            nodes = __reduce_or_sync(0xFFFFFFFFu, lane < load.s.rows ? tree_bits(tree_row(a.tree, load.s.row0, load.s.pos0, load.s.row0 + lane), t0) : 0u);
+            all = false;
+        }
 #pragma unroll
         for (int i = 0; i < kTile / 512; ++i) {
             const int row = i * kRowsAtOnce + my_row, t = t0 + row;
-            const bool real = all || (in_pool && t <= last && (t >= load.s.lo || t < a.n_sink));
+            const bool real = all || (in_pool && t <= last && (t >= load.s.lo || t < a.n_sink) && (!TREE || (nodes >> row & 1u)));
             const uint32_t to = dst + row * kRow + ((my_chunk ^ (row & 7)) << 4);
             cp_async16(to, real ? k : c.k, real);
             cp_async16(to + kTile, real ? v : c.v, real);
@@ -288,11 +297,13 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
         }
     };
 
+    bool some_absent = false;         // TREE: a row of the item has no place in its tree
     uint32_t qf[NT][8][2];            // Q^T, 16 dimensions at a time
     float q_scale[NT][2];             // 8-bit: the power of two that Q's row was divided by
     float o[8][NT][4];                // O^T: 16 dimensions at a time
     float m[NT][2], l[NT][2];         // per row: reference (log2 units, a warp's), sum of this lane's keys
     auto load_q = [&]() {
+        if (TREE) some_absent = __any_sync(0xFFFFFFFFu, lane < use.s.rows && tree_row(a.tree, use.s.row0, use.s.pos0, use.s.row0 + lane).words == 0);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int r = nt * 8 + oct;  // this lane's row of Q
@@ -377,7 +388,8 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
                     auto* out = static_cast<__nv_bfloat16*>(a.out) + row * a.out_stride + h * kHeadDim;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float y0 = o[i][nt][e] * inv, y1 = o[i][nt][2 + e] * inv;
+                        float y0 = o[i][nt][e] * inv, y1 = o[i][nt][2 + e] * inv;
+                        if (TREE && sum == 0.f) y0 = y1 = 0.f;  // beside values that are not finite too
                         if (E4M3) {
                             *reinterpret_cast<uint32_t*>(out + 16 * i + 2 * oct) = pack_bf16x2(y0, y1);
                         } else {
@@ -474,7 +486,25 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
         }
         const int t0 = token_of(use, use.step);
         const int last = use.s.pos0 + use.s.rows - 1;
-        if (t0 + kStep - 1 > use.s.pos0 || (a.n_local >= 0 && last - t0 > a.n_local && t0 + kStep - 1 >= a.n_sink)) {
+        if (TREE) {
+            if (t0 + kStep - 1 >= use.s.pos0 || some_absent || (a.n_local >= 0 && t0 + kStep - 1 >= a.n_sink)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int r = (nt * 8 + 2 * quad + e) / a.g;
+                        const TreeRow x = tree_row(a.tree, use.s.row0, use.s.pos0, use.s.row0 + (r < use.s.rows ? r : 0));
+                        const uint32_t seen = tree_bits(x, t0);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const int t = t0 + oct + 8 * i;
+                            if (!(seen >> (oct + 8 * i) & 1u) || t > last ||
+                                (a.n_local >= 0 && t < x.pos0 && x.position - t > a.n_local && t >= a.n_sink))
+                                s[nt][2 * i + e] = -INFINITY;
+                        }
+                    }
+            }
+        } else if (t0 + kStep - 1 > use.s.pos0 || (a.n_local >= 0 && last - t0 > a.n_local && t0 + kStep - 1 >= a.n_sink)) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -755,6 +785,7 @@ __global__ void __launch_bounds__(256) k_rows_merge(const __grid_constant__ Rows
             }
             if (live && sub == 0 && real) {
                 const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+                if (sum == 0.f) acc = make_float4(0.f, 0.f, 0.f, 0.f);  // no keys, beside values that are not finite too
                 const int64_t row = s.row0 + r / a.g;
                 const int h = j * a.g + r % a.g;
                 auto* out = static_cast<__nv_bfloat16*>(a.out) + row * a.out_stride + h * kHeadDim;
@@ -800,7 +831,7 @@ template <int NT, bool E4M3>
 cudaError_t run_rows(const RowsArgs& r, int sms, cudaStream_t st)
 {
     constexpr int kWarps = rows_warps(NT, E4M3);
-    auto kern = k_rows<NT, E4M3>;
+    auto kern = r.a.tree.masks ? k_rows<NT, E4M3, true> : k_rows<NT, E4M3, false>;
     const size_t smem = rows_ring_bytes(NT, E4M3) + (static_cast<size_t>(r.b.n_seqs) + 1) * sizeof(int64_t);
     // the largest call's, whatever this one's: calls from several threads set the same
     constexpr size_t kMost = rows_ring_bytes(NT, E4M3) + (kMaxSeqs + 1) * sizeof(int64_t);

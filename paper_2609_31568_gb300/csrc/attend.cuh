@@ -37,6 +37,39 @@ __device__ __forceinline__ Seq seq_of(const AttendView& a, const BatchView& b, i
     return seq_of(a, b, b.row_start[i], b.row_start[i + 1], b.kv_len[i]);
 }
 
+// Drafted trees: row `row` of the batch, whose sequence's node 0 is its row `row0` and token `pos0`. Bits of the 32 tokens from
+// t0 on that it sees: those before pos0, as far as the window goes (not here), and its mask's nodes. None without a
+// position, or where the row's own token has no place.
+struct TreeRow {
+    const uint32_t* mask;
+    int words;     // 0: it sees nothing
+    int position;  // at least pos0
+    int pos0;
+};
+
+__device__ __forceinline__ TreeRow tree_row(const TreeView& tree, int row0, int pos0, int row)
+{
+    TreeRow x;
+    const int p = tree.positions[row];
+    x.mask = tree.masks + static_cast<int64_t>(row) * tree.words;
+    x.words = p < 0 || pos0 + (row - row0) < 0 ? 0 : tree.words;
+    x.position = p > pos0 ? p : pos0;
+    x.pos0 = pos0;
+    return x;
+}
+
+// The lowest n bits, 0 <= n <= 32 or beyond either end.
+__device__ __forceinline__ uint32_t ones_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1u; }
+
+__device__ __forceinline__ uint32_t tree_bits(const TreeRow& x, int t0)
+{
+    if (x.words == 0) return 0u;
+    const int c = t0 - x.pos0, w = c >> 5;  // node of t0, negative before them
+    const uint32_t lo = static_cast<uint32_t>(w) < static_cast<uint32_t>(x.words) ? x.mask[w] : 0u;
+    const uint32_t hi = static_cast<uint32_t>(w + 1) < static_cast<uint32_t>(x.words) ? x.mask[w + 1] : 0u;
+    return __funnelshift_r(lo, hi, c & 31) | ones_below(-c);
+}
+
 // Exponent of the power of two that brings values of at most `top` (fp32 bits, finite) below 2^15, inside f16;
 // it and its negative are exponents of normal fp32 values.
 __device__ __forceinline__ int f16_exponent(uint32_t top)

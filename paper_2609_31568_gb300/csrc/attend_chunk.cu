@@ -52,8 +52,9 @@ constexpr int kMergeTiles = 4;        // what writing and merging one piece per 
 // it, 332 and 329 us at 1,024 over 16K (476 where they did not, with a limit of 2^3).
 constexpr int kRowsApart = 5;
 
-// A CTA's work. Rows [row0, row0 + ntok) of the row tensors are tokens pos ..; key tiles
-// [k0, k1) of those the job's rows see; slot >= 0: partial results there.
+// A CTA's work. Rows [row0, row0 + ntok) of the row tensors are tokens pos .. (of drafted trees, where a row may see any
+// node: pos is the token of the sequence's first); key tiles [k0, k1) of those the job's rows see; slot >= 0:
+// partial results there.
 struct ChunkJob {
     int b, j, row0, ntok;
     int pos, k0, k1, slot;
@@ -197,9 +198,9 @@ __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_consta
         const int first = (n - 1 - (rem - jb->j * n)) * per_item;
         jb->row0 = s.row0 + first;
         jb->ntok = s.rows - first < per_item ? s.rows - first : per_item;
-        jb->pos = s.pos0 + first;
+        jb->pos = s.pos0 + (a.a.tree.masks ? 0 : first);
         jb->k0 = 0;
-        jb->k1 = tiles_of(a.a, jb->pos, jb->ntok).n;
+        jb->k1 = tiles_of(a.a, jb->pos, a.a.tree.masks ? s.rows : jb->ntok).n;
         jb->slot = -1;
     };
     const int whole = items > 2 * kMaxSms ? static_cast<int>(items) / a.sms * a.sms : 0;
@@ -352,9 +353,6 @@ static_assert(chunk_smem(true) <= 227 * 1024 && chunk_smem(false) <= 227 * 1024,
 // for whole groups of four warps in the register split: 2 x 128 x 192 + 2 x 128 x 64 = 512 x 128).
 __host__ __device__ constexpr int chunk_threads(bool e4m3) { return e4m3 ? 512 : 320; }
 
-// The lowest n bits, 0 <= n <= 32 or beyond either end.
-__device__ __forceinline__ uint32_t ones_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1u; }
-
 __device__ __forceinline__ float4 lds_f4(uint32_t addr)
 {
     float4 r;
@@ -367,6 +365,7 @@ struct JobView {
     ChunkJob job;
     Tiles tiles;
     int nq, last, lo, T, n_sink;
+    int first_row;  // of the job's sequence, where its rows are drafted nodes
     // first token of the job's key tile t
     __device__ __forceinline__ int token_of(int t) const
     {
@@ -377,9 +376,17 @@ struct JobView {
     __device__ __forceinline__ bool unseen(int t) const { return t > last || (t < lo && t >= n_sink); }
     // whether that holds for a token of the tile at t0
     __device__ __forceinline__ bool has_unseen(int t0) const { return t0 + kTile - 1 > last || (t0 < lo && t0 + kTile - 1 >= n_sink); }
+    // Drafted nodes: of the 32 tokens from t0 on those that a row of the job sees (a window aside). The warp's lanes share the rows.
+    __device__ __forceinline__ uint32_t nodes_seen(const TreeView& tree, int t0) const
+    {
+        uint32_t bits = 0;
+        for (int i = threadIdx.x & 31; i < job.ntok; i += 32) bits |= tree_bits(tree_row(tree, first_row, job.pos, job.row0 + i), t0);
+        return __reduce_or_sync(0xFFFFFFFFu, bits);
+    }
 };
 
 // Waits for the plan, then reads the job of this CTA.
+template <bool TREE>
 __device__ __forceinline__ JobView load_job(const ChunkArgs& a)
 {
     pdl_enter();
@@ -388,10 +395,17 @@ __device__ __forceinline__ JobView load_job(const ChunkArgs& a)
     const int4 x = reinterpret_cast<const int4*>(a.p.jobs + blockIdx.x)[0], y = reinterpret_cast<const int4*>(a.p.jobs + blockIdx.x)[1];
     v.job = ChunkJob{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
     v.nq = v.job.ntok > a.tile_tokens ? 2 : 1;
-    v.last = v.job.pos + v.job.ntok - 1;
+    int n = v.job.ntok;
+    v.first_row = 0;
+    if (TREE && static_cast<int>(blockIdx.x) < n_jobs) {
+        const Seq s = seq_of(a.a, a.b, v.job.b);
+        v.first_row = s.row0;
+        n = s.rows;
+    }
+    v.last = v.job.pos + n - 1;
     v.lo = a.a.n_local >= 0 && v.job.pos > a.a.n_local ? v.job.pos - a.a.n_local : 0;
     v.n_sink = a.a.n_sink;
-    v.tiles = tiles_of(a.a, v.job.pos, v.job.ntok);
+    v.tiles = tiles_of(a.a, v.job.pos, n);
     v.T = static_cast<int>(blockIdx.x) < n_jobs ? v.job.k1 - v.job.k0 : 0;
     return v;
 }
@@ -456,7 +470,9 @@ __device__ __forceinline__ bool mma_issue_codes(ChunkShared& sh, uint32_t tmem, 
     return true;
 }
 
-template <bool E4M3>
+// TREE: the new tokens are nodes of drafted trees. A row's mask joins the logits of the tiles that hold new tokens, 32
+// columns a word; positions say where its window ends. Every other tile is as it was.
+template <bool E4M3, bool TREE>
 __global__ void __launch_bounds__(chunk_threads(E4M3), 1)
 k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
         const __grid_constant__ CUtensorMap tv, const __grid_constant__ ChunkArgs a)
@@ -520,7 +536,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
 
     if (warp >= 8) {
         if (E4M3) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        const JobView jv = load_job(a);
+        const JobView jv = load_job<TREE>(a);
         const ChunkJob& job = jv.job;
         const int T = jv.T, nq = jv.nq;
         if (T == 0) {
@@ -601,7 +617,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 const uint64_t kdesc0 = sdesc_sw128(smem_addr(smem + kOffK), 16, 1024);
                 const uint64_t vdesc0 = sdesc_sw128(smem_addr(smem + off_v(E4M3)), kHalf, 1024);
                 // the last key tile may lie after every row of the first query tile
-                const bool skip_last = T > 1 && jv.token_of(T - 1) > job.pos + tt - 1;
+                const bool skip_last = !TREE && T > 1 && jv.token_of(T - 1) > job.pos + tt - 1;
                 if (ok && E4M3) {
                     ok = mma_issue_codes(sh, tmem, qdesc0, kdesc0, vdesc0, nq, T, skip_last, a.timeout_ns);
                 } else if (ok) {
@@ -651,7 +667,14 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 uint8_t* const to0 = to + (((c0 + late) ^ (r16 & 7)) << 4);
                 uint8_t* const to1 = to + (((c0 + 1 - late) ^ (r16 & 7)) << 4);
                 const int t0 = jv.token_of(t);
-                const bool unseen = jv.has_unseen(t0);
+                bool unseen = jv.has_unseen(t0);
+                uint64_t nodes[2] = {~0ull, ~0ull};  // of the tile's keys those that a row sees
+                if (TREE && t0 + kTile - 1 >= job.pos) {
+                    unseen = true;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        nodes[i] = jv.nodes_seen(a.a.tree, t0 + 64 * i) | static_cast<uint64_t>(jv.nodes_seen(a.a.tree, t0 + 64 * i + 32)) << 32;
+                }
 #pragma unroll 1  // (the instruction cache: see mma_issue_codes)
                 for (int i = 0; i < 8; ++i) {
                     const uint4 w = *reinterpret_cast<const uint4*>(from + i * 16 * kHeadDim);
@@ -659,7 +682,8 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                     const uint2 y0 = e4m3x4_to_bf16(w.x, f), y1 = e4m3x4_to_bf16(w.y, f);
                     const uint2 y2 = e4m3x4_to_bf16(w.z, f), y3 = e4m3x4_to_bf16(w.w, f);
                     uint4 p = make_uint4(y0.x, y0.y, y1.x, y1.y), q = make_uint4(y2.x, y2.y, y3.x, y3.y);
-                    if (unseen && jv.unseen(t0 + 16 * i + r16)) p = q = make_uint4(0, 0, 0, 0);
+                    if (unseen && (jv.unseen(t0 + 16 * i + r16) || (TREE && !((i < 4 ? nodes[0] : nodes[1]) >> ((16 * i + r16) & 63) & 1u))))
+                        p = q = make_uint4(0, 0, 0, 0);
                     *reinterpret_cast<uint4*>(to0 + i * 16 * 128) = late ? q : p;
                     *reinterpret_cast<uint4*>(to1 + i * 16 * 128) = late ? p : q;
                 }
@@ -717,6 +741,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
         // the tile's first, which is also the last that all of the tile's rows see (8-bit: or -1, to mask every tile), and the
         // first from which the window hides nothing of the tile; the CTA's last token
         int T = 0, k0 = 0, sinks = 0, past = 0, p = 0, pos_first = 0, plain_to = 0, open_from = 0, last = 0;
+        TreeRow node{};  // TREE: this row's mask; pos_first is the token of the sequence's first node, p the row's position
         int seq = 0, kvh = 0;
         auto token_of = [&](int t) { return (k0 + t < sinks ? k0 + t : k0 + t + past) * kTile; };
         // 8-bit: lane x looks up the scales of the keys 4 x .. 4 x + 3 of a tile, its page two tiles ahead, the bytes one
@@ -742,7 +767,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
 #pragma unroll 1
         for (int t = first_wave ? -1 : 0;; ++t) {
             if (t == 0) {
-                const JobView jv = load_job(a);
+                const JobView jv = load_job<TREE>(a);
                 T = qt < jv.nq ? jv.T : 0;
                 k0 = jv.job.k0;
                 sinks = jv.tiles.sinks;
@@ -750,11 +775,23 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 seq = jv.job.b;
                 kvh = jv.job.j;
                 last = jv.last;
-                pos_first = plain_to = jv.job.pos + qt * tt;
-                const int pos_last = qt + 1 == jv.nq ? jv.last : pos_first + tt - 1;
-                p = pos_first + r / g;
-                p = p < pos_last ? p : pos_last;  // rows past the tile's end see what its last row sees
-                open_from = a.a.n_local >= 0 && pos_last > a.a.n_local ? pos_last - a.a.n_local : 0;
+                if (TREE) {
+                    const int row = qt * tt + r / g;  // rows past the tile's end see what its last row sees
+                    node = TreeRow{};
+                    if (T > 0) node = tree_row(a.a.tree, jv.first_row, jv.job.pos, jv.job.row0 + (row < jv.job.ntok ? row : jv.job.ntok - 1));
+                    p = node.position;
+                    pos_first = jv.job.pos;
+                    // a row without keys: every tile is masked
+                    plain_to = __any_sync(0xFFFFFFFFu, node.words == 0) ? -1 : pos_first - 1;
+                    const int pos_last = __reduce_max_sync(0xFFFFFFFFu, p);
+                    open_from = a.a.n_local >= 0 && pos_last > a.a.n_local ? pos_last - a.a.n_local : 0;
+                } else {
+                    pos_first = plain_to = jv.job.pos + qt * tt;
+                    const int pos_last = qt + 1 == jv.nq ? jv.last : pos_first + tt - 1;
+                    p = pos_first + r / g;
+                    p = p < pos_last ? p : pos_last;  // rows past the tile's end see what its last row sees
+                    open_from = a.a.n_local >= 0 && pos_last > a.a.n_local ? pos_last - a.a.n_local : 0;
+                }
                 m_run = -INFINITY;
                 l_run = 0.f;
                 if (E4M3 && T > 0) {
@@ -831,8 +868,10 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
             tc_fence_after();
             const int t0 = token_of(t);
             const bool masked = t < 0 || t0 + kTile - 1 > plain_to || (t0 < open_from && t0 + kTile - 1 >= a.a.n_sink);
-            const int lim = p - t0 + 1;  // keys t0 + c with c >= lim are in the future
-            const int gap = a.a.n_sink - t0, low = a.a.n_local >= 0 && p - t0 > a.a.n_local ? p - t0 - a.a.n_local : 0;
+            const int lim = (TREE ? last : p) - t0 + 1;  // keys t0 + c with c >= lim are in the future, or past the nodes
+            const int gap = a.a.n_sink - t0;
+            int low = a.a.n_local >= 0 && p - t0 > a.a.n_local ? p - t0 - a.a.n_local : 0;
+            if (TREE) low = low < pos_first - t0 ? low : pos_first - t0;  // the window does not hide nodes
             // Fast: exponentials against the reference as it stands, all of the row at once, unless something is hidden or
             // the sum shows a logit far above the reference (the limits of k_sparse_attn). Slow: the maximum first, and 32
             // columns at a time in loops, so that its instructions leave the fast path's in the cache (4,096 tokens
@@ -857,7 +896,8 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 // a bit per column: columns below x of these 32 are ones_below(x - 32 c)
                 auto load_32 = [&](uint32_t (&sr)[32], int c) {
                     tmem_ld32(s_addr + c * 32, sr);
-                    const uint32_t seen = masked ? ones_below(lim - 32 * c) & ~(ones_below(low - 32 * c) & ~ones_below(gap - 32 * c)) : 0xFFFFFFFFu;
+                    uint32_t seen = 0xFFFFFFFFu;
+                    if (masked) seen = (TREE ? tree_bits(node, t0 + 32 * c) : 0xFFFFFFFFu) & ones_below(lim - 32 * c) & ~(ones_below(low - 32 * c) & ~ones_below(gap - 32 * c));
                     tmem_ld_wait();
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
@@ -937,8 +977,9 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                     ok = false;
                     break;
                 }
+                const uint32_t nodes = TREE && t0 + kTile - 1 >= pos_first ? load_job<TREE>(a).nodes_seen(a.a.tree, t0 + 32 * quarter) : 0xFFFFFFFFu;
                 const int tok = t0 + r, lo = a.a.n_local >= 0 && pos_first > a.a.n_local ? pos_first - a.a.n_local : 0;
-                if (tok > last || (tok < lo && tok >= a.a.n_sink)) {
+                if (tok > last || (tok < lo && tok >= a.a.n_sink) || !(nodes >> lane & 1u)) {
                     uint8_t* row = smem + off_v(false) + (t & 1) * kTileBytes + r * 128;
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
@@ -950,7 +991,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
             mbar_arrive(&bars.p_full[qt]);
         }
         if (T > 0) {
-            const JobView jv = load_job(a);  // (again: nothing of it is kept through the loop)
+            const JobView jv = load_job<TREE>(a);  // (again: nothing of it is kept through the loop)
             const ChunkJob& job = jv.job;
             bool go = __all_sync(0xFFFFFFFFu, ok && !abort_flag);
             if (go) go = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.o_full, 0, a.timeout_ns, &abort_flag));
@@ -1094,6 +1135,7 @@ __global__ void __launch_bounds__(256, kMergeCtas) k_chunk_merge(const __grid_co
             const int x = live_row(r + i);
             if (x >= y0.z * a.a.g) continue;
             const float inv = l == 0.f ? 0.f : 1.0f / l;
+            if (l == 0.f) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);  // no keys, beside values that are not finite too
             const int64_t row = y0.y + x / a.a.g;
             const int h = y0.x * a.a.g + x % a.a.g;
             auto* out = static_cast<__nv_bfloat16*>(a.a.out) + row * a.a.out_stride + h * kHeadDim;
@@ -1143,7 +1185,7 @@ ChunkWs chunk_layout(int g, int Hkv, int n_seqs, int n_rows, int max_rows)
     return w;
 }
 
-template <bool E4M3>
+template <bool E4M3, bool TREE>
 cudaError_t run_chunks(const ChunkArgs& a, cudaStream_t st)
 {
     CUtensorMap tq, tk, tv;
@@ -1156,10 +1198,10 @@ cudaError_t run_chunks(const ChunkArgs& a, cudaStream_t st)
         ok = ok && scale_host::make_token_major_map(&tk, a.c.k, kHeadDim, a.c.Hkv, pool, 64, a.box) &&
              scale_host::make_token_major_map(&tv, a.c.v, kHeadDim, a.c.Hkv, pool, 64, a.box);
     if (!ok) return cudaErrorInvalidValue;
-    cudaError_t e = cudaFuncSetAttribute(k_chunk<E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(chunk_smem(E4M3)));
+    cudaError_t e = cudaFuncSetAttribute(k_chunk<E4M3, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(chunk_smem(E4M3)));
     if (e == cudaSuccess) e = launch_after(st, dim3(1), kPlanThreads, 0, 1, k_chunk_plan, a);
     if (e == cudaSuccess)
-        e = launch_after(st, dim3(a.p.max_jobs), chunk_threads(E4M3), chunk_smem(E4M3), 1, k_chunk<E4M3>, tq, tk, tv, a);
+        e = launch_after(st, dim3(a.p.max_jobs), chunk_threads(E4M3), chunk_smem(E4M3), 1, k_chunk<E4M3, TREE>, tq, tk, tv, a);
     const int merge_ctas = a.p.max_merges * (a.part_rows / 32), most = a.sms * kMergeCtas;
     if (e == cudaSuccess) e = launch_after(st, dim3(merge_ctas < most ? merge_ctas : most), 256, 0, 1, k_chunk_merge, a);
     return e;
@@ -1191,7 +1233,8 @@ cudaError_t launch_chunks(const AttendView& a, const CacheView& c, bool e4m3, co
     x.part_rows = w.part_rows;
     x.status = status;
     x.timeout_ns = timeout_ns;
-    return e4m3 ? run_chunks<true>(x, st) : run_chunks<false>(x, st);
+    if (a.tree.masks) return e4m3 ? run_chunks<true, true>(x, st) : run_chunks<false, true>(x, st);
+    return e4m3 ? run_chunks<true, false>(x, st) : run_chunks<false, false>(x, st);
 }
 
 }  // namespace scale

@@ -110,6 +110,13 @@ cudaError_t launch_append(const CacheView& c, bool e4m3, const BatchView& b, con
 cudaError_t launch_cache_read(const CacheView& c, bool e4m3, const BatchView& b, void* k_out, int64_t k_stride,
                               void* v_out, int64_t v_stride, cudaStream_t st);
 
+// The drafted trees of a batch; without masks its rows attend causally.
+struct TreeView {
+    const int32_t* positions;
+    const uint32_t* masks;
+    int words;
+};
+
 struct AttendView {
     int Hq, g, n_sink, n_local;
     float scale_log2;
@@ -118,6 +125,7 @@ struct AttendView {
     void* out;
     int64_t out_stride;
     float* lse;
+    TreeView tree;
 };
 size_t attend_ws_bytes(int Hq, int Hkv, bool e4m3, int n_seqs, int n_rows, int max_rows);
 cudaError_t launch_attend(const AttendView& a, const CacheView& c, bool e4m3, const BatchView& b, uint8_t* ws,

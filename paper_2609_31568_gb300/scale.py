@@ -29,6 +29,8 @@ SCALE_MODE_PER_CLUSTER = 0
 SCALE_MODE_PER_SUBCHUNK = 1
 SCALE_CACHE_BF16 = 0
 SCALE_CACHE_E4M3 = 1
+SCALE_LOGITS_BF16 = 0
+SCALE_LOGITS_FP32 = 1
 
 
 class ScaleLibraryMissing(RuntimeError):
@@ -113,6 +115,27 @@ class ScaleAttend(ctypes.Structure):
                 ("attn_scale", ctypes.c_float)]
 
 
+class ScaleTree(ctypes.Structure):
+    """scale_tree_t: the drafted trees of a batch (device pointers)."""
+
+    _fields_ = [("parents", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("masks", ctypes.c_void_p),
+                ("mask_words", ctypes.c_int32)]
+
+
+class ScaleMoves(ctypes.Structure):
+    """scale_moves_t: rows that move within a cache (device pointers)."""
+
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("start", ctypes.c_void_p),
+                ("n_groups", ctypes.c_int32), ("n_moves", ctypes.c_int32)]
+
+
+class ScaleBeam(ctypes.Structure):
+    """scale_beam_t."""
+
+    _fields_ = [("n_groups", ctypes.c_int32), ("n_beams", ctypes.c_int32), ("vocab", ctypes.c_int32),
+                ("n_best", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
 def kv_cache(k_pages, v_pages, k_scales=None, v_scales=None) -> ScaleCache:
     """Descriptor of a paged cache: pages bf16 [num_pages][page_size][H_kv][128], or 8-bit (uint8 or
     float8_e4m3fn) with scales uint8 [num_pages][H_kv][page_size]. It keeps the tensors alive."""
@@ -184,6 +207,51 @@ def attend_params(*, num_q_heads: int, n_sink: int = 0, n_local: int = -1, attn_
     return ScaleAttend(num_q_heads, n_sink, n_local, attn_scale)
 
 
+def draft_tree(parents, positions, masks) -> ScaleTree:
+    """Descriptor of a batch's drafted trees: parents and positions int32 [n_rows] (parents may be None where only
+    the attention is called), masks int32 or uint32 [n_rows][mask_words]. It keeps the tensors alive."""
+    if positions.dim() != 1 or masks.dim() != 2 or masks.shape[0] != positions.shape[0]:
+        raise ValueError("a tree has positions [n_rows] and masks [n_rows][mask_words]")
+    if parents is not None and parents.shape != positions.shape:
+        raise ValueError("parents are [n_rows] as the positions are")
+    _int32(positions, masks, *(() if parents is None else (parents,)))
+    t = ScaleTree(_ptr(parents), _ptr(positions), _ptr(masks), masks.shape[1])
+    t.n_rows = positions.shape[0]
+    t.tensors = (parents, positions, masks)
+    return t
+
+
+def cache_moves(src, dst, start=None, n_groups: int | None = None) -> ScaleMoves:
+    """Descriptor of rows that move within a cache: src and dst int32 [n_moves], in groups from `start` int32
+    [n_groups + 1] on, or in `n_groups` of the same size. It keeps the tensors alive."""
+    if src.dim() != 1 or src.shape != dst.shape or (start is None) == (n_groups is None):
+        raise ValueError("moves are src and dst [n_moves], and either start [n_groups + 1] or n_groups")
+    _int32(src, dst, *(() if start is None else (start,)))
+    if start is not None and (start.dim() != 1 or start.shape[0] < 2):
+        raise ValueError("start is int32 [n_groups + 1]")
+    n_groups = start.shape[0] - 1 if n_groups is None else n_groups
+    _in_int32(n_groups=n_groups, n_moves=src.shape[0])
+    m = ScaleMoves(_ptr(src), _ptr(dst), _ptr(start), n_groups, src.shape[0])
+    m.tensors = (src, dst, start)
+    return m
+
+
+def cache_layers(caches) -> ctypes.Array:
+    """The caches of a batch's layers (as kv_cache gives them) for the calls that take all of them. It keeps their
+    tensors alive."""
+    layers = (ScaleCache * len(caches))(*caches)
+    layers.tensors = [c.tensors for c in caches]
+    return layers
+
+
+def beam_params(*, n_groups: int, n_beams: int, vocab: int, n_best: int) -> ScaleBeam:
+    """Groups of beams; the type of the logits is that of the tensor that a call gets."""
+    _in_int32(n_groups=n_groups, n_beams=n_beams, vocab=vocab, n_best=n_best)
+    b = ScaleBeam(n_groups, n_beams, vocab, n_best, SCALE_LOGITS_BF16)
+    b.fp32 = ScaleBeam(n_groups, n_beams, vocab, n_best, SCALE_LOGITS_FP32)
+    return b
+
+
 def params(*, num_q_heads, num_kv_heads, head_dim=128, sub_chunk, n_tokens, max_cluster_subchunks,
            outer_chunk=0, theta=-1.0, block_size, top_k, n_sink, n_local, select_scale=1.0,
            attn_scale=0.0) -> ScaleParams:
@@ -230,6 +298,7 @@ def load() -> ctypes.CDLL:
         kp = ctypes.POINTER(ScaleKvPages)
         cp, bp = ctypes.POINTER(ScaleCache), ctypes.POINTER(ScaleBatch)
         rp, ap = ctypes.POINTER(ScaleRope), ctypes.POINTER(ScaleAttend)
+        tp, mp, ep = ctypes.POINTER(ScaleTree), ctypes.POINTER(ScaleMoves), ctypes.POINTER(ScaleBeam)
         sig = {
             "scale_workspace_size": [pp, i32, ctypes.POINTER(sz)],
             "scale_workspace_init": [P, sz, P],
@@ -252,6 +321,13 @@ def load() -> ctypes.CDLL:
             "scale_cache_read": [cp, bp, P, i64, P, i64, P],
             "scale_cache_attend_workspace_size": [ap, cp, bp, ctypes.POINTER(sz)],
             "scale_cache_attend": [ap, cp, bp, P, i64, P, i64, P, P, sz, P],
+            "scale_tree_plan": [tp, bp, i32, i32, P],
+            "scale_cache_attend_tree": [ap, tp, cp, bp, P, i64, P, i64, P, P, sz, P],
+            "scale_cache_move": [cp, i32, mp, P],
+            "scale_tree_accept": [tp, cp, bp, P, P, P, P, P, P, P, mp, P],
+            "scale_beam_workspace_size": [ep, ctypes.POINTER(sz)],
+            "scale_beam_select": [ep, P, i64, P, P, P, P, P, sz, P],
+            "scale_beam_reorder": [cp, i32, i32, P, P, P, i32, P, mp, P],
             "scale_get_device_status": [P, P, ctypes.POINTER(i32)],
             "scale_retrieval_calls": [pp, i32, P, i32, ctypes.POINTER(i64), ctypes.POINTER(i64)],
             "scale_prefill_host_arena_size": [pp, i32, ctypes.POINTER(sz)],
@@ -549,6 +625,102 @@ def scale_cache_attend(attend: ScaleAttend, cache: ScaleCache, batch: ScaleBatch
     _check("scale_cache_attend", load().scale_cache_attend(
         ctypes.byref(attend), ctypes.byref(cache), ctypes.byref(batch), qp, qs, op, os_, _ptr(lse), _ptr(ws),
         _nbytes(ws), _stream(stream)))
+
+
+def _numbers(x, n: int, what: str) -> int | None:
+    """Address of an int32 tensor of at least n numbers."""
+    if x.itemsize != 4 or x.is_floating_point() or x.numel() < n or not x.is_contiguous():
+        raise ValueError(f"{what} is a contiguous int32 tensor of {n} numbers; got {x.dtype} {tuple(x.shape)}")
+    return x.data_ptr()
+
+
+def _floats(x, n: int, what: str) -> int | None:
+    """Address of an fp32 tensor of at least n numbers."""
+    if x.itemsize != 4 or not x.is_floating_point() or x.numel() < n or not x.is_contiguous():
+        raise ValueError(f"{what} is a contiguous fp32 tensor of {n} numbers; got {x.dtype} {tuple(x.shape)}")
+    return x.data_ptr()
+
+
+def _tree_rows(tree: ScaleTree, batch: ScaleBatch) -> None:
+    if tree.n_rows < batch.n_rows:
+        raise ValueError(f"the tree's tensors have {tree.n_rows} rows, the batch {batch.n_rows}")
+
+
+def scale_tree_plan(tree: ScaleTree, batch: ScaleBatch, n_sink: int = 0, n_local: int = -1, stream=None) -> None:
+    """The positions and masks of the batch's drafted nodes from their parents."""
+    _tree_rows(tree, batch)
+    _in_int32(n_sink=n_sink, n_local=n_local)
+    _check("scale_tree_plan", load().scale_tree_plan(ctypes.byref(tree), ctypes.byref(batch), n_sink, n_local,
+                                                     _stream(stream)))
+
+
+def scale_cache_attend_tree(attend: ScaleAttend, tree: ScaleTree, cache: ScaleCache, batch: ScaleBatch, q, out, lse, ws,
+                            stream=None) -> None:
+    """Attention of drafted nodes over their sequences in the cache and their masks' nodes; lse fp32 [n_rows][H_q]
+    or None. Workspace as scale_cache_attend's."""
+    _tree_rows(tree, batch)
+    qp, qs, _ = _rows(q, batch.n_rows, attend.num_q_heads)
+    op, os_, _ = _rows(out, batch.n_rows, attend.num_q_heads)
+    lp = None if lse is None else _floats(lse, batch.n_rows * attend.num_q_heads, "lse")
+    _check("scale_cache_attend_tree", load().scale_cache_attend_tree(
+        ctypes.byref(attend), ctypes.byref(tree), ctypes.byref(cache), ctypes.byref(batch), qp, qs, op, os_, lp,
+        _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
+def scale_cache_move(caches, moves: ScaleMoves, stream=None) -> None:
+    """Rows moved within each of the caches (cache_layers)."""
+    _check("scale_cache_move", load().scale_cache_move(caches, len(caches), ctypes.byref(moves), _stream(stream)))
+
+
+def scale_tree_accept(tree: ScaleTree, caches, batch: ScaleBatch, tokens, choices, first, n_accepted, path, next_token,
+                      new_len, moves: ScaleMoves, stream=None) -> None:
+    """The walk down each drafted tree along the model's choices; `first` may be None. `moves` (with the batch's
+    row_start as its start) get the accepted rows' moves for scale_cache_move over `caches`."""
+    _tree_rows(tree, batch)
+    if tree.parents is None and batch.n_rows:
+        raise ValueError("the tree has no parents")
+    n, seqs = batch.n_rows, batch.n_seqs
+    _check("scale_tree_accept", load().scale_tree_accept(
+        ctypes.byref(tree), caches, ctypes.byref(batch), _numbers(tokens, n, "tokens"), _numbers(choices, n, "choices"),
+        None if first is None else _numbers(first, seqs, "first"), _numbers(n_accepted, seqs, "n_accepted"),
+        _numbers(path, n, "path"), _numbers(next_token, seqs, "next_token"), _numbers(new_len, seqs, "new_len"),
+        ctypes.byref(moves), _stream(stream)))
+
+
+def scale_beam_workspace_size(beam: ScaleBeam) -> int:
+    n = ctypes.c_size_t()
+    _check("scale_beam_workspace_size", load().scale_beam_workspace_size(ctypes.byref(beam), ctypes.byref(n)))
+    return n.value
+
+
+def scale_beam_select(beam: ScaleBeam, logits, scores, best_scores, best_beams, best_tokens, ws, stream=None) -> None:
+    """The best continuations of each group of beams. logits bf16 or fp32 [n_groups * n_beams][vocab], whose rows may
+    lie apart; scores fp32 [n_groups][n_beams]; the outputs [n_groups][n_best] (fp32, int32, int32)."""
+    rows, kept = beam.n_groups * beam.n_beams, beam.n_groups * beam.n_best
+    torch = _torch or _imported_torch()
+    if logits.dim() != 2 or logits.shape[0] < rows or logits.shape[1] != beam.vocab or logits.stride(1) != 1 or \
+            logits.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"logits are bf16 or fp32 [{rows}][{beam.vocab}]; got {logits.dtype} {tuple(logits.shape)}")
+    b = beam if logits.dtype is torch.bfloat16 else beam.fp32
+    stride = logits.stride(0) if logits.shape[0] > 1 else beam.vocab
+    _check("scale_beam_select", load().scale_beam_select(
+        ctypes.byref(b), logits.data_ptr(), stride, _floats(scores, rows, "scores"),
+        _floats(best_scores, kept, "best_scores"), _numbers(best_beams, kept, "best_beams"),
+        _numbers(best_tokens, kept, "best_tokens"), _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
+def scale_beam_reorder(caches, page_table, kv_len, parents, table_out, moves: ScaleMoves, stream=None) -> None:
+    """The beams' page tables in their new order. parents int32 [n_groups][n_beams], kv_len [n_groups * n_beams],
+    page_table and table_out (which may be the same) [n_groups * n_beams][pages]; `moves` [beams * page_size], in a
+    group for each beam, are for scale_cache_move over `caches`."""
+    if parents.dim() != 2 or page_table.dim() != 2 or page_table.shape != table_out.shape or \
+            page_table.shape[0] != parents.numel():
+        raise ValueError("parents are [n_groups][n_beams], the tables [n_groups * n_beams][pages]")
+    beams = parents.numel()
+    _check("scale_beam_reorder", load().scale_beam_reorder(
+        caches, parents.shape[0], parents.shape[1], _numbers(parents, beams, "parents"), _numbers(kv_len, beams, "kv_len"),
+        _numbers(page_table, 0, "page_table"), page_table.shape[1], _numbers(table_out, 0, "table_out"),
+        ctypes.byref(moves), _stream(stream)))
 
 
 def scale_get_device_status(ws, stream=None) -> int:
