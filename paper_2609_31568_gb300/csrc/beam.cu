@@ -16,11 +16,10 @@ using namespace scale_ptx;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kPer = 32;                       // logits of a thread in a step
+constexpr int kPer = 16;                       // logits of a thread in a step
 constexpr int kStepLogits = kThreads * kPer;   // of a CTA
-constexpr int kQuarter = kStepLogits / 4;
-constexpr int kList = kQuarter + kMaxBest;     // candidates that a CTA holds
-constexpr int kMine = (kList + kThreads - 1) / kThreads;
+constexpr int kHalf = kStepLogits / 2;
+constexpr int kList = kHalf + kMaxBest;        // candidates that a CTA holds
 constexpr int kResident = 4;                   // CTAs of an SM
 constexpr int kMaxCandidates = 4096;           // of a group, for k_beam_pick
 constexpr int kMaxParts = 32;                  // of a row
@@ -53,15 +52,16 @@ struct SelectArgs {
 };
 
 struct SelectShared {
-    uint64_t list[kList];
+    uint64_t list[kList], other[kList];
     uint64_t bound[kWarps];
     float2 sums[kWarps];
     int n, kept;
+    float4 x[kWarps][kPer / 4][32];  // a warp's logits of a step, where it has candidates among them or the row ends
 };
 
-// A key that at least `keep` of the threads' `mine` reach (each its thread's largest candidate): every warp's largest but
-// each - 1, each = keep / warps rounded up, and the least of those. 0 where a warp has fewer.
-__device__ __forceinline__ uint64_t bound_of(SelectShared& sh, uint64_t mine, int keep)
+// A key that at least `keep` of the threads' `mine` reach (all different, or 0): every warp's each-th largest, each = keep /
+// warps rounded up, and the least of those. 0 where a warp has fewer.
+__device__ __noinline__ uint64_t bound_of(SelectShared& sh, uint64_t mine, int keep)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int each = (keep + kWarps - 1) / kWarps;
@@ -74,48 +74,54 @@ __device__ __forceinline__ uint64_t bound_of(SelectShared& sh, uint64_t mine, in
     if (lane == 0) sh.bound[warp] = bound;
     __syncthreads();
     bound = sh.bound[0];
-#pragma unroll
+#pragma unroll 1
     for (int w = 1; w < kWarps; ++w) bound = sh.bound[w] < bound ? sh.bound[w] : bound;
     return bound;
 }
 
-// The best `keep` of the list's candidates, in descending order at its front. Those below bound_of() go first; the others,
-// a few more than are kept, are ranked one against the other. Every thread calls it, behind a barrier, and leaves
-// through one.
-__device__ __forceinline__ void tighten(SelectShared& sh, int keep)
+// The best `keep` of the list's n candidates, in descending order at its front; returns how many those are. Those below
+// bound_of() go first; the others, a few more than are kept, are ranked one against the other. Every thread calls
+// it, behind a barrier, and leaves through one.
+__device__ __noinline__ int tighten(SelectShared& sh, int n, int keep)
 {
-    const int tid = threadIdx.x, n = sh.n;
-    uint64_t mine[kMine], top = 0;
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-        const int at = i * kThreads + (tid & 31) * kWarps + (tid >> 5);  // every warp gets its share of a short list
-        mine[i] = at < n ? sh.list[at] : 0;
-        top = mine[i] > top ? mine[i] : top;
-    }
+    const int tid = threadIdx.x, at0 = (tid & 31) * kWarps + (tid >> 5);  // every warp gets its share of a short list
+    uint64_t top = 0;
+#pragma unroll 1
+    for (int at = at0; at < n; at += kThreads) top = sh.list[at] > top ? sh.list[at] : top;
     if (tid == 0) sh.kept = 0;
     const uint64_t bound = bound_of(sh, top, keep);
-#pragma unroll
-    for (int i = 0; i < kMine; ++i)
-        if (mine[i] != 0 && mine[i] >= bound) sh.list[atomicAdd(&sh.kept, 1)] = mine[i];
-    __syncthreads();
-    const int m = sh.kept;
-    int rank[kMine];
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-        const int at = i * kThreads + tid;
-        rank[i] = keep;
-        if (at < m) {
-            mine[i] = sh.list[at];
-            rank[i] = 0;
-            for (int j = 0; j < m; ++j) rank[i] += sh.list[j] > mine[i];
-        }
+#pragma unroll 1
+    for (int at = at0; at < n; at += kThreads) {
+        const uint64_t x = sh.list[at];
+        if (x >= bound) sh.other[atomicAdd(&sh.kept, 1)] = x;
     }
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kMine; ++i)
-        if (rank[i] < keep) sh.list[rank[i]] = mine[i];
-    if (tid == 0) sh.n = m < keep ? m : keep;
+    const int m = sh.kept;
+#pragma unroll 1
+    for (int at = tid; at < m; at += kThreads) {
+        const uint64_t x = sh.other[at];
+        int rank = 0;
+#pragma unroll 4
+        for (int j = 0; j < m; ++j) rank += sh.other[j] > x;
+        if (rank < keep) sh.list[rank] = x;
+    }
+    n = m < keep ? m : keep;
+    if (tid == 0) sh.n = n;
     __syncthreads();
+    return n;
+}
+
+// 16 bytes from `shift` (2 to 14) bytes on of 32.
+__device__ __forceinline__ uint4 from_two(const uint4& a, const uint4& b, int shift)
+{
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 6; ++i) w[i] = shift & 8 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = shift & 4 ? w[i + 1] : w[i];
+    const int bits = (shift & 3) * 8;
+    return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
+                      __funnelshift_r(w[3], w[4], bits));
 }
 
 template <typename T>
@@ -139,32 +145,106 @@ __device__ __forceinline__ void unpack<__nv_bfloat16>(const uint4& w, float* x)
     }
 }
 
-// 16 bytes from `shift` (2 to 14) bytes on of 32.
-__device__ __forceinline__ uint4 from_two(const uint4& a, const uint4& b, int shift)
+template <typename T>
+struct Step {
+    static constexpr int kLoad = 16 / sizeof(T);  // logits of a load
+    static constexpr int kLoads = kPer / kLoad;
+    // the i-th logit of the thread whose first is that of token `first`
+    static __device__ __forceinline__ int token(int first, int i) { return first + i / kLoad * (kThreads * kLoad) + i % kLoad; }
+};
+
+// Candidates of a warp's step whose logits lie in sh.x, of the lanes in `who`: those that reach the bound go into the list, as
+// far as it has room; sh.n counts them all. `first`: token of this lane's first logit.
+template <typename T>
+__device__ __noinline__ void collect(SelectShared& sh, uint32_t who, int first, int vocab, uint64_t bound)
 {
-    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-    for (int i = 0; i < 6; ++i) w[i] = shift & 8 ? w[i + 2] : w[i];
-#pragma unroll
-    for (int i = 0; i < 5; ++i) w[i] = shift & 4 ? w[i + 1] : w[i];
-    const int bits = (shift & 3) * 8;
-    return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
-                      __funnelshift_r(w[3], w[4], bits));
+    const int lane = threadIdx.x & 31, i = lane & (kPer - 1);
+    const float* x = reinterpret_cast<const float*>(sh.x[threadIdx.x >> 5][i >> 2]) + (i & 3);
+#pragma unroll 1
+    for (; who; who &= who - 1) {  // a lane for each of its logits
+        const int from = __ffs(who) - 1;
+        const int t = Step<T>::token(__shfl_sync(0xFFFFFFFFu, first, from), i);
+        const uint64_t c = candidate(x[from * 4], t);
+        const uint32_t in = __ballot_sync(0xFFFFFFFFu, lane < kPer && t < vocab && c >= bound);
+        if (in == 0) continue;
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&sh.n, __popc(in));
+        at = __shfl_sync(0xFFFFFFFFu, at, 0) + __popc(in & ((1u << lane) - 1u));
+        if ((in >> lane & 1u) && at < kList) sh.list[at] = c;
+    }
+}
+
+// A thread's logits of a step that the row ends in, or begins in behind a 16-byte boundary, to sh.x; -inf behind the row.
+template <typename T>
+__device__ __noinline__ void load_edge(SelectShared& sh, const T* logits, int first, int vocab)
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll 4
+    for (int i = 0; i < kPer; ++i) {
+        const int t = Step<T>::token(first, i);
+        reinterpret_cast<float*>(&sh.x[threadIdx.x >> 5][i >> 2][lane])[i & 3] = t < vocab ? static_cast<float>(logits[t]) : -INFINITY;
+    }
+}
+
+// sum of exp(x - top) of a thread's step with NaN among its logits, which count as -inf
+template <typename T>
+__device__ __noinline__ float sum_without_nan(const T* logits, int first, int vocab, float top)
+{
+    float y = 0.f;
+#pragma unroll 1
+    for (int i = 0; i < kPer; ++i) {
+        const int t = Step<T>::token(first, i);
+        if (t >= vocab) continue;
+        const float x = static_cast<float>(logits[t]);
+        if (x > -INFINITY) y += ex2((x - top) * kLog2e);
+    }
+    return y;
+}
+
+// The part's candidates again, where the list ran over: logits that come in ascending order, say. Half a step at a time, the
+// list cut and the bound raised before each.
+template <typename T>
+__device__ __noinline__ int collect_carefully(SelectShared& sh, const T* logits, int vocab, int s0, int s1, int keep)
+{
+    uint64_t bound = 0;
+    __syncthreads();
+    if (threadIdx.x == 0) sh.n = 0;
+#pragma unroll 1
+    for (int s = s0; s < s1; ++s) {
+        const int first = s * kStepLogits + static_cast<int>(threadIdx.x) * Step<T>::kLoad;
+        load_edge<T>(sh, logits, first, vocab);
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+            __syncthreads();
+            int n = sh.n;
+            __syncthreads();
+            if (n > kMaxBest) {
+                n = tighten(sh, n, keep);
+                bound = sh.list[keep - 1];  // (n was more than is kept)
+                __syncthreads();
+            }
+            collect<T>(sh, 0xFFFFu << 16 * half, first, vocab, bound);
+        }
+    }
+    __syncthreads();
+    return sh.n;
 }
 
 // Largest logit, sum of exponentials and best candidates of a part of a row of logits, one pass over them.
 //
-// A step is 8,192 logits, 32 a thread, in 16-byte loads. A row may begin anywhere; behind a 16-byte boundary a thread puts its
-// logits together from two loads, so that it has the same tokens wherever the row lies: rows of the same logits have the
-// same sum to the bit, and equal scores stay equal. The sum is a thread's own against its own largest logit, with what a step's sum loses carried to the
-// next. The first step sets the bound that a candidate has to pass (bound_of); from then on a step whose threads all stay
-// below it, which their largest logits tell, needs nothing more. The candidates wait in a list, which is cut to
-// the n_best largest, and the bound raised to the least of them, when it could run over, and at the end.
-template <typename T>
+// A step is 4,096 logits, 16 a thread, in 16-byte loads that are made two steps ahead. SKEW: rows begin anywhere; behind a
+// 16-byte boundary a thread puts its logits together from its load and its neighbour's, so that it has the same tokens
+// wherever the row lies: rows of the same logits have the same sum to the bit, and equal scores stay equal. The sum is a
+// thread's own against its own largest logit, with what a step's sum loses carried to the next. The first step sets the
+// bound that a candidate has to reach (bound_of, then the least of the n_best best of the step); from then on warps go on
+// without barriers, and one whose threads all stay at or below the bound, which their largest logits tell, needs nothing
+// more. The candidates wait in a list, which is cut at the end. What is rare lies in functions of its own: the loop has to
+// stay in the instruction cache (unrolled for 32 logits with the candidates' code in it, 64 x 8 rows of 128,000 took 90 to
+// 300 us, by where the code came to lie).
+template <typename T, bool SKEW>
 __global__ void __launch_bounds__(kThreads, kResident) k_beam_part(const __grid_constant__ SelectArgs a)
 {
-    constexpr int kLoad = 16 / sizeof(T);  // logits of a load
-    constexpr int kLoads = kPer / kLoad;
+    constexpr int kLoad = Step<T>::kLoad, kLoads = Step<T>::kLoads;
     __shared__ SelectShared sh;
     pdl_enter();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -172,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, kResident) k_beam_part(const __grid_
     const int keep = a.b.n_best, vocab = a.b.vocab;
     uint64_t* const out = a.best + static_cast<int64_t>(blockIdx.x) * keep;
     const T* const logits = static_cast<const T*>(a.b.logits) + static_cast<int64_t>(row) * a.b.stride;
-    const int skew = static_cast<int>(reinterpret_cast<uintptr_t>(logits) % 16 / sizeof(T));  // of the row behind a 16-byte boundary
+    const int skew = SKEW ? static_cast<int>(reinterpret_cast<uintptr_t>(logits) % 16 / sizeof(T)) : 0;
     const float score = a.b.scores[row];
     if (!(fabsf(score) < INFINITY)) {  // its candidates are no matter of its logits
         if (tid == 0) a.sums[blockIdx.x] = make_float2(-INFINITY, 0.f);
@@ -181,25 +261,43 @@ __global__ void __launch_bounds__(kThreads, kResident) k_beam_part(const __grid_
     if (tid == 0) sh.n = 0;
     const int steps = (vocab + kStepLogits - 1) / kStepLogits;
     const int s0 = part * a.part_steps, s1 = s0 + a.part_steps < steps ? s0 + a.part_steps : steps;
+    // whether all loads of step s, and the neighbour's behind the last, lie in the row
+    auto inside = [&](int s) { return (skew == 0 || s > 0) && (s + 1) * kStepLogits + (skew == 0 ? 0 : kLoad) <= vocab; };
+    uint4 next[2][kLoads];
+    auto load = [&](uint4 (&w)[kLoads], int s) {
+        if (s >= s1 || !inside(s)) return;
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u)
+            w[u] = __ldcs(reinterpret_cast<const uint4*>(logits + (s * kStepLogits - skew + tid * kLoad + u * kThreads * kLoad)));
+    };
+    load(next[0], s0);
+    load(next[1], s0 + 1);
     float top = -INFINITY, sum = 0.f, lost = 0.f;
-    float limit = -INFINITY;  // a candidate's logit is larger
+    uint64_t bound = 0;
 #pragma unroll 1
     for (int s = s0; s < s1; ++s) {
         const int first = s * kStepLogits + tid * kLoad;  // token of this thread's first logit
         float x[kPer];
+        if (inside(s)) {
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) {
-            const int t = first + u * kThreads * kLoad;
-            if (skew == 0 ? t + kLoad <= vocab : t >= skew && t - skew + 2 * kLoad <= vocab) {
-                const uint4* from = reinterpret_cast<const uint4*>(logits + (t - skew));
-                unpack<T>(skew == 0 ? __ldcs(from) : from_two(from[0], from[1], skew * static_cast<int>(sizeof(T))), x + u * kLoad);
-            } else {
-#pragma unroll
-                for (int e = 0; e < kLoad; ++e) x[u * kLoad + e] = t + e < vocab ? static_cast<float>(logits[t + e]) : -INFINITY;
+            for (int u = 0; u < kLoads; ++u) {
+                uint4 w = next[0][u];
+                if (SKEW && skew != 0) {
+                    uint4 y = make_uint4(__shfl_down_sync(0xFFFFFFFFu, w.x, 1), __shfl_down_sync(0xFFFFFFFFu, w.y, 1),
+                                         __shfl_down_sync(0xFFFFFFFFu, w.z, 1), __shfl_down_sync(0xFFFFFFFFu, w.w, 1));
+                    if (lane == 31) y = *reinterpret_cast<const uint4*>(logits + (first - skew + (u * kThreads + 1) * kLoad));
+                    w = from_two(w, y, skew * static_cast<int>(sizeof(T)));
+                }
+                unpack<T>(w, x + u * kLoad);
             }
+        } else {
+            load_edge<T>(sh, logits, first, vocab);
+#pragma unroll
+            for (int i = 0; i < kPer; i += 4) *reinterpret_cast<float4*>(x + i) = sh.x[warp][i >> 2][lane];
         }
-        auto token = [&](int i) { return first + i / kLoad * (kThreads * kLoad) + i % kLoad; };
-        auto valid = [&](int i) { return static_cast<uint32_t>(token(i)) < static_cast<uint32_t>(vocab); };
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) next[0][u] = next[1][u];
+        load(next[1], s + 2);
         float m = x[0];
 #pragma unroll
         for (int i = 1; i < kPer; ++i) m = fmaxf(m, x[i]);
@@ -213,94 +311,56 @@ __global__ void __launch_bounds__(kThreads, kResident) k_beam_part(const __grid_
         {
             // the largest goes off first, which costs no bits where it counts; one product with both would leave its rounding
             const float neg = top == -INFINITY ? 0.f : -top;
-            float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < kPer; i += 2) {
                 float d0, d1;
                 fadd2(d0, d1, x[i], x[i + 1], neg, neg);
                 fmul2(d0, d1, d0, d1, kLog2e, kLog2e);
-                fadd2(acc[i & 7], acc[(i & 7) + 1], acc[i & 7], acc[(i & 7) + 1], ex2(d0), ex2(d1));
+                fadd2(acc[i & 3], acc[(i & 3) + 1], acc[i & 3], acc[(i & 3) + 1], ex2(d0), ex2(d1));
             }
-            float y = ((acc[0] + acc[1]) + (acc[2] + acc[3])) + ((acc[4] + acc[5]) + (acc[6] + acc[7]));
-            if (!(y >= 0.f)) {  // a NaN counts as -inf
-                y = 0.f;
-#pragma unroll
-                for (int i = 0; i < kPer; ++i) y += x[i] == x[i] ? ex2((x[i] + neg) * kLog2e) : 0.f;
-            }
+            float y = (acc[0] + acc[1]) + (acc[2] + acc[3]);
+            if (!(y >= 0.f)) y = sum_without_nan<T>(logits, first, vocab, -neg);
             y -= lost;
             const float t = sum + y;
             lost = (t - sum) - y;
             sum = t;
         }
         // ---- candidates
-        bool all = s > s0;  // of those above the limit
-        uint64_t bound = 0;
-        if (!all) {
-            uint64_t best = 0;
+        if (s == s0) {
+            int at = 0;  // the thread's best: the lowest of its largest
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const uint64_t c = valid(i) ? candidate(x[i], token(i)) : 0;
-                best = c > best ? c : best;
-            }
-            bound = bound_of(sh, best, keep);
+            for (int i = kPer - 1; i > 0; --i) at = x[i] == m ? i : at;
+            at = x[0] == m ? 0 : at;
+            bound = bound_of(sh, first < vocab ? candidate(m, Step<T>::token(first, at)) : 0, keep);
         }
-        // whether logit i is one
-        auto fits = [&](int i) { return all ? x[i] > limit : valid(i) && candidate(x[i], token(i)) >= bound; };
-        const int hits = __syncthreads_count(all ? m > limit : true);
-        if (hits == 0) continue;
-        int mine = 0;
-        if (!all || m > limit) {
+        // equal logits of later steps have higher tokens; a first step that holds n_best has set the bound
+        const float least = bound ? value_of(static_cast<uint32_t>(bound >> 32)) : -INFINITY;
+        const uint32_t who = __ballot_sync(0xFFFFFFFFu, s == s0 || bound == 0 ? !(m < least) : m > least);  // (a NaN counts as -inf)
+        if (who) {
+            __syncwarp();
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) mine += fits(i);
+            for (int i = 0; i < kPer; i += 4) sh.x[warp][i >> 2][lane] = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+            __syncwarp();
+            collect<T>(sh, who, first, vocab, bound);
         }
-        // room for all of them at once, or a quarter of the step at a time
-        int before = sh.n;
-        int incl = mine;
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-            if (lane >= o) incl += y;
-        }
-        __syncthreads();
-        int at = 0;
-        if (lane == 31) at = atomicAdd(&sh.n, incl);
-        at = __shfl_sync(0xFFFFFFFFu, at, 31) + incl - mine;
-        __syncthreads();
-        if (sh.n <= kList) {
-            if (mine > 0) {
-#pragma unroll
-                for (int i = 0; i < kPer; ++i)
-                    if (fits(i)) sh.list[at++] = candidate(x[i], token(i));
-            }
+        if (s == s0) {
             __syncthreads();
-        } else {
-            __syncthreads();  // every thread has seen that there is none
-            if (tid == 0) sh.n = before;
-            __syncthreads();
-#pragma unroll 1
-            for (int q = 0; q < 4; ++q) {
-                const int held = sh.n;
-                __syncthreads();  // every thread has read it
-                if (held > kMaxBest) {
-                    tighten(sh, keep);
-                    if (sh.n == keep) {
-                        bound = sh.list[keep - 1];
-                        all = false;
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < kPer; ++i)
-                    if (i / (kPer / 4) == q && fits(i)) sh.list[atomicAdd(&sh.n, 1)] = candidate(x[i], token(i));
+            const int n = sh.n;
+            __syncthreads();  // every thread has read it before the list grows on
+            if (s + 1 < s1 && n > keep && n <= kList) {
+                tighten(sh, n, keep);
+                bound = sh.list[keep - 1];
                 __syncthreads();
             }
-            tighten(sh, keep);
-            bound = sh.list[keep - 1];  // more than the list holds have come
-            all = false;
         }
-        if (!all && bound != 0) limit = value_of(static_cast<uint32_t>(bound >> 32));
     }
     __syncthreads();
-    tighten(sh, keep);
-    for (int i = tid; i < keep; i += kThreads) out[i] = i < sh.n ? sh.list[i] : 0;
+    int held = sh.n;
+    if (held > kList) held = collect_carefully<T>(sh, logits, vocab, s0, s1, keep);
+    __syncthreads();
+    held = tighten(sh, held, keep);
+    for (int i = tid; i < keep; i += kThreads) out[i] = i < held ? sh.list[i] : 0;
     // ---- the threads' sums
     float m = top;
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
@@ -309,8 +369,10 @@ __global__ void __launch_bounds__(kThreads, kResident) k_beam_part(const __grid_
     if (lane == 0) sh.sums[warp] = make_float2(m, y);
     __syncthreads();
     if (tid == 0) {
+#pragma unroll 1
         for (int w = 0; w < kWarps; ++w) m = fmaxf(m, sh.sums[w].x);
         y = 0.f;
+#pragma unroll 1
         for (int w = 0; w < kWarps; ++w)
             if (sh.sums[w].x > -INFINITY) y += sh.sums[w].y * ex2((sh.sums[w].x - m) * kLog2e);
         a.sums[blockIdx.x] = make_float2(m, y);
@@ -331,86 +393,100 @@ __device__ __forceinline__ double score_of(uint64_t order)
     return __longlong_as_double(static_cast<long long>(order >> 63 ? order & ~(1ull << 63) : ~order));
 }
 
-// The best of a group, a CTA: the logarithms of its beams' sums, the scores of all candidates in 64 bits (next to another
-// beam's, 32 would decide wrongly), and one warp that takes the best head of the descending lists n_best times.
-constexpr int kPickThreads = 256;
-
-__global__ void __launch_bounds__(kPickThreads) k_beam_pick(const __grid_constant__ SelectArgs a)
+// The best of a group, a CTA: the logarithms of its beams' sums, and the scores of all candidates in 64 bits (next to another
+// beam's, 32 would decide wrongly). A bound on the score as in bound_of leaves a few more than are kept, which are ranked
+// one against the other. All latency: the parts' sums, their logarithm, then the candidates, which come meanwhile.
+__global__ void __launch_bounds__(kThreads) k_beam_pick(const __grid_constant__ SelectArgs a)
 {
     extern __shared__ uint64_t s_pick[];
     __shared__ double s_lse[kMaxBeams];
-    __shared__ int s_next[kMaxBeams * kMaxParts];
+    __shared__ uint64_t s_bound[kWarps];
+    __shared__ int s_n;
     pdl_enter();
-    const int tid = threadIdx.x, lane = tid & 31;
-    const int beams = a.b.n_beams, keep = a.b.n_best, lists = beams * a.parts, group = blockIdx.x;
-    uint64_t* const scores = s_pick;                  // [lists][keep]
-    uint64_t* const keys = s_pick + lists * keep;
-    for (int i = tid; i < beams; i += kPickThreads) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int beams = a.b.n_beams, keep = a.b.n_best, per_beam = a.parts * keep, all = beams * per_beam, group = blockIdx.x;
+    uint64_t* const scores = s_pick;      // of the candidates; then of those that reach the bound,
+    uint64_t* const keys = s_pick + all;  // whose logit and token,
+    uint64_t* const ties = s_pick + 2 * all;  // and which of equal scores come first
+    const uint64_t* const best = a.best + static_cast<int64_t>(group) * all;
+    uint64_t early = tid < all ? best[tid] : 0;  // on its way while the sums are
+    if (tid == 0) s_n = 0;
+    for (int i = warp; i < beams; i += kWarps) {
         const int row = group * beams + i;
-        const float2* s = a.sums + static_cast<int64_t>(row) * a.parts;
-        float top = -INFINITY, sum = 0.f;
-        for (int p = 0; p < a.parts; ++p) top = fmaxf(top, s[p].x);
-        for (int p = 0; p < a.parts; ++p)
-            if (s[p].x > -INFINITY) sum += s[p].y * ex2((s[p].x - top) * kLog2e);
+        const float2 part = lane < a.parts ? a.sums[static_cast<int64_t>(row) * a.parts + lane] : make_float2(-INFINITY, 0.f);
+        float top = part.x;
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        float sum = part.x > -INFINITY ? part.y * ex2((part.x - top) * kLog2e) : 0.f;
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
         const bool live = fabsf(top) < INFINITY && fabsf(a.b.scores[row]) < INFINITY;
-        s_lse[i] = live ? static_cast<double>(top) + log(static_cast<double>(sum)) : INFINITY;
+        if (lane == 0) s_lse[i] = live ? static_cast<double>(top) + log(static_cast<double>(sum)) : INFINITY;
     }
-    for (int i = tid; i < lists; i += kPickThreads) s_next[i] = 0;
     __syncthreads();
-    for (int i = tid; i < lists * keep; i += kPickThreads) {
-        const int list = i / keep, beam = list / a.parts, row = group * beams + beam;
-        uint64_t key = a.best[static_cast<int64_t>(group) * lists * keep + i], score = 0;
+    // ---- scores: a thread has every 256th candidate; the best of its own
+    uint64_t top = 0;
+#pragma unroll 1
+    for (int i = tid; i < all; i += kThreads) {
+        const int beam = i / per_beam;
+        uint64_t key = i == tid ? early : best[i], score = 0;
         if (s_lse[beam] < INFINITY) {
-            if (key != 0)
-                score = order_of(static_cast<double>(a.b.scores[row]) + (static_cast<double>(value_of(static_cast<uint32_t>(key >> 32))) - s_lse[beam]));
+            if (key != 0) score = order_of(static_cast<double>(a.b.scores[group * beams + beam]) + (static_cast<double>(value_of(static_cast<uint32_t>(key >> 32))) - s_lse[beam]));
         } else {  // its tokens in their order
-            const int token = i - list * keep;
-            const bool any = list == beam * a.parts && token < a.b.vocab;
+            const int token = i - beam * per_beam;
+            const bool any = token < keep && token < a.b.vocab;
             key = any ? candidate(-INFINITY, token) : 0;
             if (any) score = order_of(static_cast<double>(-INFINITY));
         }
         scores[i] = score;
         keys[i] = key;
+        top = score > top ? score : top;
     }
+    // ---- the bound: least of the warps' each-th largest. Warp w takes the threads w, w + 8, ...: each list is shared by all warps.
     __syncthreads();
-    if (tid >= 32) return;
-    // the best head of this lane's lists
-    uint64_t score = 0, key = 0;
-    int from = 0;
-    auto look = [&]() {
-        score = key = 0;
-        for (int l = lane; l < lists; l += 32) {
-            const int n = s_next[l];
-            if (n >= keep) continue;
-            const uint64_t s = scores[l * keep + n], k = keys[l * keep + n];
-            // equal scores: the lower beam, whose lists a lane meets first, unless they are of the same
-            if (s > score || (s == score && s != 0 && l / a.parts == from / a.parts && k > key)) {
-                score = s;
-                key = k;
-                from = l;
-            }
+    top = 0;
+#pragma unroll 1
+    for (int i = lane * kWarps + warp; i < all; i += kThreads) top = scores[i] > top ? scores[i] : top;
+    const int each = (keep + kWarps - 1) / kWarps;
+    uint64_t bound = 0;
+#pragma unroll 1
+    for (int i = 0; i < each; ++i) {
+        bound = warp_max(top);
+        const uint32_t who = __ballot_sync(0xFFFFFFFFu, top == bound);
+        if (lane == __ffs(who) - 1) top = 0;
+    }
+    if (lane == 0) s_bound[warp] = bound;
+    __syncthreads();
+    bound = s_bound[0];
+    for (int w = 1; w < kWarps; ++w) bound = s_bound[w] < bound ? s_bound[w] : bound;
+    // ---- those that reach it, to the front: a block of the list at a time
+#pragma unroll 1
+    for (int i0 = 0; i0 < all; i0 += kThreads) {
+        const int i = i0 + tid;
+        const uint64_t score = i < all ? scores[i] : 0, key = i < all ? keys[i] : 0;
+        __syncthreads();
+        if (score != 0 && score >= bound) {
+            const int at = atomicAdd(&s_n, 1);
+            scores[at] = score;
+            keys[at] = key;
+            // equal scores: the lower beam, then the logit, then the lower token
+            ties[at] = static_cast<uint64_t>(kMaxBeams - 1 - i / per_beam) << 56 | (key >> 32) << 24 | (key & 0xFFFFFFu);
         }
-    };
-    look();
-    for (int i = 0; i < keep; ++i) {
-        const uint64_t best = warp_max(score);
-        uint32_t who = __ballot_sync(0xFFFFFFFFu, score == best);
-        if (who & (who - 1)) {  // the lowest beam of them, then its largest key
-            const bool tied = score == best;
-            const uint32_t beam = __reduce_min_sync(0xFFFFFFFFu, tied ? static_cast<uint32_t>(from / a.parts) : 0xFFFFFFFFu);
-            const bool in = tied && static_cast<uint32_t>(from / a.parts) == beam;
-            const uint64_t largest = warp_max(in ? key : 0);
-            who = __ballot_sync(0xFFFFFFFFu, in && key == largest);
+        __syncthreads();
+    }
+    const int n = s_n;
+#pragma unroll 1
+    for (int i = tid; i < n; i += kThreads) {
+        const uint64_t score = scores[i], tie = ties[i];
+        int rank = 0;
+#pragma unroll 2
+        for (int j = 0; j < n; ++j) {
+            const uint64_t other = scores[j];
+            rank += other > score || (other == score && ties[j] > tie);
         }
-        if (lane == __ffs(who) - 1) {
-            const int64_t at = static_cast<int64_t>(group) * keep + i;
-            a.b.best_scores[at] = static_cast<float>(score_of(score));
-            a.b.best_beams[at] = from / a.parts;
-            a.b.best_tokens[at] = static_cast<int32_t>(~static_cast<uint32_t>(key));
-            ++s_next[from];
-            look();
-        }
-        __syncwarp();
+        if (rank >= keep) continue;
+        const int64_t at = static_cast<int64_t>(group) * keep + rank;
+        a.b.best_scores[at] = static_cast<float>(score_of(score));
+        a.b.best_beams[at] = kMaxBeams - 1 - static_cast<int>(tie >> 56);
+        a.b.best_tokens[at] = static_cast<int32_t>(~static_cast<uint32_t>(keys[i]));
     }
 }
 
@@ -510,14 +586,16 @@ cudaError_t launch_beam_select(const BeamArgs& b, bool fp32, uint8_t* ws, cudaSt
     const BeamWs w = beam_layout(b.n_groups, b.n_beams, b.vocab, b.n_best);
     const SelectArgs a{b, w.parts, w.part_steps, reinterpret_cast<float2*>(ws + w.sums), reinterpret_cast<uint64_t*>(ws + w.best)};
     const dim3 grid(static_cast<unsigned>(b.n_groups * b.n_beams * w.parts));
-    cudaError_t e = fp32 ? launch_after(st, grid, kThreads, 0, 1, k_beam_part<float>, a)
-                         : launch_after(st, grid, kThreads, 0, 1, k_beam_part<__nv_bfloat16>, a);
+    const bool skew = reinterpret_cast<uintptr_t>(b.logits) % 16 || b.stride * (fp32 ? 4 : 2) % 16;
+    auto* const kern = fp32 ? (skew ? k_beam_part<float, true> : k_beam_part<float, false>)
+                            : (skew ? k_beam_part<__nv_bfloat16, true> : k_beam_part<__nv_bfloat16, false>);
+    cudaError_t e = launch_after(st, grid, kThreads, 0, 1, kern, a);
     if (e != cudaSuccess) return e;
-    constexpr int kMost = 2 * kMaxCandidates * static_cast<int>(sizeof(uint64_t));
+    constexpr int kMost = 3 * kMaxCandidates * static_cast<int>(sizeof(uint64_t));
     e = cudaFuncSetAttribute(k_beam_pick, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
     if (e != cudaSuccess) return e;
-    const size_t smem = 2 * sizeof(uint64_t) * static_cast<size_t>(b.n_beams) * w.parts * b.n_best;
-    return launch_after(st, dim3(b.n_groups), kPickThreads, smem, 1, k_beam_pick, a);
+    const size_t smem = 3 * sizeof(uint64_t) * static_cast<size_t>(b.n_beams) * w.parts * b.n_best;
+    return launch_after(st, dim3(b.n_groups), kThreads, smem, 1, k_beam_pick, a);
 }
 
 cudaError_t launch_reorder(const ReorderArgs& a, cudaStream_t st)
