@@ -127,11 +127,20 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
 
 // One KV head's item of a sequence, as a warp walks it.
 struct Item {
-    int b, j;    // sequence, KV head
-    int step;    // next step of it
+    int b, j;         // sequence, KV head
+    int blk, blocks;  // of the sequence's rows
+    int step;         // next step of it
     Seq s;
     Steps x;
 };
+
+// Drafted trees may have more rows than the route's registers hold: their items are blocks of `most` rows, a KV head's one
+// after another, each with a walk over the keys of its own.
+template <bool TREE>
+__device__ __forceinline__ int blocks_of(const Seq& s, int g, int most)
+{
+    return TREE ? static_cast<int>(static_cast<uint32_t>(s.rows * g + most - 1) / static_cast<uint32_t>(most)) : 1;
+}
 
 // Attention of sequences with at most rows_max rows (new tokens times query heads of a KV head).
 //
@@ -188,7 +197,7 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
         for (int i = i0; i < i1; ++i) {
             const Seq s = seq_of(a, bt, i);
             before[i] = sum;
-            if (s.rows > 0) sum += steps_of(a, s).n;
+            if (s.rows > 0) sum += static_cast<int64_t>(steps_of(a, s).n) * blocks_of<TREE>(s, a.g, NT * 8);
         }
         int64_t incl = sum;
         for (int o = 1; o < 32; o <<= 1) {
@@ -217,6 +226,7 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
         it.b = b;
         it.s = seq_of(a, bt, b);
         it.x = steps_of(a, it.s);
+        it.blocks = blocks_of<TREE>(it.s, a.g, NT * 8);
     };
     Item load, use;
     int lp = 0, slot = 0, page = -1;  // where the step to load lies: page of the table, row in it, page of the pool
@@ -230,8 +240,10 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
         }
         enter(load, lo);
         const int64_t rem = x0 - before[load.b] * c.Hkv;
-        load.j = static_cast<int>(quotient(rem, load.x.n));
-        load.step = static_cast<int>(rem - static_cast<int64_t>(load.j) * load.x.n);
+        const int item = static_cast<int>(quotient(rem, load.x.n));
+        load.j = TREE ? item / load.blocks : item;
+        load.blk = item - load.j * load.blocks;
+        load.step = static_cast<int>(rem - static_cast<int64_t>(item) * load.x.n);
         use = load;
     }
     // first token of step i of an item
@@ -239,6 +251,10 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
     auto advance = [&](Item& it) {
         if (++it.step < it.x.n) return;
         it.step = 0;
+        if (TREE) {
+            if (++it.blk < it.blocks) return;
+            it.blk = 0;
+        }
         if (++it.j < c.Hkv) return;
         it.j = 0;
         if (it.b + 1 < bt.n_seqs && before[it.b + 1] < before[bt.n_seqs]) enter(it, it.b + 1);
@@ -278,7 +294,8 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
         bool all = in_pool && t0 + kStep - 1 <= last && (t0 >= load.s.lo || t0 + kStep - 1 < a.n_sink);
         uint32_t nodes = 0xFFFFFFFFu;
         if (TREE && t0 + kStep - 1 >= load.s.pos0) {
-            nodes = __reduce_or_sync(0xFFFFFFFFu, lane < load.s.rows ? tree_bits(tree_row(a.tree, load.s.row0, load.s.pos0, load.s.row0 + lane), t0) : 0u);
+            const int r = load.blk * NT * 8 / a.g + lane, end = (load.blk + 1) * NT * 8;  // a row of the block for each lane
+            nodes = __reduce_or_sync(0xFFFFFFFFu, r < load.s.rows && r * a.g < end ? tree_bits(tree_row(a.tree, load.s.row0, load.s.pos0, load.s.row0 + r), t0) : 0u);
             all = false;
         }
 #pragma unroll
@@ -303,10 +320,14 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
     float o[8][NT][4];                // O^T: 16 dimensions at a time
     float m[NT][2], l[NT][2];         // per row: reference (log2 units, a warp's), sum of this lane's keys
     auto load_q = [&]() {
-        if (TREE) some_absent = __any_sync(0xFFFFFFFFu, lane < use.s.rows && tree_row(a.tree, use.s.row0, use.s.pos0, use.s.row0 + lane).words == 0);
+        const int row0 = TREE ? use.blk * NT * 8 : 0;
+        if (TREE) {
+            const int r = row0 / a.g + lane;
+            some_absent = __any_sync(0xFFFFFFFFu, r < use.s.rows && tree_row(a.tree, use.s.row0, use.s.pos0, use.s.row0 + r).words == 0);
+        }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int r = nt * 8 + oct;  // this lane's row of Q
+            const int r = row0 + nt * 8 + oct;  // this lane's row of Q
             const bool live = r < use.s.rows * a.g;
             const auto* q = static_cast<const __nv_bfloat16*>(a.q) + static_cast<int64_t>(use.s.row0 + (live ? r / a.g : 0)) * a.q_stride +
                             (use.j * a.g + (live ? r % a.g : 0)) * kHeadDim;
@@ -369,7 +390,7 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
         if (at_end && !whole) {
             cp_async_wait<0>();
             __syncwarp();
-            open = static_cast<int64_t>(use.b) * c.Hkv + use.j;
+            open = (static_cast<int64_t>(use.b) * c.Hkv + use.j) << 16 | (TREE ? use.blk : 0);
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -379,7 +400,7 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
                 sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 4);
                 sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 8);
                 sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 16);
-                const int r = nt * 8 + 2 * quad + e;
+                const int in_part = nt * 8 + 2 * quad + e, r = (TREE ? use.blk * NT * 8 : 0) + in_part;
                 if (r >= use.s.rows * a.g) continue;
                 const int64_t row = use.s.row0 + r / a.g;
                 const int h = use.j * a.g + r % a.g;
@@ -402,10 +423,10 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
                 } else {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        part[r * kHeadDim + 16 * i + (E4M3 ? 2 * oct : oct)] = o[i][nt][e];
-                        part[r * kHeadDim + 16 * i + (E4M3 ? 2 * oct + 1 : 8 + oct)] = o[i][nt][2 + e];
+                        part[in_part * kHeadDim + 16 * i + (E4M3 ? 2 * oct : oct)] = o[i][nt][e];
+                        part[in_part * kHeadDim + 16 * i + (E4M3 ? 2 * oct + 1 : 8 + oct)] = o[i][nt][2 + e];
                     }
-                    if (oct == 0) part_ml[r] = make_float2(m[nt][e], sum);
+                    if (oct == 0) part_ml[in_part] = make_float2(m[nt][e], sum);
                 }
             }
     };
@@ -492,7 +513,7 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const int r = (nt * 8 + 2 * quad + e) / a.g;
+                        const int r = (use.blk * NT * 8 + nt * 8 + 2 * quad + e) / a.g;
                         const TreeRow x = tree_row(a.tree, use.s.row0, use.s.pos0, use.s.row0 + (r < use.s.rows ? r : 0));
                         const uint32_t seen = tree_bits(x, t0);
 #pragma unroll
@@ -643,6 +664,8 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
     }
 }
 
+constexpr int kTreeMergeRows = 4;  // rows of a CTA of k_rows_merge for drafted trees, which have more rows than single tokens do
+
 // Items that several CTAs or warps of k_rows share: a CTA per item, four dimensions a lane, one warp to eight for a row by
 // how many rows there are. A CTA of k_rows left one piece of the item, under the first of its runs that has a part of it, and
 // where the item ends inside a run, that run another one. Bound by latency: a lane looks a piece up and weighs it, then
@@ -653,7 +676,9 @@ __global__ void __launch_bounds__(256) k_rows_merge(const __grid_constant__ Rows
     __shared__ float2 s_ml[8];
     __shared__ int64_t s_first[8], s_total[8];
     const AttendView& a = args.a;
-    const int b = blockIdx.x / args.c.Hkv, j = blockIdx.x - b * args.c.Hkv;
+    const bool tree = a.tree.masks != nullptr;
+    const int b = blockIdx.x / args.c.Hkv, j = blockIdx.x - b * args.c.Hkv, blk = blockIdx.y;
+    auto blocks = [&](const Seq& x) { return tree ? blocks_of<true>(x, a.g, args.part_rows) : 1; };
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     // Steps of the sequences before this one, its own and all, from the batch's lists while k_rows still runs: every CTA of
     // k_rows is past its own wait when this kernel starts, so what wrote the lists is complete, and k_rows writes
@@ -670,7 +695,7 @@ __global__ void __launch_bounds__(256) k_rows_merge(const __grid_constant__ Rows
         int64_t mine = 0;
         if (i < args.b.n_seqs) {
             const Seq x = read_seq(i);
-            mine = x.rows > 0 ? steps_of(a, x).n : 0;
+            mine = x.rows > 0 ? static_cast<int64_t>(steps_of(a, x).n) * blocks(x) : 0;
         }
         int64_t lower = i < b ? mine : 0;
         for (int o = 16; o > 0; o >>= 1) {
@@ -690,14 +715,14 @@ __global__ void __launch_bounds__(256) k_rows_merge(const __grid_constant__ Rows
     } else {
         pdl_enter();
         first = args.before[b];
-        n = args.before[b + 1] - first;
+        n = s.rows > 0 ? steps_of(a, s).n : 0;
         total = args.before[args.b.n_seqs];
     }
     const Runs runs(total * args.c.Hkv, ctas, warps);
-    const int64_t x0 = first * args.c.Hkv + n * j, x1 = x0 + n;
+    const int64_t x0 = first * args.c.Hkv + n * (static_cast<int64_t>(j) * blocks(s) + blk), x1 = x0 + n;
     const int64_t c0 = quotient(x0, runs.per_cta), c1 = quotient(x1 - 1, runs.per_cta);
     const int64_t w0 = quotient(x0 - c0 * runs.per_cta, runs.per_warp), w1 = quotient(x1 - 1 - c1 * runs.per_cta, runs.per_warp);
-    if (n == 0 || (c0 == c1 && w0 == w1)) {
+    if (n == 0 || blk >= blocks(s) || (c0 == c1 && w0 == w1)) {
         if (early) pdl_enter();
         return;
     }
@@ -709,16 +734,21 @@ __global__ void __launch_bounds__(256) k_rows_merge(const __grid_constant__ Rows
         if (c < c1 || (c == c1 && c1_piece)) return 2 * (c * warps + (i == 0 ? w0 : 0)) + 1;
         return 2 * (c1 * warps + w1);
     };
-    const int rows = s.rows * a.g;
-    const int share = rows > 4 ? 1 : rows > 2 ? 2 : rows > 1 ? 4 : 8;  // warps of a row
+    const int row0 = blk * args.part_rows;
+    // the rows of this CTA: all of the block's, or (drafted trees) kTreeMergeRows of them
+    const int first_row = blockIdx.z * kTreeMergeRows;
+    int rows = s.rows * a.g - row0 < args.part_rows ? s.rows * a.g - row0 : args.part_rows;
+    if (gridDim.z > 1 && rows > first_row + kTreeMergeRows) rows = first_row + kTreeMergeRows;
+    const int n_rows = rows - first_row;
+    const int share = n_rows > 4 ? 1 : n_rows > 2 ? 2 : n_rows > 1 ? 4 : 8;  // warps of a row
     // A few CTAs, which start before k_rows has left all SMs, go through it twice: once without loads and stores while they
     // would wait, which brings the code into the instruction cache. One token at 4K, 32 query heads, bf16 11.6 -> 10.5 us;
     // 8 tokens at 4K, 64 CTAs, whose first pass nothing hides, 29.8 us and 30.6 with it.
 #pragma unroll 1
-    for (int pass = early && gridDim.x <= 32 ? 0 : 1; pass < 2; ++pass) {
+    for (int pass = early && gridDim.x * gridDim.y * gridDim.z <= 32 ? 0 : 1; pass < 2; ++pass) {
         const bool real = pass == 1;
         if (real && early) pdl_enter();
-        for (int r0 = 0; r0 < rows; r0 += 8 / share) {
+        for (int r0 = first_row; r0 < rows; r0 += 8 / share) {
             const int r = r0 + warp / share, sub = warp % share;
             const bool live = r < rows;
             float top = -INFINITY, sum = 0.f;
@@ -786,8 +816,8 @@ __global__ void __launch_bounds__(256) k_rows_merge(const __grid_constant__ Rows
             if (live && sub == 0 && real) {
                 const float inv = sum == 0.f ? 0.f : 1.0f / sum;
                 if (sum == 0.f) acc = make_float4(0.f, 0.f, 0.f, 0.f);  // no keys, beside values that are not finite too
-                const int64_t row = s.row0 + r / a.g;
-                const int h = j * a.g + r % a.g;
+                const int64_t row = s.row0 + (row0 + r) / a.g;
+                const int h = j * a.g + (row0 + r) % a.g;
                 auto* out = static_cast<__nv_bfloat16*>(a.out) + row * a.out_stride + h * kHeadDim;
                 reinterpret_cast<uint2*>(out)[lane] = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
                 if (a.lse && lane == 0) a.lse[row * a.Hq + h] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * 0.6931471805599453f;
@@ -797,13 +827,16 @@ __global__ void __launch_bounds__(256) k_rows_merge(const __grid_constant__ Rows
     }
 }
 
+constexpr int64_t kFewKeys = 110000;  // of drafted trees' walks, see in_blocks
+
 // Workspace regions (byte offsets) of the route that a call takes; the status word comes first.
 struct AttendWs {
     size_t before, part_ml, part_o, chunks, end;
     int part_rows;
 };
 
-AttendWs attend_layout(int Hq, int Hkv, bool e4m3, int n_seqs, int n_rows, int max_rows)
+// `blocks`: drafted trees in blocks of rows_max rows.
+AttendWs attend_layout(int Hq, int Hkv, bool e4m3, int n_seqs, int n_rows, int max_rows, bool blocks = false)
 {
     AttendWs w{};
     size_t off = 256;
@@ -813,10 +846,10 @@ AttendWs attend_layout(int Hq, int Hkv, bool e4m3, int n_seqs, int n_rows, int m
         return at;
     };
     const int64_t rows = static_cast<int64_t>(max_rows) * (Hq / Hkv);
-    if (rows > rows_max(e4m3)) {
+    if (rows > rows_max(e4m3) && !blocks) {
         w.chunks = take(chunk_ws_bytes(Hq / Hkv, Hkv, n_seqs, n_rows, max_rows));
     } else {
-        const int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 3;
+        const int nt = rows <= 8 ? 1 : rows <= 16 || (blocks && !e4m3) ? 2 : 3;
         const size_t parts = 2 * kMaxSms * rows_warps(nt, e4m3);  // two of a run
         w.part_rows = 8 * nt;
         w.before = take((static_cast<size_t>(n_seqs) + 1) * sizeof(int64_t));
@@ -828,7 +861,7 @@ AttendWs attend_layout(int Hq, int Hkv, bool e4m3, int n_seqs, int n_rows, int m
 }
 
 template <int NT, bool E4M3>
-cudaError_t run_rows(const RowsArgs& r, int sms, cudaStream_t st)
+cudaError_t run_rows(const RowsArgs& r, int sms, cudaStream_t st, int blocks = 1)
 {
     constexpr int kWarps = rows_warps(NT, E4M3);
     auto kern = r.a.tree.masks ? k_rows<NT, E4M3, true> : k_rows<NT, E4M3, false>;
@@ -840,7 +873,25 @@ cudaError_t run_rows(const RowsArgs& r, int sms, cudaStream_t st)
     if (e != cudaSuccess) return e;
     e = launch_after(st, dim3(sms), 32 * kWarps, smem, 1, kern, r);
     if (e != cudaSuccess) return e;
-    return launch_after(st, dim3(r.b.n_seqs * r.c.Hkv), 256, 0, 1, k_rows_merge, r, sms, kWarps);
+    return launch_after(st, dim3(r.b.n_seqs * r.c.Hkv, blocks, r.a.tree.masks ? r.part_rows / kTreeMergeRows : 1), 256, 0, 1, k_rows_merge, r, sms, kWarps);
+}
+
+// Whether drafted trees of more rows than rows_max go to k_rows all the same, in blocks: where the blocks' walks over the keys are
+// short, as the table's width (or the window) bounds them, that has no plan to wait for. It takes 12 us and, per block of a KV head, the
+// time of its keys and of 600 more; the tensor cores' route 18 to 22 us over few keys. 32 query heads on 8, bf16, by either: 8
+// nodes at 2,048 15.0 and 21.2 us, 32 at 2,048 22.8 and 22.0, 12 sequences of 8 at 256 23.7 and 19.9; 4 on 1, 8 at 2,048 13.1
+// and 20.5, 12 sequences of 16 at 2,048 20.2 and 22.5. 8-bit: 8 at 2,048 17.5 and 24.5, 3 sequences of 8 at 4,096 30.8 and 30.8.
+bool in_blocks(const AttendView& a, const CacheView& c, bool e4m3, const BatchView& b)
+{
+    const int64_t rows = static_cast<int64_t>(b.max_rows) * a.g, most = rows_max(e4m3);
+    if (!a.tree.masks || rows <= rows_max(e4m3)) return false;
+    int64_t keys = static_cast<int64_t>(b.stride) * c.page_size;
+    if (a.n_local >= 0) {
+        const int64_t window = static_cast<int64_t>(a.n_sink) + a.n_local + b.max_rows;
+        keys = window < keys ? window : keys;
+    }
+    const int64_t walks = static_cast<int64_t>(b.n_seqs) * c.Hkv * ((rows + most - 1) / most);
+    return keys < kFewKeys && walks * (keys + 600) <= kFewKeys;
 }
 
 }  // namespace
@@ -852,7 +903,7 @@ size_t attend_ws_bytes(int Hq, int Hkv, bool e4m3, int n_seqs, int n_rows, int m
     const size_t own = attend_layout(Hq, Hkv, e4m3, n_seqs, n_rows, max_rows).end;
     const int most = rows_max(e4m3) / (Hq / Hkv);
     if (max_rows <= most) return own;
-    const size_t few = attend_layout(Hq, Hkv, e4m3, n_seqs, n_rows, most).end;
+    const size_t few = attend_layout(Hq, Hkv, e4m3, n_seqs, n_rows, max_rows, true).end;
     return own > few ? own : few;
 }
 
@@ -863,15 +914,20 @@ cudaError_t launch_attend(const AttendView& a, const CacheView& c, bool e4m3, co
     cudaError_t e = device_sms(&sms);
     if (e != cudaSuccess) return e;
     sms = sms < kMaxSms ? sms : kMaxSms;
-    const AttendWs lay = attend_layout(a.Hq, c.Hkv, e4m3, b.n_seqs, b.n_rows, b.max_rows);
     const int64_t rows = static_cast<int64_t>(b.max_rows) * a.g;
-    if (rows > rows_max(e4m3)) {
+    const bool blocks = in_blocks(a, c, e4m3, b);
+    const AttendWs lay = attend_layout(a.Hq, c.Hkv, e4m3, b.n_seqs, b.n_rows, b.max_rows, blocks);
+    if (rows > rows_max(e4m3) && !blocks) {
         // Batches with longer pieces go there whole, and no second route follows: a sequence of few rows takes its share of
         // that kernel's jobs, at the pace of its keys (17 tokens at 128K, 537 MB of bf16: 103 us, 5.2 TB/s).
         return launch_chunks(a, c, e4m3, b, sms, reinterpret_cast<int32_t*>(ws + kStatusOffset), ws + lay.chunks, timeout_ns, st);
     }
     const RowsArgs r{a, c, b, reinterpret_cast<int64_t*>(ws + lay.before), reinterpret_cast<float*>(ws + lay.part_o),
                      reinterpret_cast<float2*>(ws + lay.part_ml), lay.part_rows};
+    if (blocks) {
+        const int n = static_cast<int>((rows + lay.part_rows - 1) / lay.part_rows);
+        return e4m3 ? run_rows<3, true>(r, sms, st, n) : run_rows<2, false>(r, sms, st, n);
+    }
     if (rows <= 8) return e4m3 ? run_rows<1, true>(r, sms, st) : run_rows<1, false>(r, sms, st);
     if (rows <= 16) return e4m3 ? run_rows<2, true>(r, sms, st) : run_rows<2, false>(r, sms, st);
     return run_rows<3, true>(r, sms, st);

@@ -1071,16 +1071,22 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
 // 176 pairs in two or three pieces: the call takes 129 us, and 134 with a warp per row that looks the weights up piece by
 // piece. A grid of what the SMs hold walks the rows: one CTA for eight of every row that could be cut took 12 us, most of
 // it for CTAs without a row.
+//
+// Drafted trees, whose few rows may be in a hundred pieces: where every four rows have a CTA, its warps share their pieces, eight
+// in turn, and add up what they have.
 constexpr int kMergeCtas = 4;  // per SM, of 256 threads
 
 __global__ void __launch_bounds__(256, kMergeCtas) k_chunk_merge(const __grid_constant__ ChunkArgs a)
 {
+    __shared__ float4 s_o[8][4][32];
+    __shared__ float2 s_ml[8][4];
     pdl_enter();
-    const int lane = threadIdx.x & 31, per_tile = a.tile_tokens * a.a.g;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per_tile = a.tile_tokens * a.a.g;
     const int total = a.p.counts[1] * (a.part_rows / 4);  // at most 2 kMaxSms pairs of 64
-    const int step = gridDim.x * 8;
+    const bool shared = a.a.tree.masks && total <= static_cast<int>(gridDim.x);
+    const int step = shared ? gridDim.x : gridDim.x * 8;
 #pragma unroll 1
-    for (int w = blockIdx.x * 8 + (threadIdx.x >> 5); w < total; w += step) {
+    for (int w = shared ? blockIdx.x : blockIdx.x * 8 + warp; w < total; w += step) {
         const int m = w / (a.part_rows / 4);
         const int r = (w - m * (a.part_rows / 4)) * 4;       // first row of the pair's tiles
         const int4 y0 = reinterpret_cast<const int4*>(a.p.merges + m)[0];  // KV head, first row, tokens, slot
@@ -1094,8 +1100,9 @@ __global__ void __launch_bounds__(256, kMergeCtas) k_chunk_merge(const __grid_co
         float4 acc[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        const int mine = shared ? 8 * warp : 0;
 #pragma unroll 1
-        for (int p0 = 0; p0 < pieces; p0 += 8) {
+        for (int p0 = mine; p0 < pieces; p0 += shared ? 64 : 8) {
             const int p = p0 + (lane & 7);
             const float2 ml = p < pieces ? __ldcg(ml_at + static_cast<int64_t>(p) * a.part_rows) : make_float2(-INFINITY, 0.f);
             float mx = ml.x;
@@ -1107,7 +1114,7 @@ __global__ void __launch_bounds__(256, kMergeCtas) k_chunk_merge(const __grid_co
             for (int o = 4; o > 0; o >>= 1) part += __shfl_xor_sync(0xFFFFFFFFu, part, o);
             sum = fmaf(sum, old, part);
             top = now;
-            if (p0 > 0) {
+            if (p0 > mine) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float x = __shfl_sync(0xFFFFFFFFu, old, 8 * i);
@@ -1129,18 +1136,38 @@ __global__ void __launch_bounds__(256, kMergeCtas) k_chunk_merge(const __grid_co
                 }
             }
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float l = __shfl_sync(0xFFFFFFFFu, sum, 8 * i), mx = __shfl_sync(0xFFFFFFFFu, top, 8 * i);
+        auto store = [&](int i, float4 o, float l, float mx) {
             const int x = live_row(r + i);
-            if (x >= y0.z * a.a.g) continue;
+            if (x >= y0.z * a.a.g) return;
             const float inv = l == 0.f ? 0.f : 1.0f / l;
-            if (l == 0.f) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);  // no keys, beside values that are not finite too
+            if (l == 0.f) o = make_float4(0.f, 0.f, 0.f, 0.f);  // no keys, beside values that are not finite too
             const int64_t row = y0.y + x / a.a.g;
             const int h = y0.x * a.a.g + x % a.a.g;
             auto* out = static_cast<__nv_bfloat16*>(a.a.out) + row * a.a.out_stride + h * kHeadDim;
-            reinterpret_cast<uint2*>(out)[lane] = make_uint2(pack_bf16x2(acc[i].x * inv, acc[i].y * inv), pack_bf16x2(acc[i].z * inv, acc[i].w * inv));
+            reinterpret_cast<uint2*>(out)[lane] = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
             if (a.a.lse && lane == 0) a.a.lse[row * a.a.Hq + h] = l == 0.f ? -INFINITY : (mx + __log2f(l)) * 0.6931471805599453f;
+        };
+        if (!shared) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) store(i, acc[i], __shfl_sync(0xFFFFFFFFu, sum, 8 * i), __shfl_sync(0xFFFFFFFFu, top, 8 * i));
+            continue;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s_o[warp][i][lane] = acc[i];
+        if ((lane & 7) == 0) s_ml[warp][lane >> 3] = make_float2(top, sum);
+        __syncthreads();
+        if (warp < 4) {  // a row each
+            float mx = -INFINITY, l = 0.f;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int x = 0; x < 8; ++x) mx = fmaxf(mx, s_ml[x][warp].x);
+            const float base = mx == -INFINITY ? 0.f : mx;
+            for (int x = 0; x < 8; ++x) {
+                const float f = ex2(s_ml[x][warp].x - base);
+                const float4 y = s_o[x][warp][lane];
+                l = fmaf(s_ml[x][warp].y, f, l);
+                o = make_float4(fmaf(y.x, f, o.x), fmaf(y.y, f, o.y), fmaf(y.z, f, o.z), fmaf(y.w, f, o.w));
+            }
+            store(warp, o, l, mx);
         }
     }
 }
@@ -1202,7 +1229,7 @@ cudaError_t run_chunks(const ChunkArgs& a, cudaStream_t st)
     if (e == cudaSuccess) e = launch_after(st, dim3(1), kPlanThreads, 0, 1, k_chunk_plan, a);
     if (e == cudaSuccess)
         e = launch_after(st, dim3(a.p.max_jobs), chunk_threads(E4M3), chunk_smem(E4M3), 1, k_chunk<E4M3, TREE>, tq, tk, tv, a);
-    const int merge_ctas = a.p.max_merges * (a.part_rows / 32), most = a.sms * kMergeCtas;
+    const int merge_ctas = a.p.max_merges * (a.part_rows / (TREE ? 4 : 32)), most = a.sms * kMergeCtas;
     if (e == cudaSuccess) e = launch_after(st, dim3(merge_ctas < most ? merge_ctas : most), 256, 0, 1, k_chunk_merge, a);
     return e;
 }

@@ -591,10 +591,12 @@ cudaError_t launch_beam_select(const BeamArgs& b, bool fp32, uint8_t* ws, cudaSt
                             : (skew ? k_beam_part<__nv_bfloat16, true> : k_beam_part<__nv_bfloat16, false>);
     cudaError_t e = launch_after(st, grid, kThreads, 0, 1, kern, a);
     if (e != cudaSuccess) return e;
-    constexpr int kMost = 3 * kMaxCandidates * static_cast<int>(sizeof(uint64_t));
-    e = cudaFuncSetAttribute(k_beam_pick, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
-    if (e != cudaSuccess) return e;
     const size_t smem = 3 * sizeof(uint64_t) * static_cast<size_t>(b.n_beams) * w.parts * b.n_best;
+    if (smem > kPlainSmem) {
+        constexpr int kMost = 3 * kMaxCandidates * static_cast<int>(sizeof(uint64_t));
+        e = cudaFuncSetAttribute(k_beam_pick, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+        if (e != cudaSuccess) return e;
+    }
     return launch_after(st, dim3(b.n_groups), kThreads, smem, 1, k_beam_pick, a);
 }
 

@@ -12,6 +12,7 @@ constexpr int kMaxBest = 64;        // continuations kept of a group
 constexpr int kMaxVocab = 1 << 24;
 constexpr int kMaxCaches = 1024;    // of scale_cache_move
 constexpr int kMoveCaches = 64;     // of them in a launch
+constexpr size_t kPlainSmem = 32 * 1024;  // dynamic shared memory that a kernel has without asking
 
 struct TreeArgs {
     const int32_t* parents;

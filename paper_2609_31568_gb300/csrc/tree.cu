@@ -238,10 +238,12 @@ cudaError_t launch_tree_plan(const TreeArgs& a, cudaStream_t st)
 {
     const int threads = a.b.max_rows <= 32 ? 32 : (a.b.max_rows + 31) / 32 * 32;
     const size_t smem = static_cast<size_t>(threads / 32) * threads * sizeof(uint32_t);
-    // the largest call's, whatever this one's: calls from several threads set the same
-    constexpr int kMost = kMaxNodes / 32 * kMaxNodes * static_cast<int>(sizeof(uint32_t));
-    const cudaError_t e = cudaFuncSetAttribute(k_tree_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
-    if (e != cudaSuccess) return e;
+    if (smem > kPlainSmem) {
+        // the largest call's, whatever this one's: calls from several threads set the same
+        constexpr int kMost = kMaxNodes / 32 * kMaxNodes * static_cast<int>(sizeof(uint32_t));
+        const cudaError_t e = cudaFuncSetAttribute(k_tree_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+        if (e != cudaSuccess) return e;
+    }
     return launch_after(st, dim3(a.b.n_seqs), threads, smem, 1, k_tree_plan, a);
 }
 

@@ -346,15 +346,16 @@ def load() -> ctypes.CDLL:
         return lib
 
 
-_torch = _bf16 = None  # the torch module and its bf16 type, once a call has needed them
+_torch = _bf16 = _i32 = _f32 = None  # the torch module and its types, once a call has needed them
 
 
 def _imported_torch():
-    global _torch, _bf16
+    global _torch, _bf16, _i32, _f32
     if _torch is None:
         import torch
 
-        _torch, _bf16 = torch, torch.bfloat16
+        _bf16, _i32, _f32 = torch.bfloat16, torch.int32, torch.float32
+        _torch = torch
     return _torch
 
 
@@ -629,14 +630,14 @@ def scale_cache_attend(attend: ScaleAttend, cache: ScaleCache, batch: ScaleBatch
 
 def _numbers(x, n: int, what: str) -> int | None:
     """Address of an int32 tensor of at least n numbers."""
-    if x.itemsize != 4 or x.is_floating_point() or x.numel() < n or not x.is_contiguous():
+    if x.dtype is not _i32 or x.numel() < n or not x.is_contiguous():
         raise ValueError(f"{what} is a contiguous int32 tensor of {n} numbers; got {x.dtype} {tuple(x.shape)}")
     return x.data_ptr()
 
 
 def _floats(x, n: int, what: str) -> int | None:
     """Address of an fp32 tensor of at least n numbers."""
-    if x.itemsize != 4 or not x.is_floating_point() or x.numel() < n or not x.is_contiguous():
+    if x.dtype is not _f32 or x.numel() < n or not x.is_contiguous():
         raise ValueError(f"{what} is a contiguous fp32 tensor of {n} numbers; got {x.dtype} {tuple(x.shape)}")
     return x.data_ptr()
 
@@ -661,6 +662,8 @@ def scale_cache_attend_tree(attend: ScaleAttend, tree: ScaleTree, cache: ScaleCa
     _tree_rows(tree, batch)
     qp, qs, _ = _rows(q, batch.n_rows, attend.num_q_heads)
     op, os_, _ = _rows(out, batch.n_rows, attend.num_q_heads)
+    if _torch is None:
+        _imported_torch()
     lp = None if lse is None else _floats(lse, batch.n_rows * attend.num_q_heads, "lse")
     _check("scale_cache_attend_tree", load().scale_cache_attend_tree(
         ctypes.byref(attend), ctypes.byref(tree), ctypes.byref(cache), ctypes.byref(batch), qp, qs, op, os_, lp,
@@ -679,6 +682,8 @@ def scale_tree_accept(tree: ScaleTree, caches, batch: ScaleBatch, tokens, choice
     _tree_rows(tree, batch)
     if tree.parents is None and batch.n_rows:
         raise ValueError("the tree has no parents")
+    if _torch is None:
+        _imported_torch()
     n, seqs = batch.n_rows, batch.n_seqs
     _check("scale_tree_accept", load().scale_tree_accept(
         ctypes.byref(tree), caches, ctypes.byref(batch), _numbers(tokens, n, "tokens"), _numbers(choices, n, "choices"),
@@ -696,15 +701,16 @@ def scale_beam_workspace_size(beam: ScaleBeam) -> int:
 def scale_beam_select(beam: ScaleBeam, logits, scores, best_scores, best_beams, best_tokens, ws, stream=None) -> None:
     """The best continuations of each group of beams. logits bf16 or fp32 [n_groups * n_beams][vocab], whose rows may
     lie apart; scores fp32 [n_groups][n_beams]; the outputs [n_groups][n_best] (fp32, int32, int32)."""
-    rows, kept = beam.n_groups * beam.n_beams, beam.n_groups * beam.n_best
-    torch = _torch or _imported_torch()
-    if logits.dim() != 2 or logits.shape[0] < rows or logits.shape[1] != beam.vocab or logits.stride(1) != 1 or \
-            logits.dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError(f"logits are bf16 or fp32 [{rows}][{beam.vocab}]; got {logits.dtype} {tuple(logits.shape)}")
-    b = beam if logits.dtype is torch.bfloat16 else beam.fp32
-    stride = logits.stride(0) if logits.shape[0] > 1 else beam.vocab
+    if _torch is None:
+        _imported_torch()
+    groups, vocab = beam.n_groups, beam.vocab
+    rows, kept = groups * beam.n_beams, groups * beam.n_best
+    shape, stride, kind = logits.shape, logits.stride(), logits.dtype
+    if len(shape) != 2 or shape[0] < rows or shape[1] != vocab or stride[1] != 1 or (kind is not _bf16 and kind is not _f32):
+        raise ValueError(f"logits are bf16 or fp32 [{rows}][{vocab}]; got {kind} {tuple(shape)}")
+    b = beam if kind is _bf16 else beam.fp32
     _check("scale_beam_select", load().scale_beam_select(
-        ctypes.byref(b), logits.data_ptr(), stride, _floats(scores, rows, "scores"),
+        ctypes.byref(b), logits.data_ptr(), stride[0] if shape[0] > 1 else vocab, _floats(scores, rows, "scores"),
         _floats(best_scores, kept, "best_scores"), _numbers(best_beams, kept, "best_beams"),
         _numbers(best_tokens, kept, "best_tokens"), _ptr(ws), _nbytes(ws), _stream(stream)))
 
@@ -713,14 +719,16 @@ def scale_beam_reorder(caches, page_table, kv_len, parents, table_out, moves: Sc
     """The beams' page tables in their new order. parents int32 [n_groups][n_beams], kv_len [n_groups * n_beams],
     page_table and table_out (which may be the same) [n_groups * n_beams][pages]; `moves` [beams * page_size], in a
     group for each beam, are for scale_cache_move over `caches`."""
-    if parents.dim() != 2 or page_table.dim() != 2 or page_table.shape != table_out.shape or \
-            page_table.shape[0] != parents.numel():
+    if _torch is None:
+        _imported_torch()
+    groups, table = parents.shape, page_table.shape
+    if len(groups) != 2 or len(table) != 2 or table != table_out.shape or table[0] != groups[0] * groups[1]:
         raise ValueError("parents are [n_groups][n_beams], the tables [n_groups * n_beams][pages]")
-    beams = parents.numel()
+    beams = table[0]
     _check("scale_beam_reorder", load().scale_beam_reorder(
-        caches, parents.shape[0], parents.shape[1], _numbers(parents, beams, "parents"), _numbers(kv_len, beams, "kv_len"),
-        _numbers(page_table, 0, "page_table"), page_table.shape[1], _numbers(table_out, 0, "table_out"),
-        ctypes.byref(moves), _stream(stream)))
+        caches, groups[0], groups[1], _numbers(parents, beams, "parents"), _numbers(kv_len, beams, "kv_len"),
+        _numbers(page_table, 0, "page_table"), table[1], _numbers(table_out, 0, "table_out"), ctypes.byref(moves),
+        _stream(stream)))
 
 
 def scale_get_device_status(ws, stream=None) -> int:

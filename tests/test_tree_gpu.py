@@ -139,18 +139,24 @@ def planned(bt, parents, n_sink=0, n_local=-1):
 @pytest.mark.parametrize("news,lens,hq,hkv,page", ATTENDS)
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("n_sink,n_local", [(0, -1), (5, 40), (0, 3)])
-def test_attend_trees(news, lens, hq, hkv, page, e4m3, n_sink, n_local):
-    bt = Batch(news, lens, hq=hq, hkv=hkv, page=page, e4m3=e4m3, seed=sum(lens) + hq, n_rows=sum(news) + 2)
+@pytest.mark.parametrize("wide", [False, True])
+def test_attend_trees(news, lens, hq, hkv, page, e4m3, n_sink, n_local, wide):
+    """`wide`: a table of 120,000 tokens, by which calls of few rows leave the route of few keys."""
+    if wide and n_local >= 0 and n_sink + n_local < 40:
+        pytest.skip("the window bounds the keys")
+    bt = Batch(news, lens, hq=hq, hkv=hkv, page=page, e4m3=e4m3, seed=sum(lens) + hq, n_rows=sum(news) + 2,
+               wider=120000 // page if wide else 0)
     seen, positions = planned(bt, trees(news, hq + sum(news)), n_sink, n_local)
     check_attend(bt, seen, positions, n_sink, n_local)
 
 
 @pytest.mark.parametrize("news,lens,hq,hkv,page", ATTENDS[1:])
 @pytest.mark.parametrize("e4m3", [False, True])
-def test_attend_any_masks_and_absent_rows(news, lens, hq, hkv, page, e4m3):
+@pytest.mark.parametrize("wide", [False, True])
+def test_attend_any_masks_and_absent_rows(news, lens, hq, hkv, page, e4m3, wide):
     """Masks that are no trees: later nodes, not the row itself, none at all; rows that are no nodes; nodes that nobody sees
     hold NaN, and bits of nodes past the sequence are set."""
-    bt = Batch(news, lens, hq=hq, hkv=hkv, page=page, e4m3=e4m3, seed=sum(lens) + hkv)
+    bt = Batch(news, lens, hq=hq, hkv=hkv, page=page, e4m3=e4m3, seed=sum(lens) + hkv, wider=120000 // page if wide else 0)
     rng = random.Random(hq + sum(lens))
     seen, positions = [], []
     for b, (a, n) in enumerate(zip(news, lens)):
