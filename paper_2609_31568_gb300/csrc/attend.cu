@@ -52,6 +52,7 @@ struct RowsArgs {
     float* part_o;     // [2 of each run][rows][128]
     float2* part_ml;   // [2 of each run][rows] (reference, sum)
     int part_rows;
+    TreeView tree;
 };
 
 // x / n, mostly of 32-bit numbers.
@@ -295,7 +296,7 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
         uint32_t nodes = 0xFFFFFFFFu;
         if (TREE && t0 + kStep - 1 >= load.s.pos0) {
             const int r = load.blk * NT * 8 / a.g + lane, end = (load.blk + 1) * NT * 8;  // a row of the block for each lane
-            nodes = __reduce_or_sync(0xFFFFFFFFu, r < load.s.rows && r * a.g < end ? tree_bits(tree_row(a.tree, load.s.row0, load.s.pos0, load.s.row0 + r), t0) : 0u);
+            nodes = __reduce_or_sync(0xFFFFFFFFu, r < load.s.rows && r * a.g < end ? tree_bits(tree_row(args.tree, load.s.row0, load.s.pos0, load.s.row0 + r), t0) : 0u);
             all = false;
         }
 #pragma unroll
@@ -323,7 +324,7 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
         const int row0 = TREE ? use.blk * NT * 8 : 0;
         if (TREE) {
             const int r = row0 / a.g + lane;
-            some_absent = __any_sync(0xFFFFFFFFu, r < use.s.rows && tree_row(a.tree, use.s.row0, use.s.pos0, use.s.row0 + r).words == 0);
+            some_absent = __any_sync(0xFFFFFFFFu, r < use.s.rows && tree_row(args.tree, use.s.row0, use.s.pos0, use.s.row0 + r).words == 0);
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -514,7 +515,7 @@ __global__ void __launch_bounds__(32 * rows_warps(NT, E4M3), 1) k_rows(const __g
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int r = (use.blk * NT * 8 + nt * 8 + 2 * quad + e) / a.g;
-                        const TreeRow x = tree_row(a.tree, use.s.row0, use.s.pos0, use.s.row0 + (r < use.s.rows ? r : 0));
+                        const TreeRow x = tree_row(args.tree, use.s.row0, use.s.pos0, use.s.row0 + (r < use.s.rows ? r : 0));
                         const uint32_t seen = tree_bits(x, t0);
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
@@ -676,7 +677,7 @@ __global__ void __launch_bounds__(256) k_rows_merge(const __grid_constant__ Rows
     __shared__ float2 s_ml[8];
     __shared__ int64_t s_first[8], s_total[8];
     const AttendView& a = args.a;
-    const bool tree = a.tree.masks != nullptr;
+    const bool tree = args.tree.masks != nullptr;
     const int b = blockIdx.x / args.c.Hkv, j = blockIdx.x - b * args.c.Hkv, blk = blockIdx.y;
     auto blocks = [&](const Seq& x) { return tree ? blocks_of<true>(x, a.g, args.part_rows) : 1; };
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -864,7 +865,7 @@ template <int NT, bool E4M3>
 cudaError_t run_rows(const RowsArgs& r, int sms, cudaStream_t st, int blocks = 1)
 {
     constexpr int kWarps = rows_warps(NT, E4M3);
-    auto kern = r.a.tree.masks ? k_rows<NT, E4M3, true> : k_rows<NT, E4M3, false>;
+    auto kern = r.tree.masks ? k_rows<NT, E4M3, true> : k_rows<NT, E4M3, false>;
     const size_t smem = rows_ring_bytes(NT, E4M3) + (static_cast<size_t>(r.b.n_seqs) + 1) * sizeof(int64_t);
     // the largest call's, whatever this one's: calls from several threads set the same
     constexpr size_t kMost = rows_ring_bytes(NT, E4M3) + (kMaxSeqs + 1) * sizeof(int64_t);
@@ -873,7 +874,7 @@ cudaError_t run_rows(const RowsArgs& r, int sms, cudaStream_t st, int blocks = 1
     if (e != cudaSuccess) return e;
     e = launch_after(st, dim3(sms), 32 * kWarps, smem, 1, kern, r);
     if (e != cudaSuccess) return e;
-    return launch_after(st, dim3(r.b.n_seqs * r.c.Hkv, blocks, r.a.tree.masks ? r.part_rows / kTreeMergeRows : 1), 256, 0, 1, k_rows_merge, r, sms, kWarps);
+    return launch_after(st, dim3(r.b.n_seqs * r.c.Hkv, blocks, r.tree.masks ? r.part_rows / kTreeMergeRows : 1), 256, 0, 1, k_rows_merge, r, sms, kWarps);
 }
 
 // Whether drafted trees of more rows than rows_max go to k_rows all the same, in blocks: where the blocks' walks over the keys are
@@ -881,10 +882,10 @@ cudaError_t run_rows(const RowsArgs& r, int sms, cudaStream_t st, int blocks = 1
 // time of its keys and of 600 more; the tensor cores' route 18 to 22 us over few keys. 32 query heads on 8, bf16, by either: 8
 // nodes at 2,048 15.0 and 21.2 us, 32 at 2,048 22.8 and 22.0, 12 sequences of 8 at 256 23.7 and 19.9; 4 on 1, 8 at 2,048 13.1
 // and 20.5, 12 sequences of 16 at 2,048 20.2 and 22.5. 8-bit: 8 at 2,048 17.5 and 24.5, 3 sequences of 8 at 4,096 30.8 and 30.8.
-bool in_blocks(const AttendView& a, const CacheView& c, bool e4m3, const BatchView& b)
+bool in_blocks(const AttendView& a, const TreeView& tree, const CacheView& c, bool e4m3, const BatchView& b)
 {
     const int64_t rows = static_cast<int64_t>(b.max_rows) * a.g, most = rows_max(e4m3);
-    if (!a.tree.masks || rows <= rows_max(e4m3)) return false;
+    if (!tree.masks || rows <= rows_max(e4m3)) return false;
     int64_t keys = static_cast<int64_t>(b.stride) * c.page_size;
     if (a.n_local >= 0) {
         const int64_t window = static_cast<int64_t>(a.n_sink) + a.n_local + b.max_rows;
@@ -907,7 +908,7 @@ size_t attend_ws_bytes(int Hq, int Hkv, bool e4m3, int n_seqs, int n_rows, int m
     return own > few ? own : few;
 }
 
-cudaError_t launch_attend(const AttendView& a, const CacheView& c, bool e4m3, const BatchView& b, uint8_t* ws,
+cudaError_t launch_attend(const AttendView& a, const TreeView& tree, const CacheView& c, bool e4m3, const BatchView& b, uint8_t* ws,
                           uint64_t timeout_ns, cudaStream_t st)
 {
     int sms = 0;
@@ -915,15 +916,16 @@ cudaError_t launch_attend(const AttendView& a, const CacheView& c, bool e4m3, co
     if (e != cudaSuccess) return e;
     sms = sms < kMaxSms ? sms : kMaxSms;
     const int64_t rows = static_cast<int64_t>(b.max_rows) * a.g;
-    const bool blocks = in_blocks(a, c, e4m3, b);
+    const bool blocks = in_blocks(a, tree, c, e4m3, b);
     const AttendWs lay = attend_layout(a.Hq, c.Hkv, e4m3, b.n_seqs, b.n_rows, b.max_rows, blocks);
     if (rows > rows_max(e4m3) && !blocks) {
         // Batches with longer pieces go there whole, and no second route follows: a sequence of few rows takes its share of
         // that kernel's jobs, at the pace of its keys (17 tokens at 128K, 537 MB of bf16: 103 us, 5.2 TB/s).
-        return launch_chunks(a, c, e4m3, b, sms, reinterpret_cast<int32_t*>(ws + kStatusOffset), ws + lay.chunks, timeout_ns, st);
+        return (tree.masks ? launch_chunks<true> : launch_chunks<false>)(a, tree, c, e4m3, b, sms, reinterpret_cast<int32_t*>(ws + kStatusOffset), ws + lay.chunks,
+                                                                          timeout_ns, st);
     }
     const RowsArgs r{a, c, b, reinterpret_cast<int64_t*>(ws + lay.before), reinterpret_cast<float*>(ws + lay.part_o),
-                     reinterpret_cast<float2*>(ws + lay.part_ml), lay.part_rows};
+                     reinterpret_cast<float2*>(ws + lay.part_ml), lay.part_rows, tree};
     if (blocks) {
         const int n = static_cast<int>((rows + lay.part_rows - 1) / lay.part_rows);
         return e4m3 ? run_rows<3, true>(r, sms, st, n) : run_rows<2, false>(r, sms, st, n);

@@ -80,7 +80,8 @@ __device__ __forceinline__ int f16_exponent(uint32_t top)
 
 // Calls whose sequences may have more than rows_max rows per KV head: tcgen05, 128 rows at a time.
 size_t chunk_ws_bytes(int g, int Hkv, int n_seqs, int n_rows, int max_rows);
-cudaError_t launch_chunks(const AttendView& a, const CacheView& c, bool e4m3, const BatchView& b, int sms,
+template <bool TREE>
+cudaError_t launch_chunks(const AttendView& a, const TreeView& tree, const CacheView& c, bool e4m3, const BatchView& b, int sms,
                           int32_t* status, uint8_t* ws, uint64_t timeout_ns, cudaStream_t st);
 
 }  // namespace scale

@@ -24,6 +24,10 @@
 // as 16-bit halves put together by a byte permutation are half the reads and 3,855 us: the softmax's chain is next.
 // Few query tiles are bound by the plan (7 to 8 us), a CTA's start and end (kPieceTiles tiles) and the
 // unevenness of the last wave.
+#ifndef CHUNK_TREE
+#define CHUNK_TREE 0  // 1 in attend_chunk_tree.cu
+#endif
+
 #include <cuda_bf16.h>
 
 #include "attend.cuh"
@@ -86,6 +90,7 @@ struct ChunkArgs {
     int part_rows;     // 256 or 128
     int32_t* status;
     uint64_t timeout_ns;
+    TreeView tree;
 };
 
 // Key tiles that rows at tokens [pos, pos + n) see: those of the sinks, then from
@@ -198,9 +203,9 @@ __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_consta
         const int first = (n - 1 - (rem - jb->j * n)) * per_item;
         jb->row0 = s.row0 + first;
         jb->ntok = s.rows - first < per_item ? s.rows - first : per_item;
-        jb->pos = s.pos0 + (a.a.tree.masks ? 0 : first);
+        jb->pos = s.pos0 + (CHUNK_TREE ? 0 : first);
         jb->k0 = 0;
-        jb->k1 = tiles_of(a.a, jb->pos, a.a.tree.masks ? s.rows : jb->ntok).n;
+        jb->k1 = tiles_of(a.a, jb->pos, CHUNK_TREE ? s.rows : jb->ntok).n;
         jb->slot = -1;
     };
     const int whole = items > 2 * kMaxSms ? static_cast<int>(items) / a.sms * a.sms : 0;
@@ -673,7 +678,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                     unseen = true;
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
-                        nodes[i] = jv.nodes_seen(a.a.tree, t0 + 64 * i) | static_cast<uint64_t>(jv.nodes_seen(a.a.tree, t0 + 64 * i + 32)) << 32;
+                        nodes[i] = jv.nodes_seen(a.tree, t0 + 64 * i) | static_cast<uint64_t>(jv.nodes_seen(a.tree, t0 + 64 * i + 32)) << 32;
                 }
 #pragma unroll 1  // (the instruction cache: see mma_issue_codes)
                 for (int i = 0; i < 8; ++i) {
@@ -778,7 +783,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 if (TREE) {
                     const int row = qt * tt + r / g;  // rows past the tile's end see what its last row sees
                     node = TreeRow{};
-                    if (T > 0) node = tree_row(a.a.tree, jv.first_row, jv.job.pos, jv.job.row0 + (row < jv.job.ntok ? row : jv.job.ntok - 1));
+                    if (T > 0) node = tree_row(a.tree, jv.first_row, jv.job.pos, jv.job.row0 + (row < jv.job.ntok ? row : jv.job.ntok - 1));
                     p = node.position;
                     pos_first = jv.job.pos;
                     // a row without keys: every tile is masked
@@ -977,7 +982,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                     ok = false;
                     break;
                 }
-                const uint32_t nodes = TREE && t0 + kTile - 1 >= pos_first ? load_job<TREE>(a).nodes_seen(a.a.tree, t0 + 32 * quarter) : 0xFFFFFFFFu;
+                const uint32_t nodes = TREE && t0 + kTile - 1 >= pos_first ? load_job<TREE>(a).nodes_seen(a.tree, t0 + 32 * quarter) : 0xFFFFFFFFu;
                 const int tok = t0 + r, lo = a.a.n_local >= 0 && pos_first > a.a.n_local ? pos_first - a.a.n_local : 0;
                 if (tok > last || (tok < lo && tok >= a.a.n_sink) || !(nodes >> lane & 1u)) {
                     uint8_t* row = smem + off_v(false) + (t & 1) * kTileBytes + r * 128;
@@ -1078,12 +1083,12 @@ constexpr int kMergeCtas = 4;  // per SM, of 256 threads
 
 __global__ void __launch_bounds__(256, kMergeCtas) k_chunk_merge(const __grid_constant__ ChunkArgs a)
 {
-    __shared__ float4 s_o[8][4][32];
+    __shared__ float4 s_o[CHUNK_TREE ? 8 : 1][4][32];
     __shared__ float2 s_ml[8][4];
     pdl_enter();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per_tile = a.tile_tokens * a.a.g;
     const int total = a.p.counts[1] * (a.part_rows / 4);  // at most 2 kMaxSms pairs of 64
-    const bool shared = a.a.tree.masks && total <= static_cast<int>(gridDim.x);
+    const bool shared = CHUNK_TREE && total <= static_cast<int>(gridDim.x);
     const int step = shared ? gridDim.x : gridDim.x * 8;
 #pragma unroll 1
     for (int w = shared ? blockIdx.x : blockIdx.x * 8 + warp; w < total; w += step) {
@@ -1147,7 +1152,7 @@ __global__ void __launch_bounds__(256, kMergeCtas) k_chunk_merge(const __grid_co
             reinterpret_cast<uint2*>(out)[lane] = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
             if (a.a.lse && lane == 0) a.a.lse[row * a.a.Hq + h] = l == 0.f ? -INFINITY : (mx + __log2f(l)) * 0.6931471805599453f;
         };
-        if (!shared) {
+        if (!CHUNK_TREE || !shared) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) store(i, acc[i], __shfl_sync(0xFFFFFFFFu, sum, 8 * i), __shfl_sync(0xFFFFFFFFu, top, 8 * i));
             continue;
@@ -1236,12 +1241,15 @@ cudaError_t run_chunks(const ChunkArgs& a, cudaStream_t st)
 
 }  // namespace
 
+#if !CHUNK_TREE
 size_t chunk_ws_bytes(int g, int Hkv, int n_seqs, int n_rows, int max_rows)
 {
     return chunk_layout(g, Hkv, n_seqs, n_rows, max_rows).end;
 }
+#endif
 
-cudaError_t launch_chunks(const AttendView& a, const CacheView& c, bool e4m3, const BatchView& b, int sms,
+template <bool TREE>
+cudaError_t launch_chunks(const AttendView& a, const TreeView& tree, const CacheView& c, bool e4m3, const BatchView& b, int sms,
                           int32_t* status, uint8_t* ws, uint64_t timeout_ns, cudaStream_t st)
 {
     const ChunkWs w = chunk_layout(a.g, c.Hkv, b.n_seqs, b.n_rows, b.max_rows);
@@ -1260,8 +1268,11 @@ cudaError_t launch_chunks(const AttendView& a, const CacheView& c, bool e4m3, co
     x.part_rows = w.part_rows;
     x.status = status;
     x.timeout_ns = timeout_ns;
-    if (a.tree.masks) return e4m3 ? run_chunks<true, true>(x, st) : run_chunks<false, true>(x, st);
-    return e4m3 ? run_chunks<true, false>(x, st) : run_chunks<false, false>(x, st);
+    x.tree = tree;
+    return e4m3 ? run_chunks<true, TREE>(x, st) : run_chunks<false, TREE>(x, st);
 }
+
+template cudaError_t launch_chunks<CHUNK_TREE>(const AttendView&, const TreeView&, const CacheView&, bool, const BatchView&, int, int32_t*, uint8_t*,
+                                               uint64_t, cudaStream_t);
 
 }  // namespace scale

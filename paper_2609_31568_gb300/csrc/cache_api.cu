@@ -71,9 +71,9 @@ int attend_call(const scale_attend_t* attend, const scale_tree_t* tree, const sc
     if (b.max_rows == 0) return SCALE_OK;
     const float scale = attend->attn_scale > 0.f ? attend->attn_scale : 1.0f / std::sqrt(static_cast<float>(kHeadDim));
     const AttendView a{Hq, Hq / c.Hkv, attend->n_sink, attend->n_local, scale * 1.4426950408889634f,
-                       q, q_stride, out, out_stride, lse,
-                       tree ? TreeView{tree->positions, tree->masks, tree->mask_words} : TreeView{}};
-    return status_of(launch_attend(a, c, e4m3, b, static_cast<uint8_t*>(ws), wait_timeout_ns(), stream));
+                       q, q_stride, out, out_stride, lse};
+    const TreeView nodes = tree ? TreeView{tree->positions, tree->masks, tree->mask_words} : TreeView{};
+    return status_of(launch_attend(a, nodes, c, e4m3, b, static_cast<uint8_t*>(ws), wait_timeout_ns(), stream));
 }
 
 }  // namespace
