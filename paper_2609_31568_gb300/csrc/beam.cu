@@ -16,11 +16,12 @@ using namespace scale_ptx;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kPer = 16;                       // logits of a thread in a step
+constexpr int kPer = 32;                       // logits of a thread in a step
 constexpr int kStepLogits = kThreads * kPer;   // of a CTA
-constexpr int kHalf = kStepLogits / 2;
-constexpr int kList = kHalf + kMaxBest;        // candidates that a CTA holds
-constexpr int kResident = 4;                   // CTAs of an SM
+constexpr int kQuarter = kStepLogits / 4;
+constexpr int kList = kQuarter + kMaxBest;     // candidates that a CTA holds
+template <typename T>
+constexpr int kResident = sizeof(T) == 2 ? 4 : 3;  // CTAs of an SM: 64 registers are few beside fp32 logits
 constexpr int kMaxCandidates = 4096;           // of a group, for k_beam_pick
 constexpr int kMaxParts = 32;                  // of a row
 constexpr float kLog2e = 1.4426950408889634f;
@@ -52,11 +53,14 @@ struct SelectArgs {
 };
 
 struct SelectShared {
-    uint64_t list[kList], other[kList];
+    uint64_t list[kList];
+    union {
+        uint64_t other[kList];           // the list in tighten()
+        float4 x[kWarps][kPer / 4][32];  // a warp's logits of a step, where it has candidates among them or the row ends
+    };
     uint64_t bound[kWarps];
     float2 sums[kWarps];
     int n, kept;
-    float4 x[kWarps][kPer / 4][32];  // a warp's logits of a step, where it has candidates among them or the row ends
 };
 
 // A key that at least `keep` of the threads' `mine` reach (all different, or 0): every warp's each-th largest, each = keep /
@@ -158,14 +162,15 @@ struct Step {
 template <typename T>
 __device__ __noinline__ void collect(SelectShared& sh, uint32_t who, int first, int vocab, uint64_t bound)
 {
-    const int lane = threadIdx.x & 31, i = lane & (kPer - 1);
+    static_assert(kPer == 32, "a lane for each of a thread's logits");
+    const int lane = threadIdx.x & 31, i = lane;
     const float* x = reinterpret_cast<const float*>(sh.x[threadIdx.x >> 5][i >> 2]) + (i & 3);
 #pragma unroll 1
     for (; who; who &= who - 1) {  // a lane for each of its logits
         const int from = __ffs(who) - 1;
         const int t = Step<T>::token(__shfl_sync(0xFFFFFFFFu, first, from), i);
         const uint64_t c = candidate(x[from * 4], t);
-        const uint32_t in = __ballot_sync(0xFFFFFFFFu, lane < kPer && t < vocab && c >= bound);
+        const uint32_t in = __ballot_sync(0xFFFFFFFFu, t < vocab && c >= bound);
         if (in == 0) continue;
         int at = 0;
         if (lane == 0) at = atomicAdd(&sh.n, __popc(in));
@@ -179,11 +184,14 @@ template <typename T>
 __device__ __noinline__ void load_edge(SelectShared& sh, const T* logits, int first, int vocab)
 {
     const int lane = threadIdx.x & 31;
-#pragma unroll 4
+    float x[kPer];
+#pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int t = Step<T>::token(first, i);
-        reinterpret_cast<float*>(&sh.x[threadIdx.x >> 5][i >> 2][lane])[i & 3] = t < vocab ? static_cast<float>(logits[t]) : -INFINITY;
+        x[i] = t < vocab ? static_cast<float>(logits[t]) : -INFINITY;
     }
+#pragma unroll
+    for (int i = 0; i < kPer; i += 4) sh.x[threadIdx.x >> 5][i >> 2][lane] = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
 }
 
 // sum of exp(x - top) of a thread's step with NaN among its logits, which count as -inf
@@ -201,8 +209,8 @@ __device__ __noinline__ float sum_without_nan(const T* logits, int first, int vo
     return y;
 }
 
-// The part's candidates again, where the list ran over: logits that come in ascending order, say. Half a step at a time, the
-// list cut and the bound raised before each.
+// The part's candidates again, where the list ran over: logits that come in ascending order, say. A quarter of a step at a
+// time, the list cut and the bound raised before each.
 template <typename T>
 __device__ __noinline__ int collect_carefully(SelectShared& sh, const T* logits, int vocab, int s0, int s1, int keep)
 {
@@ -212,9 +220,8 @@ __device__ __noinline__ int collect_carefully(SelectShared& sh, const T* logits,
 #pragma unroll 1
     for (int s = s0; s < s1; ++s) {
         const int first = s * kStepLogits + static_cast<int>(threadIdx.x) * Step<T>::kLoad;
-        load_edge<T>(sh, logits, first, vocab);
 #pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
+        for (int q = 0; q < 4; ++q) {
             __syncthreads();
             int n = sh.n;
             __syncthreads();
@@ -223,7 +230,9 @@ __device__ __noinline__ int collect_carefully(SelectShared& sh, const T* logits,
                 bound = sh.list[keep - 1];  // (n was more than is kept)
                 __syncthreads();
             }
-            collect<T>(sh, 0xFFFFu << 16 * half, first, vocab, bound);
+            load_edge<T>(sh, logits, first, vocab);
+            __syncwarp();
+            collect<T>(sh, 0xFFu << 8 * q, first, vocab, bound);
         }
     }
     __syncthreads();
@@ -232,7 +241,7 @@ __device__ __noinline__ int collect_carefully(SelectShared& sh, const T* logits,
 
 // Largest logit, sum of exponentials and best candidates of a part of a row of logits, one pass over them.
 //
-// A step is 4,096 logits, 16 a thread, in 16-byte loads that are made two steps ahead. SKEW: rows begin anywhere; behind a
+// A step is 8,192 logits, 32 a thread, in 16-byte loads that are made a step ahead. SKEW: rows begin anywhere; behind a
 // 16-byte boundary a thread puts its logits together from its load and its neighbour's, so that it has the same tokens
 // wherever the row lies: rows of the same logits have the same sum to the bit, and equal scores stay equal. The sum is a
 // thread's own against its own largest logit, with what a step's sum loses carried to the next. The first step sets the
@@ -242,7 +251,7 @@ __device__ __noinline__ int collect_carefully(SelectShared& sh, const T* logits,
 // stay in the instruction cache (unrolled for 32 logits with the candidates' code in it, 64 x 8 rows of 128,000 took 90 to
 // 300 us, by where the code came to lie).
 template <typename T, bool SKEW>
-__global__ void __launch_bounds__(kThreads, kResident) k_beam_part(const __grid_constant__ SelectArgs a)
+__global__ void __launch_bounds__(kThreads, kResident<T>) k_beam_part(const __grid_constant__ SelectArgs a)
 {
     constexpr int kLoad = Step<T>::kLoad, kLoads = Step<T>::kLoads;
     __shared__ SelectShared sh;
@@ -253,25 +262,20 @@ __global__ void __launch_bounds__(kThreads, kResident) k_beam_part(const __grid_
     uint64_t* const out = a.best + static_cast<int64_t>(blockIdx.x) * keep;
     const T* const logits = static_cast<const T*>(a.b.logits) + static_cast<int64_t>(row) * a.b.stride;
     const int skew = SKEW ? static_cast<int>(reinterpret_cast<uintptr_t>(logits) % 16 / sizeof(T)) : 0;
-    const float score = a.b.scores[row];
-    if (!(fabsf(score) < INFINITY)) {  // its candidates are no matter of its logits
-        if (tid == 0) a.sums[blockIdx.x] = make_float2(-INFINITY, 0.f);
-        return;
-    }
+    const bool live = fabsf(a.b.scores[row]) < INFINITY;  // otherwise its candidates are no matter of its logits
     if (tid == 0) sh.n = 0;
     const int steps = (vocab + kStepLogits - 1) / kStepLogits;
-    const int s0 = part * a.part_steps, s1 = s0 + a.part_steps < steps ? s0 + a.part_steps : steps;
+    const int s0 = part * a.part_steps, s1 = !live ? s0 : s0 + a.part_steps < steps ? s0 + a.part_steps : steps;
     // whether all loads of step s, and the neighbour's behind the last, lie in the row
     auto inside = [&](int s) { return (skew == 0 || s > 0) && (s + 1) * kStepLogits + (skew == 0 ? 0 : kLoad) <= vocab; };
-    uint4 next[2][kLoads];
-    auto load = [&](uint4 (&w)[kLoads], int s) {
+    uint4 next[kLoads];
+    auto load = [&](int s) {
         if (s >= s1 || !inside(s)) return;
 #pragma unroll
         for (int u = 0; u < kLoads; ++u)
-            w[u] = __ldcs(reinterpret_cast<const uint4*>(logits + (s * kStepLogits - skew + tid * kLoad + u * kThreads * kLoad)));
+            next[u] = __ldcs(reinterpret_cast<const uint4*>(logits + (s * kStepLogits - skew + tid * kLoad + u * kThreads * kLoad)));
     };
-    load(next[0], s0);
-    load(next[1], s0 + 1);
+    load(s0);
     float top = -INFINITY, sum = 0.f, lost = 0.f;
     uint64_t bound = 0;
 #pragma unroll 1
@@ -281,7 +285,7 @@ __global__ void __launch_bounds__(kThreads, kResident) k_beam_part(const __grid_
         if (inside(s)) {
 #pragma unroll
             for (int u = 0; u < kLoads; ++u) {
-                uint4 w = next[0][u];
+                uint4 w = next[u];
                 if (SKEW && skew != 0) {
                     uint4 y = make_uint4(__shfl_down_sync(0xFFFFFFFFu, w.x, 1), __shfl_down_sync(0xFFFFFFFFu, w.y, 1),
                                          __shfl_down_sync(0xFFFFFFFFu, w.z, 1), __shfl_down_sync(0xFFFFFFFFu, w.w, 1));
@@ -292,12 +296,11 @@ __global__ void __launch_bounds__(kThreads, kResident) k_beam_part(const __grid_
             }
         } else {
             load_edge<T>(sh, logits, first, vocab);
+            __syncwarp();
 #pragma unroll
             for (int i = 0; i < kPer; i += 4) *reinterpret_cast<float4*>(x + i) = sh.x[warp][i >> 2][lane];
         }
-#pragma unroll
-        for (int u = 0; u < kLoads; ++u) next[0][u] = next[1][u];
-        load(next[1], s + 2);
+        load(s + 1);
         float m = x[0];
 #pragma unroll
         for (int i = 1; i < kPer; ++i) m = fmaxf(m, x[i]);
@@ -398,13 +401,13 @@ __device__ __forceinline__ double score_of(uint64_t order)
 // one against the other. All latency: the parts' sums, their logarithm, then the candidates, which come meanwhile.
 __global__ void __launch_bounds__(kThreads) k_beam_pick(const __grid_constant__ SelectArgs a)
 {
-    extern __shared__ uint64_t s_pick[];
+    extern __shared__ uint64_t s_pick[];  // three words for each candidate
     __shared__ double s_lse[kMaxBeams];
     __shared__ uint64_t s_bound[kWarps];
     __shared__ int s_n;
     pdl_enter();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int beams = a.b.n_beams, keep = a.b.n_best, per_beam = a.parts * keep, all = beams * per_beam, group = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, group = blockIdx.x;
+    const int beams = a.b.n_beams, keep = a.b.n_best, per_beam = a.parts * keep, all = beams * per_beam;
     uint64_t* const scores = s_pick;      // of the candidates; then of those that reach the bound,
     uint64_t* const keys = s_pick + all;  // whose logit and token,
     uint64_t* const ties = s_pick + 2 * all;  // and which of equal scores come first
@@ -422,8 +425,7 @@ __global__ void __launch_bounds__(kThreads) k_beam_pick(const __grid_constant__ 
         if (lane == 0) s_lse[i] = live ? static_cast<double>(top) + log(static_cast<double>(sum)) : INFINITY;
     }
     __syncthreads();
-    // ---- scores: a thread has every 256th candidate; the best of its own
-    uint64_t top = 0;
+    // ---- scores
 #pragma unroll 1
     for (int i = tid; i < all; i += kThreads) {
         const int beam = i / per_beam;
@@ -438,13 +440,16 @@ __global__ void __launch_bounds__(kThreads) k_beam_pick(const __grid_constant__ 
         }
         scores[i] = score;
         keys[i] = key;
-        top = score > top ? score : top;
     }
-    // ---- the bound: least of the warps' each-th largest. Warp w takes the threads w, w + 8, ...: each list is shared by all warps.
     __syncthreads();
-    top = 0;
-#pragma unroll 1
-    for (int i = lane * kWarps + warp; i < all; i += kThreads) top = scores[i] > top ? scores[i] : top;
+    // ---- the bound: least of the warps' each-th largest. A warp has every eighth of a list, from another one on in every list,
+    // whose best is its first; a lane has a list.
+    uint64_t top = 0;
+    for (int l = lane; l < beams * a.parts; l += 32) {
+        const int first = (warp - l) & (kWarps - 1);
+        const uint64_t x = first < keep ? scores[l * keep + first] : 0;
+        top = x > top ? x : top;
+    }
     const int each = (keep + kWarps - 1) / kWarps;
     uint64_t bound = 0;
 #pragma unroll 1
@@ -477,10 +482,11 @@ __global__ void __launch_bounds__(kThreads) k_beam_pick(const __grid_constant__ 
     for (int i = tid; i < n; i += kThreads) {
         const uint64_t score = scores[i], tie = ties[i];
         int rank = 0;
-#pragma unroll 2
+#pragma unroll 4
         for (int j = 0; j < n; ++j) {
             const uint64_t other = scores[j];
-            rank += other > score || (other == score && ties[j] > tie);
+            rank += other > score;
+            if (other == score) rank += ties[j] > tie;
         }
         if (rank >= keep) continue;
         const int64_t at = static_cast<int64_t>(group) * keep + rank;
@@ -551,13 +557,14 @@ struct BeamWs {
     int parts, part_steps;
 };
 
-// Parts of a row: so many that the rows fill the SMs.
+// Parts of a row: so many that the rows give every SM two CTAs. (64 x 8 rows of 128,000, bf16, in one part each 66 us, in two 79;
+// 11 x 5 of 100,003, fp32, in five 29, in eleven 37.)
 BeamWs beam_layout(int n_groups, int n_beams, int vocab, int n_best)
 {
     BeamWs w{};
     const int64_t rows = static_cast<int64_t>(n_groups) * n_beams;
     const int steps = (vocab + kStepLogits - 1) / kStepLogits;
-    int64_t parts = (152 * kResident + rows - 1) / rows;
+    int64_t parts = (2 * 152 + rows - 1) / rows;
     const int most = kMaxCandidates / (n_beams * n_best);
     if (parts > most) parts = most;
     if (parts > kMaxParts) parts = kMaxParts;
