@@ -20,6 +20,7 @@ constexpr int kPer = 32;                       // logits of a thread in a step
 constexpr int kStepLogits = kThreads * kPer;   // of a CTA
 constexpr int kQuarter = kStepLogits / 4;
 constexpr int kList = kQuarter + kMaxBest;     // candidates that a CTA holds
+constexpr int kRanked = 128;                   // of them that are ranked without a bound; at most kThreads
 template <typename T>
 constexpr int kResident = sizeof(T) == 2 ? 4 : 3;  // CTAs of an SM: 64 registers are few beside fp32 logits
 constexpr int kMaxCandidates = 4096;           // of a group, for k_beam_pick
@@ -63,12 +64,12 @@ struct SelectShared {
     int n, kept;
 };
 
-// A key that at least `keep` of the threads' `mine` reach (all different, or 0): every warp's each-th largest, each = keep /
-// warps rounded up, and the least of those. 0 where a warp has fewer.
-__device__ __noinline__ uint64_t bound_of(SelectShared& sh, uint64_t mine, int keep)
+// A key that at least `keep` of the threads' `mine` reach (all different, or 0): the each-th largest of each of the first `warps`
+// warps, each = keep / warps rounded up, and the least of those. 0 where a warp has fewer.
+__device__ __noinline__ uint64_t bound_of(SelectShared& sh, uint64_t mine, int keep, int warps)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int each = (keep + kWarps - 1) / kWarps;
+    const int each = warps > 0 ? (keep + warps - 1) / warps : 0;
     uint64_t bound = 0;
 #pragma unroll 1
     for (int i = 0; i < each; ++i) {
@@ -79,40 +80,64 @@ __device__ __noinline__ uint64_t bound_of(SelectShared& sh, uint64_t mine, int k
     __syncthreads();
     bound = sh.bound[0];
 #pragma unroll 1
-    for (int w = 1; w < kWarps; ++w) bound = sh.bound[w] < bound ? sh.bound[w] : bound;
-    return bound;
+    for (int w = 1; w < warps; ++w) bound = sh.bound[w] < bound ? sh.bound[w] : bound;
+    return each > 32 ? 0 : bound;
 }
 
-// The best `keep` of the list's n candidates, in descending order at its front; returns how many those are. Those below
-// bound_of() go first; the others, a few more than are kept, are ranked one against the other. Every thread calls
-// it, behind a barrier, and leaves through one.
+// How many of n keys are larger than x.
+__device__ __forceinline__ int rank_of(const uint64_t* keys, int n, uint64_t x)
+{
+    int rank = 0;
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) rank += keys[j] > x;
+    return rank;
+}
+
+// The best `keep` of the list's n candidates, in descending order at its front; returns how many those are. Of more than kRanked
+// those below bound_of() go first; the others, a few more than are kept, are ranked one against the other. Every thread
+// calls it, behind a barrier, and leaves through one.
 __device__ __noinline__ int tighten(SelectShared& sh, int n, int keep)
 {
-    const int tid = threadIdx.x, at0 = (tid & 31) * kWarps + (tid >> 5);  // every warp gets its share of a short list
-    uint64_t top = 0;
-#pragma unroll 1
-    for (int at = at0; at < n; at += kThreads) top = sh.list[at] > top ? sh.list[at] : top;
-    if (tid == 0) sh.kept = 0;
-    const uint64_t bound = bound_of(sh, top, keep);
-#pragma unroll 1
-    for (int at = at0; at < n; at += kThreads) {
-        const uint64_t x = sh.list[at];
-        if (x >= bound) sh.other[atomicAdd(&sh.kept, 1)] = x;
-    }
-    __syncthreads();
-    const int m = sh.kept;
-#pragma unroll 1
-    for (int at = tid; at < m; at += kThreads) {
-        const uint64_t x = sh.other[at];
-        int rank = 0;
-#pragma unroll 4
-        for (int j = 0; j < m; ++j) rank += sh.other[j] > x;
+    const int tid = threadIdx.x;
+    if (n <= kRanked) {
+        const uint64_t x = tid < n ? sh.list[tid] : 0;
+        const int rank = tid < n ? rank_of(sh.list, n, x) : keep;
+        __syncthreads();
         if (rank < keep) sh.list[rank] = x;
+        n = n < keep ? n : keep;
+    } else {
+        const int at0 = (tid & 31) * kWarps + (tid >> 5);  // every warp gets its share of a short list
+        uint64_t top = 0;
+#pragma unroll 1
+        for (int at = at0; at < n; at += kThreads) top = sh.list[at] > top ? sh.list[at] : top;
+        if (tid == 0) sh.kept = 0;
+        const uint64_t bound = bound_of(sh, top, keep, kWarps);
+#pragma unroll 1
+        for (int at = at0; at < n; at += kThreads) {
+            const uint64_t x = sh.list[at];
+            if (x >= bound) sh.other[atomicAdd(&sh.kept, 1)] = x;
+        }
+        __syncthreads();
+        const int m = sh.kept;
+#pragma unroll 1
+        for (int at = tid; at < m; at += kThreads) {
+            const uint64_t x = sh.other[at];
+            const int rank = rank_of(sh.other, m, x);
+            if (rank < keep) sh.list[rank] = x;
+        }
+        n = m < keep ? m : keep;
     }
-    n = m < keep ? m : keep;
     if (tid == 0) sh.n = n;
     __syncthreads();
     return n;
+}
+
+// A load that stays where it is written, a step ahead of its use.
+__device__ __forceinline__ uint4 load_once(const void* p)
+{
+    uint4 x;
+    asm volatile("ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "l"(p));
+    return x;
 }
 
 // 16 bytes from `shift` (2 to 14) bytes on of 32.
@@ -245,9 +270,9 @@ __device__ __noinline__ int collect_carefully(SelectShared& sh, const T* logits,
 // 16-byte boundary a thread puts its logits together from its load and its neighbour's, so that it has the same tokens
 // wherever the row lies: rows of the same logits have the same sum to the bit, and equal scores stay equal. The sum is a
 // thread's own against its own largest logit, with what a step's sum loses carried to the next. The first step sets the
-// bound that a candidate has to reach (bound_of, then the least of the n_best best of the step); from then on warps go on
-// without barriers, and one whose threads all stay at or below the bound, which their largest logits tell, needs nothing
-// more. The candidates wait in a list, which is cut at the end. What is rare lies in functions of its own: the loop has to
+// bound that a candidate has to reach (bound_of, then the least of the n_best best so far, again after 2, 4, 8 .. steps if as many follow);
+// between these warps go on without barriers, and one whose threads all stay at or below the bound, which their largest logits tell,
+// needs nothing more. The candidates wait in a list, which is cut at the end. What is rare lies in functions of its own: the loop has to
 // stay in the instruction cache (unrolled for 32 logits with the candidates' code in it, 64 x 8 rows of 128,000 took 90 to
 // 300 us, by where the code came to lie).
 template <typename T, bool SKEW>
@@ -262,10 +287,11 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) k_beam_part(const __gr
     uint64_t* const out = a.best + static_cast<int64_t>(blockIdx.x) * keep;
     const T* const logits = static_cast<const T*>(a.b.logits) + static_cast<int64_t>(row) * a.b.stride;
     const int skew = SKEW ? static_cast<int>(reinterpret_cast<uintptr_t>(logits) % 16 / sizeof(T)) : 0;
-    const bool live = fabsf(a.b.scores[row]) < INFINITY;  // otherwise its candidates are no matter of its logits
+    const float score = a.b.scores[row];
     if (tid == 0) sh.n = 0;
     const int steps = (vocab + kStepLogits - 1) / kStepLogits;
-    const int s0 = part * a.part_steps, s1 = !live ? s0 : s0 + a.part_steps < steps ? s0 + a.part_steps : steps;
+    const int s0 = part * a.part_steps;
+    int s1 = s0 + a.part_steps < steps ? s0 + a.part_steps : steps;
     // whether all loads of step s, and the neighbour's behind the last, lie in the row
     auto inside = [&](int s) { return (skew == 0 || s > 0) && (s + 1) * kStepLogits + (skew == 0 ? 0 : kLoad) <= vocab; };
     uint4 next[kLoads];
@@ -273,9 +299,10 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) k_beam_part(const __gr
         if (s >= s1 || !inside(s)) return;
 #pragma unroll
         for (int u = 0; u < kLoads; ++u)
-            next[u] = __ldcs(reinterpret_cast<const uint4*>(logits + (s * kStepLogits - skew + tid * kLoad + u * kThreads * kLoad)));
+            next[u] = load_once(logits + (s * kStepLogits - skew + tid * kLoad + u * kThreads * kLoad));
     };
     load(s0);
+    if (!(fabsf(score) < INFINITY)) s1 = s0;  // its candidates are no matter of its logits
     float top = -INFINITY, sum = 0.f, lost = 0.f;
     uint64_t bound = 0;
 #pragma unroll 1
@@ -335,11 +362,13 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) k_beam_part(const __gr
 #pragma unroll
             for (int i = kPer - 1; i > 0; --i) at = x[i] == m ? i : at;
             at = x[0] == m ? 0 : at;
-            bound = bound_of(sh, first < vocab ? candidate(m, Step<T>::token(first, at)) : 0, keep);
+            // warps whose threads all have logits
+            const int full = (vocab - s * kStepLogits) / (32 * kLoad);
+            bound = bound_of(sh, first < vocab ? candidate(m, Step<T>::token(first, at)) : 0, keep, full < kWarps ? full : kWarps);
         }
         // equal logits of later steps have higher tokens; a first step that holds n_best has set the bound
         const float least = bound ? value_of(static_cast<uint32_t>(bound >> 32)) : -INFINITY;
-        const uint32_t who = __ballot_sync(0xFFFFFFFFu, s == s0 || bound == 0 ? !(m < least) : m > least);  // (a NaN counts as -inf)
+        const uint32_t who = __ballot_sync(0xFFFFFFFFu, first < vocab && (s == s0 || bound == 0 ? !(m < least) : m > least));  // (a NaN counts as -inf)
         if (who) {
             __syncwarp();
 #pragma unroll
@@ -347,11 +376,12 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) k_beam_part(const __gr
             __syncwarp();
             collect<T>(sh, who, first, vocab, bound);
         }
-        if (s == s0) {
+        const int done = s + 1 - s0;
+        if (s1 - s - 1 >= done && (done & (done - 1)) == 0) {
             __syncthreads();
             const int n = sh.n;
             __syncthreads();  // every thread has read it before the list grows on
-            if (s + 1 < s1 && n > keep && n <= kList) {
+            if (n > keep && n <= kList) {
                 tighten(sh, n, keep);
                 bound = sh.list[keep - 1];
                 __syncthreads();
@@ -371,14 +401,13 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) k_beam_part(const __gr
     for (int o = 16; o > 0; o >>= 1) y += __shfl_xor_sync(0xFFFFFFFFu, y, o);
     if (lane == 0) sh.sums[warp] = make_float2(m, y);
     __syncthreads();
-    if (tid == 0) {
-#pragma unroll 1
-        for (int w = 0; w < kWarps; ++w) m = fmaxf(m, sh.sums[w].x);
-        y = 0.f;
-#pragma unroll 1
-        for (int w = 0; w < kWarps; ++w)
-            if (sh.sums[w].x > -INFINITY) y += sh.sums[w].y * ex2((sh.sums[w].x - m) * kLog2e);
-        a.sums[blockIdx.x] = make_float2(m, y);
+    if (warp == 0) {
+        const float2 mine = lane < kWarps ? sh.sums[lane] : make_float2(-INFINITY, 0.f);
+        m = mine.x;
+        for (int o = kWarps / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+        y = mine.x > -INFINITY ? mine.y * ex2((mine.x - m) * kLog2e) : 0.f;
+        for (int o = kWarps / 2; o > 0; o >>= 1) y += __shfl_xor_sync(0xFFFFFFFFu, y, o);
+        if (lane == 0) a.sums[blockIdx.x] = make_float2(m, y);
     }
 }
 
@@ -401,16 +430,15 @@ __device__ __forceinline__ double score_of(uint64_t order)
 // one against the other. All latency: the parts' sums, their logarithm, then the candidates, which come meanwhile.
 __global__ void __launch_bounds__(kThreads) k_beam_pick(const __grid_constant__ SelectArgs a)
 {
-    extern __shared__ uint64_t s_pick[];  // three words for each candidate
+    extern __shared__ uint64_t s_pick[];  // two words for each candidate
     __shared__ double s_lse[kMaxBeams];
     __shared__ uint64_t s_bound[kWarps];
     __shared__ int s_n;
     pdl_enter();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, group = blockIdx.x;
     const int beams = a.b.n_beams, keep = a.b.n_best, per_beam = a.parts * keep, all = beams * per_beam;
-    uint64_t* const scores = s_pick;      // of the candidates; then of those that reach the bound,
-    uint64_t* const keys = s_pick + all;  // whose logit and token,
-    uint64_t* const ties = s_pick + 2 * all;  // and which of equal scores come first
+    uint64_t* const scores = s_pick;       // of the candidates; then of those that reach the bound
+    uint64_t* const ties = s_pick + all;   // which of equal scores come first: beam, logit and token
     const uint64_t* const best = a.best + static_cast<int64_t>(group) * all;
     uint64_t early = tid < all ? best[tid] : 0;  // on its way while the sums are
     if (tid == 0) s_n = 0;
@@ -439,48 +467,51 @@ __global__ void __launch_bounds__(kThreads) k_beam_pick(const __grid_constant__ 
             if (any) score = order_of(static_cast<double>(-INFINITY));
         }
         scores[i] = score;
-        keys[i] = key;
+        // equal scores: the lower beam, then the logit, then the lower token
+        ties[i] = static_cast<uint64_t>(kMaxBeams - 1 - beam) << 56 | (key >> 32) << 24 | (key & 0xFFFFFFu);
     }
     __syncthreads();
-    // ---- the bound: least of the warps' each-th largest. A warp has every eighth of a list, from another one on in every list,
-    // whose best is its first; a lane has a list.
-    uint64_t top = 0;
-    for (int l = lane; l < beams * a.parts; l += 32) {
-        const int first = (warp - l) & (kWarps - 1);
-        const uint64_t x = first < keep ? scores[l * keep + first] : 0;
-        top = x > top ? x : top;
-    }
-    const int each = (keep + kWarps - 1) / kWarps;
-    uint64_t bound = 0;
-#pragma unroll 1
-    for (int i = 0; i < each; ++i) {
-        bound = warp_max(top);
-        const uint32_t who = __ballot_sync(0xFFFFFFFFu, top == bound);
-        if (lane == __ffs(who) - 1) top = 0;
-    }
-    if (lane == 0) s_bound[warp] = bound;
-    __syncthreads();
-    bound = s_bound[0];
-    for (int w = 1; w < kWarps; ++w) bound = s_bound[w] < bound ? s_bound[w] : bound;
-    // ---- those that reach it, to the front: a block of the list at a time
-#pragma unroll 1
-    for (int i0 = 0; i0 < all; i0 += kThreads) {
-        const int i = i0 + tid;
-        const uint64_t score = i < all ? scores[i] : 0, key = i < all ? keys[i] : 0;
-        __syncthreads();
-        if (score != 0 && score >= bound) {
-            const int at = atomicAdd(&s_n, 1);
-            scores[at] = score;
-            keys[at] = key;
-            // equal scores: the lower beam, then the logit, then the lower token
-            ties[at] = static_cast<uint64_t>(kMaxBeams - 1 - i / per_beam) << 56 | (key >> 32) << 24 | (key & 0xFFFFFFu);
+    int n = all;
+    if (all > kRanked) {
+        // ---- the bound: least of the warps' each-th largest. A warp has every eighth of a list, from another one on in every list,
+        // whose best is its first; a lane has a list.
+        uint64_t top = 0;
+        for (int l = lane; l < beams * a.parts; l += 32) {
+            const int first = (warp - l) & (kWarps - 1);
+            const uint64_t x = first < keep ? scores[l * keep + first] : 0;
+            top = x > top ? x : top;
         }
+        const int each = (keep + kWarps - 1) / kWarps;
+        uint64_t bound = 0;
+#pragma unroll 1
+        for (int i = 0; i < each; ++i) {
+            bound = warp_max(top);
+            const uint32_t who = __ballot_sync(0xFFFFFFFFu, top == bound);
+            if (lane == __ffs(who) - 1) top = 0;
+        }
+        if (lane == 0) s_bound[warp] = bound;
         __syncthreads();
+        bound = s_bound[0];
+        for (int w = 1; w < kWarps; ++w) bound = s_bound[w] < bound ? s_bound[w] : bound;
+        // ---- those that reach it, to the front: a block of the list at a time
+#pragma unroll 1
+        for (int i0 = 0; i0 < all; i0 += kThreads) {
+            const int i = i0 + tid;
+            const uint64_t score = i < all ? scores[i] : 0, tie = i < all ? ties[i] : 0;
+            __syncthreads();
+            if (score != 0 && score >= bound) {
+                const int at = atomicAdd(&s_n, 1);
+                scores[at] = score;
+                ties[at] = tie;
+            }
+            __syncthreads();
+        }
+        n = s_n;
     }
-    const int n = s_n;
 #pragma unroll 1
     for (int i = tid; i < n; i += kThreads) {
         const uint64_t score = scores[i], tie = ties[i];
+        if (score == 0) continue;
         int rank = 0;
 #pragma unroll 4
         for (int j = 0; j < n; ++j) {
@@ -492,7 +523,7 @@ __global__ void __launch_bounds__(kThreads) k_beam_pick(const __grid_constant__ 
         const int64_t at = static_cast<int64_t>(group) * keep + rank;
         a.b.best_scores[at] = static_cast<float>(score_of(score));
         a.b.best_beams[at] = kMaxBeams - 1 - static_cast<int>(tie >> 56);
-        a.b.best_tokens[at] = static_cast<int32_t>(~static_cast<uint32_t>(keys[i]));
+        a.b.best_tokens[at] = static_cast<int32_t>(~static_cast<uint32_t>(tie) & 0xFFFFFFu);
     }
 }
 
@@ -598,9 +629,9 @@ cudaError_t launch_beam_select(const BeamArgs& b, bool fp32, uint8_t* ws, cudaSt
                             : (skew ? k_beam_part<__nv_bfloat16, true> : k_beam_part<__nv_bfloat16, false>);
     cudaError_t e = launch_after(st, grid, kThreads, 0, 1, kern, a);
     if (e != cudaSuccess) return e;
-    const size_t smem = 3 * sizeof(uint64_t) * static_cast<size_t>(b.n_beams) * w.parts * b.n_best;
+    const size_t smem = 2 * sizeof(uint64_t) * static_cast<size_t>(b.n_beams) * w.parts * b.n_best;
     if (smem > kPlainSmem) {
-        constexpr int kMost = 3 * kMaxCandidates * static_cast<int>(sizeof(uint64_t));
+        constexpr int kMost = 2 * kMaxCandidates * static_cast<int>(sizeof(uint64_t));
         e = cudaFuncSetAttribute(k_beam_pick, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
         if (e != cudaSuccess) return e;
     }
