@@ -88,7 +88,7 @@ __device__ __noinline__ uint64_t bound_of(SelectShared& sh, uint64_t mine, int k
 __device__ __forceinline__ int rank_of(const uint64_t* keys, int n, uint64_t x)
 {
     int rank = 0;
-#pragma unroll 4
+#pragma unroll 8
     for (int j = 0; j < n; ++j) rank += keys[j] > x;
     return rank;
 }
@@ -425,6 +425,19 @@ __device__ __forceinline__ double score_of(uint64_t order)
     return __longlong_as_double(static_cast<long long>(order >> 63 ? order & ~(1ull << 63) : ~order));
 }
 
+// The natural logarithm of a sum of 1 or more, whose own accuracy is 2^-22 of it: x = 2^e f with f in [0.75, 1.5), and
+// log f = 2 atanh(t), t = (f - 1) / (f + 1), at most 0.2, from its series in 32 bits, off by 2^-24 at most; e log 2 joins it in 64.
+// (log() in 64 bits is a chain of 64-bit products, 4,000 cycles here.)
+__device__ __forceinline__ double log_of_sum(float x)
+{
+    const uint32_t u = __float_as_uint(x);
+    const int e = static_cast<int>(u - 0x3F400000u) >> 23;
+    const float f = __uint_as_float(u - (static_cast<uint32_t>(e) << 23));
+    const float t = __fdiv_rn(f - 1.0f, f + 1.0f), q = t * t;
+    const float series = fmaf(q, fmaf(q, fmaf(q, fmaf(q, 2.0f / 9.0f, 2.0f / 7.0f), 2.0f / 5.0f), 2.0f / 3.0f), 2.0f);
+    return fma(static_cast<double>(e), 0.6931471805599453, static_cast<double>(t * series));
+}
+
 // The best of a group, a CTA: the logarithms of its beams' sums, and the scores of all candidates in 64 bits (next to another
 // beam's, 32 would decide wrongly). A bound on the score as in bound_of leaves a few more than are kept, which are ranked
 // one against the other. All latency: the parts' sums, their logarithm, then the candidates, which come meanwhile.
@@ -442,15 +455,20 @@ __global__ void __launch_bounds__(kThreads) k_beam_pick(const __grid_constant__ 
     const uint64_t* const best = a.best + static_cast<int64_t>(group) * all;
     uint64_t early = tid < all ? best[tid] : 0;  // on its way while the sums are
     if (tid == 0) s_n = 0;
-    for (int i = warp; i < beams; i += kWarps) {
+    // a power of two of lanes for each beam's parts
+    int width = 1;
+    while (width < a.parts) width *= 2;
+    for (int i0 = 0; i0 < beams; i0 += kThreads / width) {
+        const int i = i0 + tid / width, p = tid & (width - 1);
+        const bool in = i < beams;
         const int row = group * beams + i;
-        const float2 part = lane < a.parts ? a.sums[static_cast<int64_t>(row) * a.parts + lane] : make_float2(-INFINITY, 0.f);
+        const float2 part = in && p < a.parts ? a.sums[static_cast<int64_t>(row) * a.parts + p] : make_float2(-INFINITY, 0.f);
         float top = part.x;
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        for (int o = width / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
         float sum = part.x > -INFINITY ? part.y * ex2((part.x - top) * kLog2e) : 0.f;
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-        const bool live = fabsf(top) < INFINITY && fabsf(a.b.scores[row]) < INFINITY;
-        if (lane == 0) s_lse[i] = live ? static_cast<double>(top) + log(static_cast<double>(sum)) : INFINITY;
+        for (int o = width / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        const bool live = in && fabsf(top) < INFINITY && fabsf(a.b.scores[row]) < INFINITY;
+        if (in && p == 0) s_lse[i] = live ? static_cast<double>(top) + log_of_sum(sum) : INFINITY;
     }
     __syncthreads();
     // ---- scores
@@ -512,12 +530,16 @@ __global__ void __launch_bounds__(kThreads) k_beam_pick(const __grid_constant__ 
     for (int i = tid; i < n; i += kThreads) {
         const uint64_t score = scores[i], tie = ties[i];
         if (score == 0) continue;
-        int rank = 0;
-#pragma unroll 4
+        int rank = 0, equal = 0;
+#pragma unroll 8
         for (int j = 0; j < n; ++j) {
             const uint64_t other = scores[j];
             rank += other > score;
-            if (other == score) rank += ties[j] > tie;
+            equal += other == score;
+        }
+        if (equal > 1) {
+#pragma unroll 8
+            for (int j = 0; j < n; ++j) rank += static_cast<int>(scores[j] == score) & static_cast<int>(ties[j] > tie);
         }
         if (rank >= keep) continue;
         const int64_t at = static_cast<int64_t>(group) * keep + rank;
