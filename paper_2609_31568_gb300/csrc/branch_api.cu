@@ -109,7 +109,11 @@ int scale_cache_move(const scale_cache_t* caches, int32_t n_caches, const scale_
     if (!moves->start && moves->n_moves % moves->n_groups) return SCALE_ERR_INVALID_ARG;
     if (moves->n_moves == 0) return SCALE_OK;
     Pointers p;
-    for (int i = 0; i < n_caches; ++i) need_cache(&p, views[i], e4m3);
+    // by kind: layers often lie in one allocation for each
+    for (int i = 0; i < n_caches; ++i) p.need(views[i].k, 16);
+    for (int i = 0; i < n_caches; ++i) p.need(views[i].v, 16);
+    for (int i = 0; e4m3 && i < n_caches; ++i) p.need(views[i].ks, 16);
+    for (int i = 0; e4m3 && i < n_caches; ++i) p.need(views[i].vs, 16);
     p.need(moves->src, 4);
     p.need(moves->dst, 4);
     if (moves->start) p.need(moves->start, 4);

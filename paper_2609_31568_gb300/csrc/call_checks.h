@@ -1,6 +1,9 @@
 // call_checks.h -- argument checks that the calls over a paged cache share.
 #pragma once
 
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
 #include "branch.cuh"
 #include "scale_internal.h"
 
@@ -8,16 +11,47 @@ namespace scale {
 
 constexpr int64_t kMaxPoolRows = (1ll << 31) - 256;
 
-// Pointer checks of one call: device (or managed) memory of the current device, aligned.
+// cuPointerGetAttributes, resolved once through the runtime's driver entry point; null where there is none.
+inline PFN_cuPointerGetAttributes_v7000 pointer_attributes()
+{
+    static const PFN_cuPointerGetAttributes_v7000 fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q{};
+        const bool ok = cudaGetDriverEntryPointByVersion("cuPointerGetAttributes", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+                        q == cudaDriverEntryPointSuccess;
+        if (!ok) cudaGetLastError();
+        return ok ? reinterpret_cast<PFN_cuPointerGetAttributes_v7000>(p) : nullptr;
+    }();
+    return fn;
+}
+
+// Pointer checks of one call: device (or managed) memory of the current device, aligned. A pointer into the allocation of the one
+// before it is not looked up again: the caches of 32 layers are 128 pointers, 80 ns each.
 struct Pointers {
     int dev = -1;
     bool ok = true;
+    uintptr_t lo = 0, hi = 0;  // the allocation that was looked up last
     Pointers() { ok = cudaGetDevice(&dev) == cudaSuccess; }
     void need(const void* p, size_t align)
     {
         if (!ok) return;
         if (!p || reinterpret_cast<uintptr_t>(p) % align) {
             ok = false;
+            return;
+        }
+        const uintptr_t x = reinterpret_cast<uintptr_t>(p);
+        if (x >= lo && x < hi) return;
+        if (const auto look_up = pointer_attributes()) {
+            unsigned int type = 0, managed = 0;
+            int ordinal = -1;
+            void* start = nullptr;
+            size_t size = 0;
+            CUpointer_attribute which[5] = {CU_POINTER_ATTRIBUTE_MEMORY_TYPE, CU_POINTER_ATTRIBUTE_DEVICE_ORDINAL, CU_POINTER_ATTRIBUTE_IS_MANAGED,
+                                            CU_POINTER_ATTRIBUTE_RANGE_START_ADDR, CU_POINTER_ATTRIBUTE_RANGE_SIZE};
+            void* to[5] = {&type, &ordinal, &managed, &start, &size};
+            ok = look_up(5, which, to, static_cast<CUdeviceptr>(x)) == CUDA_SUCCESS && (managed || (type == CU_MEMORYTYPE_DEVICE && ordinal == dev));
+            lo = ok ? reinterpret_cast<uintptr_t>(start) : 0;
+            hi = ok ? lo + size : 0;
             return;
         }
         cudaPointerAttributes at{};
