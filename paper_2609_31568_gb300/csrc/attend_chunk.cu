@@ -150,6 +150,9 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* s_warp, int64_
 __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_constant__ ChunkArgs a)
 {
     __shared__ int s_before[kMaxSeqs + 1];  // items (of one KV head) of the sequences before
+#if CHUNK_TREE
+    __shared__ int s_tiles[kPlanThreads], s_order[kPlanThreads];
+#endif
     __shared__ int64_t s_warp[32];
     __shared__ int s_longest, s_long[32], s_tail[32], s_split[32], s_cut;
     __shared__ float s_cut_tail;
@@ -160,10 +163,34 @@ __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_consta
     const int per_item = 2 * a.tile_tokens;
     const int per = (a.b.n_seqs + kPlanThreads - 1) / kPlanThreads;
     const int i0 = tid * per < a.b.n_seqs ? tid * per : a.b.n_seqs, i1 = i0 + per < a.b.n_seqs ? i0 + per : a.b.n_seqs;
+#if CHUNK_TREE
+    // The sequences by their keys, most first, where there is a thread for each: CTAs take jobs in order, and those of a short
+    // sequence fill up what long ones leave uneven. (Causal calls keep their order: a sequence's pairs differ in length there.)
+    const bool ordered = a.b.n_seqs <= kPlanThreads;
+    if (ordered) {
+        int n = -1;
+        if (tid < a.b.n_seqs) {
+            const Seq s = seq_of(a.a, a.b, tid);
+            n = s.rows > 0 ? tiles_of(a.a, s.pos0, s.rows).n : 0;
+        }
+        s_tiles[tid] = n;
+        __syncthreads();
+        if (tid < a.b.n_seqs) {
+            int rank = 0;
+#pragma unroll 4
+            for (int j = 0; j < a.b.n_seqs; ++j) rank += s_tiles[j] > n || (s_tiles[j] == n && j < tid);
+            s_order[rank] = tid;
+        }
+        __syncthreads();
+    }
+    auto seq_at = [&](int i) { return ordered ? s_order[i] : i; };
+#else
+    auto seq_at = [](int i) { return i; };
+#endif
     int64_t mine = 0;
 #pragma unroll 1
     for (int i = i0; i < i1; ++i) {
-        const Seq s = seq_of(a.a, a.b, i);
+        const Seq s = seq_of(a.a, a.b, seq_at(i));
         s_before[i] = static_cast<int>(mine);
         if (s.rows > 0) mine += static_cast<uint32_t>(s.rows + per_item - 1) / static_cast<uint32_t>(per_item);
     }
@@ -197,8 +224,9 @@ __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_consta
         }
         const int n = s_before[lo + 1] - s_before[lo];
         const int rem = x - s_before[lo] * a.c.Hkv;
-        const Seq s = seq_of(a.a, a.b, lo);
-        jb->b = lo;
+        const int b = seq_at(lo);
+        const Seq s = seq_of(a.a, a.b, b);
+        jb->b = b;
         jb->j = static_cast<int>(static_cast<uint32_t>(rem) / static_cast<uint32_t>(n));
         const int first = (n - 1 - (rem - jb->j * n)) * per_item;
         jb->row0 = s.row0 + first;
@@ -339,32 +367,6 @@ __host__ __device__ constexpr uint32_t off_raw(bool e4m3) { return kOffK + 2 * (
 __host__ __device__ constexpr uint32_t off_v(bool e4m3) { return off_raw(e4m3) + (e4m3 ? 2 * kCodeBytes : 0); }
 __host__ __device__ constexpr uint32_t off_shared(bool e4m3) { return off_v(e4m3) + 2 * kTileBytes; }
 
-struct ChunkShared {
-    Barriers bars;
-    uint32_t tmem_slot;
-    volatile int abort_flag;
-    // 8-bit only
-    uint64_t q_ready;                    // Q is in its parts
-    uint64_t raw_full[2], raw_empty[2];  // codes of V: landed; turned
-    uint64_t v_full[2];                  // V is bf16
-};
-// 8-bit: per softmax warp, what the products with each key of its tile are multiplied by
-__host__ __device__ constexpr uint32_t off_scales(bool e4m3) { return off_shared(e4m3) + 256; }
-__host__ __device__ constexpr uint32_t chunk_smem(bool e4m3) { return off_scales(e4m3) + (e4m3 ? 8 * kTile * 4 : 0); }
-static_assert(sizeof(ChunkShared) <= 256 && off_scales(true) % 16 == 0, "scales are read four at a time");
-static_assert(chunk_smem(true) <= 227 * 1024 && chunk_smem(false) <= 227 * 1024, "shared memory of a CTA");
-
-// Threads: warps 0-7 softmax, 8 producer, 9 MMA; 8-bit: 12-15 turn V into bf16 (10 and 11 idle,
-// for whole groups of four warps in the register split: 2 x 128 x 192 + 2 x 128 x 64 = 512 x 128).
-__host__ __device__ constexpr int chunk_threads(bool e4m3) { return e4m3 ? 512 : 320; }
-
-__device__ __forceinline__ float4 lds_f4(uint32_t addr)
-{
-    float4 r;
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(r.x), "=f"(r.y), "=f"(r.z), "=f"(r.w) : "r"(addr));
-    return r;
-}
-
 // A CTA's job as its roles see it; T = 0: none.
 struct JobView {
     ChunkJob job;
@@ -389,6 +391,36 @@ struct JobView {
         return __reduce_or_sync(0xFFFFFFFFu, bits);
     }
 };
+
+constexpr uint32_t kSharedBytes = CHUNK_TREE ? 1024 : 256;
+struct ChunkShared {
+    Barriers bars;
+    uint32_t tmem_slot;
+    volatile int abort_flag;
+    // 8-bit only
+    uint64_t q_ready;                    // Q is in its parts
+    uint64_t raw_full[2], raw_empty[2];  // codes of V: landed; turned
+    uint64_t v_full[2];                  // V is bf16
+#if CHUNK_TREE
+    JobView jobs[8];  // of the softmax warps, for what comes after their loops (lists and job again: 1.5 us)
+#endif
+};
+// 8-bit: per softmax warp, what the products with each key of its tile are multiplied by
+__host__ __device__ constexpr uint32_t off_scales(bool e4m3) { return off_shared(e4m3) + kSharedBytes; }
+__host__ __device__ constexpr uint32_t chunk_smem(bool e4m3) { return off_scales(e4m3) + (e4m3 ? 8 * kTile * 4 : 0); }
+static_assert(sizeof(ChunkShared) <= kSharedBytes && off_scales(true) % 16 == 0, "scales are read four at a time");
+static_assert(chunk_smem(true) <= 227 * 1024 && chunk_smem(false) <= 227 * 1024, "shared memory of a CTA");
+
+// Threads: warps 0-7 softmax, 8 producer, 9 MMA; 8-bit: 12-15 turn V into bf16 (10 and 11 idle,
+// for whole groups of four warps in the register split: 2 x 128 x 192 + 2 x 128 x 64 = 512 x 128).
+__host__ __device__ constexpr int chunk_threads(bool e4m3) { return e4m3 ? 512 : 320; }
+
+__device__ __forceinline__ float4 lds_f4(uint32_t addr)
+{
+    float4 r;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(r.x), "=f"(r.y), "=f"(r.z), "=f"(r.w) : "r"(addr));
+    return r;
+}
 
 // Waits for the plan, then reads the job of this CTA.
 template <bool TREE>
@@ -746,6 +778,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
         // the tile's first, which is also the last that all of the tile's rows see (8-bit: or -1, to mask every tile), and the
         // first from which the window hides nothing of the tile; the CTA's last token
         int T = 0, k0 = 0, sinks = 0, past = 0, p = 0, pos_first = 0, plain_to = 0, open_from = 0, last = 0;
+        uint32_t last_nodes = 0xFFFFFFFFu;  // TREE, bf16: of the last tile's keys of this warp's rows of V those that a row sees
         TreeRow node{};  // TREE: this row's mask; pos_first is the token of the sequence's first node, p the row's position
         int seq = 0, kvh = 0;
         auto token_of = [&](int t) { return (k0 + t < sinks ? k0 + t : k0 + t + past) * kTile; };
@@ -780,6 +813,10 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 seq = jv.job.b;
                 kvh = jv.job.j;
                 last = jv.last;
+#if CHUNK_TREE
+                if (lane == 0) sh.jobs[warp] = jv;
+                __syncwarp();
+#endif
                 if (TREE) {
                     const int row = qt * tt + r / g;  // rows past the tile's end see what its last row sees
                     node = TreeRow{};
@@ -788,6 +825,8 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                     pos_first = jv.job.pos;
                     // a row without keys: every tile is masked
                     plain_to = __any_sync(0xFFFFFFFFu, node.words == 0) ? -1 : pos_first - 1;
+                    // the last tile's nodes, while the first products are made
+                    if (!E4M3 && qt == 0 && T > 0 && token_of(T - 1) + kTile - 1 >= pos_first) last_nodes = jv.nodes_seen(a.tree, token_of(T - 1) + 32 * quarter);
                     const int pos_last = __reduce_max_sync(0xFFFFFFFFu, p);
                     open_from = a.a.n_local >= 0 && pos_last > a.a.n_local ? pos_last - a.a.n_local : 0;
                 } else {
@@ -863,6 +902,11 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 next_scales = scales_of(next_place);
                 next_place = place_of(t + 2);
             }
+            uint32_t bits[4] = {~0u, ~0u, ~0u, ~0u};  // TREE: of the tile's keys those that the row sees, on their way while S is
+            if (TREE && t >= 0 && token_of(t) + kTile - 1 > plain_to) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) bits[c] = tree_bits(node, token_of(t) + 32 * c);
+            }
             if (t >= 0) {
                 const bool got = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.s_full[qt][t & 1], (t >> 1) & 1, a.timeout_ns, &abort_flag));
                 if (!got) {
@@ -902,7 +946,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 auto load_32 = [&](uint32_t (&sr)[32], int c) {
                     tmem_ld32(s_addr + c * 32, sr);
                     uint32_t seen = 0xFFFFFFFFu;
-                    if (masked) seen = (TREE ? tree_bits(node, t0 + 32 * c) : 0xFFFFFFFFu) & ones_below(lim - 32 * c) & ~(ones_below(low - 32 * c) & ~ones_below(gap - 32 * c));
+                    if (masked) seen = (TREE ? (c & 2 ? (c & 1 ? bits[3] : bits[2]) : c & 1 ? bits[1] : bits[0]) : 0xFFFFFFFFu) & ones_below(lim - 32 * c) & ~(ones_below(low - 32 * c) & ~ones_below(gap - 32 * c));
                     tmem_ld_wait();
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
@@ -982,7 +1026,12 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                     ok = false;
                     break;
                 }
-                const uint32_t nodes = TREE && t0 + kTile - 1 >= pos_first ? load_job<TREE>(a).nodes_seen(a.tree, t0 + 32 * quarter) : 0xFFFFFFFFu;
+#if CHUNK_TREE
+                uint32_t nodes = 0xFFFFFFFFu;
+                if (t0 + kTile - 1 >= pos_first) nodes = t == T - 1 ? last_nodes : sh.jobs[warp].nodes_seen(a.tree, t0 + 32 * quarter);
+#else
+                constexpr uint32_t nodes = 0xFFFFFFFFu;
+#endif
                 const int tok = t0 + r, lo = a.a.n_local >= 0 && pos_first > a.a.n_local ? pos_first - a.a.n_local : 0;
                 if (tok > last || (tok < lo && tok >= a.a.n_sink) || !(nodes >> lane & 1u)) {
                     uint8_t* row = smem + off_v(false) + (t & 1) * kTileBytes + r * 128;
@@ -996,7 +1045,11 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
             mbar_arrive(&bars.p_full[qt]);
         }
         if (T > 0) {
+#if CHUNK_TREE
+            const JobView& jv = sh.jobs[warp];
+#else
             const JobView jv = load_job<TREE>(a);  // (again: nothing of it is kept through the loop)
+#endif
             const ChunkJob& job = jv.job;
             bool go = __all_sync(0xFFFFFFFFu, ok && !abort_flag);
             if (go) go = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.o_full, 0, a.timeout_ns, &abort_flag));
