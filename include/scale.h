@@ -508,7 +508,8 @@ int scale_cache_attend_tree(const scale_attend_t *attend, const scale_tree_t *tr
 typedef struct {
     int32_t *src, *dst;   /* [n_moves]                                                              */
     const int32_t *start; /* [n_groups + 1], ascending: group g has the moves [start[g], start[g + 1])
-                             (those within n_moves); NULL: n_moves / n_groups moves each            */
+                             (those within n_moves); NULL: n_moves / n_groups moves each, in no
+                             order: no move reads a row that any writes                             */
     int32_t n_groups;     /* 1..4096                                                                */
     int32_t n_moves;
 } scale_moves_t;

@@ -136,8 +136,9 @@ __global__ void __launch_bounds__(kAcceptThreads) k_tree_accept(const __grid_con
 }
 
 // Moves. A warp has 512 bytes (or the whole row, where that is less) of every row of a group's keys or values in one cache, or
-// the scales of either, so that no two warps touch the same bytes and a group's order is a warp's own. Moves that are none
-// are left out 32 at a time; of the others the rows of kAtOnce copies are read before any is written.
+// the scales of either, so that no two warps touch the same bytes and a group's order is a warp's own (groups of equal
+// size, whose moves have none, are shared by warps 32 moves at a time). Moves that are none are left out 32 at a time; of the others
+// the rows of kAtOnce copies are read before any is written.
 constexpr int kMoveWarps = 8;
 constexpr int kAtOnce = 8;
 
@@ -150,18 +151,19 @@ struct MoveArgs {
     int row_bytes;  // of all heads
     int parts;      // pieces of 512 bytes of a row
     int units;      // parts (and one for scales) of keys and of values
+    int blocks;     // of 32 moves of a group whose moves may come in any order; 1 where they may not
     MoveLayer layers[kMoveCaches];
 };
 
-__global__ void __launch_bounds__(32 * kMoveWarps) k_move(const __grid_constant__ MoveArgs a)
+__global__ void __launch_bounds__(32 * kMoveWarps, 3) k_move(const __grid_constant__ MoveArgs a)
 {
     __shared__ int2 s_moves[kMoveWarps][32];
     pdl_enter();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int unit = blockIdx.x * kMoveWarps + warp;
-    const int group = unit / a.units;
+    const int block = unit / a.units, group = block / a.blocks;
     if (group >= a.m.n_groups) return;
-    const int part = (unit - group * a.units) >> 1;
+    const int part = (unit - block * a.units) >> 1;
     const bool values = unit & 1;
     const MoveLayer& layer = a.layers[blockIdx.y];
     int begin, end;
@@ -171,9 +173,9 @@ __global__ void __launch_bounds__(32 * kMoveWarps) k_move(const __grid_constant_
         begin = begin > 0 ? begin : 0;
         end = end < a.m.n_moves ? end : a.m.n_moves;
     } else {
-        const int each = a.m.n_moves / a.m.n_groups;
-        begin = group * each;
-        end = begin + each;
+        const int each = a.m.n_moves / a.m.n_groups, first = (block - group * a.blocks) * 32;
+        begin = group * each + first;
+        end = begin + (each - first < 32 ? each - first : 32);
     }
     int2* const list = s_moves[warp];
     const int left = a.row_bytes - part * 512;
@@ -262,7 +264,8 @@ cudaError_t launch_moves(const CacheView* caches, int n, bool e4m3, const MovesV
     a.row_bytes = a.Hkv * kHeadDim * (e4m3 ? 1 : 2);
     a.parts = (a.row_bytes + 511) / 512;
     a.units = 2 * (a.parts + (e4m3 ? 1 : 0));
-    const int64_t warps = static_cast<int64_t>(m.n_groups) * a.units;
+    a.blocks = m.start ? 1 : (m.n_moves / m.n_groups + 31) / 32;
+    const int64_t warps = static_cast<int64_t>(m.n_groups) * a.blocks * a.units;
     for (int i0 = 0; i0 < n; i0 += kMoveCaches) {
         const int layers = n - i0 < kMoveCaches ? n - i0 : kMoveCaches;
         for (int i = 0; i < layers; ++i) a.layers[i] = MoveLayer{caches[i0 + i].k, caches[i0 + i].v, caches[i0 + i].ks, caches[i0 + i].vs};
