@@ -185,6 +185,17 @@ def test_select_in_a_graph_on_two_streams():
         assert all(same_bits(x, y) for x, y in zip(mine[:3], other[:3]))
 
 
+def test_rows_far_apart():
+    """A stride by which the last rows lie more than 2^31 logits behind the first."""
+    rows, vocab = 20, 5001
+    buf = torch.empty(rows, 1 << 27, dtype=torch.bfloat16, device="cuda")
+    view = buf[:, 77: 77 + vocab]
+    view.copy_(random_logits(rows, vocab, 3, torch.bfloat16))
+    scores = -5 * torch.rand(5, 4, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
+    want = select(view.contiguous(), scores, 9)
+    assert all(same_bits(x, y) for x, y in zip(select(view, scores, 9), want))
+
+
 # ---------------------------------------------------------------- reordering
 
 
@@ -240,6 +251,48 @@ def test_reorder(groups, beams, page, stride, e4m3, in_place, seed):
     assert dst.view(n, page).tolist() == [[x for _, x in m] for m in flat]
     for kv, w in zip(held, want):
         assert all(same_bits(x, y) for x, y in zip(kv, w))
+
+
+def test_a_captured_reordering_follows_its_lists():
+    groups, beams, page, stride = 3, 4, 16, 5
+    n = groups * beams
+    held, layers = caches_of(2, n * stride, page, 2, True)
+    fresh = [[x.clone() for x in kv] for kv in held]
+    table = torch.randperm(n * stride, device="cuda").int().view(n, stride)
+    kv_len, parents = ints([37] * n), torch.zeros(groups, beams, dtype=torch.int32, device="cuda")
+    moves = S.cache_moves(ints([0] * (n * page)), ints([0] * (n * page)), n_groups=n)
+    out = torch.empty_like(table)
+
+    def call():
+        S.scale_beam_reorder(layers, table, kv_len, parents, out, moves)
+        S.scale_cache_move(layers, moves)
+
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for seed in (1, 2, 3):
+        rng = random.Random(seed)
+        p = [[rng.randrange(beams) for _ in range(beams)] for _ in range(groups)]
+        parents.copy_(ints(p))
+        kv_len.fill_(20 + seed)
+        want_t = []
+        want = [[x.clone() for x in kv] for kv in fresh]
+        for b in range(groups):
+            rows, m = reorder(table[b * beams: (b + 1) * beams].tolist(), p[b], 20 + seed, page)
+            want_t += rows
+            for kv in want:
+                for x in kv:
+                    for y in m:
+                        apply_moves(x, y, page)
+        for kv, f in zip(held, fresh):
+            for x, y in zip(kv, f):
+                x.copy_(y)
+        g.replay()
+        torch.cuda.synchronize()
+        assert out.tolist() == want_t
+        assert all(same_bits(x, y) for kv, w in zip(held, want) for x, y in zip(kv, w))
 
 
 def test_beam_search_over_the_cache_equals_copied_sequences():

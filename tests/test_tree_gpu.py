@@ -390,6 +390,97 @@ def test_moves(e4m3, hkv, layers):
         assert all(same_bits(x, y) for x, y in zip(kv, want))
 
 
+def test_rows_past_max_rows_stay():
+    """A bound below a sequence's rows: the rows past it are left as they were, and their nodes are none."""
+    bt = Batch([9, 3], [60, 30], hq=4, hkv=1, page=16, e4m3=False)
+    bt.batch = S.kv_batch(bt.row_start, bt.kv_len, bt.table, bt.n_rows, 4)
+    parents = [[-1, 0, 0, 1, 3, 4, 0, 0, 1], [-1, 0, 1]]
+    seen, positions = planned(bt, parents)
+    masks = torch.from_numpy(as_words(seen, 1)).cuda()
+    masks |= 1 << 7  # a node past max_rows
+    a = S.attend_params(num_q_heads=4)
+    ws = torch.empty(S.scale_cache_attend_workspace_size(a, bt.cache, bt.batch), dtype=torch.uint8, device="cuda")
+    S.scale_workspace_init(ws)
+    out = torch.full((12, 4, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    S.scale_cache_attend_tree(a, S.draft_tree(None, ints(positions), masks), bt.cache, bt.batch, bt.q, out, None, ws)
+    want, _, tol, _ = attend_tree64(bt, bt.q, seen, positions)
+    rows = [0, 1, 2, 3, 9, 10, 11]
+    within(out[rows], want[rows], tol[rows])
+    assert bool((out[4:9] == 7.0).all())
+    path, src, dst = (ints([-77] * 12) for _ in range(3))
+    out = [ints([-77] * 2) for _ in range(3)]
+    tokens, choices = ints([1, 2, 9, 3, 4, 5, 6, 7, 8, 1, 2, 3]), ints([2, 3, 0, 4, 0, 0, 0, 0, 0, 2, 3, 6])
+    moves = S.cache_moves(src, dst, bt.row_start)
+    S.scale_tree_accept(S.draft_tree(ints([p for x in parents for p in x]), ints([0] * 12), ints([[0]] * 12)), S.cache_layers([bt.cache]),
+                        bt.batch, tokens, choices, ints([1, 1]), out[0], path, out[1], out[2], moves)
+    assert path.tolist() == [0, 1, 3, -1] + [-77] * 5 + [0, 1, 2]
+    assert [x.tolist() for x in out] == [[3, 3], [4, 6], [54, 30]]
+    assert src.tolist()[4:9] == [-77] * 5
+
+
+def test_a_captured_step_follows_its_lists_on_another_stream():
+    """Plan, walk and moves captured once and replayed with other trees, beside eager calls on a stream of their own."""
+    nodes, seqs, page, hkv = 24, 3, 16, 2
+    table = torch.randperm(seqs * 8, device="cuda").int().view(seqs, 8)
+    row_start, kv_len = ints(np.arange(seqs + 1) * nodes), ints([100, 40, 77])
+    rows = seqs * nodes
+    parents, tokens, choices, first = ints([-1] * rows), ints([0] * rows), ints([0] * rows), ints([0] * seqs)
+    fresh = torch.randn(2, seqs * 8, page, hkv, 128, device="cuda").bfloat16()
+
+    def side():
+        pages = [fresh[i].clone() for i in range(2)]
+        layers = S.cache_layers([S.kv_cache(*pages)])
+        batch = S.kv_batch(row_start, kv_len, table, rows, nodes)
+        tree = S.draft_tree(parents, ints([0] * rows), ints([[0]] * rows))
+        moves = S.cache_moves(ints([0] * rows), ints([0] * rows), row_start)
+        outs = [ints([0] * seqs), ints([0] * rows), ints([0] * seqs), ints([0] * seqs)]
+
+        def call(stream=None):
+            S.scale_tree_plan(tree, batch, stream=stream)
+            S.scale_tree_accept(tree, layers, batch, tokens, choices, first, *outs, moves, stream=stream)
+            S.scale_cache_move(layers, moves, stream=stream)
+
+        return pages, list(tree.tensors[1:]) + outs + list(moves.tensors[:2]), call
+
+    mine, other = side(), side()
+    mine[2]()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        mine[2]()
+    stream = torch.cuda.Stream()
+    for seed in (1, 2, 3):
+        rng = random.Random(seed)
+        parents.copy_(ints([p for _ in range(seqs) for p in random_parents(rng, nodes, gone=0.1)]))
+        tokens.copy_(ints([rng.randrange(2) for _ in range(rows)]))
+        choices.copy_(ints([rng.randrange(2) for _ in range(rows)]))
+        for pages, _, _ in (mine, other):
+            for x, y in zip(pages, fresh):
+                x.copy_(y)
+        torch.cuda.synchronize()
+        g.replay()
+        other[2](stream)
+        torch.cuda.synchronize()
+        assert all(same_bits(x, y) for x, y in zip(mine[0] + mine[1], other[0] + other[1]))
+        assert int(mine[1][2].sum()) > 0
+
+
+def test_moves_beyond_32_bits():
+    """A pool of more than 2^32 bytes of keys."""
+    hkv, page = 64, 16
+    pages = (1 << 32) // (hkv * 256 * page) + 100
+    kv = [torch.zeros(pages, page, hkv, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    far = pages * page - 3
+    for x in kv:
+        x.view(-1, hkv, 128)[far] = torch.randn(hkv, 128, device="cuda").bfloat16()
+    layers = S.cache_layers([S.kv_cache(*kv)])
+    S.scale_cache_move(layers, S.cache_moves(ints([far, far]), ints([5, far - 40]), n_groups=2))
+    for x in kv:
+        rows = x.view(-1, hkv, 128)
+        assert same_bits(rows[5], rows[far]) and same_bits(rows[far - 40], rows[far]) and bool((rows[far] != 0).any())
+        assert not bool(rows[6: far - 40].any()) and not bool(rows[:5].any())
+
+
 # ---------------------------------------------------------------- a step
 
 
