@@ -511,7 +511,7 @@ typedef struct {
                              (those within n_moves); NULL: n_moves / n_groups moves each, in no
                              order: no move reads a row that any writes                             */
     int32_t n_groups;     /* 1..4096                                                                */
-    int32_t n_moves;
+    int32_t n_moves;      /* at most 2^28 (SCALE_ERR_UNSUPPORTED)                                     */
 } scale_moves_t;
 
 /* The moves in each of n_caches caches (1..1024; the layers' of one batch: all of the same type,
@@ -553,7 +553,7 @@ typedef struct {
 /* The best continuations of each group of beams. Token v after beam i of a group scores
  *   scores[i] + log softmax(logits of the beam)[v],
  * in 64 bits from sums in 32 that are kept to 2^-22 of them; the n_best largest are written in descending order, equal ones
- * by the lower beam, then the lower token. A NaN logit counts as -inf; every continuation of a beam whose score
+ * by the lower beam, then the larger logit, then the lower token. A NaN logit counts as -inf; every continuation of a beam whose score
  * is not finite, or whose logits have no finite maximum, scores -inf and is taken in its turn like any other.
  *   logits      [n_groups * n_beams][vocab], rows logits_stride elements apart (at least vocab), aligned to their type
  *   scores      fp32 [n_groups][n_beams]

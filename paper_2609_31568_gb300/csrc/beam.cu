@@ -662,7 +662,7 @@ cudaError_t launch_beam_select(const BeamArgs& b, bool fp32, uint8_t* ws, cudaSt
 
 cudaError_t launch_reorder(const ReorderArgs& a, cudaStream_t st)
 {
-    const dim3 grid((a.stride + kColumns - 1) / kColumns, a.n_groups);
+    const dim3 grid((a.stride - 1) / kColumns + 1, a.n_groups);
     return launch_after(st, grid, kColumns, 0, 1, k_reorder, a);
 }
 

@@ -12,6 +12,7 @@ constexpr int kMaxBest = 64;        // continuations kept of a group
 constexpr int kMaxVocab = 1 << 24;
 constexpr int kMaxCaches = 1024;    // of scale_cache_move
 constexpr int kMoveCaches = 64;     // of them in a launch
+constexpr int kMaxMoves = 1 << 28;  // k_move numbers its warps in 31 bits: 66 at most for 32 moves, or for a group of 33 twice as many
 constexpr size_t kPlainSmem = 32 * 1024;  // dynamic shared memory that a kernel has without asking
 
 struct TreeArgs {

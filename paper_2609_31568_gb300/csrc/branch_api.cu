@@ -16,7 +16,7 @@ bool share(const void* x, size_t xn, const void* y, size_t yn)
 int check_moves(const scale_moves_t* m)
 {
     if (!m || m->n_groups <= 0 || m->n_moves < 0) return SCALE_ERR_INVALID_ARG;
-    return m->n_groups > kMaxSeqs ? SCALE_ERR_UNSUPPORTED : SCALE_OK;
+    return m->n_groups > kMaxSeqs || m->n_moves > kMaxMoves ? SCALE_ERR_UNSUPPORTED : SCALE_OK;
 }
 
 int check_beam(const scale_beam_t* b)

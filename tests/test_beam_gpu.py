@@ -185,6 +185,19 @@ def test_select_in_a_graph_on_two_streams():
         assert all(same_bits(x, y) for x, y in zip(mine[:3], other[:3]))
 
 
+def test_scores_that_round_alike_go_by_the_logit():
+    """Logits far below 64 bits of the score: among equal scores of a beam the larger logit comes first."""
+    z = torch.zeros(2, 300, device="cuda")
+    z[0, 7], z[0, 200], z[1, 250] = 1e-30, 2e-30, 1e-30
+    scores, beams, tokens = select(z, torch.zeros(1, 2, device="cuda"), 5)
+    assert bool((scores == scores[0, 0]).all())
+    assert beams.tolist() == [[0] * 5] and tokens.tolist() == [[200, 7, 0, 1, 2]]
+    z[1] = -math.inf
+    z[1, [3, 250]] = 1e-30
+    z[1, 260] = 2e-30
+    assert select(z[1:], torch.zeros(1, 1, device="cuda"), 4)[2].tolist() == [[260, 3, 250, 0]]
+
+
 def test_rows_far_apart():
     """A stride by which the last rows lie more than 2^31 logits behind the first."""
     rows, vocab = 20, 5001

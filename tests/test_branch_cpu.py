@@ -120,6 +120,8 @@ def test_moves_are_checked(lib):
     assert call([_cache()], start, 0) == S.SCALE_ERR_INVALID_ARG
     assert call([_cache()] * 1025, start) == S.SCALE_ERR_UNSUPPORTED
     assert call([_cache()], _moves(start=AT, n_groups=4097)) == S.SCALE_ERR_UNSUPPORTED
+    assert call([_cache()], _moves(n_moves=(1 << 28) + 2)) == S.SCALE_ERR_UNSUPPORTED
+    assert call([_cache()], _moves(start=AT, n_moves=2**31 - 1)) == S.SCALE_ERR_UNSUPPORTED
     assert call([_cache()], _moves(n_groups=0)) == S.SCALE_ERR_INVALID_ARG
     assert call([_cache()], _moves(n_moves=-1)) == S.SCALE_ERR_INVALID_ARG
     assert call([_cache()], _moves(n_moves=9)) == S.SCALE_ERR_INVALID_ARG  # not the same for both groups
@@ -159,6 +161,7 @@ def test_beam_calls_refuse_bad_pointers(lib):
     assert call(1, 33, m) == S.SCALE_ERR_UNSUPPORTED and call(4096, 2, m) == S.SCALE_ERR_UNSUPPORTED
     assert call(0, 2, m) == S.SCALE_ERR_INVALID_ARG and call(2, 2, m, stride=0) == S.SCALE_ERR_INVALID_ARG
     assert call(2, 2, _moves(n_groups=4, n_moves=255)) == S.SCALE_ERR_INVALID_ARG
+    assert call(2, 2, m, stride=2**31 - 1) == S.SCALE_ERR_INVALID_ARG  # (the pointers: any width will do)
     assert call(2, 2, m, out=AT + 16) == S.SCALE_ERR_INVALID_ARG  # tables that overlap
 
 
