@@ -49,6 +49,7 @@ constexpr int kCandidates = kUniform + kTails * kTailCuts;
 static_assert(kCandidates <= 32, "a lane for each");
 constexpr int kPieceTiles = 5;        // what a CTA's start and end take, in key tiles
 constexpr int kMergeTiles = 4;        // what writing and merging one piece per SM takes
+constexpr float kLeastRun = 8.0f;     // of equal runs, see k_chunk_plan
 
 // 8-bit: log2 of the sizes of queries that share a power of two. At most 2^-12 of a row's largest |q| is lost so, 2^-4 of what
 // bf16 itself leaves of that value. Rows of sizes up to 2^12 apart, each with its own power, take 1.33 times as long
@@ -147,12 +148,19 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* s_warp, int64_
 // tokens, 200 items, 8-bit: 116 us; 113, and 129 with all cut alike, when the choice was made. 4,096 tokens over 64K: 512
 // items, 208 of them cut.)
 // The plan takes 7 to 8 us, most of it latency: lengths from memory, scans, the lists' way back.
+//
+// RUNS: drafted trees of which each fills one pair of tiles at most, so that no two items read the same keys. Then one more way is
+// looked at: the items one after another in equal runs, one for each SM, cut where runs end; the jobs' pieces by their
+// length, longest first, so that what is left of one SM's run goes to where the other part of it was. 16 sequences of 20,000 to 32,768
+// tokens, 128 items: 271 jobs in place of 456, and 335 us in place of 357. Runs of a few tiles would be mostly starts and ends.
+template <bool RUNS>
 __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_constant__ ChunkArgs a)
 {
     __shared__ int s_before[kMaxSeqs + 1];  // items (of one KV head) of the sequences before
 #if CHUNK_TREE
     __shared__ int s_tiles[kPlanThreads], s_order[kPlanThreads];
 #endif
+    __shared__ int s_lengths[32];  // jobs of a length, longest first; then where the next of that length goes
     __shared__ int64_t s_warp[32];
     __shared__ int s_longest, s_long[32], s_tail[32], s_split[32], s_cut;
     __shared__ float s_cut_tail;
@@ -212,6 +220,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_consta
         s_longest = 0;
     }
     if (tid < 32) s_long[tid] = s_tail[tid] = s_split[tid] = 0;
+    if (RUNS && tid < 32) s_lengths[tid] = 0;
     __syncthreads();
     // item x: sequences outermost, then KV heads, then pairs from the last
     auto item = [&](int x, ChunkJob* jb) {
@@ -311,9 +320,68 @@ __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const __grid_consta
         if (lane == __ffs(__ballot_sync(0xFFFFFFFFu, bits == best)) - 1) {
             s_cut = my_cut;
             s_cut_tail = my_tail;
+            // or equal runs
+            const float run = (R + static_cast<float>(rest * kPieceTiles)) * per_sm;
+            const float cut_up = static_cast<float>(a.sms + (rest < a.sms ? rest : a.sms));
+            if (RUNS && whole == 0 && run >= kLeastRun && run + static_cast<float>(kPieceTiles + 1) + kMergeTiles * cut_up * per_sm < time) s_cut = 0;
         }
     }
     __syncthreads();
+    if (RUNS && s_cut == 0) {
+        // Boundary r of the runs lies r * all / sms along the items, each of which is kPieceTiles longer than its keys; those
+        // that would leave an item's piece of one tile are none. r0: the first inside this item.
+        const int64_t all_runs = rest_work + static_cast<int64_t>(rest) * kPieceTiles, start = work_before + static_cast<int64_t>(tid + 1) * kPieceTiles;
+        const int n = jb.k1;
+        int r0 = 0, pieces = 0;
+        if (n > 0) {
+            r0 = static_cast<int>(((start + 2) * a.sms + all_runs - 1) / all_runs);
+            const int r1 = static_cast<int>(((start + n - 1) * a.sms - 1) / all_runs);
+            pieces = r1 < r0 ? 1 : r1 - r0 + 2;
+        }
+        auto end_of = [&](int i) { return i + 1 < pieces ? static_cast<int>((r0 + i) * all_runs / a.sms - start) : n; };
+        const float to_class = 32.0f / (fminf(static_cast<float>(s_longest), static_cast<float>(all_runs) * per_sm + 4.0f) + 1.0f);
+        auto class_of = [&](int len) {
+            const int x = static_cast<int>(static_cast<float>(len) * to_class);
+            return 31 - (x < 31 ? x : 31);
+        };
+        for (int i = 0, k0 = 0; i < pieces; ++i) {
+            const int k1 = end_of(i);
+            atomicAdd(&s_lengths[class_of(k1 - k0)], 1);
+            k0 = k1;
+        }
+        int64_t sums;
+        const int64_t mask = (1 << 21) - 1;
+        const int64_t before = block_scan(pieces > 1 ? pieces | static_cast<int64_t>(pieces) << 21 | 1ll << 42 : pieces, s_warp, &sums);
+        const int jobs = static_cast<int>(sums & mask), slots = static_cast<int>((sums >> 21) & mask), merges = static_cast<int>(sums >> 42);
+        const int my_slot = static_cast<int>((before >> 21) & mask);
+        if (tid < 32) {
+            const int mine = s_lengths[lane];
+            int at = mine;
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xFFFFFFFFu, at, o);
+                if (lane >= o) at += y;
+            }
+            s_lengths[lane] = at - mine;
+        }
+        __syncthreads();
+        const bool fits = jobs <= a.p.max_jobs && slots <= a.p.max_slots && merges <= a.p.max_merges;
+        if (fits) {
+            for (int i = 0, k0 = 0; i < pieces; ++i) {
+                const int k1 = end_of(i);
+                int4* to = reinterpret_cast<int4*>(a.p.jobs + atomicAdd(&s_lengths[class_of(k1 - k0)], 1));
+                to[0] = make_int4(jb.b, jb.j, jb.row0, jb.ntok);
+                to[1] = make_int4(jb.pos, k0, k1, pieces > 1 ? my_slot + i : -1);
+                k0 = k1;
+            }
+            if (pieces > 1) a.p.merges[before >> 42] = ChunkMerge{jb.j, jb.row0, jb.ntok, my_slot, pieces, {0, 0, 0}};
+        }
+        if (tid == 0) {
+            if (!fits) record_status(a.status, SCALE_ERR_DEVICE);
+            a.p.counts[0] = fits ? jobs : 0;
+            a.p.counts[1] = fits ? merges : 0;
+        }
+        return;
+    }
     // Jobs, a block of items at a time; at, slot and merge count jobs, partial results and merges so far.
     int at = 0, slot = 0, merge = 0;
 #pragma unroll 1
@@ -590,6 +658,14 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                         tma_load_3d(smem + kOffQ + qt * kTileBytes + h * kHalf, &tq, &bars.q_full, h * 64, job.j * g,
                                     job.row0 + qt * tt);
             }
+            // Drafted trees: keys and values leave L2 before anything else does, since no other CTA, or few, read them; what
+            // stays is the kernels' code, partial results and lists. 25 nodes at 128K, 8-bit, 121 us without and 117 with it, 33 trees of
+            // 1 to 40 91 and 83, 16 of 64 at 32K 335 and 330; 256 nodes, whose four pairs of tiles read the same keys, 660 and 655.
+            const uint64_t policy = TREE ? policy_evict_first() : 0;
+            auto copy = [&](void* to, const CUtensorMap* map, uint64_t* bar, int column, int row) {
+                if (TREE) tma_load_3d_hint(to, map, bar, column, job.j, row, policy);
+                else tma_load_3d(to, map, bar, column, job.j, row);
+            };
             uint64_t* const s_last = bars.s_full[nq - 1];
             int steps = 0, steps_v = 0;
             auto row_of = [&](int t) {
@@ -608,14 +684,14 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                     ++steps;
                     __syncwarp();
                     const uint32_t to = st * kCodeBytes + bx * a.box * kHeadDim;
-                    if (mine) tma_load_3d(smem + kOffK + to, &tk, &bars.kv_full[st], 0, job.j, row_k);
+                    if (mine) copy(smem + kOffK + to, &tk, &bars.kv_full[st], 0, row_k);
                     ok = t < 2 || mbar_wait_bounded(&sh.raw_empty[st], ((t - 2) >> 1) & 1, a.timeout_ns, &abort_flag);
                     ok = __all_sync(0xFFFFFFFFu, ok);
                     if (ok) {
                         if (lane == 0) mbar_arrive_expect_tx(&sh.raw_full[st], kCodeBytes);
                         ++steps_v;
                         __syncwarp();
-                        if (mine) tma_load_3d(smem + off_raw(true) + to, &tv, &sh.raw_full[st], 0, job.j, row_k);
+                        if (mine) copy(smem + off_raw(true) + to, &tv, &sh.raw_full[st], 0, row_k);
                     }
                 } else if (ok) {
                     const bool has_k = t < T, has_v = t >= 1;
@@ -625,9 +701,9 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                     __syncwarp();
                     const uint32_t to = hf * kHalf + bx * a.box * 128;
                     if (mine && has_v)
-                        tma_load_3d(smem + off_v(false) + (st ^ 1) * kTileBytes + to, &tv, &bars.kv_full[st], hf * 64, job.j, row_v);
+                        copy(smem + off_v(false) + (st ^ 1) * kTileBytes + to, &tv, &bars.kv_full[st], hf * 64, row_v);
                     if (mine && has_k)
-                        tma_load_3d(smem + kOffK + st * kTileBytes + to, &tk, &bars.kv_full[st], hf * 64, job.j, row_k);
+                        copy(smem + kOffK + st * kTileBytes + to, &tk, &bars.kv_full[st], hf * 64, row_k);
                 }
                 if (!ok) {
                     if (lane == 0) fail(&abort_flag, a.status);
@@ -848,14 +924,16 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                     // tiles take the slow path, which multiplies its logits by it. Not finite becomes NaN.
                     ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&bars.q_full, 0, a.timeout_ns, &abort_flag));
                     uint8_t* row = smem + kOffQ + qt * kTileBytes + r * 128;
-                    uint4 w[16];  // dimensions 8 i .. 8 i + 7
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) w[i] = *reinterpret_cast<const uint4*>(row + (i >> 3) * kHalf + (((i & 7) ^ (r & 7)) << 4));
+                    // Drafted trees in loops: code that runs once a CTA is fetched from far (unrolled, 60 nodes in 9 windows took 65.5 us
+                    // for 63.4, 8 x 256 at 32K 927 for 891; causal rows of 1 to 700 tokens 116.7, and 117.8 in loops).
+                    constexpr int kRolled = TREE ? 1 : 16;
+                    auto piece = [&](int i) { return *reinterpret_cast<const uint4*>(row + (i >> 3) * kHalf + (((i & 7) ^ (r & 7)) << 4)); };  // dimensions 8 i .. 8 i + 7
                     uint32_t top = 0;
                     if (r < (qt + 1 == jv.nq ? jv.job.ntok - qt * tt : tt) * g) {
-#pragma unroll
+#pragma unroll(kRolled)
                         for (int i = 0; i < 16; ++i) {
-                            const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+                            const uint4 w = piece(i);
+                            const uint32_t v[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 const uint32_t x = (v[e] << 16) & 0x7FFFFFFFu, y = v[e] & 0x7FFF0000u;
@@ -871,9 +949,14 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                     row_scale = rows_apart ? up : 1.f;
                     if (rows_apart) plain_to = -1;
                     q_scale = rows_apart ? a.a.scale_log2 : a.a.scale_log2 * up;
+                    uint4 w[16];  // all of it: the parts go where it lies
 #pragma unroll
+                    for (int i = 0; i < 16; ++i) w[i] = piece(i);
+#pragma unroll(kRolled)
                     for (int i = 0; i < 8; ++i) {  // 16 dimensions: one 16-byte piece of each part
-                        const uint32_t v[8] = {w[2 * i].x, w[2 * i].y, w[2 * i].z, w[2 * i].w, w[2 * i + 1].x, w[2 * i + 1].y, w[2 * i + 1].z, w[2 * i + 1].w};
+                        const uint32_t v[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w};
+#pragma unroll
+                        for (int k = 0; k < 14; ++k) w[k] = w[k + 2];
                         uint32_t hi[4], lo[4];
 #pragma unroll
                         for (int e4 = 0; e4 < 4; ++e4) {
@@ -1284,7 +1367,9 @@ cudaError_t run_chunks(const ChunkArgs& a, cudaStream_t st)
              scale_host::make_token_major_map(&tv, a.c.v, kHeadDim, a.c.Hkv, pool, 64, a.box);
     if (!ok) return cudaErrorInvalidValue;
     cudaError_t e = cudaFuncSetAttribute(k_chunk<E4M3, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(chunk_smem(E4M3)));
-    if (e == cudaSuccess) e = launch_after(st, dim3(1), kPlanThreads, 0, 1, k_chunk_plan, a);
+    // a KV head's pairs that share keys stay together
+    auto* const plan = TREE && a.b.max_rows <= 2 * a.tile_tokens ? k_chunk_plan<TREE> : k_chunk_plan<false>;
+    if (e == cudaSuccess) e = launch_after(st, dim3(1), kPlanThreads, 0, 1, plan, a);
     if (e == cudaSuccess)
         e = launch_after(st, dim3(a.p.max_jobs), chunk_threads(E4M3), chunk_smem(E4M3), 1, k_chunk<E4M3, TREE>, tq, tk, tv, a);
     const int merge_ctas = a.p.max_merges * (a.part_rows / (TREE ? 4 : 32)), most = a.sms * kMergeCtas;

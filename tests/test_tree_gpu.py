@@ -181,6 +181,24 @@ def test_attend_any_masks_and_absent_rows(news, lens, hq, hkv, page, e4m3, wide)
     assert bool((out == 0).all()) and bool((lse == -math.inf).all())
 
 
+MANY = [  # as ATTENDS, of so many keys that the SMs share them in equal runs; then of more sequences and pairs than SMs
+    ([33, 1, 20, 64, 7], [60000, 30001, 129, 40000, 45003], 4, 1, 16), ([300, 70], [30000, 22222], 16, 4, 64),
+    ([40] * 19, [5000 + 731 * i for i in range(19)], 4, 1, 64), ([30, 64] * 75, [700 + 13 * i for i in range(150)], 8, 2, 16),
+    ([17 + i % 3 for i in range(700)], [20 + i % 211 for i in range(700)], 1, 1, 16),
+]
+
+
+@pytest.mark.parametrize("news,lens,hq,hkv,page", MANY)
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("n_sink,n_local", [(0, -1), (130, 9000)])
+def test_attend_trees_of_many_keys(news, lens, hq, hkv, page, e4m3, n_sink, n_local):
+    bt = Batch(news, lens, hq=hq, hkv=hkv, page=page, e4m3=e4m3)
+    seen, positions = planned(bt, trees(news, 3 + sum(lens), gone=0.1), n_sink, n_local)
+    out, lse = check_attend(bt, seen, positions, n_sink, n_local)
+    again, sums = run_attend(bt, seen, positions, n_sink, n_local)
+    assert same_bits(out, again) and same_bits(lse, sums)
+
+
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("hq,hkv,news,lens", [(4, 1, [4, 2], [700, 90]), (8, 2, [33, 70], [900, 300]), (4, 4, [16], [16])])
 def test_a_chain_is_causal_attention(e4m3, hq, hkv, news, lens):
