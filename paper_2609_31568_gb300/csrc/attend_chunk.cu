@@ -1141,21 +1141,25 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                 // Every MMA is done and every copy landed, so the tiles in shared memory are free: a warp
                 // stages its 32 output rows there and stores whole rows.
                 const int rows = (qt + 1 == jv.nq ? job.ntok - qt * tt : tt) * g - quarter * 32;  // of this warp, if more than 0
+                constexpr int kAtOnce = TREE ? 1 : 4;  // pieces of 32 columns (trees: as the split of Q; 8 x 256 nodes at 32K, 8-bit, 885 us with 4, 876 with 1)
                 if (job.slot < 0) {
                     const float inv_l = l_run > 0.f ? 1.0f / l_run : 0.f;
-                    uint32_t v[128];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_ld32(o_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&v[c * 32]));
-                    tmem_ld_wait();
                     uint8_t* stage = smem + kOffQ + qt * kTileBytes + quarter * 32 * 256;
+#pragma unroll 1
+                    for (int c0 = 0; c0 < 16; c0 += 4 * kAtOnce) {
+                        uint32_t v[32 * kAtOnce];
 #pragma unroll
-                    for (int c = 0; c < 16; ++c) {
-                        uint32_t w[4];
+                        for (int c = 0; c < kAtOnce; ++c) tmem_ld32(o_addr + c0 * 8 + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&v[c * 32]));
+                        tmem_ld_wait();
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            w[i] = pack_bf16x2(__uint_as_float(v[8 * c + 2 * i]) * inv_l, __uint_as_float(v[8 * c + 2 * i + 1]) * inv_l);
-                        if (!(l_run > 0.f)) w[0] = w[1] = w[2] = w[3] = l_run == 0.f ? 0u : 0x7FFF7FFFu;  // no keys: 0; NaN stays
-                        *reinterpret_cast<uint4*>(stage + lane * 256 + ((c ^ (lane & 15)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        for (int c = 0; c < 4 * kAtOnce; ++c) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                w[i] = pack_bf16x2(__uint_as_float(v[8 * c + 2 * i]) * inv_l, __uint_as_float(v[8 * c + 2 * i + 1]) * inv_l);
+                            if (!(l_run > 0.f)) w[0] = w[1] = w[2] = w[3] = l_run == 0.f ? 0u : 0x7FFF7FFFu;  // no keys: 0; NaN stays
+                            *reinterpret_cast<uint4*>(stage + lane * 256 + (((c0 + c) ^ (lane & 15)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
                     }
                     __syncwarp();
                     const int c = lane & 15;
@@ -1174,7 +1178,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                             l_run == 0.f ? -INFINITY : (m_run + __log2f(l_run)) * 0.6931471805599453f;
                 } else {
                     uint8_t* stage = smem + warp * 32 * 512;  // 128 KB of tiles
-#pragma unroll
+#pragma unroll(kAtOnce)
                     for (int c = 0; c < 4; ++c) {
                         uint32_t v[32];
                         tmem_ld32(o_addr + c * 32, v);
@@ -1187,7 +1191,7 @@ k_chunk(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensor
                     __syncwarp();
                     const int64_t at = static_cast<int64_t>(job.slot) * a.part_rows + qt * kTile + quarter * 32;
                     uint4* dst = reinterpret_cast<uint4*>(a.part_o + at * kHeadDim) + lane;
-#pragma unroll 8
+#pragma unroll(2 * kAtOnce)
                     for (int x = 0; x < 32; ++x)
                         if (x < rows) dst[x * (kHeadDim / 4)] = *reinterpret_cast<const uint4*>(stage + x * 512 + ((lane ^ x) << 4));
                     if (lane < rows) a.part_ml[at + lane] = make_float2(m_run, l_run);
