@@ -613,8 +613,8 @@ struct BeamWs {
     int parts, part_steps;
 };
 
-// Parts of a row: so many that the rows give every SM two CTAs. (64 x 8 rows of 128,000, bf16, in one part each 66 us, in two 79;
-// 11 x 5 of 100,003, fp32, in five 29, in eleven 37.)
+// Parts of a row: so many that the rows give every SM two CTAs. (64 x 8 rows of 128,000, bf16, in one part each 40.9 us, in two 47.7;
+// 24 x 8 of 100,000, fp32, in two 21.8, in three 27.3; 11 x 5 of 100,003, fp32, in five 16.7, in thirteen 21.2.)
 BeamWs beam_layout(int n_groups, int n_beams, int vocab, int n_best)
 {
     BeamWs w{};
