@@ -436,6 +436,30 @@ def test_rows_past_max_rows_stay():
     assert src.tolist()[4:9] == [-77] * 5
 
 
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("n_sink,n_local", [(0, -1), (3, 50)])
+def test_long_trees_past_max_rows(e4m3, n_sink, n_local):
+    """The same on the route of many rows: the nodes past the bound are neither rows nor seen."""
+    news, lens, most = [100, 30, 71], [900, 200, 71], 70
+    bt = Batch(news, lens, hq=8, hkv=2, page=16, e4m3=e4m3)
+    bt.batch = S.kv_batch(bt.row_start, bt.kv_len, bt.table, bt.n_rows, most)
+    seen, positions = planned(bt, trees(news, 17), n_sink, n_local)
+    kept = [c < most for n in news for c in range(n)]
+    masks = torch.from_numpy(as_words(seen, 4)).cuda()
+    masks[:, 2] |= 0x7FFFFFC0  # nodes 70 to 94
+    masks[:, 3] = -1
+    a = S.attend_params(num_q_heads=8, n_sink=n_sink, n_local=n_local)
+    ws = torch.empty(S.scale_cache_attend_workspace_size(a, bt.cache, bt.batch), dtype=torch.uint8, device="cuda")
+    S.scale_workspace_init(ws)
+    out = torch.full((bt.rows, 8, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    S.scale_cache_attend_tree(a, S.draft_tree(None, ints(positions), masks), bt.cache, bt.batch, bt.q, out, None, ws)
+    assert S.scale_get_device_status(ws) == S.SCALE_OK
+    want, _, tol, _ = attend_tree64(bt, bt.q, seen, positions, n_sink, n_local)
+    kept = torch.tensor(kept, device="cuda")
+    within(out[kept], want[kept], tol[kept])
+    assert bool((out[~kept] == 7.0).all())
+
+
 def test_a_captured_step_follows_its_lists_on_another_stream():
     """Plan, walk and moves captured once and replayed with other trees, beside eager calls on a stream of their own."""
     nodes, seqs, page, hkv = 24, 3, 16, 2
