@@ -553,8 +553,9 @@ typedef struct {
 /* The best continuations of each group of beams. Token v after beam i of a group scores
  *   scores[i] + log softmax(logits of the beam)[v],
  * in 64 bits from sums in 32 that are kept to 2^-22 of them; the n_best largest are written in descending order, equal ones
- * by the lower beam, then the larger logit, then the lower token. A NaN logit counts as -inf; every continuation of a beam whose score
- * is not finite, or whose logits have no finite maximum, scores -inf and is taken in its turn like any other.
+ * by the lower beam, then the larger logit, then the lower token. A NaN logit counts as -inf, one below the normal numbers
+ * (of a size under 2^-126) as 0; every continuation of a beam whose score is not finite, or whose logits have no finite
+ * maximum, scores -inf and is taken in its turn like any other.
  *   logits      [n_groups * n_beams][vocab], rows logits_stride elements apart (at least vocab), aligned to their type
  *   scores      fp32 [n_groups][n_beams]
  *   best_scores fp32 [n_groups][n_best], best_beams int32 (0..n_beams - 1), best_tokens int32: out

@@ -27,13 +27,14 @@ constexpr int kMaxCandidates = 4096;           // of a group, for k_beam_pick
 constexpr int kMaxParts = 32;                  // of a row
 constexpr float kLog2e = 1.4426950408889634f;
 
-// Candidates are 64-bit keys: the logit's order (0 below all; NaN as -inf, both zeros alike), then the tokens from the
-// highest down, so that of equal logits the lower token is the larger key. 0: no candidate.
+// Candidates are 64-bit keys: the logit's order (0 below all; NaN as -inf; both zeros, and what lies between them and the normal
+// numbers, alike, as the kernels' comparisons of logits take them), then the tokens from the highest down, so that of equal
+// logits the lower token is the larger key. 0: no candidate.
 __device__ __forceinline__ uint32_t order_of(float x)
 {
     uint32_t u = __float_as_uint(x);
     if ((u & 0x7FFFFFFFu) > 0x7F800000u) u = 0xFF800000u;
-    if (u == 0x80000000u) u = 0u;
+    if ((u & 0x7F800000u) == 0u) u = 0u;
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float value_of(uint32_t order) { return __uint_as_float(order & 0x80000000u ? order & 0x7FFFFFFFu : ~order); }
