@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(kAcceptThreads) k_tree_accept(const __grid_con
         s_count = n;
         a.n_accepted[b] = n;
         a.next[b] = n > 0 ? a.choices[s.row0 + s_path[n - 1]] : first;
-        a.new_len[b] = nodes > 0 ? s.base + n : a.b.kv_len[b];
+        a.new_len[b] = s.n > 0 && s.base >= 0 ? s.base + n : a.b.kv_len[b];
     }
     __syncthreads();
     const int n = s_count;
