@@ -532,8 +532,8 @@ int scale_cache_move(const scale_cache_t *caches, int32_t n_caches, const scale_
  *   moves      src and dst [n_rows] out: the moves of the accepted nodes' rows to tokens base .., for
  *              scale_cache_move with start = row_start; n_groups is n_seqs and n_moves n_rows
  * A sequence without rows, or with kv_len less than its rows, accepts none and keeps kv_len. `cache` says the
- * page size and the number of pages; its pages are not touched. max_rows is at most 1024; rows past it are no nodes,
- * and what is written for rows is left as it was there. */
+ * page size and the number of pages; its pages are not touched. max_rows is at most 1024; rows past it are no nodes:
+ * path and src are left as they were there, and dst is -1, so that they are no moves. */
 int scale_tree_accept(const scale_tree_t *tree, const scale_cache_t *cache, const scale_batch_t *batch,
                       const int32_t *tokens, const int32_t *choices, const int32_t *first, int32_t *n_accepted,
                       int32_t *path, int32_t *next, int32_t *new_len, const scale_moves_t *moves, scale_stream_t stream);

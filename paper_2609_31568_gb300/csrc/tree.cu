@@ -135,6 +135,9 @@ __global__ void __launch_bounds__(kAcceptThreads) k_tree_accept(const __grid_con
         a.src[s.row0 + i] = src;
         a.dst[s.row0 + i] = dst;
     }
+    // The moves of the rows that are not looked at belong to the group all the same: whatever their lists held, they are none.
+    const int listed = s.n < a.b.n_rows - s.row0 ? s.n : a.b.n_rows - s.row0;
+    for (int i = s.nodes + tid; i < listed; i += kAcceptThreads) a.dst[s.row0 + i] = -1;
 }
 
 // Moves. A warp has 512 bytes (or the whole row, where that is less) of every row of a group's keys or values in one cache, or
