@@ -552,9 +552,10 @@ typedef struct {
 
 /* The best continuations of each group of beams. Token v after beam i of a group scores
  *   scores[i] + log softmax(logits of the beam)[v],
- * in 64 bits from sums in 32 that are kept to 2^-22 of them; the n_best largest are written in descending order, equal ones
- * by the lower beam, then the larger logit, then the lower token. A NaN logit counts as -inf, one below the normal numbers
- * (of a size under 2^-126) as 0; every continuation of a beam whose score is not finite, or whose logits have no finite
+ * in 64 bits from sums in 32 that are off by 2^-18 of them at most, whatever the logits' range, and as a rule by less than
+ * 2^-21 (continuations of one beam share its sum: only those of different beams can change places by it). The n_best
+ * largest are written in descending order, equal ones by the lower beam, then the larger logit, then the lower token. A NaN
+ * logit counts as -inf, one below the normal numbers (of a size under 2^-126) as 0; every continuation of a beam whose score is not finite, or whose logits have no finite
  * maximum, scores -inf and is taken in its turn like any other.
  *   logits      [n_groups * n_beams][vocab], rows logits_stride elements apart (at least vocab), aligned to their type
  *   scores      fp32 [n_groups][n_beams]

@@ -60,8 +60,8 @@ struct SelectShared {
         uint64_t other[kList];           // the list in tighten()
         float4 x[kWarps][kPer / 4][32];  // a warp's logits of a step, where it has candidates among them or the row ends
     };
-    uint64_t bound[kWarps];
-    float2 sums[kWarps];
+    uint64_t bound[kWarps], sums[kWarps];
+    float tops[kWarps];
     int n, kept;
 };
 
@@ -220,6 +220,35 @@ __device__ __noinline__ void load_edge(SelectShared& sh, const T* logits, int fi
     for (int i = 0; i < kPer; i += 4) sh.x[threadIdx.x >> 5][i >> 2][lane] = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
 }
 
+// e^(a - b), off by 2^-22.7 of it at most however far a lies below b (0 beyond 87), for a - b of at most kApart: ex2(fl(a - b) log2 e) is off
+// by as much as the roundings of the difference and of the product are, 2^-20 each at 16. What the difference loses is kept
+// (Knuth's sum of two), multiples of log 2 go off it (Cody and Waite), and the rest, at most 0.35, has its series. A NaN, or -inf
+// from -inf, gives 0.
+constexpr float kApart = 8.0f;
+
+__device__ __forceinline__ float exp_of(float a, float b)
+{
+    const float d = __fadd_rn(a, -b);
+    if (!(d >= -87.0f)) return 0.f;
+    const float back = __fadd_rn(d, -a);
+    const float lost = __fadd_rn(__fadd_rn(a, -__fadd_rn(d, -back)), -__fadd_rn(b, back));
+    const float i = rintf(d * kLog2e);
+    const float r = fmaf(i, 1.9046543e-9f, fmaf(i, -0.69314718f, d)) + lost;  // log 2 is 0.69314718246 (the fp32 number) - 1.9046543e-9
+    float y = fmaf(r, 1.0f / 5040, 1.0f / 720);
+    y = fmaf(r, y, 1.0f / 120);
+    y = fmaf(r, y, 1.0f / 24);
+    y = fmaf(r, y, 1.0f / 6);
+    y = fmaf(r, y, 0.5f);
+    y = fmaf(r, y, 1.0f);
+    y = fmaf(r, y, 1.0f);
+    return y * __uint_as_float(static_cast<uint32_t>(127 + static_cast<int>(i)) << 23);
+}
+
+// Sums across lanes, warps and parts are of whole multiples of 2^-32 of the largest term's (at least 1 in all, and below 2^25), which lose nothing
+// and come to the same in any order.
+__device__ __forceinline__ uint64_t fixed_of(float x) { return __float2ull_rn(x * 4294967296.0f); }
+__device__ __forceinline__ float of_fixed(uint64_t x) { return __ull2float_rn(x) * (1.0f / 4294967296.0f); }
+
 // sum of exp(x - top) of a thread's step with NaN among its logits, which count as -inf
 template <typename T>
 __device__ __noinline__ float sum_without_nan(const T* logits, int first, int vocab, float top)
@@ -269,8 +298,11 @@ __device__ __noinline__ int collect_carefully(SelectShared& sh, const T* logits,
 //
 // A step is 8,192 logits, 32 a thread, in 16-byte loads that are made a step ahead. SKEW: rows begin anywhere; behind a
 // 16-byte boundary a thread puts its logits together from its load and its neighbour's, so that it has the same tokens
-// wherever the row lies: rows of the same logits have the same sum to the bit, and equal scores stay equal. The sum is a
-// thread's own against its own largest logit, with what a step's sum loses carried to the next. The first step sets the
+// wherever the row lies: rows of the same logits have the same sum to the bit, and equal scores stay equal. A step's sum is against
+// its own largest logit, its thread's against the thread's, with what a step loses carried to the next; those of threads and parts
+// meet in whole numbers. It is off by 2^-18 of itself at most (in units of 2^-24: ex2 3, distances in a step 4, its ten sums 9, four or five of exp_of
+// with their products 18, the rest 6), and by 2^-21.3 in the worst of 50,000 rows of many kinds. (Steps against the thread's
+// largest logit so far, all joined by ex2: 41.8 us in place of 42.9, but 128,000 logits 11 below one were 2^-20.9 off.) The first step sets the
 // bound that a candidate has to reach (bound_of, then the least of the n_best best so far, again after 2, 4, 8 .. steps if as many follow);
 // between these warps go on without barriers, and one whose threads all stay at or below the bound, which their largest logits tell,
 // needs nothing more. The candidates wait in a list, which is cut at the end. What is rare lies in functions of its own: the loop has to
@@ -278,7 +310,7 @@ __device__ __noinline__ int collect_carefully(SelectShared& sh, const T* logits,
 // 300 us, by where the code came to lie).
 //
 // Bound by the loop's latency and the instructions of one wave of CTAs, not by HBM: 64 x 8 rows of 128,000 in bf16 (131 MB), select and pick,
-// 40.6 us; 11 x 5 of 100,003 in fp32 (22 MB) 16.5, 4 of 32,000 9.8, of which the pick is about 5.
+// 42.9 us; 11 x 5 of 100,003 in fp32 (22 MB) 17.0, 4 of 32,000 10.1, of which the pick is about 5.
 template <typename T, bool SKEW>
 __global__ void __launch_bounds__(kThreads, kResident<T>) k_beam_part(const __grid_constant__ SelectArgs a)
 {
@@ -335,16 +367,10 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) k_beam_part(const __gr
         float m = x[0];
 #pragma unroll
         for (int i = 1; i < kPer; ++i) m = fmaxf(m, x[i]);
-        // ---- the sum
-        if (m > top) {
-            const float f = ex2((top - m) * kLog2e);
-            sum *= f;
-            lost *= f;
-            top = m;
-        }
+        // ---- the sum, against the step's own largest logit: what is far below that counts for little among 32
         {
             // the largest goes off first, which costs no bits where it counts; one product with both would leave its rounding
-            const float neg = top == -INFINITY ? 0.f : -top;
+            const float neg = fabsf(m) < INFINITY ? -m : 0.f;
             float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < kPer; i += 2) {
@@ -355,6 +381,16 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) k_beam_part(const __gr
             }
             float y = (acc[0] + acc[1]) + (acc[2] + acc[3]);
             if (!(y >= 0.f)) y = sum_without_nan<T>(logits, first, vocab, -neg);
+            // `top` follows by kApart at least, so that no term is multiplied often on its way
+            const bool ahead = m - top > kApart;
+            const float f = exp_of(ahead ? top : m, ahead ? m : top);
+            if (ahead) {
+                sum *= f;
+                lost *= f;
+                top = m;
+            } else {
+                y *= f;
+            }
             y -= lost;
             const float t = sum + y;
             lost = (t - sum) - y;
@@ -392,6 +428,9 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) k_beam_part(const __gr
             }
         }
     }
+    float m = top;
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    if (lane == 0) sh.tops[warp] = m;
     __syncthreads();
     int held = sh.n;
     if (held > kList) held = collect_carefully<T>(sh, logits, vocab, s0, s1, keep);
@@ -399,19 +438,14 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) k_beam_part(const __gr
     held = tighten(sh, held, keep);
     for (int i = tid; i < keep; i += kThreads) out[i] = i < held ? sh.list[i] : 0;
     // ---- the threads' sums
-    float m = top;
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-    float y = top == -INFINITY ? 0.f : (sum - lost) * ex2((top - m) * kLog2e);
+    for (int w = 0; w < kWarps; ++w) m = fmaxf(m, sh.tops[w]);
+    uint64_t y = fixed_of((sum - lost) * exp_of(top, m));
     for (int o = 16; o > 0; o >>= 1) y += __shfl_xor_sync(0xFFFFFFFFu, y, o);
-    if (lane == 0) sh.sums[warp] = make_float2(m, y);
+    if (lane == 0) sh.sums[warp] = y;
     __syncthreads();
-    if (warp == 0) {
-        const float2 mine = lane < kWarps ? sh.sums[lane] : make_float2(-INFINITY, 0.f);
-        m = mine.x;
-        for (int o = kWarps / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-        y = mine.x > -INFINITY ? mine.y * ex2((mine.x - m) * kLog2e) : 0.f;
-        for (int o = kWarps / 2; o > 0; o >>= 1) y += __shfl_xor_sync(0xFFFFFFFFu, y, o);
-        if (lane == 0) a.sums[blockIdx.x] = make_float2(m, y);
+    if (tid == 0) {
+        for (int w = 1; w < kWarps; ++w) y += sh.sums[w];
+        a.sums[blockIdx.x] = make_float2(m, of_fixed(y));
     }
 }
 
@@ -429,7 +463,7 @@ __device__ __forceinline__ double score_of(uint64_t order)
     return __longlong_as_double(static_cast<long long>(order >> 63 ? order & ~(1ull << 63) : ~order));
 }
 
-// The natural logarithm of a sum of 1 or more, whose own accuracy is 2^-22 of it: x = 2^e f with f in [0.75, 1.5), and
+// The natural logarithm of a sum of 1 or more, whose own accuracy is 2^-18 of it, mostly 2^-22: x = 2^e f with f in [0.75, 1.5), and
 // log f = 2 atanh(t), t = (f - 1) / (f + 1), at most 0.2, from its series in 32 bits, off by 2^-24 at most; e log 2 joins it in 64.
 // (log() in 64 bits is a chain of 64-bit products, 4,000 cycles here.)
 __device__ __forceinline__ double log_of_sum(float x)
@@ -469,10 +503,10 @@ __global__ void __launch_bounds__(kThreads) k_beam_pick(const __grid_constant__ 
         const float2 part = in && p < a.parts ? a.sums[static_cast<int64_t>(row) * a.parts + p] : make_float2(-INFINITY, 0.f);
         float top = part.x;
         for (int o = width / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        float sum = part.x > -INFINITY ? part.y * ex2((part.x - top) * kLog2e) : 0.f;
+        uint64_t sum = fixed_of(part.y * exp_of(part.x, top));
         for (int o = width / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
         const bool live = in && fabsf(top) < INFINITY && fabsf(a.b.scores[row]) < INFINITY;
-        if (in && p == 0) s_lse[i] = live ? static_cast<double>(top) + log_of_sum(sum) : INFINITY;
+        if (in && p == 0) s_lse[i] = live ? static_cast<double>(top) + log_of_sum(of_fixed(sum)) : INFINITY;
     }
     __syncthreads();
     // ---- scores

@@ -1,4 +1,5 @@
-"""Beam selection at the ends of its range: logits below the normal numbers."""
+"""Beam selection at the ends of its range: logits below the normal numbers, sums of many logits far below the largest, scores
+that lie next to each other."""
 
 import math
 
@@ -80,3 +81,65 @@ def test_choices_of_rows_below_the_normal_numbers():
     z[1:, 9] = 0.0  # equal to the others
     _, beam, token = select(z, torch.zeros(40, 1, device="cuda"), 1)
     assert beam.tolist() == [[0]] * 40 and token.tolist() == [[0]] * 40
+
+
+# ---------------------------------------------------------------- sums
+
+# One logit of 0, all others `low`. The roundings of these sums, followed in 32 bits on the CPU with 2^x exact, come to 2^-24.7 of
+# them or less, in any number of parts; of 2^x only those of the 31 logits beside the largest one are not 1, and 2^-22 of these
+# is below 2^-30 of the sum. The logarithm is good to 2^-24, so a score to 2^-23, and it is rounded to 32 bits once.
+FAR = [(32000, -5.625), (128000, -11.25), (128000, -5.625), (1 << 22, -11.25)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("vocab,low", FAR)
+@pytest.mark.parametrize("rows", [1, 100, 400])
+def test_many_logits_far_below_the_largest(dtype, vocab, low, rows):
+    if rows * vocab > 1 << 26:
+        rows = 3
+    z = torch.full((rows, vocab), low, dtype=dtype, device="cuda")
+    at = [(7 + 4099 * i) % vocab for i in range(rows)]
+    z[list(range(rows)), at] = 0.0
+    score, _, token = select(z, torch.zeros(rows, 1, device="cuda"), 1)
+    want = -math.log1p((vocab - 1) * math.exp(low))
+    assert token[:, 0].tolist() == at
+    assert np.abs(score.astype(np.float64) - want).max() <= 2.0 ** -23 + abs(want) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("vocab,low", FAR[:3])
+@pytest.mark.parametrize("gap", [1.5, -1.5])
+def test_scores_next_to_each_other(vocab, low, gap):
+    """Two beams whose best continuations are 1.5 * 2^-22 apart: one of a sum of many logits, one of a single logit."""
+    z = torch.full((2, vocab), low, device="cuda")
+    z[0, 11] = 0.0
+    z[1] = -math.inf
+    z[1, 13] = 0.0
+    mine = -math.log1p((vocab - 1) * math.exp(low))
+    ahead = 0.25 * math.floor(-4 * mine)  # the better it, the finer fp32 holds the other
+    mine += ahead
+    other = np.float32(mine + gap * 2.0 ** -22)
+    assert abs((float(other) - mine) / (gap * 2.0 ** -22) - 1) < 0.2  # fp32 holds it closely enough
+    score, beam, token = select(z, torch.tensor([[ahead, float(other)]], device="cuda"), 2)
+    assert beam.tolist() == [[1, 0] if gap > 0 else [0, 1]] and token.tolist() == [[13, 11] if gap > 0 else [11, 13]]
+
+
+def test_select_of_random_groups_far_enough_apart():
+    """A larger batch by torch's stable sort in 64 bits, the groups whose neighbours of different beams lie 2^-17 apart (a sum's
+    2^-18 for each); continuations of one beam may lie as close as they like."""
+    groups, beams, vocab, k = 20, 6, 12345, 12
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    z = (torch.randn(groups * beams, vocab, generator=gen, device="cuda") * 2.5)
+    z.scatter_add_(1, torch.randint(0, vocab, (groups * beams, 6), generator=gen, device="cuda"),
+                   torch.rand(groups * beams, 6, generator=gen, device="cuda") * 12)
+    s = -10 * torch.rand(groups, beams, device="cuda", generator=gen)
+    flat = (torch.log_softmax(z.double(), -1).view(groups, beams, vocab) + s.double()[..., None]).flatten(1)
+    value, at = flat.sort(dim=-1, descending=True, stable=True)
+    apart = (value[:, :k] - value[:, 1: k + 1]).cpu()
+    across = (at[:, :k] // vocab != at[:, 1: k + 1] // vocab).cpu()
+    sure = (apart > 2.0 ** -17) | ~across
+    rows = sure.all(-1).nonzero()[:, 0].tolist()
+    assert len(rows) >= groups - 2
+    score, beam, token = select(z, s, k)
+    for g in rows:
+        assert (beam[g].astype(np.int64) * vocab + token[g]).tolist() == at[g, :k].tolist()
+    assert (np.abs(score - value[:, :k].cpu().numpy()) <= 2.0 ** -18 + np.abs(score) * 2.0 ** -24).all()
