@@ -560,7 +560,8 @@ typedef struct {
  *   logits      [n_groups * n_beams][vocab], rows logits_stride elements apart (at least vocab), aligned to their type
  *   scores      fp32 [n_groups][n_beams]
  *   best_scores fp32 [n_groups][n_best], best_beams int32 (0..n_beams - 1), best_tokens int32: out
- *   ws          scale_beam_workspace_size() bytes, 256-byte aligned, not initialised */
+ *   ws          scale_beam_workspace_size() bytes, 256-byte aligned, not initialised; the size for the largest call does for
+ *               every one with no more groups, beams, vocab and n_best */
 int scale_beam_workspace_size(const scale_beam_t *beam, size_t *bytes);
 int scale_beam_select(const scale_beam_t *beam, const void *logits, int64_t logits_stride, const float *scores,
                       float *best_scores, int32_t *best_beams, int32_t *best_tokens, void *ws, size_t ws_bytes,

@@ -25,6 +25,7 @@ template <typename T>
 constexpr int kResident = sizeof(T) == 2 ? 4 : 3;  // CTAs of an SM: 64 registers are few beside fp32 logits
 constexpr int kMaxCandidates = 4096;           // of a group, for k_beam_pick
 constexpr int kMaxParts = 32;                  // of a row
+constexpr int kFill = 2 * 152;                 // CTAs that rows of several parts make: two an SM
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Candidates are 64-bit keys: the logit's order (0 below all; NaN as -inf; both zeros, and what lies between them and the normal
@@ -644,7 +645,7 @@ __global__ void __launch_bounds__(kColumns) k_reorder(const __grid_constant__ Re
 }
 
 struct BeamWs {
-    size_t sums, best, end;
+    size_t sums, best;
     int parts, part_steps;
 };
 
@@ -655,7 +656,7 @@ BeamWs beam_layout(int n_groups, int n_beams, int vocab, int n_best)
     BeamWs w{};
     const int64_t rows = static_cast<int64_t>(n_groups) * n_beams;
     const int steps = (vocab + kStepLogits - 1) / kStepLogits;
-    int64_t parts = (2 * 152 + rows - 1) / rows;
+    int64_t parts = (kFill + rows - 1) / rows;
     const int most = kMaxCandidates / (n_beams * n_best);
     if (parts > most) parts = most;
     if (parts > kMaxParts) parts = kMaxParts;
@@ -663,21 +664,22 @@ BeamWs beam_layout(int n_groups, int n_beams, int vocab, int n_best)
     if (parts < 1) parts = 1;
     w.part_steps = static_cast<int>((steps + parts - 1) / parts);
     w.parts = (steps + w.part_steps - 1) / w.part_steps;
-    size_t off = 0;
-    auto take = [&](size_t bytes) {
-        const size_t at = off;
-        off = align_up(off + bytes, kAlign);
-        return at;
-    };
-    w.sums = take(static_cast<size_t>(rows) * w.parts * sizeof(float2));
-    w.best = take(static_cast<size_t>(rows) * w.parts * n_best * sizeof(uint64_t));
-    w.end = off;
+    w.sums = 0;
+    w.best = align_up(static_cast<size_t>(rows) * w.parts * sizeof(float2), kAlign);
     return w;
 }
 
 }  // namespace
 
-size_t beam_ws_bytes(int n_groups, int n_beams, int vocab, int n_best) { return beam_layout(n_groups, n_beams, vocab, n_best).end; }
+// Of every call with no more of any of these: fewer rows have more parts each, but rows times parts stays below rows + kFill, and is
+// at most rows times the most parts of one.
+size_t beam_ws_bytes(int n_groups, int n_beams, int vocab, int n_best)
+{
+    const int64_t rows = static_cast<int64_t>(n_groups) * n_beams, steps = (vocab + kStepLogits - 1) / kStepLogits;
+    const int64_t each = rows * (steps < kMaxParts ? steps : kMaxParts), all = rows + kFill - 1;
+    const size_t lists = static_cast<size_t>(each < all ? each : all);
+    return align_up(lists * sizeof(float2), kAlign) + align_up(lists * n_best * sizeof(uint64_t), kAlign);
+}
 
 cudaError_t launch_beam_select(const BeamArgs& b, bool fp32, uint8_t* ws, cudaStream_t st)
 {

@@ -1,0 +1,32 @@
+"""Sizes of the calls for drafted trees and beams, without a GPU: workspaces."""
+
+import pytest
+
+import paper_2609_31568_gb300 as pkg
+from paper_2609_31568_gb300 import scale as S
+
+
+@pytest.fixture(scope="module")
+def lib():
+    pkg.build()
+    return S.load()
+
+
+def size(groups, beams, vocab, n_best):
+    return S.scale_beam_workspace_size(S.beam_params(n_groups=groups, n_beams=beams, vocab=vocab, n_best=n_best))
+
+
+@pytest.mark.parametrize("beams,n_best", [(1, 1), (1, 8), (3, 2), (8, 16), (32, 64)])
+@pytest.mark.parametrize("vocab", [70, 8192, 8193, 32000, 128000, 1 << 24])
+def test_a_workspace_does_for_every_smaller_call(lib, beams, n_best, vocab):
+    """A batch's finished groups leave; the workspace stays the largest batch's."""
+    sizes = [size(g, beams, vocab, n_best) for g in range(1, min(700, 4096 // beams) + 1)]
+    assert sizes == sorted(sizes)
+
+
+def test_a_workspace_does_for_fewer_beams_tokens_and_continuations(lib):
+    for groups in (1, 9, 37, 38, 100):
+        for at, values in ((1, range(1, 33)), (2, [64, 100, 8191, 8192, 8193, 16384, 16385, 50000, 100003, 128000, 2 ** 20, 2 ** 24]), (3, range(1, 65))):
+            for call in ([groups, 8, 128000, 16], [groups, 2, 40000, 4], [groups, 32, 64, 64]):
+                sizes = [size(*call[:at], x, *call[at + 1:]) for x in values]
+                assert sizes == sorted(sizes), (call, at)
