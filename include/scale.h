@@ -543,7 +543,8 @@ typedef enum { SCALE_LOGITS_BF16 = 0, SCALE_LOGITS_FP32 = 1 } scale_logits_dtype
 
 /* Groups of beams that are searched together. */
 typedef struct {
-    int32_t n_groups; /* n_groups * n_beams at most 4096                                            */
+    int32_t n_groups; /* n_groups * n_beams at most 4096; with one beam, the choices after the nodes
+                         of drafted trees, n_groups at most 2^22                                    */
     int32_t n_beams;  /* beams of a group, 1..32                                                    */
     int32_t vocab;    /* 1..2^24                                                                    */
     int32_t n_best;   /* continuations kept of a group: 1..64, at most n_beams * vocab              */

@@ -9,6 +9,7 @@ namespace scale {
 constexpr int kMaxNodes = 1024;     // rows of a sequence's tree
 constexpr int kMaxBeams = 32;       // of a group: a lane each
 constexpr int kMaxBest = 64;        // continuations kept of a group
+constexpr int kMaxSingles = kMaxSeqs * kMaxNodes;  // groups of one beam: every node of a batch
 constexpr int kMaxVocab = 1 << 24;
 constexpr int kMaxCaches = 1024;    // of scale_cache_move
 constexpr int kMoveCaches = 64;     // of them in a launch

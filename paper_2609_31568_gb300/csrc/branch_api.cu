@@ -26,7 +26,7 @@ int check_beam(const scale_beam_t* b)
         return SCALE_ERR_INVALID_ARG;
     if (b->n_best > static_cast<int64_t>(b->n_beams) * b->vocab) return SCALE_ERR_INVALID_ARG;
     if (b->n_beams > kMaxBeams || b->n_best > kMaxBest || b->vocab > kMaxVocab ||
-        static_cast<int64_t>(b->n_groups) * b->n_beams > kMaxSeqs)
+        static_cast<int64_t>(b->n_groups) * b->n_beams > (b->n_beams == 1 ? kMaxSingles : kMaxSeqs))
         return SCALE_ERR_UNSUPPORTED;
     return SCALE_OK;
 }

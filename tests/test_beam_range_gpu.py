@@ -1,5 +1,5 @@
 """Beam selection at the ends of its range: logits below the normal numbers, sums of many logits far below the largest, scores
-that lie next to each other."""
+that lie next to each other, more rows of one beam than a group's beams may have."""
 
 import math
 
@@ -143,3 +143,18 @@ def test_select_of_random_groups_far_enough_apart():
     for g in rows:
         assert (beam[g].astype(np.int64) * vocab + token[g]).tolist() == at[g, :k].tolist()
     assert (np.abs(score - value[:, :k].cpu().numpy()) <= 2.0 ** -18 + np.abs(score) * 2.0 ** -24).all()
+
+
+# ---------------------------------------------------------------- rows of one beam
+
+
+@pytest.mark.parametrize("rows,vocab,n_best", [(4097, 1000, 1), (12800, 301, 1), (12800, 301, 3), (70001, 40, 2)])
+def test_rows_of_one_beam_are_not_bounded_as_beams_are(rows, vocab, n_best):
+    """The choices after every node of a batch's trees."""
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    z = torch.randn(rows, vocab, generator=gen, device="cuda").bfloat16()
+    score, beam, token = select(z, torch.zeros(rows, 1, device="cuda"), n_best)
+    value, at = torch.log_softmax(z.double(), -1).sort(dim=-1, descending=True, stable=True)
+    assert (beam == 0).all() and (token == at[:, :n_best].cpu().numpy()).all()
+    want = value[:, :n_best].cpu().numpy()
+    assert (np.abs(score - want) <= 2.0 ** -18 + np.abs(want) * 2.0 ** -24).all()
