@@ -575,6 +575,10 @@ int scale_beam_select(const scale_beam_t *beam, const void *logits, int64_t logi
  * beams that go on from the same one, that one itself, or else the lowest, keeps them; the others get, in
  * their order, those of the beams that none goes on from, into which the rows so far are copied by
  * `moves`. So no page is needed, and pages that no table names any more stay the caller's.
+ * Beams begin so: the prompt is appended to one beam's pages, the others' rows of the table get its complete pages and then
+ * pages of their own, and the rows in its last page, if that is not complete, are copied into theirs by scale_cache_move with
+ * a list of the caller's (any order: none reads what another writes). No two beams of a group name the same page for what is
+ * behind the complete ones.
  *   page_table int32 [n_groups * n_beams][table_stride]; table_out the same, or page_table itself
  *   parents    int32 [n_groups][n_beams];  kv_len int32 [n_groups * n_beams]
  *   moves      src and dst [n_groups * n_beams][page_size] out, for scale_cache_move with start = NULL;

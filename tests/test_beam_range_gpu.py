@@ -158,3 +158,72 @@ def test_rows_of_one_beam_are_not_bounded_as_beams_are(rows, vocab, n_best):
     assert (beam == 0).all() and (token == at[:, :n_best].cpu().numpy()).all()
     want = value[:, :n_best].cpu().numpy()
     assert (np.abs(score - want) <= 2.0 ** -18 + np.abs(want) * 2.0 ** -24).all()
+
+
+# ---------------------------------------------------------------- beams that begin from one prompt
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("prompt", [5, 16, 21])
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_beams_begin_from_one_prompt(prompt, e4m3):
+    """The prompt goes into beam 0's pages; the others share its complete pages, and what is in the page being filled is copied
+    into theirs by a list of moves of the program's own. Every beam then holds its own tokens, step by step."""
+    hkv, page, groups, beams, vocab, steps, pages_each = 2, 16, 2, 3, 50, 25, 4
+    n = groups * beams
+    gen = torch.Generator(device="cuda").manual_seed(prompt)
+    k_of, v_of = (torch.randn(vocab, hkv, 128, generator=gen, device="cuda").bfloat16() for _ in range(2))
+    table = torch.randperm(n * pages_each, generator=gen, device="cuda").int().view(n, pages_each).clone()
+    cache = S.allocate_kv_cache(n * pages_each, page, hkv, e4m3=True) if e4m3 else S.allocate_kv_cache(n * pages_each, page, hkv)
+    layers = S.cache_layers([cache])
+    # ---- the prompts, a sequence for each group
+    said = [[(7 * g + t) % vocab for t in range(prompt)] for g in range(groups)]
+    rows = torch.tensor(said, device="cuda").flatten()
+    first = S.kv_batch(ints([prompt * g for g in range(groups + 1)]), ints([prompt] * groups), table[::beams].contiguous(), groups * prompt, prompt)
+    S.scale_cache_append(cache, first, k_of[rows].contiguous(), v_of[rows].contiguous())
+    # ---- the beams
+    full, rest = divmod(prompt, page)
+    for i in range(n):
+        table[i, :full] = table[i - i % beams, :full]
+    src, dst = [], []
+    for i in range(n):
+        for t in range(page):
+            copied = i % beams > 0 and t < rest
+            src.append(int(table[i - i % beams, full]) * page + t if copied else -1)
+            dst.append(int(table[i, full]) * page + t if copied else -1)
+    S.scale_cache_move(layers, S.cache_moves(ints(src), ints(dst), n_groups=n))
+    said = [list(said[i // beams]) for i in range(n)]
+    # ---- steps
+    moves = S.cache_moves(ints([0] * (n * page)), ints([0] * (n * page)), n_groups=n)
+    kv_len = ints([prompt] * n)
+    batch = S.kv_batch(torch.arange(n + 1, dtype=torch.int32, device="cuda"), kv_len, table, n, 1)
+    p = S.beam_params(n_groups=groups, n_beams=beams, vocab=vocab, n_best=beams)
+    ws = torch.empty(S.scale_beam_workspace_size(p), dtype=torch.uint8, device="cuda")
+    score = torch.tensor([[0.0, -math.inf, -math.inf]] * groups, device="cuda")
+    new = torch.empty_like(score), ints([[0] * beams] * groups), ints([[0] * beams] * groups)
+    for _ in range(steps):
+        logits = torch.randn(n, vocab, generator=gen, device="cuda") * 2
+        S.scale_beam_select(p, logits, score, *new, ws)
+        S.scale_beam_reorder(layers, table, kv_len, new[1], table, moves)
+        S.scale_cache_move(layers, moves)
+        score = new[0].clone()
+        parent, token = new[1].flatten().tolist(), new[2].flatten().tolist()
+        said = [said[i - i % beams + b] + [t] for i, (b, t) in enumerate(zip(parent, token))]
+        kv_len += 1
+        rows = new[2].flatten().long()
+        S.scale_cache_append(cache, batch, k_of[rows].contiguous(), v_of[rows].contiguous())
+    # ---- the same sequences, each on its own in a cache of its own
+    length = prompt + steps
+    alone = S.allocate_kv_cache(n * pages_each, page, hkv, e4m3=True) if e4m3 else S.allocate_kv_cache(n * pages_each, page, hkv)
+    own = torch.arange(n * pages_each, dtype=torch.int32, device="cuda").view(n, pages_each)
+    every = lambda t: S.kv_batch(ints([length * i for i in range(n + 1)]), ints([length] * n), t, n * length, length)  # noqa: E731
+    rows = torch.tensor(said, device="cuda").flatten()
+    S.scale_cache_append(alone, every(own), k_of[rows].contiguous(), v_of[rows].contiguous())
+    out = [[torch.empty(n * length, hkv, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2)] for _ in range(2)]
+    S.scale_cache_read(cache, every(table), *out[0])
+    S.scale_cache_read(alone, every(own), *out[1])
+    assert all(torch.equal(x.view(torch.int16), y.view(torch.int16)) for x, y in zip(*out))
+    assert len({tuple(x) for x in said[:beams]}) == beams
