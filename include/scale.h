@@ -379,8 +379,8 @@ typedef struct {
     int32_t n_seqs;            /* 1..4096                                                    */
     int32_t table_stride;
     int32_t n_rows;            /* rows of the row tensors: at least row_start[n_seqs]        */
-    int32_t max_rows;          /* bound on a sequence's rows; only scale_cache_attend uses
-                                  it: rows of a sequence past it are left as they were       */
+    int32_t max_rows;          /* bound on a sequence's rows, for the attention and the calls
+                                  with drafted trees: rows past it are left as they were     */
 } scale_batch_t;
 
 /* Rotary positions with several axes. Pair i of a head turns by the angle
@@ -496,7 +496,8 @@ int scale_tree_plan(const scale_tree_t *tree, const scale_batch_t *batch, int32_
  * later nodes, or not itself; bits of nodes past the sequence's rows or max_rows are ignored.
  * Nodes that no row of their sequence sees, and tokens that a window ending at `base` hides, may hold anything; a value row
  * that is not finite makes the rows that see it not finite and may make so the other rows of its sequence. Heads, NaN queries, lse,
- * precision and the workspace (its size too) are as there. max_rows is at most 1024. */
+ * precision and the workspace (its size too) are as there, but that weights keep the bits of few pairs of a row and a head in calls
+ * with more of them too, where the table's width or the window allows few keys. max_rows is at most 1024. */
 int scale_cache_attend_tree(const scale_attend_t *attend, const scale_tree_t *tree, const scale_cache_t *cache,
                             const scale_batch_t *batch, const void *q, int64_t q_stride, void *out,
                             int64_t out_stride, float *lse, void *ws, size_t ws_bytes, scale_stream_t stream);
@@ -556,8 +557,9 @@ typedef struct {
  * in 64 bits from sums in 32 that are off by 2^-18 of them at most, whatever the logits' range, and as a rule by less than
  * 2^-21 (continuations of one beam share its sum: only those of different beams can change places by it). The n_best
  * largest are written in descending order, equal ones by the lower beam, then the larger logit, then the lower token. A NaN
- * logit counts as -inf, one below the normal numbers (of a size under 2^-126) as 0; every continuation of a beam whose score is not finite, or whose logits have no finite
- * maximum, scores -inf and is taken in its turn like any other.
+ * logit counts as -inf, one below the normal numbers (of a size under 2^-126) as 0. Every continuation of a beam whose score
+ * is not finite, or whose logits have no finite maximum, scores -inf and is taken in its turn like any other, those of such a beam in
+ * the order of their tokens, whatever its logits.
  *   logits      [n_groups * n_beams][vocab], rows logits_stride elements apart (at least vocab), aligned to their type
  *   scores      fp32 [n_groups][n_beams]
  *   best_scores fp32 [n_groups][n_best], best_beams int32 (0..n_beams - 1), best_tokens int32: out
