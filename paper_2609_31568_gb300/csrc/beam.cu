@@ -225,7 +225,7 @@ __device__ __noinline__ void load_edge(SelectShared& sh, const T* logits, int fi
 // by as much as the roundings of the difference and of the product are, 2^-20 each at 16. What the difference loses is kept
 // (Knuth's sum of two), multiples of log 2 go off it (Cody and Waite), and the rest, at most 0.35, has its series. A NaN, or -inf
 // from -inf, gives 0.
-constexpr float kApart = 8.0f;
+constexpr float kApart = 4.0f;
 
 __device__ __forceinline__ float exp_of(float a, float b)
 {
@@ -245,8 +245,8 @@ __device__ __forceinline__ float exp_of(float a, float b)
     return y * __uint_as_float(static_cast<uint32_t>(127 + static_cast<int>(i)) << 23);
 }
 
-// Sums across lanes, warps and parts are of whole multiples of 2^-32 of the largest term's (at least 1 in all, and below 2^25), which lose nothing
-// and come to the same in any order.
+// Sums across lanes, warps and parts are of whole multiples of 2^-32, which lose nothing and come to the same in any order. They
+// stay below 2^62: 2^24 terms, none above e^kApart of what they are against.
 __device__ __forceinline__ uint64_t fixed_of(float x) { return __float2ull_rn(x * 4294967296.0f); }
 __device__ __forceinline__ float of_fixed(uint64_t x) { return __ull2float_rn(x) * (1.0f / 4294967296.0f); }
 
@@ -301,8 +301,8 @@ __device__ __noinline__ int collect_carefully(SelectShared& sh, const T* logits,
 // 16-byte boundary a thread puts its logits together from its load and its neighbour's, so that it has the same tokens
 // wherever the row lies: rows of the same logits have the same sum to the bit, and equal scores stay equal. A step's sum is against
 // its own largest logit, its thread's against the thread's, with what a step loses carried to the next; those of threads and parts
-// meet in whole numbers. It is off by 2^-18 of itself at most (in units of 2^-24: ex2 3, distances in a step 4, its ten sums 9, four or five of exp_of
-// with their products 18, the rest 6), and by 2^-21.3 in the worst of 50,000 rows of many kinds. (Steps against the thread's
+// meet in whole numbers. It is off by 2^-18 of itself at most (in units of 2^-24: ex2 3, distances in a step 4, its ten sums 9, six of exp_of
+// with their products 21, the rest 6), and by 2^-21.3 in the worst of 50,000 rows of many kinds. (Steps against the thread's
 // largest logit so far, all joined by ex2: 41.8 us in place of 42.9, but 128,000 logits 11 below one were 2^-20.9 off.) The first step sets the
 // bound that a candidate has to reach (bound_of, then the least of the n_best best so far, again after 2, 4, 8 .. steps if as many follow);
 // between these warps go on without barriers, and one whose threads all stay at or below the bound, which their largest logits tell,
@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) k_beam_part(const __gr
             }
             float y = (acc[0] + acc[1]) + (acc[2] + acc[3]);
             if (!(y >= 0.f)) y = sum_without_nan<T>(logits, first, vocab, -neg);
-            // `top` follows by kApart at least, so that no term is multiplied often on its way
+            // `top` follows the largest logit by steps of more than kApart, so that no term is multiplied often on its way
             const bool ahead = m - top > kApart;
             const float f = exp_of(ahead ? top : m, ahead ? m : top);
             if (ahead) {

@@ -106,6 +106,19 @@ def test_many_logits_far_below_the_largest(dtype, vocab, low, rows):
     assert np.abs(score.astype(np.float64) - want).max() <= 2.0 ** -23 + abs(want) * 2.0 ** -24
 
 
+@pytest.mark.parametrize("rise", [1.5, 3.75, 4.25, 7.75, 12.0])
+@pytest.mark.parametrize("rows,vocab", [(1, 1 << 24), (310, 1 << 22), (2, 1 << 20)])
+def test_sums_whose_first_logits_are_the_smaller(rows, vocab, rise):
+    """Now and then 8,192 logits of 0, all others `rise` above: the largest sums that there are, against what comes first."""
+    z = torch.full((rows, vocab), rise, dtype=torch.bfloat16, device="cuda")
+    z[:, : vocab // 8192 * 8192].view(rows, -1, 8192)[:, ::64] = 0.0
+    score, _, token = select(z, torch.zeros(rows, 1, device="cuda"), 1)
+    small = 8192 * len(range(0, vocab // 8192, 64))
+    want = -math.log((vocab - small) + small * math.exp(-rise))
+    assert (token == 8192).all()
+    assert np.abs(score.astype(np.float64) - want).max() <= 2.0 ** -18 + abs(want) * 2.0 ** -24
+
+
 @pytest.mark.parametrize("vocab,low", FAR[:3])
 @pytest.mark.parametrize("gap", [1.5, -1.5])
 def test_scores_next_to_each_other(vocab, low, gap):
